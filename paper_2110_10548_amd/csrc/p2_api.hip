@@ -2722,6 +2722,11 @@ int32_t run_batch(const p2_query* queries, int32_t n_queries, const double* msg_
 
 }  // namespace
 
+namespace p2 {                                             // for the entry points of p2_train_api.hip
+int32_t api_fail(int32_t code, const std::string& text) { return fail(code, text); }
+int32_t api_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
+}  // namespace p2
+
 extern "C" {
 
 const char* p2_last_error(void) { return g_err.c_str(); }
