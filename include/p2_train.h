@@ -15,7 +15,7 @@
  *  - Every pointer to data is a DEVICE pointer, aligned to its element type; `stream` is a hipStream_t or NULL.
  *    A call checks its arguments, queues its kernels on the stream and returns; it neither waits nor allocates,
  *    so it may be captured into a graph.  Outputs must not overlap inputs or each other, except where a call says so.
- *  - Workspaces are the caller's: *_workspace gives the bytes, the pointer is aligned to 256.  A workspace may be
+ *  - Workspaces are the caller's: *_workspace gives the bytes (0: NULL will do), the pointer is aligned to 256.  A workspace may be
  *    used again as soon as the call's kernels are done; two streams need two.  Nothing in it outlives a call.
  *  - Rows are contiguous; `*_stride` is the distance between rows in elements and may be larger than the row.
  *  - Element types: P2_F32, P2_BF16, P2_F16.  Sums, statistics and products are accumulated in 32 bits or more

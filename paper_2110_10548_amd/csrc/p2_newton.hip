@@ -8,8 +8,8 @@
 // largest singular value).
 //
 // Layout.  Every operand is stored with the summed index contiguous, so a product is always rows times rows:
-// C[i][j] = sum_k P[i][k] Q[j][k].  32 values of k lie together as 64 bytes of highs and 64 bytes of lows: what one
-// step of the product's loop needs of a row is one line of 128 bytes.  A and B are symmetric and are their own transposes; only
+// C[i][j] = sum_k P[i][k] Q[j][k].  32 values of k lie together as 64 bytes of highs and 64 bytes of lows: what a
+// stage of the product's loop needs of a row is one line of 128 bytes.  A and B are symmetric and are their own transposes; only
 // tiles on and below the diagonal are computed, and written to both sides.  X is kept in both orders (m x n for X X^T, n x m
 // for B X).  Sizes are padded to whole tiles with zeros, which stay zeros through all steps.
 #include <algorithm>
@@ -24,65 +24,105 @@ namespace {
 typedef half_t half8 __attribute__((ext_vector_type(8)));
 typedef half_t half4 __attribute__((ext_vector_type(4)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4), may_alias));
 
 constexpr int kLine = 128;                     // bytes of 32 pairs
-constexpr int kNormParts = 64;                 // blocks that a matrix's norm is summed by
+constexpr int64_t kMostNormParts = 1024;       // blocks that a matrix's norm is summed by
 
 // Byte of the high half of pair k in a row; its low half is 64 further.
 __device__ __forceinline__ int64_t pair_at(int64_t k) { return (k >> 5) * kLine + (k & 31) * 2; }
+__device__ __forceinline__ float4_t multiply(half8 p, half8 q, float4_t sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, sum, 0, 0, 0); }
 __device__ __forceinline__ void split(float v, half_t& high, half_t& low) {
     high = (half_t)v;
     low = (half_t)(v - (float)high);
 }
 
-// Sum of squares, in 64 bits: entries of any size, and no overflow before the root.
-template <typename T> __global__ __launch_bounds__(256) void k_newton_norm(const T* g, int64_t stride, int64_t matrix_stride, int64_t rows, int64_t cols,
-                                                                           double* parts) {
-    __shared__ double buf[4];
-    const T* m = g + (int64_t)blockIdx.y * matrix_stride;
-    double s = 0.0;
-    for (int64_t r = blockIdx.x; r < rows; r += kNormParts)
-        for (int64_t c = threadIdx.x; c < cols; c += 256) { const double v = (double)(float)m[r * stride + c]; s += v * v; }
+__device__ __forceinline__ uint32_t pack(float v) {
+    half_t h, l;
+    split(v, h, l);
+    return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+}
+__device__ __forceinline__ void store_pairs(char* at, const uint32_t (&v)[4]) {
+    uint2 high, low;
+    high.x = __builtin_amdgcn_perm(v[1], v[0], 0x05040100);
+    high.y = __builtin_amdgcn_perm(v[3], v[2], 0x05040100);
+    low.x = __builtin_amdgcn_perm(v[1], v[0], 0x07060302);
+    low.y = __builtin_amdgcn_perm(v[3], v[2], 0x07060302);
+    *reinterpret_cast<uint2*>(at) = high;
+    *reinterpret_cast<uint2*>(at + kLine / 2) = low;
+}
+
+// Sum over a block of 256 threads, the same for all of them.
+__device__ __forceinline__ double block_sum_256(double s, double* buf) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNormParts + blockIdx.x] = buf[0] + buf[1] + buf[2] + buf[3];
+    return (buf[0] + buf[1]) + (buf[2] + buf[3]);
+}
+// What a matrix whose squares sum to s is multiplied by; zeros stay zeros without an eps, too.
+__device__ __forceinline__ double scale_factor(double s, double eps, double unit) {
+    s = sqrt(s) + eps;
+    return s == 0.0 ? 0.0 : unit / s;
+}
+
+// Sum of squares, in 64 bits: entries of any size, and no overflow before the root.  `across` threads (a power of two) take a
+// row, 256 / across rows at a time.
+template <typename T> __global__ __launch_bounds__(256) void k_newton_norm(const T* g, int64_t stride, int64_t matrix_stride, int64_t rows, int64_t cols,
+                                                                           int32_t across, double* parts) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ double buf[4];
+    const T* m = g + (int64_t)blockIdx.y * matrix_stride;
+    const int tall = 256 / across;
+    double s = 0.0;
+    for (int64_t r = (int64_t)blockIdx.x * tall + threadIdx.x / across; r < rows; r += (int64_t)gridDim.x * tall)
+        for (int64_t c = (int64_t)(threadIdx.x % across) * V; c < cols; c += (int64_t)across * V) {
+            float v[V];
+            load_part<T, V>(m + r * stride + c, cols - c, v, 0.0f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s += (double)v[i] * (double)v[i];
+        }
+    s = block_sum_256(s, buf);
+    if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
 // G / (||G|| + eps) as pairs in both orders: `straight` (rows x cols) and `turned` (cols x rows), zeros in the padding.
 template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(const T* g, int64_t stride, int64_t matrix_stride, int64_t rows, int64_t cols,
-                                                                            const double* parts, double eps, double unit, char* straight, char* turned,
-                                                                            int64_t rows_padded, int64_t cols_padded, int64_t plane) {
-    __shared__ float tile[32][33];
-    __shared__ double factor;
-    if (threadIdx.x == 0) {
-        double s = 0.0;
-        for (int i = 0; i < kNormParts; ++i) s += parts[(int64_t)blockIdx.z * kNormParts + i];
-        s = sqrt(s) + eps;
-        factor = s == 0.0 ? 0.0 : unit / s;
-    }
-    __syncthreads();
+                                                                            const double* parts, int32_t n_parts, double eps, double unit, char* straight,
+                                                                            char* turned, int64_t rows_padded, int64_t cols_padded, int64_t plane) {
+    __shared__ float tile[64][65];
+    __shared__ double buf[4];
     const T* m = g + (int64_t)blockIdx.z * matrix_stride;
-    const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    for (int i = y; i < 32; i += 8) {
-        const int64_t r = r0 + i, c = c0 + x;
-        const float v = r < rows && c < cols ? (float)((double)(float)m[r * stride + c] * factor) : 0.0f;
-        tile[i][x] = v;
-        half_t high, low;
-        split(v, high, low);
-        char* at = straight + blockIdx.z * plane + r * cols_padded * 4 + pair_at(c);
-        *reinterpret_cast<half_t*>(at) = high;
-        *reinterpret_cast<half_t*>(at + 64) = low;
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
+    float v[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + y + i * 16, c = c0 + x;
+        load_part<T, 4>(m + r * stride + c, r < rows ? cols - c : 0, v[i], 0.0f);
+    }
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n_parts; i += 256) s += parts[(int64_t)blockIdx.z * n_parts + i];
+    s = block_sum_256(s, buf);
+    const double factor = scale_factor(s, eps, unit);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[i][j] = (float)((double)v[i][j] * factor);
+            tile[y + i * 16][x + j] = v[i][j];
+            w[j] = pack(v[i][j]);
+        }
+        store_pairs(straight + blockIdx.z * plane + (r0 + y + i * 16) * cols_padded * 4 + pair_at(c0 + x), w);
     }
     __syncthreads();
-    for (int i = y; i < 32; i += 8) {
-        half_t high, low;
-        split(tile[x][i], high, low);
-        char* at = turned + blockIdx.z * plane + (c0 + i) * rows_padded * 4 + pair_at(r0 + x);
-        *reinterpret_cast<half_t*>(at) = high;
-        *reinterpret_cast<half_t*>(at + 64) = low;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack(tile[x + j][y + i * 16]);
+        store_pairs(turned + blockIdx.z * plane + (c0 + y + i * 16) * rows_padded * 4 + pair_at(r0 + x), w);
     }
 }
 
@@ -102,64 +142,114 @@ struct Product {
     int32_t out_turned, out_type;
 };
 
-// One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q for 32 (64) values of k are
-// brought to LDS while those before are multiplied; a row takes 128 bytes there, its 16-byte pieces exchanged by the row's
-// number, so that the 16 rows that a wavefront reads at once lie in different banks.
-template <int kTile, int kWavesM, int kWavesN, int kTerms, int kKind>
+// Four values in a row of the result, of which `n` are inside it.
+__device__ __forceinline__ void store_four(void* p, int32_t type, int64_t at, int64_t n, const float (&v)[4]) {
+    if (type == P2_F32) store_part<float, 4>(static_cast<float*>(p) + at, n, v);
+    else if (type == P2_BF16) store_part<bf16_t, 4>(static_cast<bf16_t*>(p) + at, n, v);
+    else store_part<half_t, 4>(static_cast<half_t*>(p) + at, n, v);
+}
+
+// Rows of an operand, `bytes` long altogether, and 16 bytes a lane of them to LDS (`to`: the wavefront's, lanes one after
+// the other); what lies past the end comes as zeros.  Only the device's compiler knows the descriptor's type.
+struct Rows {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __amdgpu_buffer_rsrc_t at;
+    __device__ __forceinline__ Rows(const char* p, int bytes) : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, bytes, 0x00027000)) {}
+    __device__ __forceinline__ void bring(char* to, int lane_offset, int offset) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (__attribute__((address_space(3))) void*)to, 16, lane_offset, offset, 0, 0);
+    }
+#else
+    __device__ Rows(const char*, int) {}
+    __device__ void bring(char*, int, int) const {}
+#endif
+};
+
+// What the wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void wavefront_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Waits until at most kLoads of this wavefront's loads are under way (and all its LDS reads are done), then for the others.
+template <int kLoads> __device__ __forceinline__ void stage_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((kLoads & 15) | (kLoads >> 4) << 14 | 0x70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q come to LDS in stages of 32 values of k
+// (64 for upper halves), kStages - 1 of them under way while one is multiplied.  A row of a stage takes 128 bytes; its
+// 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
+// Rows past the end of P or Q are zeros: the loads' descriptors end with the matrix.
+template <int kTile, int kWavesM, int kWavesN, int kStages, int kTerms, int kKind>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Product a) {
     constexpr int kWaves = kWavesM * kWavesN;
     constexpr int FM = kTile / kWavesM / 16, FN = kTile / kWavesN / 16;
-    constexpr int kStep = kTerms == 3 ? 32 : 64;
     constexpr int kStepBytes = kTerms == 3 ? kLine : 2 * kLine;
-    constexpr int kLoads = kTile / 8 / kWaves;             // a wavefront's loads of each operand a step, 8 rows each
-    static_assert(kLoads * 8 * kWaves == kTile, "rows are dealt out evenly");
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][kTile * kLine];
+    constexpr int kLoads = kTile / 8 / kWaves;             // of each operand a stage; one brings 8 rows
+    constexpr int kAhead = kStages - 1;
+    static_assert(kLoads * 8 * kWaves == kTile && FM * kWavesM * 16 == kTile && FN * kWavesN * 16 == kTile, "rows are dealt out evenly");
+    static_assert(2 * kLoads * (kAhead - 1) < 64, "the loads' counter");
+    __shared__ __attribute__((aligned(1024))) char lds[kStages][2][kTile * kLine];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // Blocks go to the eight dies in turn: tile numbers are dealt out so that a die's tiles are neighbours.
+    int t = blockIdx.x;
+    {
+        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = t & 7;
+        t = die * whole + min(die, rest) + (t >> 3);
+    }
     int bi, bj;
     if constexpr (kKind == kGram || kKind == kPoly) {      // the t-th tile on or below the diagonal
-        const int t = blockIdx.x;
         bi = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
         while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
         while (bi * (bi + 1) / 2 > t) --bi;
         bj = t - bi * (bi + 1) / 2;
-    } else {
-        const int across = (int)(a.cols / kTile);
-        bi = (int)blockIdx.x / across;
-        bj = (int)blockIdx.x % across;
+    } else {                                               // column by column of four rows of tiles
+        const int down = (int)((a.rows + kTile - 1) / kTile), across = (int)((a.cols + kTile - 1) / kTile);
+        const int band = t / (4 * across), first = band * 4, high = min(4, down - first), in = t - first * across;
+        bi = first + in % high;
+        bj = in / high;
     }
     const int64_t pitch = a.k * 4;
-    const char* p = a.p + blockIdx.y * a.p_plane + (int64_t)bi * kTile * pitch;
-    const char* q = a.q + blockIdx.y * a.q_plane + (int64_t)bj * kTile * pitch;
-    const int piece = (lane & 7) ^ (lane >> 3);
-    const int64_t from = (int64_t)(wave * kLoads * 8 + (lane >> 3)) * pitch +
-                         (kTerms == 3 ? piece * 16 : (piece >> 2) * kLine + (piece & 3) * 16);
-    auto bring = [&](int buf, int64_t at) {
+    auto rows_of = [&](const char* m, int64_t first, int64_t rows) {
+        return Rows(m + first * pitch, (int)(min(rows - first, (int64_t)kTile) * pitch));
+    };
+    const Rows p = rows_of(a.p + blockIdx.y * a.p_plane, (int64_t)bi * kTile, a.rows);
+    const Rows q = rows_of(a.q + blockIdx.y * a.q_plane, (int64_t)bj * kTile, a.cols);
+    const int part = (lane & 7) ^ (lane >> 3);
+    const int from = (wave * kLoads * 8 + (lane >> 3)) * (int)pitch + (kTerms == 3 ? part * 16 : (part >> 2) * kLine + (part & 3) * 16);
+    auto bring = [&](int stage, int at) {
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
-            const int64_t src = from + (int64_t)l * 8 * pitch + at;
-            const int dst = (wave * kLoads + l) * 8 * kLine;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + src),
-                                             (__attribute__((address_space(3))) void*)(&lds[buf][0][dst]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(q + src),
-                                             (__attribute__((address_space(3))) void*)(&lds[buf][1][dst]), 16, 0, 0);
+            const int src = from + l * 8 * (int)pitch;
+            const int dst = (wave * kLoads + l) * 1024;
+            p.bring(&lds[stage][0][dst], src, at);
+            q.bring(&lds[stage][1][dst], src, at);
         }
     };
     const int wm = wave / kWavesN, wn = wave % kWavesN;
     const int row = lane & 15, quad = lane >> 4;
+    const int64_t i0 = (int64_t)bi * kTile + wm * FM * 16, j0 = (int64_t)bj * kTile + wn * FN * 16;
+    const int steps = (int)(a.k / (kTerms == 3 ? 32 : 64));
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) if (s < steps) bring(s, s * kStepBytes);
     float4_t acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int steps = (int)(a.k / kStep);
-    bring(0, 0);
+    // where this lane's 16 bytes of a row lie: highs and lows, or two pieces of highs
+    const int at0 = row * kLine + (quad ^ (row & 7)) * 16, at1 = row * kLine + ((quad + 4) ^ (row & 7)) * 16;
+    int stage = 0, next = kAhead;
     for (int s = 0; s < steps; ++s) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): this wavefront's loads of the step are in LDS
-        __syncthreads();
-        if (s + 1 < steps) bring((s + 1) & 1, (int64_t)(s + 1) * kStepBytes);
-        const char* tp = lds[s & 1][0] + (wm * FM * 16 + row) * kLine;
-        const char* tq = lds[s & 1][1] + (wn * FN * 16 + row) * kLine;
-        const int at0 = (quad ^ (row & 7)) * 16, at1 = ((quad + 4) ^ (row & 7)) * 16;
+        if (s + kAhead <= steps) stage_barrier<2 * kLoads * (kAhead - 1)>();
+        else stage_barrier<0>();
+        if (s + kAhead < steps) bring(next, (s + kAhead) * kStepBytes);
+        const char* tp = lds[stage][0] + wm * FM * 16 * kLine;
+        const char* tq = lds[stage][1] + wn * FN * 16 * kLine;
+        next = stage;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
         half8 q0[FN], q1[FN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
@@ -173,68 +263,268 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 if constexpr (kTerms == 3) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, q0[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q1[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q0[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = multiply(p1, q0[j], acc[i][j]);
+                    acc[i][j] = multiply(p0, q1[j], acc[i][j]);
+                    acc[i][j] = multiply(p0, q0[j], acc[i][j]);
                 } else {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q0[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, q1[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = multiply(p0, q0[j], acc[i][j]);
+                    acc[i][j] = multiply(p1, q1[j], acc[i][j]);
                 }
             }
         }
     }
-    // a lane has four rows i of one column j
+    stage_barrier<0>();                                    // LDS changes its use: a strip of 16 rows for each wavefront
+    // A lane has four rows i of one column j, which are four values in a row of the transpose.  For the result's own rows a
+    // strip goes through LDS, where a lane picks up four columns of one row.
+    constexpr int kPitch = FN * 16 + 4;
+    static_assert(kWaves * 16 * kPitch * 4 <= (int)sizeof(lds), "the strips fit");
+    uint32_t* strip = reinterpret_cast<uint32_t*>(&lds[0][0][0]) + wave * 16 * kPitch;
+    half4 high[FN], low[FN];
+    auto fetch = [&](int fi) {
+        if constexpr (kKind != kGram) {
+            if (i0 + fi * 16 >= a.rows) return;
 #pragma unroll
-    for (int fi = 0; fi < FM; ++fi)
-#pragma unroll
-        for (int fj = 0; fj < FN; ++fj) {
-            const int64_t i = (int64_t)bi * kTile + wm * FM * 16 + fi * 16 + quad * 4;
-            const int64_t j = (int64_t)bj * kTile + wn * FN * 16 + fj * 16 + row;
-            float v[4];
-            if constexpr (kKind == kGram) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = acc[fi][fj][r] * a.sum_factor;
-            } else {
-                const char* o = a.old + blockIdx.y * a.old_plane + j * a.rows * 4 + pair_at(i);
-                const half4 high = *reinterpret_cast<const half4*>(o), low = *reinterpret_cast<const half4*>(o + 64);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = ((float)high[r] + (float)low[r]) * a.old_factor + acc[fi][fj][r] * a.sum_factor;
+            for (int fj = 0; fj < FN; ++fj) {
+                if (j0 + fj * 16 >= a.cols) continue;
+                const char* o = a.old + blockIdx.y * a.old_plane + (j0 + fj * 16 + row) * a.rows * 4 + pair_at(i0 + fi * 16 + quad * 4);
+                high[fj] = *reinterpret_cast<const half4*>(o);
+                low[fj] = *reinterpret_cast<const half4*>(o + kLine / 2);
             }
-            if constexpr (kKind == kLast) {
+        }
+    };
+    fetch(0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (i + r >= a.out_rows || j >= a.out_cols) continue;
-                    const int64_t at = blockIdx.y * a.out_plane + (a.out_turned ? j * a.out_stride + i + r : (i + r) * a.out_stride + j);
-                    store_typed(a.out, a.out_type, at, v[r] * a.gain);
-                }
-            } else {
-                half4 high, low;
+    for (int fi = 0; fi < FM; ++fi) {
+        if (i0 + fi * 16 >= a.rows) break;                 // (padded sizes are whole fragments)
+        uint32_t w[FN][4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    half_t h, l;
-                    split(v[r], h, l);
-                    high[r] = h;
-                    low[r] = l;
-                }
-                char* t = a.turned + blockIdx.y * a.q_plane;
-                if constexpr (kKind != kApply) t = a.straight + blockIdx.y * a.old_plane;
-                t += j * a.rows * 4 + pair_at(i);
-                *reinterpret_cast<half4*>(t) = high;
-                *reinterpret_cast<half4*>(t + 64) = low;
-                if (kKind == kApply || bi != bj) {
-                    char* st = a.straight + blockIdx.y * a.old_plane;
+        for (int fj = 0; fj < FN; ++fj)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        char* at = st + (i + r) * a.cols * 4 + pair_at(j);
-                        *reinterpret_cast<half_t*>(at) = high[r];
-                        *reinterpret_cast<half_t*>(at + 64) = low[r];
-                    }
+            for (int r = 0; r < 4; ++r) {
+                float v = acc[fi][fj][r] * a.sum_factor;
+                if constexpr (kKind != kGram) v += ((float)high[fj][r] + (float)low[fj][r]) * a.old_factor;
+                w[fj][r] = kKind == kLast ? __float_as_uint(v * a.gain) : pack(v);
+            }
+        if (fi + 1 < FM) fetch(fi + 1);
+        const int64_t i = i0 + fi * 16 + quad * 4;
+        if (kKind != kLast || a.out_turned) {
+            char* t = kKind == kApply ? a.turned + blockIdx.y * a.q_plane : kKind == kLast ? nullptr : a.straight + blockIdx.y * a.old_plane;
+#pragma unroll
+            for (int fj = 0; fj < FN; ++fj) {
+                const int64_t j = j0 + fj * 16 + row;
+                if constexpr (kKind == kLast) {
+                    const float f[4] = {__uint_as_float(w[fj][0]), __uint_as_float(w[fj][1]), __uint_as_float(w[fj][2]), __uint_as_float(w[fj][3])};
+                    if (j < a.out_cols) store_four(a.out, a.out_type, blockIdx.y * a.out_plane + j * a.out_stride + i, a.out_rows - i, f);
+                } else {
+                    if (j < a.cols) store_pairs(t + j * a.rows * 4 + pair_at(i), w[fj]);
                 }
             }
         }
+        if (kKind == kApply || (kKind == kLast ? !a.out_turned : bi != bj)) {
+#pragma unroll
+            for (int fj = 0; fj < FN; ++fj)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) strip[(quad * 4 + r) * kPitch + fj * 16 + row] = w[fj][r];
+            wavefront_exchange();
+#pragma unroll
+            for (int x = 0; x < FN; ++x) {
+                const int item = x * 64 + lane, si = item / (FN * 4), sj = item % (FN * 4) * 4;
+                const u32x4 u = *reinterpret_cast<const u32x4*>(strip + si * kPitch + sj);
+                const int64_t ri = i0 + fi * 16 + si, rj = j0 + sj;
+                if constexpr (kKind == kLast) {
+                    const float f[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+                    if (ri < a.out_rows) store_four(a.out, a.out_type, blockIdx.y * a.out_plane + ri * a.out_stride + rj, a.out_cols - rj, f);
+                } else if (rj < a.cols) {
+                    const uint32_t f[4] = {u.x, u.y, u.z, u.w};
+                    store_pairs(a.straight + blockIdx.y * a.old_plane + ri * a.cols * 4 + pair_at(rj), f);
+                }
+            }
+            wavefront_exchange();
+        }
+    }
 }
 
-constexpr int64_t kPad = 128;                  // tiles divide it
+// A matrix whose smaller side is at most 32 kBlocks (128) and which fits in LDS goes through all its steps there: one block
+// of eight wavefronts a matrix, one launch altogether.  X lies in rows (highs and lows apart, rows 16 bytes further apart
+// than they are long: 16 rows' pieces lie in different banks), A and then B beside it.  A product's operands come from
+// there; only X in B X is needed by columns, and a wavefront picks those of its 16 columns up value by value, once for all
+// rows of the result.  What it writes are the same 16 columns, which nobody else reads meanwhile.
+struct Small {
+    const void* g; void* out;
+    int64_t stride, matrix_stride, out_stride, out_plane;
+    int32_t rows, cols, n;                     // n: the longer side, padded to 32
+    int32_t out_type, steps, last_terms;
+    double eps, unit;
+    float gain;
+    float gram[64], poly_old[64], poly_sum[64], apply_old[64], apply_sum[64];
+};
+constexpr int kSmallBlock = 512;
+constexpr int64_t kLdsBytes = 160 * 1024;
+constexpr int64_t kSmallSpare = 128;                       // for the sums at its beginning
+constexpr int64_t small_bytes(int64_t m, int64_t n) { return 4 * m * (n + 8) + 4 * m * (m + 8) + kSmallSpare; }
+
+template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) void k_newton_small(Small a) {
+    constexpr int M = 32 * kBlocks, kWaves = kSmallBlock / 64;
+    constexpr int kOwn = (kBlocks * kBlocks + kWaves - 1) / kWaves;        // 32 x 32 blocks of A that a wavefront has
+    constexpr int AP = M + 8;
+    extern __shared__ __attribute__((aligned(16))) char small_lds[];
+    const int XP = a.n + 8;
+    half_t* xh = reinterpret_cast<half_t*>(small_lds + kSmallSpare);
+    half_t* xl = xh + M * XP;
+    half_t* ah = xl + M * XP;
+    half_t* al = ah + M * AP;
+    double* buf = reinterpret_cast<double*>(small_lds);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, quad = lane >> 4;
+    const T* g = static_cast<const T*>(a.g) + (int64_t)blockIdx.x * a.matrix_stride;
+    const bool tall = a.rows > a.cols;
+    const int rp = tall ? a.n : M, cp = tall ? M : a.n;    // padded sizes as G lies
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    double s = 0.0;
+    for (int r = ty; r < a.rows; r += kSmallBlock / 32)
+        for (int c = tx; c < a.cols; c += 32) { const double v = (double)(float)g[r * a.stride + c]; s += v * v; }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if (lane == 0) buf[wave] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s += buf[w];
+    const double factor = scale_factor(s, a.eps, a.unit);
+    for (int r = ty; r < rp; r += kSmallBlock / 32)
+        for (int c = tx; c < cp; c += 32) {
+            const float v = r < a.rows && c < a.cols ? (float)((double)(float)g[r * a.stride + c] * factor) : 0.0f;
+            const int at = tall ? c * XP + r : r * XP + c;
+            split(v, xh[at], xl[at]);
+        }
+    __syncthreads();
+    for (int step = 0; step < a.steps; ++step) {
+        const bool last = step + 1 == a.steps, pairs = !last || a.last_terms == 3;
+        float4_t acc[kOwn][2][2];
+        // C = P P^T for this wavefront's blocks
+        auto square = [&](const half_t* ph, const half_t* pl, int pitch, int length) {
+#pragma unroll
+            for (int o = 0; o < kOwn; ++o) {
+                const int b = wave + o * kWaves;
+                if (b >= kBlocks * kBlocks) break;
+                const int pi = (b / kBlocks * 32 + row) * pitch + quad * 8, pj = (b % kBlocks * 32 + row) * pitch + quad * 8;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) acc[o][x][y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+                for (int k = 0; k < length; k += 32) {
+                    half8 p0[2], p1[2], q0[2], q1[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        p0[x] = *reinterpret_cast<const half8*>(ph + pi + x * 16 * pitch + k);
+                        q0[x] = *reinterpret_cast<const half8*>(ph + pj + x * 16 * pitch + k);
+                        p1[x] = *reinterpret_cast<const half8*>(pl + pi + x * 16 * pitch + k);
+                        q1[x] = *reinterpret_cast<const half8*>(pl + pj + x * 16 * pitch + k);
+                    }
+                    if (pairs) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p1[x], q0[y], acc[o][x][y]);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p0[x], q1[y], acc[o][x][y]);
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p0[x], q0[y], acc[o][x][y]);
+                }
+            }
+        };
+        // acc * sum_factor (+ A * old_factor) for this wavefront's blocks; the result is symmetric, so a lane's four rows of one
+        // column are four values of a row
+        auto place = [&](float sum_factor, float old_factor, bool old, bool write) {
+#pragma unroll
+            for (int o = 0; o < kOwn; ++o) {
+                const int b = wave + o * kWaves;
+                if (b >= kBlocks * kBlocks) break;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int at = (b % kBlocks * 32 + y * 16 + row) * AP + b / kBlocks * 32 + x * 16 + quad * 4;
+                        if (old) {
+                            const half4 h = *reinterpret_cast<const half4*>(ah + at), l = *reinterpret_cast<const half4*>(al + at);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[o][x][y][r] = acc[o][x][y][r] * sum_factor + ((float)h[r] + (float)l[r]) * old_factor;
+                        }
+                        if (write) {
+                            half4 h, l;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                half_t hr, lr;
+                                split(old ? acc[o][x][y][r] : acc[o][x][y][r] * sum_factor, hr, lr);
+                                h[r] = hr;
+                                l[r] = lr;
+                            }
+                            *reinterpret_cast<half4*>(ah + at) = h;
+                            *reinterpret_cast<half4*>(al + at) = l;
+                        }
+                    }
+            }
+        };
+        square(xh, xl, XP, a.n);
+        place(a.gram[step], 0.0f, false, true);
+        __syncthreads();
+        square(ah, al, AP, M);
+        place(a.poly_sum[step], a.poly_old[step], true, false);
+        __syncthreads();                                   // everybody has read A
+        place(1.0f, 0.0f, false, true);
+        __syncthreads();
+#pragma unroll 1
+        for (int j0 = wave * 16; j0 < a.n; j0 += kWaves * 16) {
+            half8 q0[kBlocks], q1[kBlocks];
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = (k * 32 + quad * 8 + e) * XP + j0 + row;
+                    q0[k][e] = xh[at];
+                    q1[k][e] = xl[at];
+                }
+            float4_t c[2 * kBlocks];
+#pragma unroll
+            for (int i = 0; i < 2 * kBlocks; ++i) {
+                c[i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k) {
+                    const half8 p0 = *reinterpret_cast<const half8*>(ah + (i * 16 + row) * AP + k * 32 + quad * 8);
+                    const half8 p1 = *reinterpret_cast<const half8*>(al + (i * 16 + row) * AP + k * 32 + quad * 8);
+                    if (pairs) {
+                        c[i] = multiply(p1, q0[k], c[i]);
+                        c[i] = multiply(p0, q1[k], c[i]);
+                    }
+                    c[i] = multiply(p0, q0[k], c[i]);
+                }
+            }
+            wavefront_exchange();                          // (all lanes have their columns)
+#pragma unroll
+            for (int i = 0; i < 2 * kBlocks; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int ri = i * 16 + quad * 4 + r, rj = j0 + row, at = ri * XP + rj;
+                    const float v = c[i][r] * a.apply_sum[step] + ((float)xh[at] + (float)xl[at]) * a.apply_old[step];
+                    if (!last) {
+                        split(v, xh[at], xl[at]);
+                    } else {
+                        const int or_ = tall ? rj : ri, oc = tall ? ri : rj;
+                        if (or_ < a.rows && oc < a.cols)
+                            store_typed(a.out, a.out_type, (int64_t)blockIdx.x * a.out_plane + or_ * a.out_stride + oc, v * a.gain);
+                    }
+                }
+        }
+        __syncthreads();
+    }
+}
+
+constexpr int64_t kPad = 64;                   // two fragments of k, four of rows; tiles may be larger
 inline int64_t padded(int64_t v) { return ceil_div(v, kPad) * kPad; }
 inline int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
@@ -269,11 +559,11 @@ double unit_for(double bound) {
     return std::ldexp(1.0, -e);
 }
 
-template <int kTile, int kWavesM, int kWavesN> void product(const Product& p, int terms, int kind, int64_t count, hipStream_t s) {
-    const int64_t tm = p.rows / kTile, tn = p.cols / kTile;
+template <int kTile, int kWavesM, int kWavesN, int kStages> void product(const Product& p, int terms, int kind, int64_t count, hipStream_t s) {
+    const int64_t tm = ceil_div(p.rows, kTile), tn = ceil_div(p.cols, kTile);
     const dim3 grid((unsigned)(kind == kGram || kind == kPoly ? tm * (tm + 1) / 2 : tm * tn), (unsigned)count);
     const dim3 block(kWavesM * kWavesN * 64);
-#define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, TERMS, KIND><<<grid, block, 0, s>>>(p)
+#define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, TERMS, KIND><<<grid, block, 0, s>>>(p)
     if (terms == 3) {
         if (kind == kGram) P2_PRODUCT(3, kGram);
         else if (kind == kPoly) P2_PRODUCT(3, kPoly);
@@ -287,12 +577,38 @@ template <int kTile, int kWavesM, int kWavesN> void product(const Product& p, in
 #undef P2_PRODUCT
 }
 
+// The tile of a product.  What a stage of 32 values of k takes, in us on a compute unit that has one tile of its size
+// (measured, products of 1000 to 4096 rows): 256 x 256 2.45, 192 x 192 1.4, 128 x 128 0.7; of 64 x 64 several share a
+// unit's time, 0.25 for each.  Larger tiles need less of each operand's traffic and smaller ones leave fewer units idle:
+// X X^T of 4096 x 4096 takes 266 us in 136 tiles of 256, 200 in 253 of 192, 240 in 528 of 128, 340 in 2080 of 64, and B X
+// 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.
+void product_by_size(const Product& p, int terms, int kind, int64_t count, hipStream_t s) {
+    auto cost = [&](int64_t tile, double stage, bool shared) {
+        const int64_t down = ceil_div(p.rows, tile), across = ceil_div(p.cols, tile);
+        const int64_t tiles = (kind == kGram || kind == kPoly ? down * (down + 1) / 2 : down * across) * count;
+        return stage * (shared ? std::max(1.0, (double)tiles / 256) : (double)ceil_div(tiles, 256));
+    };
+    const double c64 = cost(64, 0.25, true), c128 = cost(128, 0.7, false), c192 = cost(192, 1.4, false), c256 = cost(256, 2.45, false);
+    const double least = std::min({c64, c128, c192, c256});
+    if (c256 == least) product<256, 2, 4, 2>(p, terms, kind, count, s);
+    else if (c192 == least) product<192, 2, 4, 3>(p, terms, kind, count, s);
+    else if (c128 == least) product<128, 2, 4, 2>(p, terms, kind, count, s);
+    else product<64, 2, 2, 3>(p, terms, kind, count, s);
+}
+
+int64_t norm_parts(int64_t rows, int64_t cols) {           // 8192 values a block, and not more than rows
+    return std::max<int64_t>(1, std::min({kMostNormParts, ceil_div(rows * cols, 8192), rows}));
+}
+
 template <typename T> void to_pairs(const Orthogonalize& a, double unit, double* parts, char* straight, char* turned, int64_t rp, int64_t cp,
                                     int64_t plane, hipStream_t s) {
     const T* g = static_cast<const T*>(a.g);
-    k_newton_norm<T><<<dim3(kNormParts, (unsigned)a.count), dim3(256), 0, s>>>(g, a.stride, a.matrix_stride, a.rows, a.cols, parts);
-    k_newton_scale<T><<<dim3((unsigned)(cp / 32), (unsigned)(rp / 32), (unsigned)a.count), dim3(256), 0, s>>>(
-        g, a.stride, a.matrix_stride, a.rows, a.cols, parts, a.eps, unit, straight, turned, rp, cp, plane);
+    const int n = (int)norm_parts(a.rows, a.cols);
+    int across = 1;
+    while (across < 256 && across * (16 / (int)sizeof(T)) < a.cols) across *= 2;
+    k_newton_norm<T><<<dim3((unsigned)n, (unsigned)a.count), dim3(256), 0, s>>>(g, a.stride, a.matrix_stride, a.rows, a.cols, across, parts);
+    k_newton_scale<T><<<dim3((unsigned)(cp / 64), (unsigned)(rp / 64), (unsigned)a.count), dim3(256), 0, s>>>(
+        g, a.stride, a.matrix_stride, a.rows, a.cols, parts, n, a.eps, unit, straight, turned, rp, cp, plane);
 }
 
 }  // namespace
@@ -307,65 +623,128 @@ bool orthogonalize_bounds(const Orthogonalize& a, double* bounds) {
     return true;
 }
 
+namespace {
+
+// The powers of two that a step's matrices are kept in, as factors of its products.
+struct StepFactors {
+    double unit;                               // of the X that the step makes
+    float gram, poly_old, poly_sum, apply_old, apply_sum;
+};
+StepFactors step_factors(const Orthogonalize& a, int step, double unit) {
+    const double top = a.bounds[step] * 1.001;
+    const double ua = unit_for(top * top), ub = unit_for(square_bound(a.b, a.c, top * top));
+    StepFactors f;
+    f.unit = unit_for(a.bounds[step + 1]);
+    f.gram = (float)(ua / (unit * unit));
+    f.poly_old = (float)(a.b * ub / ua);
+    f.poly_sum = (float)(a.c * ub / (ua * ua));
+    f.apply_old = (float)(a.a * f.unit / unit);
+    f.apply_sum = (float)(f.unit / (ub * unit));
+    return f;
+}
+
+bool is_small(int64_t rows, int64_t cols) {
+    const int64_t m = ceil_div(std::min(rows, cols), 32) * 32, n = ceil_div(std::max(rows, cols), 32) * 32;
+    return m <= 128 && small_bytes(m, n) <= kLdsBytes;
+}
+
+template <typename T, int kBlocks> hipError_t small_as(const Small& p, int64_t count, hipStream_t s) {
+    // (once a process: a block may have all of a compute unit's LDS)
+    static const hipError_t room = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_newton_small<T, kBlocks>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
+    if (room != hipSuccess) return room;
+    k_newton_small<T, kBlocks><<<dim3((unsigned)count), dim3(kSmallBlock), (size_t)small_bytes(32 * kBlocks, p.n), s>>>(p);
+    return hipGetLastError();
+}
+template <typename T> hipError_t small_of(const Small& p, int64_t count, hipStream_t s) {
+    switch (ceil_div(std::min(p.rows, p.cols), 32)) {
+        case 1: return small_as<T, 1>(p, count, s);
+        case 2: return small_as<T, 2>(p, count, s);
+        case 3: return small_as<T, 3>(p, count, s);
+        default: return small_as<T, 4>(p, count, s);
+    }
+}
+
+hipError_t launch_small(const Orthogonalize& a, hipStream_t s) {
+    Small p = {};
+    p.g = a.g; p.out = a.out;
+    p.stride = a.stride; p.matrix_stride = a.matrix_stride; p.out_stride = a.out_stride; p.out_plane = a.out_matrix_stride;
+    p.rows = (int32_t)a.rows; p.cols = (int32_t)a.cols; p.n = (int32_t)(ceil_div(std::max(a.rows, a.cols), 32) * 32);
+    p.out_type = a.out_type; p.steps = a.steps; p.last_terms = a.out_type == P2_BF16 ? 1 : 3;
+    p.eps = a.eps;
+    double unit = p.unit = unit_for(a.bounds[0]);
+    for (int i = 0; i < a.steps; ++i) {
+        const StepFactors f = step_factors(a, i, unit);
+        p.gram[i] = f.gram; p.poly_old[i] = f.poly_old; p.poly_sum[i] = f.poly_sum; p.apply_old[i] = f.apply_old; p.apply_sum[i] = f.apply_sum;
+        unit = f.unit;
+    }
+    p.gain = (float)(a.scale / unit);
+    if (a.type == P2_F32) return small_of<float>(p, a.count, s);
+    if (a.type == P2_BF16) return small_of<bf16_t>(p, a.count, s);
+    return small_of<half_t>(p, a.count, s);
+}
+
+}  // namespace
+
 int64_t orthogonalize_workspace(int64_t count, int64_t rows, int64_t cols) {
+    if (is_small(rows, cols)) return 0;
     const int64_t m = padded(std::min(rows, cols)), n = padded(std::max(rows, cols));
-    return align256(count * kNormParts * 8) + count * 4 * (3 * m * n + 2 * m * m);
+    return align256(count * norm_parts(rows, cols) * 8) + count * 4 * (3 * m * n + 2 * m * m);
 }
 
 hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
+    if (is_small(a.rows, a.cols)) return launch_small(a, s);
     const bool tall = a.rows > a.cols;
     const int64_t m = padded(std::min(a.rows, a.cols)), n = padded(std::max(a.rows, a.cols));
     const int64_t xb = m * n * 4, ab = m * m * 4;
     char* w = static_cast<char*>(a.workspace);
     double* parts = reinterpret_cast<double*>(w);
-    w += align256(a.count * kNormParts * 8);
+    w += align256(a.count * norm_parts(a.rows, a.cols) * 8);
     char* x = w; w += a.count * xb;
     char* xt[2];
     xt[0] = w; w += a.count * xb;
     xt[1] = w; w += a.count * xb;
     char* ga = w; w += a.count * ab;
     char* gb = w;
-    double ux = unit_for(a.bounds[0]);
+    double unit = unit_for(a.bounds[0]);
     char* straight = tall ? xt[0] : x;
     char* turned = tall ? x : xt[0];
     const int64_t rp = tall ? n : m, cp = tall ? m : n;
-    if (a.type == P2_F32) to_pairs<float>(a, ux, parts, straight, turned, rp, cp, xb, s);
-    else if (a.type == P2_BF16) to_pairs<bf16_t>(a, ux, parts, straight, turned, rp, cp, xb, s);
-    else to_pairs<half_t>(a, ux, parts, straight, turned, rp, cp, xb, s);
+    if (a.type == P2_F32) to_pairs<float>(a, unit, parts, straight, turned, rp, cp, xb, s);
+    else if (a.type == P2_BF16) to_pairs<bf16_t>(a, unit, parts, straight, turned, rp, cp, xb, s);
+    else to_pairs<half_t>(a, unit, parts, straight, turned, rp, cp, xb, s);
     hipError_t e = hipGetLastError();
     for (int i = 0; i < a.steps && e == hipSuccess; ++i) {
         const bool last = i + 1 == a.steps;
         const int terms = last && a.out_type == P2_BF16 ? 1 : 3;
-        const double top = a.bounds[i] * 1.001;
-        const double ua = unit_for(top * top), ub = unit_for(square_bound(a.b, a.c, top * top)), un = unit_for(a.bounds[i + 1]);
+        const StepFactors f = step_factors(a, i, unit);
         Product p = {};
         p.p = p.q = x; p.p_plane = p.q_plane = xb;
         p.straight = ga; p.old_plane = ab;
         p.k = n; p.rows = p.cols = m;
-        p.sum_factor = (float)(ua / (ux * ux));
-        product<128, 2, 2>(p, terms, kGram, a.count, s);
+        p.sum_factor = f.gram;
+        product_by_size(p, terms, kGram, a.count, s);
         p = {};
         p.p = p.q = p.old = ga; p.p_plane = p.q_plane = p.old_plane = ab;
         p.straight = gb;
         p.k = p.rows = p.cols = m;
-        p.old_factor = (float)(a.b * ub / ua);
-        p.sum_factor = (float)(a.c * ub / (ua * ua));
-        product<128, 2, 2>(p, terms, kPoly, a.count, s);
+        p.old_factor = f.poly_old;
+        p.sum_factor = f.poly_sum;
+        product_by_size(p, terms, kPoly, a.count, s);
         p = {};
         p.p = gb; p.p_plane = ab;
         p.q = p.old = xt[i & 1]; p.q_plane = p.old_plane = xb;
         p.straight = x; p.turned = xt[(i + 1) & 1];
         p.k = p.rows = m; p.cols = n;
-        p.old_factor = (float)(a.a * un / ux);
-        p.sum_factor = (float)(un / (ub * ux));
+        p.old_factor = f.apply_old;
+        p.sum_factor = f.apply_sum;
         if (last) {
             p.out = a.out; p.out_plane = a.out_matrix_stride; p.out_stride = a.out_stride;
             p.out_rows = std::min(a.rows, a.cols); p.out_cols = std::max(a.rows, a.cols);
             p.out_turned = tall; p.out_type = a.out_type;
-            p.gain = (float)(a.scale / un);
+            p.gain = (float)(a.scale / f.unit);
         }
-        product<128, 2, 2>(p, terms, last ? kLast : kApply, a.count, s);
-        ux = un;
+        product_by_size(p, terms, last ? kLast : kApply, a.count, s);
+        unit = f.unit;
         e = hipGetLastError();
     }
     return e;

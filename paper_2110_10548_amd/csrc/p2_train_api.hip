@@ -249,8 +249,9 @@ int32_t p2_orthogonalize(const void* g, int32_t type, int64_t stride, int64_t ma
         a.a = coefficients[0]; a.b = coefficients[1]; a.c = coefficients[2]; a.eps = eps; a.scale = scale;
         a.bounds = bounds;
         if (!orthogonalize_bounds(a, bounds)) return api_fail(P2_EUNSUPPORTED, "with these coefficients singular values may pass 2^10");
-        if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
-        if (workspace_bytes < orthogonalize_workspace(count, rows, cols)) return api_fail(P2_ENOSPC, "workspace too small");
+        const int64_t room = orthogonalize_workspace(count, rows, cols);
+        if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
         return launched(launch_orthogonalize(a, (hipStream_t)stream), "orthogonalize");
     });
 }
