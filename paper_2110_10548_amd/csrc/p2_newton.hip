@@ -27,6 +27,7 @@ typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4), may_alias));
 
 constexpr int kLine = 128;                     // bytes of 32 pairs
+constexpr int64_t kUnits = 256;                // compute units
 constexpr int64_t kMostNormParts = 1024;       // blocks that a matrix's norm is summed by
 
 // Byte of the high half of pair k in a row; its low half is 64 further.
@@ -126,20 +127,22 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(cons
     }
 }
 
-enum : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
+enum : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3, kPart = 4 };
 
 struct Product {
     const char* p; const char* q;              // pairs: rows of P and of Q
     const char* old;                           // kPoly: A; kApply, kLast: X turned
     char* straight;                            // result (kGram, kPoly: the whole result)
     char* turned;
-    void* out;                                 // kLast
+    void* out;                                 // kLast; kPart: sums of the parts of k, [parts][matrices][rows][cols]
     int64_t p_plane, q_plane, old_plane, out_plane;      // from matrix to matrix: bytes (out: elements)
     int64_t k;                                 // summed length, padded
     int64_t rows, cols;                        // padded size of the result
     int64_t out_rows, out_cols, out_stride;    // kLast: the result's own, and whether it is to be written turned
     float old_factor, sum_factor, gain;        // (old * old_factor + sum * sum_factor) * gain
     int32_t out_turned, out_type;
+    int32_t tiles, parts;                      // blocks of a matrix; kPart: parts that k is cut into
+    int64_t matrices;
 };
 
 // Four values in a row of the result, of which `n` are inside it.
@@ -189,18 +192,26 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     constexpr int kStepBytes = kTerms == 3 ? kLine : 2 * kLine;
     constexpr int kLoads = kTile / 8 / kWaves;             // of each operand a stage; one brings 8 rows
     constexpr int kAhead = kStages - 1;
+    constexpr int kPerRow = (2 * kLoads + FM - 1) / FM;    // loads issued with a row of fragments: all of them in the first half
     static_assert(kLoads * 8 * kWaves == kTile && FM * kWavesM * 16 == kTile && FN * kWavesN * 16 == kTile, "rows are dealt out evenly");
     static_assert(2 * kLoads * (kAhead - 1) < 64, "the loads' counter");
     __shared__ __attribute__((aligned(1024))) char lds[kStages][2][kTile * kLine];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // Blocks go to the eight dies in turn: tile numbers are dealt out so that a die's tiles are neighbours.
-    int t = blockIdx.x;
+    // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, of as few matrices as can be.
+    int t;
     {
-        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = t & 7;
-        t = die * whole + min(die, rest) + (t >> 3);
+        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = blockIdx.x & 7;
+        t = die * whole + min(die, rest) + (blockIdx.x >> 3);
+    }
+    const int64_t matrix = t / a.tiles;
+    t %= a.tiles;
+    int part_of_k = 0;
+    if constexpr (kKind == kPart) {
+        part_of_k = t % a.parts;
+        t /= a.parts;
     }
     int bi, bj;
-    if constexpr (kKind == kGram || kKind == kPoly) {      // the t-th tile on or below the diagonal
+    if constexpr (kKind == kGram || kKind == kPart || kKind == kPoly) {      // the t-th tile on or below the diagonal
         bi = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
         while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
         while (bi * (bi + 1) / 2 > t) --bi;
@@ -215,25 +226,29 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     auto rows_of = [&](const char* m, int64_t first, int64_t rows) {
         return Rows(m + first * pitch, (int)(min(rows - first, (int64_t)kTile) * pitch));
     };
-    const Rows p = rows_of(a.p + blockIdx.y * a.p_plane, (int64_t)bi * kTile, a.rows);
-    const Rows q = rows_of(a.q + blockIdx.y * a.q_plane, (int64_t)bj * kTile, a.cols);
+    const Rows p = rows_of(a.p + matrix * a.p_plane, (int64_t)bi * kTile, a.rows);
+    const Rows q = rows_of(a.q + matrix * a.q_plane, (int64_t)bj * kTile, a.cols);
     const int part = (lane & 7) ^ (lane >> 3);
     const int from = (wave * kLoads * 8 + (lane >> 3)) * (int)pitch + (kTerms == 3 ? part * 16 : (part >> 2) * kLine + (part & 3) * 16);
-    auto bring = [&](int stage, int at) {
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const int src = from + l * 8 * (int)pitch;
-            const int dst = (wave * kLoads + l) * 1024;
-            p.bring(&lds[stage][0][dst], src, at);
-            q.bring(&lds[stage][1][dst], src, at);
-        }
+    auto bring_one = [&](int stage, int l, int at) {       // the l-th load of each operand
+        const int src = from + l * 8 * (int)pitch;
+        const int dst = (wave * kLoads + l) * 1024;
+        p.bring(&lds[stage][0][dst], src, at);
+        q.bring(&lds[stage][1][dst], src, at);
     };
     const int wm = wave / kWavesN, wn = wave % kWavesN;
     const int row = lane & 15, quad = lane >> 4;
     const int64_t i0 = (int64_t)bi * kTile + wm * FM * 16, j0 = (int64_t)bj * kTile + wn * FN * 16;
-    const int steps = (int)(a.k / (kTerms == 3 ? 32 : 64));
+    int steps = (int)(a.k / (kTerms == 3 ? 32 : 64)), begin = 0;
+    if constexpr (kKind == kPart) {                        // (every part has a step at least)
+        begin = (int)((int64_t)steps * part_of_k / a.parts);
+        steps = (int)((int64_t)steps * (part_of_k + 1) / a.parts) - begin;
+    }
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) if (s < steps) bring(s, s * kStepBytes);
+    for (int s = 0; s < kAhead; ++s)
+        if (s < steps)
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) bring_one(s, l, (begin + s) * kStepBytes);
     float4_t acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -245,33 +260,56 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     for (int s = 0; s < steps; ++s) {
         if (s + kAhead <= steps) stage_barrier<2 * kLoads * (kAhead - 1)>();
         else stage_barrier<0>();
-        if (s + kAhead < steps) bring(next, (s + kAhead) * kStepBytes);
+        const bool more = s + kAhead < steps;
+        const int at = (begin + s + kAhead) * kStepBytes;
         const char* tp = lds[stage][0] + wm * FM * 16 * kLine;
         const char* tq = lds[stage][1] + wn * FN * 16 * kLine;
-        next = stage;
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-        half8 q0[FN], q1[FN];
+        half8 q0[FN], q1[FN], p0, p1;
+        p0 = *reinterpret_cast<const half8*>(tp + at0);
+        p1 = *reinterpret_cast<const half8*>(tp + at1);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             q0[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at0);
             q1[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at1);
         }
+        // The loads of a stage to come are spread over the first rows of fragments: issued together they would hold up this
+        // stage's products for as long as the compute unit's address unit takes for all of them.
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const half8 p0 = *reinterpret_cast<const half8*>(tp + i * 16 * kLine + at0);
-            const half8 p1 = *reinterpret_cast<const half8*>(tp + i * 16 * kLine + at1);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                if constexpr (kTerms == 3) {
-                    acc[i][j] = multiply(p1, q0[j], acc[i][j]);
-                    acc[i][j] = multiply(p0, q1[j], acc[i][j]);
-                    acc[i][j] = multiply(p0, q0[j], acc[i][j]);
-                } else {
-                    acc[i][j] = multiply(p0, q0[j], acc[i][j]);
-                    acc[i][j] = multiply(p1, q1[j], acc[i][j]);
-                }
+            half8 n0, n1;
+            if (i + 1 < FM) {
+                n0 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at0);
+                n1 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at1);
             }
+            if (more)
+#pragma unroll
+                for (int l = i * kPerRow; l < (i + 1) * kPerRow && l < kLoads; ++l) bring_one(next, l, at);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p1, q0[j], acc[i][j]) : multiply(p0, q0[j], acc[i][j]);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p0, q1[j], acc[i][j]) : multiply(p1, q1[j], acc[i][j]);
+            if constexpr (kTerms == 3)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q0[j], acc[i][j]);
+            p0 = n0;
+            p1 = n1;
+            __builtin_amdgcn_sched_barrier(0);
         }
+        next = stage;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    if constexpr (kKind == kPart) {
+        float* sums = static_cast<float*>(a.out) + (part_of_k * a.matrices + matrix) * a.rows * a.cols;
+#pragma unroll
+        for (int fi = 0; fi < FM; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < FN; ++fj)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t i = i0 + fi * 16 + quad * 4 + r, j = j0 + fj * 16 + row;
+                    if (i < a.rows && j < a.cols) sums[i * a.cols + j] = acc[fi][fj][r];
+                }
+        return;
     }
     stage_barrier<0>();                                    // LDS changes its use: a strip of 16 rows for each wavefront
     // A lane has four rows i of one column j, which are four values in a row of the transpose.  For the result's own rows a
@@ -286,7 +324,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
 #pragma unroll
             for (int fj = 0; fj < FN; ++fj) {
                 if (j0 + fj * 16 >= a.cols) continue;
-                const char* o = a.old + blockIdx.y * a.old_plane + (j0 + fj * 16 + row) * a.rows * 4 + pair_at(i0 + fi * 16 + quad * 4);
+                const char* o = a.old + matrix * a.old_plane + (j0 + fj * 16 + row) * a.rows * 4 + pair_at(i0 + fi * 16 + quad * 4);
                 high[fj] = *reinterpret_cast<const half4*>(o);
                 low[fj] = *reinterpret_cast<const half4*>(o + kLine / 2);
             }
@@ -308,13 +346,13 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
         if (fi + 1 < FM) fetch(fi + 1);
         const int64_t i = i0 + fi * 16 + quad * 4;
         if (kKind != kLast || a.out_turned) {
-            char* t = kKind == kApply ? a.turned + blockIdx.y * a.q_plane : kKind == kLast ? nullptr : a.straight + blockIdx.y * a.old_plane;
+            char* t = kKind == kApply ? a.turned + matrix * a.q_plane : kKind == kLast ? nullptr : a.straight + matrix * a.old_plane;
 #pragma unroll
             for (int fj = 0; fj < FN; ++fj) {
                 const int64_t j = j0 + fj * 16 + row;
                 if constexpr (kKind == kLast) {
                     const float f[4] = {__uint_as_float(w[fj][0]), __uint_as_float(w[fj][1]), __uint_as_float(w[fj][2]), __uint_as_float(w[fj][3])};
-                    if (j < a.out_cols) store_four(a.out, a.out_type, blockIdx.y * a.out_plane + j * a.out_stride + i, a.out_rows - i, f);
+                    if (j < a.out_cols) store_four(a.out, a.out_type, matrix * a.out_plane + j * a.out_stride + i, a.out_rows - i, f);
                 } else {
                     if (j < a.cols) store_pairs(t + j * a.rows * 4 + pair_at(i), w[fj]);
                 }
@@ -333,10 +371,10 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
                 const int64_t ri = i0 + fi * 16 + si, rj = j0 + sj;
                 if constexpr (kKind == kLast) {
                     const float f[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-                    if (ri < a.out_rows) store_four(a.out, a.out_type, blockIdx.y * a.out_plane + ri * a.out_stride + rj, a.out_cols - rj, f);
+                    if (ri < a.out_rows) store_four(a.out, a.out_type, matrix * a.out_plane + ri * a.out_stride + rj, a.out_cols - rj, f);
                 } else if (rj < a.cols) {
                     const uint32_t f[4] = {u.x, u.y, u.z, u.w};
-                    store_pairs(a.straight + blockIdx.y * a.old_plane + ri * a.cols * 4 + pair_at(rj), f);
+                    store_pairs(a.straight + matrix * a.old_plane + ri * a.cols * 4 + pair_at(rj), f);
                 }
             }
             wavefront_exchange();
@@ -344,16 +382,32 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     }
 }
 
+__device__ __forceinline__ float4_t load_halves(const half_t* high, const half_t* low) {
+    const half4 h = *reinterpret_cast<const half4*>(high), l = *reinterpret_cast<const half4*>(low);
+    return float4_t{(float)h[0] + (float)l[0], (float)h[1] + (float)l[1], (float)h[2] + (float)l[2], (float)h[3] + (float)l[3]};
+}
+__device__ __forceinline__ void store_halves(half_t* high, half_t* low, float4_t v) {
+    half4 h, l;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        half_t hr, lr;
+        split(v[r], hr, lr);
+        h[r] = hr;
+        l[r] = lr;
+    }
+    *reinterpret_cast<half4*>(high) = h;
+    *reinterpret_cast<half4*>(low) = l;
+}
+
 // A matrix whose smaller side is at most 32 kBlocks (128) and which fits in LDS goes through all its steps there: one block
-// of eight wavefronts a matrix, one launch altogether.  X lies in rows (highs and lows apart, rows 16 bytes further apart
-// than they are long: 16 rows' pieces lie in different banks), A and then B beside it.  A product's operands come from
+// of eight wavefronts a matrix, one launch altogether.  X lies in rows, highs and lows apart, A and then B beside it.  A product's operands come from
 // there; only X in B X is needed by columns, and a wavefront picks those of its 16 columns up value by value, once for all
 // rows of the result.  What it writes are the same 16 columns, which nobody else reads meanwhile.
 struct Small {
     const void* g; void* out;
     int64_t stride, matrix_stride, out_stride, out_plane;
-    int32_t rows, cols, n;                     // n: the longer side, padded to 32
-    int32_t out_type, steps, last_terms;
+    int32_t rows, cols, n;                     // n: the longer side, padded to 64
+    int32_t out_type, steps;
     double eps, unit;
     float gain;
     float gram[64], poly_old[64], poly_sum[64], apply_old[64], apply_sum[64];
@@ -361,27 +415,62 @@ struct Small {
 constexpr int kSmallBlock = 512;
 constexpr int64_t kLdsBytes = 160 * 1024;
 constexpr int64_t kSmallSpare = 128;                       // for the sums at its beginning
-constexpr int64_t small_bytes(int64_t m, int64_t n) { return 4 * m * (n + 8) + 4 * m * (m + 8) + kSmallSpare; }
+// Halves from row to row of A, and where value (r, c) lies.  16 lanes read 16 bytes each at a time, of rows 0 to 3 and 12 to 15
+// at one place and of 4 to 11 at the next: with rows of 128 bytes (an odd number of them) or of 256, pieces of 16 bytes exchanged
+// by the row's lowest three or four bits, they lie in different banks.  (Rows 16 bytes longer than that: 41 cycles in 100
+// went into conflicts.)
+__host__ __device__ constexpr int small_pitch(int m) { return m <= 64 ? 64 : 128; }
+__host__ __device__ constexpr int small_mask(int pitch) { return pitch % 128 ? 7 : 15; }
+__device__ __forceinline__ int small_at(int r, int c, int pitch, int mask) { return r * pitch + (((c >> 3) ^ (r & mask)) << 3 | (c & 7)); }
+inline int64_t small_length(int64_t rows, int64_t cols) { return ceil_div(std::max(rows, cols), 64) * 64; }
+inline int64_t small_bytes(int64_t m, int64_t n) {         // X, A, and where eight wavefronts share A's only blocks their sums
+    return kSmallSpare + 4 * m * n + 4 * m * small_pitch((int)m) + (m == 32 ? kSmallBlock / 64 * 2 * 64 * 16 : 0);
+}
 
 template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) void k_newton_small(Small a) {
     constexpr int M = 32 * kBlocks, kWaves = kSmallBlock / 64;
-    constexpr int kOwn = (kBlocks * kBlocks + kWaves - 1) / kWaves;        // 32 x 32 blocks of A that a wavefront has
-    constexpr int AP = M + 8;
+    // A wavefront has one block of A, of FM x FN fragments of 16 x 16; where there are only two blocks four wavefronts share
+    // one's sum, every fourth 32 values of k each.
+    constexpr int FM = kBlocks < 3 ? 1 : 2, FN = kBlocks < 3 ? 2 : kBlocks;
+    constexpr int kAcross = M / (16 * FN), kAll = M / (16 * FM) * kAcross, kSplit = kBlocks == 1 ? kWaves / kAll : 1;
+    constexpr int AP = small_pitch(M), kAMask = small_mask(AP);
     extern __shared__ __attribute__((aligned(16))) char small_lds[];
-    const int XP = a.n + 8;
+    const int XP = a.n, x_mask = small_mask(a.n);
     half_t* xh = reinterpret_cast<half_t*>(small_lds + kSmallSpare);
     half_t* xl = xh + M * XP;
     half_t* ah = xl + M * XP;
     half_t* al = ah + M * AP;
     double* buf = reinterpret_cast<double*>(small_lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, quad = lane >> 4;
+    const int block = wave % (kWaves / kSplit), share = wave / (kWaves / kSplit);
+    const bool has_block = block < kAll;
+    const int i0 = block / kAcross * FM * 16, j0 = block % kAcross * FN * 16;
     const T* g = static_cast<const T*>(a.g) + (int64_t)blockIdx.x * a.matrix_stride;
     const bool tall = a.rows > a.cols;
-    const int rp = tall ? a.n : M, cp = tall ? M : a.n;    // padded sizes as G lies
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    // Vectors of 16 bytes, four of a thread's under way at a time: once for the norm, once more (from the cache) for LDS.
+    constexpr int V = 16 / sizeof(T);
+    const int across = (a.cols + V - 1) / V, vecs = a.rows * across;
+    auto each = [&](auto&& use) {
+        for (int v0 = threadIdx.x; v0 < vecs; v0 += 4 * kSmallBlock) {
+            float v[4][V];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = v0 + u * kSmallBlock, r = at / across, c = at % across * V;
+                load_part<T, V>(g + (int64_t)r * a.stride + c, at < vecs ? a.cols - c : 0, v[u], 0.0f);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = v0 + u * kSmallBlock, r = at / across, c = at % across * V;
+                if (at < vecs) use(r, c, v[u]);
+            }
+        }
+    };
     double s = 0.0;
-    for (int r = ty; r < a.rows; r += kSmallBlock / 32)
-        for (int c = tx; c < a.cols; c += 32) { const double v = (double)(float)g[r * a.stride + c]; s += v * v; }
+    each([&](int, int, const float (&v)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += (double)v[e] * (double)v[e];
+    });
+    for (int i = threadIdx.x; i < 2 * M * XP / 8; i += kSmallBlock) reinterpret_cast<half8*>(xh)[i] = half8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
     if (lane == 0) buf[wave] = s;
@@ -390,135 +479,136 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += buf[w];
     const double factor = scale_factor(s, a.eps, a.unit);
-    for (int r = ty; r < rp; r += kSmallBlock / 32)
-        for (int c = tx; c < cp; c += 32) {
-            const float v = r < a.rows && c < a.cols ? (float)((double)(float)g[r * a.stride + c] * factor) : 0.0f;
-            const int at = tall ? c * XP + r : r * XP + c;
-            split(v, xh[at], xl[at]);
-        }
+    each([&](int r, int c, const float (&v)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (c + e < a.cols) {
+                const int at = tall ? small_at(c + e, r, XP, x_mask) : small_at(r, c + e, XP, x_mask);
+                split((float)((double)v[e] * factor), xh[at], xl[at]);
+            }
+    });
     __syncthreads();
     for (int step = 0; step < a.steps; ++step) {
-        const bool last = step + 1 == a.steps, pairs = !last || a.last_terms == 3;
-        float4_t acc[kOwn][2][2];
-        // C = P P^T for this wavefront's blocks
-        auto square = [&](const half_t* ph, const half_t* pl, int pitch, int length) {
+        const bool last = step + 1 == a.steps;
+        float4_t acc[FM][FN];
+        auto square = [&](const half_t* ph, const half_t* pl, int pitch, int mask, int length) {     // P P^T
 #pragma unroll
-            for (int o = 0; o < kOwn; ++o) {
-                const int b = wave + o * kWaves;
-                if (b >= kBlocks * kBlocks) break;
-                const int pi = (b / kBlocks * 32 + row) * pitch + quad * 8, pj = (b % kBlocks * 32 + row) * pitch + quad * 8;
+            for (int x = 0; x < FM; ++x)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int y = 0; y < FN; ++y) acc[x][y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            const int pi = (i0 + row) * pitch, pj = (j0 + row) * pitch;
+            if (has_block)
+                for (int k = share * 32; k < length; k += 32 * kSplit) {
+                    half8 p0[FM], p1[FM], q0[FN], q1[FN];
+                    const int kk = (((k >> 3) + quad) ^ (row & mask)) * 8;           // (of 16 rows in a row: the same for all of them)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) acc[o][x][y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-                for (int k = 0; k < length; k += 32) {
-                    half8 p0[2], p1[2], q0[2], q1[2];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        p0[x] = *reinterpret_cast<const half8*>(ph + pi + x * 16 * pitch + k);
-                        q0[x] = *reinterpret_cast<const half8*>(ph + pj + x * 16 * pitch + k);
-                        p1[x] = *reinterpret_cast<const half8*>(pl + pi + x * 16 * pitch + k);
-                        q1[x] = *reinterpret_cast<const half8*>(pl + pj + x * 16 * pitch + k);
-                    }
-                    if (pairs) {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p1[x], q0[y], acc[o][x][y]);
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p0[x], q1[y], acc[o][x][y]);
+                    for (int x = 0; x < FM; ++x) {
+                        p0[x] = *reinterpret_cast<const half8*>(ph + pi + x * 16 * pitch + kk);
+                        p1[x] = *reinterpret_cast<const half8*>(pl + pi + x * 16 * pitch + kk);
                     }
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
+                    for (int y = 0; y < FN; ++y) {
+                        q0[y] = *reinterpret_cast<const half8*>(ph + pj + y * 16 * pitch + kk);
+                        q1[y] = *reinterpret_cast<const half8*>(pl + pj + y * 16 * pitch + kk);
+                    }
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) acc[o][x][y] = multiply(p0[x], q0[y], acc[o][x][y]);
+                    for (int x = 0; x < FM; ++x)
+#pragma unroll
+                        for (int y = 0; y < FN; ++y) acc[x][y] = multiply(p1[x], q0[y], acc[x][y]);
+#pragma unroll
+                    for (int x = 0; x < FM; ++x)
+#pragma unroll
+                        for (int y = 0; y < FN; ++y) acc[x][y] = multiply(p0[x], q1[y], acc[x][y]);
+#pragma unroll
+                    for (int x = 0; x < FM; ++x)
+#pragma unroll
+                        for (int y = 0; y < FN; ++y) acc[x][y] = multiply(p0[x], q0[y], acc[x][y]);
+                }
+            if constexpr (kSplit > 1) {                    // the shares' sums in their order
+                float4_t* part = reinterpret_cast<float4_t*>(al + M * AP);
+#pragma unroll
+                for (int y = 0; y < FN; ++y) part[(wave * FN + y) * 64 + lane] = acc[0][y];
+                __syncthreads();
+#pragma unroll
+                for (int y = 0; y < FN; ++y) {
+                    acc[0][y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int p = 0; p < kSplit; ++p) acc[0][y] += part[((p * kAll + block) * FN + y) * 64 + lane];
                 }
             }
         };
-        // acc * sum_factor (+ A * old_factor) for this wavefront's blocks; the result is symmetric, so a lane's four rows of one
-        // column are four values of a row
-        auto place = [&](float sum_factor, float old_factor, bool old, bool write) {
+        // A and B are symmetric: a lane's four rows of one column are four values of a row
+        auto at_of = [&](int x, int y) { return small_at(j0 + y * 16 + row, i0 + x * 16 + quad * 4, AP, kAMask); };
+        auto place = [&](float factor) {
+            if (!has_block || share) return;
 #pragma unroll
-            for (int o = 0; o < kOwn; ++o) {
-                const int b = wave + o * kWaves;
-                if (b >= kBlocks * kBlocks) break;
+            for (int x = 0; x < FM; ++x)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int at = (b % kBlocks * 32 + y * 16 + row) * AP + b / kBlocks * 32 + x * 16 + quad * 4;
-                        if (old) {
-                            const half4 h = *reinterpret_cast<const half4*>(ah + at), l = *reinterpret_cast<const half4*>(al + at);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[o][x][y][r] = acc[o][x][y][r] * sum_factor + ((float)h[r] + (float)l[r]) * old_factor;
-                        }
-                        if (write) {
-                            half4 h, l;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                half_t hr, lr;
-                                split(old ? acc[o][x][y][r] : acc[o][x][y][r] * sum_factor, hr, lr);
-                                h[r] = hr;
-                                l[r] = lr;
-                            }
-                            *reinterpret_cast<half4*>(ah + at) = h;
-                            *reinterpret_cast<half4*>(al + at) = l;
-                        }
-                    }
-            }
+                for (int y = 0; y < FN; ++y) store_halves(ah + at_of(x, y), al + at_of(x, y), acc[x][y] * factor);
         };
-        square(xh, xl, XP, a.n);
-        place(a.gram[step], 0.0f, false, true);
+        square(xh, xl, XP, x_mask, a.n);
+        place(a.gram[step]);
         __syncthreads();
-        square(ah, al, AP, M);
-        place(a.poly_sum[step], a.poly_old[step], true, false);
+        square(ah, al, AP, kAMask, M);
+        if (has_block)
+#pragma unroll
+            for (int x = 0; x < FM; ++x)
+#pragma unroll
+                for (int y = 0; y < FN; ++y)
+                    acc[x][y] = acc[x][y] * a.poly_sum[step] + load_halves(ah + at_of(x, y), al + at_of(x, y)) * a.poly_old[step];
         __syncthreads();                                   // everybody has read A
-        place(1.0f, 0.0f, false, true);
+        place(1.0f);
         __syncthreads();
 #pragma unroll 1
-        for (int j0 = wave * 16; j0 < a.n; j0 += kWaves * 16) {
+        for (int jb = wave * 16; jb < a.n; jb += kWaves * 16) {
             half8 q0[kBlocks], q1[kBlocks];
 #pragma unroll
             for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int at = (k * 32 + quad * 8 + e) * XP + j0 + row;
+                    const int at = small_at(k * 32 + quad * 8 + e, jb + row, XP, x_mask);
                     q0[k][e] = xh[at];
                     q1[k][e] = xl[at];
                 }
+            // columns of X times rows of B: a lane has four columns j of one row i
             float4_t c[2 * kBlocks];
 #pragma unroll
             for (int i = 0; i < 2 * kBlocks; ++i) {
                 c[i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < kBlocks; ++k) {
-                    const half8 p0 = *reinterpret_cast<const half8*>(ah + (i * 16 + row) * AP + k * 32 + quad * 8);
-                    const half8 p1 = *reinterpret_cast<const half8*>(al + (i * 16 + row) * AP + k * 32 + quad * 8);
-                    if (pairs) {
-                        c[i] = multiply(p1, q0[k], c[i]);
-                        c[i] = multiply(p0, q1[k], c[i]);
-                    }
-                    c[i] = multiply(p0, q0[k], c[i]);
+                    const int at = small_at(i * 16 + row, k * 32 + quad * 8, AP, kAMask);
+                    const half8 p0 = *reinterpret_cast<const half8*>(ah + at), p1 = *reinterpret_cast<const half8*>(al + at);
+                    c[i] = multiply(q0[k], p1, c[i]);
+                    c[i] = multiply(q1[k], p0, c[i]);
+                    c[i] = multiply(q0[k], p0, c[i]);
                 }
+            }
+            // all old values before the first new one: no read then waits for a write
+#pragma unroll
+            for (int i = 0; i < 2 * kBlocks; ++i) {
+                const int at = small_at(i * 16 + row, jb + quad * 4, XP, x_mask);
+                c[i] = c[i] * a.apply_sum[step] + load_halves(xh + at, xl + at) * a.apply_old[step];
             }
             wavefront_exchange();                          // (all lanes have their columns)
 #pragma unroll
-            for (int i = 0; i < 2 * kBlocks; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int ri = i * 16 + quad * 4 + r, rj = j0 + row, at = ri * XP + rj;
-                    const float v = c[i][r] * a.apply_sum[step] + ((float)xh[at] + (float)xl[at]) * a.apply_old[step];
-                    if (!last) {
-                        split(v, xh[at], xl[at]);
+            for (int i = 0; i < 2 * kBlocks; ++i) {
+                const int ri = i * 16 + row, rj = jb + quad * 4;
+                if (!last) {
+                    const int at = small_at(ri, rj, XP, x_mask);
+                    store_halves(xh + at, xl + at, c[i]);
+                } else if (ri < (tall ? a.cols : a.rows)) {
+                    const float v[4] = {c[i][0] * a.gain, c[i][1] * a.gain, c[i][2] * a.gain, c[i][3] * a.gain};
+                    const int64_t base = (int64_t)blockIdx.x * a.out_plane;
+                    if (!tall) {
+                        store_four(a.out, a.out_type, base + ri * a.out_stride + rj, a.cols - rj, v);
                     } else {
-                        const int or_ = tall ? rj : ri, oc = tall ? ri : rj;
-                        if (or_ < a.rows && oc < a.cols)
-                            store_typed(a.out, a.out_type, (int64_t)blockIdx.x * a.out_plane + or_ * a.out_stride + oc, v * a.gain);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (rj + r < a.rows) store_typed(a.out, a.out_type, base + (rj + r) * a.out_stride + ri, v[r]);
                     }
                 }
+            }
         }
         __syncthreads();
     }
@@ -559,21 +649,61 @@ double unit_for(double bound) {
     return std::ldexp(1.0, -e);
 }
 
-template <int kTile, int kWavesM, int kWavesN, int kStages> void product(const Product& p, int terms, int kind, int64_t count, hipStream_t s) {
-    const int64_t tm = ceil_div(p.rows, kTile), tn = ceil_div(p.cols, kTile);
-    const dim3 grid((unsigned)(kind == kGram || kind == kPoly ? tm * (tm + 1) / 2 : tm * tn), (unsigned)count);
+// A = sum of its parts, in their order, as pairs on both sides of the diagonal: a block takes a tile of 64 x 64 on or below it.
+__global__ __launch_bounds__(256) void k_newton_join(const float* sums, int32_t parts, int64_t matrices, int64_t m, float factor, char* to, int64_t plane) {
+    __shared__ float tile[64][65];
+    int bi = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
+    while ((bi + 1) * (bi + 2) / 2 <= (int)blockIdx.x) ++bi;
+    while (bi * (bi + 1) / 2 > (int)blockIdx.x) --bi;
+    const int bj = (int)blockIdx.x - bi * (bi + 1) / 2;
+    const int64_t matrix = blockIdx.y, i0 = (int64_t)bi * 64, j0 = (int64_t)bj * 64;
+    const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
+    char* out = to + matrix * plane;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int64_t i = i0 + y + n * 16;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < parts; ++p) {
+            float w[4];
+            load_vec<float, 4>(sums + ((p * matrices + matrix) * m + i) * m + j0 + x, w);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += w[q];
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v[q] *= factor;
+            tile[y + n * 16][x + q] = v[q];
+            w[q] = pack(v[q]);
+        }
+        if (bi != bj) store_pairs(out + i * m * 4 + pair_at(j0 + x), w);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = pack(tile[x + q][y + n * 16]);
+        store_pairs(out + (j0 + y + n * 16) * m * 4 + pair_at(i0 + x), w);
+    }
+}
+
+int64_t tiles_of(const Product& p, int64_t tile, int kind) {
+    const int64_t down = ceil_div(p.rows, tile), across = ceil_div(p.cols, tile);
+    return kind == kGram || kind == kPart || kind == kPoly ? down * (down + 1) / 2 : down * across;
+}
+
+template <int kTile, int kWavesM, int kWavesN, int kStages> void product(Product p, int terms, int kind, hipStream_t s) {
+    p.tiles = (int32_t)tiles_of(p, kTile, kind) * (kind == kPart ? p.parts : 1);
+    const dim3 grid((unsigned)(p.tiles * p.matrices));
     const dim3 block(kWavesM * kWavesN * 64);
 #define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, TERMS, KIND><<<grid, block, 0, s>>>(p)
-    if (terms == 3) {
-        if (kind == kGram) P2_PRODUCT(3, kGram);
-        else if (kind == kPoly) P2_PRODUCT(3, kPoly);
-        else if (kind == kApply) P2_PRODUCT(3, kApply);
-        else P2_PRODUCT(3, kLast);
-    } else {
-        if (kind == kGram) P2_PRODUCT(1, kGram);
-        else if (kind == kPoly) P2_PRODUCT(1, kPoly);
-        else P2_PRODUCT(1, kLast);
-    }
+    if (kind == kGram && terms == 3) P2_PRODUCT(3, kGram);
+    else if (kind == kGram) P2_PRODUCT(1, kGram);
+    else if (kind == kPoly) P2_PRODUCT(3, kPoly);
+    else if (kind == kApply) P2_PRODUCT(3, kApply);
+    else if (terms == 3) P2_PRODUCT(3, kLast);
+    else P2_PRODUCT(1, kLast);
 #undef P2_PRODUCT
 }
 
@@ -582,18 +712,24 @@ template <int kTile, int kWavesM, int kWavesN, int kStages> void product(const P
 // unit's time, 0.25 for each.  Larger tiles need less of each operand's traffic and smaller ones leave fewer units idle:
 // X X^T of 4096 x 4096 takes 266 us in 136 tiles of 256, 200 in 253 of 192, 240 in 528 of 128, 340 in 2080 of 64, and B X
 // 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.
-void product_by_size(const Product& p, int terms, int kind, int64_t count, hipStream_t s) {
+void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     auto cost = [&](int64_t tile, double stage, bool shared) {
-        const int64_t down = ceil_div(p.rows, tile), across = ceil_div(p.cols, tile);
-        const int64_t tiles = (kind == kGram || kind == kPoly ? down * (down + 1) / 2 : down * across) * count;
-        return stage * (shared ? std::max(1.0, (double)tiles / 256) : (double)ceil_div(tiles, 256));
+        const int64_t tiles = tiles_of(p, tile, kind) * p.matrices;
+        return stage * (shared ? std::max(1.0, (double)tiles / kUnits) : (double)ceil_div(tiles, kUnits));
     };
     const double c64 = cost(64, 0.25, true), c128 = cost(128, 0.7, false), c192 = cost(192, 1.4, false), c256 = cost(256, 2.45, false);
     const double least = std::min({c64, c128, c192, c256});
-    if (c256 == least) product<256, 2, 4, 2>(p, terms, kind, count, s);
-    else if (c192 == least) product<192, 2, 4, 3>(p, terms, kind, count, s);
-    else if (c128 == least) product<128, 2, 4, 2>(p, terms, kind, count, s);
-    else product<64, 2, 2, 3>(p, terms, kind, count, s);
+    if (c256 == least) product<256, 2, 4, 2>(p, terms, kind, s);
+    else if (c192 == least) product<192, 2, 4, 3>(p, terms, kind, s);
+    else if (c128 == least) product<128, 2, 4, 2>(p, terms, kind, s);
+    else product<64, 2, 2, 3>(p, terms, kind, s);
+}
+
+// X X^T of a short and long X has few tiles and a long sum: it is cut into as many parts as there are compute units for, of 16
+// stages at least, whose sums k_newton_join adds up.  1: it is not cut.
+int64_t gram_parts(int64_t count, int64_t m, int64_t n) {
+    const int64_t down = ceil_div(m, 64), tiles = down * (down + 1) / 2 * count;
+    return std::max<int64_t>(1, std::min(kUnits / tiles, n / 512));
 }
 
 int64_t norm_parts(int64_t rows, int64_t cols) {           // 8192 values a block, and not more than rows
@@ -644,7 +780,7 @@ StepFactors step_factors(const Orthogonalize& a, int step, double unit) {
 }
 
 bool is_small(int64_t rows, int64_t cols) {
-    const int64_t m = ceil_div(std::min(rows, cols), 32) * 32, n = ceil_div(std::max(rows, cols), 32) * 32;
+    const int64_t m = ceil_div(std::min(rows, cols), 32) * 32, n = small_length(rows, cols);
     return m <= 128 && small_bytes(m, n) <= kLdsBytes;
 }
 
@@ -668,8 +804,8 @@ hipError_t launch_small(const Orthogonalize& a, hipStream_t s) {
     Small p = {};
     p.g = a.g; p.out = a.out;
     p.stride = a.stride; p.matrix_stride = a.matrix_stride; p.out_stride = a.out_stride; p.out_plane = a.out_matrix_stride;
-    p.rows = (int32_t)a.rows; p.cols = (int32_t)a.cols; p.n = (int32_t)(ceil_div(std::max(a.rows, a.cols), 32) * 32);
-    p.out_type = a.out_type; p.steps = a.steps; p.last_terms = a.out_type == P2_BF16 ? 1 : 3;
+    p.rows = (int32_t)a.rows; p.cols = (int32_t)a.cols; p.n = (int32_t)small_length(a.rows, a.cols);
+    p.out_type = a.out_type; p.steps = a.steps;
     p.eps = a.eps;
     double unit = p.unit = unit_for(a.bounds[0]);
     for (int i = 0; i < a.steps; ++i) {
@@ -688,7 +824,8 @@ hipError_t launch_small(const Orthogonalize& a, hipStream_t s) {
 int64_t orthogonalize_workspace(int64_t count, int64_t rows, int64_t cols) {
     if (is_small(rows, cols)) return 0;
     const int64_t m = padded(std::min(rows, cols)), n = padded(std::max(rows, cols));
-    return align256(count * norm_parts(rows, cols) * 8) + count * 4 * (3 * m * n + 2 * m * m);
+    const int64_t parts = gram_parts(count, m, n);
+    return align256(count * norm_parts(rows, cols) * 8) + count * 4 * (3 * m * n + (2 + (parts > 1 ? parts : 0)) * m * m);
 }
 
 hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
@@ -697,40 +834,55 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
     const int64_t m = padded(std::min(a.rows, a.cols)), n = padded(std::max(a.rows, a.cols));
     const int64_t xb = m * n * 4, ab = m * m * 4;
     char* w = static_cast<char*>(a.workspace);
-    double* parts = reinterpret_cast<double*>(w);
+    double* squares = reinterpret_cast<double*>(w);
     w += align256(a.count * norm_parts(a.rows, a.cols) * 8);
     char* x = w; w += a.count * xb;
     char* xt[2];
     xt[0] = w; w += a.count * xb;
     xt[1] = w; w += a.count * xb;
     char* ga = w; w += a.count * ab;
-    char* gb = w;
+    char* gb = w; w += a.count * ab;
+    float* sums = reinterpret_cast<float*>(w);
+    const int64_t parts = gram_parts(a.count, m, n);
     double unit = unit_for(a.bounds[0]);
     char* straight = tall ? xt[0] : x;
     char* turned = tall ? x : xt[0];
     const int64_t rp = tall ? n : m, cp = tall ? m : n;
-    if (a.type == P2_F32) to_pairs<float>(a, unit, parts, straight, turned, rp, cp, xb, s);
-    else if (a.type == P2_BF16) to_pairs<bf16_t>(a, unit, parts, straight, turned, rp, cp, xb, s);
-    else to_pairs<half_t>(a, unit, parts, straight, turned, rp, cp, xb, s);
+    if (a.type == P2_F32) to_pairs<float>(a, unit, squares, straight, turned, rp, cp, xb, s);
+    else if (a.type == P2_BF16) to_pairs<bf16_t>(a, unit, squares, straight, turned, rp, cp, xb, s);
+    else to_pairs<half_t>(a, unit, squares, straight, turned, rp, cp, xb, s);
     hipError_t e = hipGetLastError();
     for (int i = 0; i < a.steps && e == hipSuccess; ++i) {
         const bool last = i + 1 == a.steps;
+        // Nothing magnifies what the last step rounds off.  For a bf16 result (1.66e-3 off by its own rounding) upper halves will do
+        // for X X^T and B X: 0.7e-3 to 0.9e-3 more or less at random, 1.8e-3 together.  Not for A A: its rounding is common to all
+        // of the result (in fp16 3e-3 where there are few rows).
         const int terms = last && a.out_type == P2_BF16 ? 1 : 3;
         const StepFactors f = step_factors(a, i, unit);
         Product p = {};
+        p.matrices = a.count;
         p.p = p.q = x; p.p_plane = p.q_plane = xb;
         p.straight = ga; p.old_plane = ab;
         p.k = n; p.rows = p.cols = m;
         p.sum_factor = f.gram;
-        product_by_size(p, terms, kGram, a.count, s);
+        if (parts > 1) {
+            p.out = sums; p.parts = (int32_t)parts;
+            p.tiles = (int32_t)(tiles_of(p, 64, kPart) * parts);
+            k_newton_product<64, 2, 2, 3, 3, kPart><<<dim3((unsigned)(p.tiles * a.count)), dim3(256), 0, s>>>(p);
+            k_newton_join<<<dim3((unsigned)tiles_of(p, 64, kPart), (unsigned)a.count), dim3(256), 0, s>>>(sums, (int32_t)parts, a.count, m, f.gram, ga, ab);
+        } else {
+            product_by_size(p, terms, kGram, s);
+        }
         p = {};
+        p.matrices = a.count;
         p.p = p.q = p.old = ga; p.p_plane = p.q_plane = p.old_plane = ab;
         p.straight = gb;
         p.k = p.rows = p.cols = m;
         p.old_factor = f.poly_old;
         p.sum_factor = f.poly_sum;
-        product_by_size(p, terms, kPoly, a.count, s);
+        product_by_size(p, 3, kPoly, s);
         p = {};
+        p.matrices = a.count;
         p.p = gb; p.p_plane = ab;
         p.q = p.old = xt[i & 1]; p.q_plane = p.old_plane = xb;
         p.straight = x; p.turned = xt[(i + 1) & 1];
@@ -743,7 +895,7 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
             p.out_turned = tall; p.out_type = a.out_type;
             p.gain = (float)(a.scale / f.unit);
         }
-        product_by_size(p, terms, last ? kLast : kApply, a.count, s);
+        product_by_size(p, terms, last ? kLast : kApply, s);
         unit = f.unit;
         e = hipGetLastError();
     }

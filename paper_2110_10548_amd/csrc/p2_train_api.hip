@@ -69,7 +69,8 @@ int32_t check_matrices(int64_t count, int64_t rows, int64_t cols) {
 struct BalanceRoom { int64_t prob, count, ticket, bytes; };
 BalanceRoom balance_room(int64_t tokens, int32_t experts) {
     const int64_t lines = balance_forward_partials(tokens, experts);
-    BalanceRoom r;
+    BalanceRoom r = {};
+    if (lines == 1) return r;                  // one block keeps its sums to itself
     r.prob = 0;
     r.count = round256(lines * experts * 4);
     r.ticket = r.count + round256(lines * (experts + 1) * 4);
@@ -169,7 +170,7 @@ int32_t p2_balance_forward(const void* logits, int32_t type, int64_t stride, con
         if (!aligned_to(expert, 4) || !aligned_to(gate, 4) || !aligned_to(counts, 8) || !aligned_to(prob_sum, 4) || !aligned_to(kept, 8) || !aligned_to(loss, 4))
             return api_fail(P2_EINVAL, "pointer not aligned to its elements");
         const BalanceRoom room = balance_room(tokens, experts);
-        if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (room.bytes && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room.bytes) return api_fail(P2_ENOSPC, "workspace too small");
         char* w = static_cast<char*>(workspace);
         BalanceForward a = {};

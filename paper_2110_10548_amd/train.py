@@ -60,15 +60,16 @@ def _on_device(*tensors):
     """The current stream, after a look at whether all tensors are on its device."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != here:
             _refuse("tensor not on the current device")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(here)        # (a Stream object would take 3 us to make)
 
 
 def _type(t, what):
-    if t.dtype not in TYPES:
+    kind = TYPES.get(t.dtype)
+    if kind is None:
         _refuse("%s must be float32, bfloat16 or float16" % what)
-    return TYPES[t.dtype]
+    return kind
 
 
 def _rows(t):
@@ -94,7 +95,7 @@ def _vector(t, n, what, dtype=None):
 
 def _workspace(name, sizes, like):
     n = _room(name, *sizes)
-    return torch.empty(max(n, 1), dtype=torch.uint8, device=like.device), n
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
 
 
 def p2_layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
@@ -165,7 +166,7 @@ def p2_balance_forward(logits, k, keep=None):
     loss = torch.empty((), dtype=torch.float32, device=d)
     work, size = _workspace("p2_balance_forward_workspace", (n, e), logits)
     B._check(lib().p2_balance_forward(rows.data_ptr(), kind, stride, _ptr(keep), n, e, k, expert.data_ptr(), gate.data_ptr(), counts.data_ptr(),
-                                      prob_sum.data_ptr(), kept.data_ptr(), loss.data_ptr(), work.data_ptr(), size, stream))
+                                      prob_sum.data_ptr(), kept.data_ptr(), loss.data_ptr(), _ptr(work), size, stream))
     return {"expert": expert, "gate": gate, "counts": counts, "prob_sum": prob_sum, "tokens": kept, "loss": loss}
 
 
@@ -225,5 +226,5 @@ def p2_orthogonalize(g, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, scale=1.0
     work, size = _workspace("p2_orthogonalize_workspace", (count, rows, cols), g)
     B._check(lib().p2_orthogonalize(m.data_ptr(), kind, m.stride(1) if rows > 1 else max(cols, 1), m.stride(0) if count > 1 else 0, count, rows, cols,
                                     steps, (C.c_double * 3)(*coefficients), eps, scale, out.data_ptr(), out_kind, cols, rows * cols,
-                                    work.data_ptr(), size, stream))
+                                    _ptr(work), size, stream))
     return out
