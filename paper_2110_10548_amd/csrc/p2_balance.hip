@@ -12,59 +12,42 @@ namespace p2 {
 
 namespace {
 
-constexpr int kBalanceBlock = 256;
-constexpr int64_t kBalanceBlocks = 1024;               // four blocks a compute unit
+constexpr int kBalanceBlock = 512;
+constexpr int64_t kBalanceBlocks = 512;                // two blocks a compute unit
 constexpr float kLog2e = 1.44269504088896340736f;
 
-template <typename T> struct Key;                      // whole numbers in the order of T's values, with the index below them
-template <> struct Key<float> { typedef uint64_t type; typedef uint32_t bits; static constexpr int kShift = 32; };
-template <> struct Key<half_t> { typedef uint32_t type; typedef uint16_t bits; static constexpr int kShift = 16; };
-template <> struct Key<bf16_t> { typedef uint32_t type; typedef uint16_t bits; static constexpr int kShift = 16; };
+// e^(v - m), v and m finite or not; 1 ulp of 2^x and what the product rounds.
+__device__ __forceinline__ float exp_of(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
 
-// 0 for -inf (never chosen); NaN above everything; -0 and 0 alike.
-template <typename T> __device__ __forceinline__ typename Key<T>::type make_key(T v, uint32_t e) {
-    typedef typename Key<T>::bits B;
-    typedef typename Key<T>::type K;
-    constexpr B top = (B)1 << (sizeof(B) * 8 - 1);
-    constexpr B all = (B)~(B)0;
-    const float f = (float)v;
-    B b = __builtin_bit_cast(B, v);
-    if (f == 0.0f) b = 0;
-    b = (b & top) ? (B)~b : (B)(b | top);
-    if (f != f) b = all;
-    const K key = ((K)b << Key<T>::kShift) | (K)(B)(all - (B)e);
-    return f == -INFINITY ? 0 : key;
+// Keys: whole numbers in the order of the logits, and of equal ones in the order of falling indexes.  A float's bits, turned
+// over where it is negative, are in its order.  16-bit logits leave the lowest 13 of them unused: the index goes there; for 32-bit
+// ones it takes 32 bits more.  -0 is 0, NaN above everything; what is not above -inf (kNone) is never chosen.
+__device__ __forceinline__ uint32_t ordered(float f) {
+    const uint32_t b = __float_as_uint(f + 0.0f);
+    const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return f != f ? 0xffffffffu : o;
 }
-template <typename T> __device__ __forceinline__ uint32_t key_index(typename Key<T>::type key) {
-    typedef typename Key<T>::bits B;
-    return (uint32_t)(B)((B)~(B)0 - (B)key);
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+    return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
-template <typename T> __device__ __forceinline__ float key_value(typename Key<T>::type key) {
-    typedef typename Key<T>::bits B;
-    constexpr B top = (B)1 << (sizeof(B) * 8 - 1);
-    B b = (B)(key >> Key<T>::kShift);
-    b = (b & top) ? (B)(b & (B)~top) : (B)~b;
-    return (float)__builtin_bit_cast(T, b);
-}
+constexpr uint32_t kNone = 0x007fffffu;                // ordered(-inf)
+template <typename T> struct Key {                     // half_t, bf16_t
+    typedef uint32_t type;
+    static constexpr uint32_t kLow = 0x1fffu;
+    static __device__ __forceinline__ type of(float f, int e) { return (ordered(f) & ~kLow) | (kLow - (uint32_t)e); }
+    static __device__ __forceinline__ bool real(type k) { return (k & ~kLow) > (kNone & ~kLow); }
+    static __device__ __forceinline__ int index(type k) { return (int)(kLow - (k & kLow)); }
+    static __device__ __forceinline__ float value(type k) { return from_ordered(k & 0x80000000u ? k & ~kLow : k | kLow); }
+};
+template <> struct Key<float> {
+    typedef uint64_t type;
+    static __device__ __forceinline__ type of(float f, int e) { return (uint64_t)ordered(f) << 32 | (0xffffffffu - (uint32_t)e); }
+    static __device__ __forceinline__ bool real(type k) { return (uint32_t)(k >> 32) > kNone; }
+    static __device__ __forceinline__ int index(type k) { return (int)(0xffffffffu - (uint32_t)k); }
+    static __device__ __forceinline__ float value(type k) { return from_ordered((uint32_t)(k >> 32)); }
+};
 
-template <int L, typename K> __device__ __forceinline__ K group_max_key(K v) {
-#pragma unroll
-    for (int d = L / 2; d >= 1; d >>= 1) {
-        const K o = (K)__shfl_xor((unsigned long long)v, d, 64);
-        v = o > v ? o : v;
-    }
-    return v;
-}
-template <int L> __device__ __forceinline__ uint32_t group_max_key(uint32_t v) {
-#pragma unroll
-    for (int d = L / 2; d >= 1; d >>= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, d, 64);
-        v = o > v ? o : v;
-    }
-    return v;
-}
-
-__device__ __forceinline__ double block_sum(double v, double* buf) {       // kBalanceBlock threads; thread 0 gets it
+__device__ __forceinline__ double block_sum(double v, double* buf) {       // thread 0 gets it
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
@@ -116,38 +99,46 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         const int64_t t = t0 + threadIdx.x / kLanes;
         const bool there = t < a.tokens;
         const bool keep = there && (!a.keep || a.keep[t]);
-        T z[kItems];
-        R::load(static_cast<const T*>(a.logits) + (there ? t : a.tokens - 1) * a.stride, lane, a.experts, z);
+        float p[kItems];
         K key[kItems];
-        float p[kItems], m = -INFINITY;
+        {
+            T z[kItems];
+            R::load(static_cast<const T*>(a.logits) + (there ? t : a.tokens - 1) * a.stride, lane, a.experts, z);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            key[i] = keep ? make_key(z[i], (uint32_t)R::at(lane, i)) : 0;
-            m = fmaxf(m, (float)z[i]);
+            for (int i = 0; i < kItems; ++i) {
+                p[i] = (float)z[i];
+                key[i] = Key<T>::of(p[i], R::at(lane, i));
+            }
         }
+        float m = p[0];
+#pragma unroll
+        for (int i = 1; i < kItems; ++i) m = fmaxf(m, p[i]);
         m = group_max<kLanes>(m);
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            p[i] = exp2f(((float)z[i] - m) * kLog2e);
-            s += R::at(lane, i) < a.experts ? p[i] : 0.0f;
+            p[i] = R::at(lane, i) < a.experts ? exp_of(p[i], m) : 0.0f;
+            s += p[i];
         }
         const float inv = 1.0f / group_sum<kLanes>(s);
-        // the k best, one after the other; lane i % kLanes keeps the i-th until as many as there are lanes are to be written
+        // The k best, one after the other: the next is the largest key below the last, and as whole numbers that wrap around
+        // key - last is the larger the nearer the key is below.  Lane i % kLanes keeps the i-th until as many as there are lanes
+        // are to be written.
         int32_t held_expert = -1;
         float held_gate = 0.0f;
         bool on = false;
+        K last = 0;
         for (int i = 0; i < a.k; ++i) {
-            K best = 0;
+            K best = key[0] - last;
 #pragma unroll
-            for (int q = 0; q < kItems; ++q) best = key[q] > best ? key[q] : best;
-            best = group_max_key<kLanes>(best);
-            if (i == 0) on = best != 0;
-#pragma unroll
-            for (int q = 0; q < kItems; ++q) key[q] = key[q] == best ? 0 : key[q];
+            for (int q = 1; q < kItems; ++q) { const K d = key[q] - last; best = d > best ? d : best; }
+            best = group_reduce<kLanes>(best, [](K x, K y) { return x > y ? x : y; });
+            last += best;                                  // (there are k keys at least: -inf has one, too)
+            const bool real = keep && Key<T>::real(last);
+            if (i == 0) on = real;
             if (i % kLanes == lane) {
-                held_expert = best ? (int32_t)key_index<T>(best) : -1;
-                held_gate = best ? exp2f((key_value<T>(best) - m) * kLog2e) * inv : 0.0f;
+                held_expert = real ? Key<T>::index(last) : -1;
+                held_gate = real ? exp_of(Key<T>::value(last), m) * inv : 0.0f;
             }
             if ((i + 1) % kLanes == 0 || i + 1 == a.k) {
                 const int slot = i - i % kLanes + lane;
@@ -199,33 +190,37 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     }
 }
 
-// Adds up the blocks' lines: 32 experts a block (the tokens that count are one more column), 32 threads each.  The block
+// Adds up the blocks' lines: 16 experts a block (the tokens that count are one more column), 64 threads each.  The block
 // that is done last works the loss out.
 __global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t lines) {
-    __shared__ float prob[32][33];
-    __shared__ int64_t count[32][33];
+    __shared__ float prob[64][17];
+    __shared__ int64_t count[64][17];
     __shared__ double buf[16];
     __shared__ bool last;
-    const int x = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int e = blockIdx.x * 32 + x;
+    const int x = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const int e = blockIdx.x * 16 + x;
     float s = 0.0f;
     int64_t n = 0;
     if (e <= a.experts) {
-        for (int l = r; l < lines; l += 32) {
-            if (e < a.experts) s += a.part_prob[(int64_t)l * a.experts + e];
+        const int column = min(e, a.experts - 1);
+#pragma unroll 8
+        for (int l = r; l < lines; l += 64) {
+            s += a.part_prob[(int64_t)l * a.experts + column];
             n += a.part_count[(int64_t)l * (a.experts + 1) + e];
         }
     }
     prob[r][x] = s;
     count[r][x] = n;
-    __syncthreads();
+    for (int d = 32; d >= 1; d >>= 1) {
+        __syncthreads();
+        if (r < d) { prob[r][x] += prob[r + d][x]; count[r][x] += count[r + d][x]; }
+    }
     if (r == 0 && e <= a.experts) {
-        for (int q = 1; q < 32; ++q) { s += prob[q][x]; n += count[q][x]; }
         if (e < a.experts) {
-            a.prob_sum[e] = s;
-            a.counts[e] = n;
+            a.prob_sum[e] = prob[0][x];
+            a.counts[e] = count[0][x];
         } else {
-            a.kept[0] = n;
+            a.kept[0] = count[0][x];
         }
     }
     __syncthreads();
@@ -252,10 +247,15 @@ __global__ __launch_bounds__(kBalanceBlock) void k_balance_loss(const int64_t* c
     if (threadIdx.x == 0) loss[0] = loss_of(l, kept[0], experts, k);
 }
 
+// Backward.  The gates' gradients of a token go to their experts' places in a row of LDS of the token's lanes, which hold zeros
+// otherwise and are cleared again after use; only the token's own lanes, which are of one wavefront, touch that row.
 template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock) void k_balance_backward(BalanceBackward a) {
     typedef Row<T, kLanes, kItems> R;
     constexpr int kTokens = kBalanceBlock / kLanes;
+    constexpr int kWidth = kLanes * kItems;
+    __shared__ __attribute__((aligned(16))) float extra[kTokens][kWidth];
     const int lane = threadIdx.x % kLanes;
+    float* mine = extra[threadIdx.x / kLanes];
     const double kept = (double)a.kept[0];
     const double c = kept > 0 ? (a.dloss ? (double)a.dloss[0] : 1.0) * a.experts / (a.k * kept * kept) : 0.0;
     float w[kItems];
@@ -263,43 +263,49 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     for (int i = 0; i < kItems; ++i) {
         const int e = R::at(lane, i);
         w[i] = e < a.experts ? (float)(c * (double)a.counts[e]) : 0.0f;
+        mine[e] = 0.0f;
     }
     for (int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes; t < a.tokens; t += (int64_t)gridDim.x * kTokens) {
         T z[kItems];
         R::load(static_cast<const T*>(a.logits) + t * a.stride, lane, a.experts, z);
+        const bool keep = !a.keep || a.keep[t];
+        wavefront_exchange();                              // (the row is clear)
+        if (a.dgate)
+            for (int i = lane; i < a.k; i += kLanes) {
+                const uint32_t e = (uint32_t)a.expert[t * a.k + i];
+                if (e < (uint32_t)a.experts) atomicAdd(&mine[e], a.dgate[t * a.k + i]);
+            }
         float p[kItems], m = -INFINITY, any = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            m = fmaxf(m, (float)z[i]);
-            if ((float)z[i] != -INFINITY) any = 1.0f;
+            p[i] = (float)z[i];
+            m = fmaxf(m, p[i]);
+            any = p[i] != -INFINITY ? 1.0f : any;
         }
         m = group_max<kLanes>(m);
-        const bool on = (!a.keep || a.keep[t]) && group_max<kLanes>(any) > 0.0f;
+        const bool on = keep && group_max<kLanes>(any) > 0.0f;
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            p[i] = exp2f(((float)z[i] - m) * kLog2e);
-            s += R::at(lane, i) < a.experts ? p[i] : 0.0f;
+            p[i] = R::at(lane, i) < a.experts ? exp_of(p[i], m) : 0.0f;
+            s += p[i];
         }
         const float inv = 1.0f / group_sum<kLanes>(s);
-        float u[kItems];
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) u[i] = w[i];
-        if (a.dgate) {
-            for (int i = 0; i < a.k; ++i) {
-                const int e = a.expert[t * a.k + i];
-                const float d = a.dgate[t * a.k + i];
-#pragma unroll
-                for (int q = 0; q < kItems; ++q) if (R::at(lane, q) == e) u[q] += d;
-            }
-        }
-        float dot = 0.0f;
+        wavefront_exchange();                              // (all gradients are in the row)
+        float u[kItems], dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
+            u[i] = w[i] + mine[R::at(lane, i)];
             p[i] *= inv;
-            dot += R::at(lane, i) < a.experts ? p[i] * u[i] : 0.0f;
+            dot += p[i] * u[i];
         }
         dot = group_sum<kLanes>(dot);
+        wavefront_exchange();                              // (the row has been read)
+        if (a.dgate)
+            for (int i = lane; i < a.k; i += kLanes) {
+                const uint32_t e = (uint32_t)a.expert[t * a.k + i];
+                if (e < (uint32_t)a.experts) mine[e] = 0.0f;
+            }
         T* out = static_cast<T*>(a.dlogits) + t * a.dlogits_stride;
 #pragma unroll
         for (int q = 0; q < R::kVecs; ++q) {
@@ -312,10 +318,11 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     }
 }
 
-int lanes_for(int32_t experts) {               // of a token, kItems = 8 (16 above 512 experts)
+// Lanes of a token: 16 at most up to 512 experts (reductions over 16 lanes need no LDS), and a lane's logits 8 to 32.
+int lanes_for(int32_t experts) {
     int lanes = 1;
-    while (lanes < 64 && lanes * 8 < experts) lanes *= 2;
-    return lanes;
+    while (lanes < 16 && lanes * 8 < experts) lanes *= 2;
+    return experts <= 512 ? lanes : 64;
 }
 int64_t balance_blocks(int64_t tokens, int32_t experts) {
     return std::max<int64_t>(1, std::min(ceil_div(tokens, kBalanceBlock / lanes_for(experts)), kBalanceBlocks));
@@ -327,11 +334,12 @@ int64_t balance_blocks(int64_t tokens, int32_t experts) {
         case 2: KERNEL<T, 2, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
         case 4: KERNEL<T, 4, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
         case 8: KERNEL<T, 8, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
-        case 16: KERNEL<T, 16, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                         \
-        case 32: KERNEL<T, 32, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                         \
-        default:                                                                                          \
-            if (a.experts <= 512) KERNEL<T, 64, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a);               \
-            else KERNEL<T, 64, 16><<<grid, dim3(kBalanceBlock), 0, s>>>(a);                               \
+        case 16:                                                                                          \
+            if (a.experts <= 128) KERNEL<T, 16, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a);               \
+            else if (a.experts <= 256) KERNEL<T, 16, 16><<<grid, dim3(kBalanceBlock), 0, s>>>(a);         \
+            else KERNEL<T, 16, 32><<<grid, dim3(kBalanceBlock), 0, s>>>(a);                               \
+            break;                                                                                        \
+        default: KERNEL<T, 64, 16><<<grid, dim3(kBalanceBlock), 0, s>>>(a);                               \
     }
 
 }  // namespace
@@ -346,7 +354,7 @@ hipError_t launch_balance_forward(const BalanceForward& a, hipStream_t s) {
     else { P2_BALANCE_CASES(k_balance_forward, half_t) }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    k_balance_sum<<<dim3((unsigned)ceil_div(a.experts + 1, 32)), dim3(1024), 0, s>>>(a, (int32_t)blocks);
+    k_balance_sum<<<dim3((unsigned)ceil_div(a.experts + 1, 16)), dim3(1024), 0, s>>>(a, (int32_t)blocks);
     return hipGetLastError();
 }
 

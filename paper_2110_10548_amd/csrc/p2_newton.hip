@@ -167,12 +167,6 @@ struct Rows {
 #endif
 };
 
-// What the wavefront's lanes have written to LDS is there for its other lanes.
-__device__ __forceinline__ void wavefront_exchange() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Waits until at most kLoads of this wavefront's loads are under way (and all its LDS reads are done), then for the others.
 template <int kLoads> __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");

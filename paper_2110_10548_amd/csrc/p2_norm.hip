@@ -37,39 +37,81 @@ template <int kTpr> __device__ __forceinline__ float row_sum(float v, float* buf
     }
 }
 
-template <typename T, int kTpr, int kNv> __global__ __launch_bounds__(NormGroup<kTpr>::kThreads) void k_norm_forward(NormForward a) {
+// N weights from column c on, in whatever type they have; loaded like a row's vectors.
+template <int N, bool kWhole> struct WeightVec {
+    RowVec<float, N, kWhole> raw;              // 16-bit types: the first half of it
+    __device__ __forceinline__ void load(const void* p, int32_t type, int c, int cols) {
+        if (type == P2_F32) {
+            raw.load(static_cast<const float*>(p), c, cols);
+        } else {
+            RowVec<half_t, N, kWhole> r;
+            r.load(static_cast<const half_t*>(p), c, cols);
+            typedef float part_t __attribute__((ext_vector_type(N / 2)));
+            const part_t w = __builtin_bit_cast(part_t, r.raw);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) raw.raw[i] = w[i];
+        }
+    }
+    template <typename T> __device__ __forceinline__ void get_narrow(int c, int cols, float other, float (&v)[N]) const {
+        typedef float part_t __attribute__((ext_vector_type(N / 2)));
+        part_t w;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = raw.raw[i];
+        RowVec<T, N, kWhole> r;
+        r.raw = __builtin_bit_cast(decltype(r.raw), w);
+        r.get(c, cols, other, v);
+    }
+    __device__ __forceinline__ void get(int32_t type, int c, int cols, float other, float (&v)[N]) const {
+        if (type == P2_F32) raw.get(c, cols, other, v);
+        else if (type == P2_F16) get_narrow<half_t>(c, cols, other, v);
+        else get_narrow<bf16_t>(c, cols, other, v);
+    }
+};
+
+template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds__(NormGroup<kTpr>::kThreads) void k_norm_forward(NormForward a) {
     constexpr int V = 16 / sizeof(T);
     constexpr int kRows = NormGroup<kTpr>::kRows;
     __shared__ float buf[2][16];
-    const int lane = threadIdx.x % kTpr;
+    const int lane = threadIdx.x % kTpr, cols = (int)a.cols;
     const float inv = 1.0f / (float)a.cols;
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
         const int64_t row = row0 + threadIdx.x / kTpr;
         const bool there = row < a.rows;                   // (rows of a block's own threads: all of them, or none)
         const T* x = static_cast<const T*>(a.x) + (there ? row : a.rows - 1) * a.x_stride;
-        float v[kNv][V];
+        RowVec<T, V, kWhole> raw[kNv];
+        WeightVec<V, kWhole> w[kNv], b[kNv];
 #pragma unroll
-        for (int i = 0; i < kNv; ++i) {
-            const int64_t c = (int64_t)(i * kTpr + lane) * V;
-            load_part<T, V>(x + c, a.cols - c, v[i], 0.0f);
-        }
+        for (int i = 0; i < kNv; ++i) raw[i].load(x, (i * kTpr + lane) * V, cols);
+        auto ask_weights = [&] {
+            if (a.weight)
+#pragma unroll
+                for (int i = 0; i < kNv; ++i) w[i].load(a.weight, a.weight_type, (i * kTpr + lane) * V, cols);
+            if (a.bias)
+#pragma unroll
+                for (int i = 0; i < kNv; ++i) b[i].load(a.bias, a.weight_type, (i * kTpr + lane) * V, cols);
+        };
+        if constexpr (kNv <= 2) ask_weights();             // (there are registers to have them wait in)
+        float v[kNv][V];
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kNv; ++i)
+        for (int i = 0; i < kNv; ++i) {
+            raw[i].get((i * kTpr + lane) * V, cols, 0.0f, v[i]);
 #pragma unroll
             for (int j = 0; j < V; ++j) s += v[i][j];
+        }
         const float mean = row_sum<kTpr>(s, buf[0]) * inv;
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kNv; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int64_t c = (int64_t)(i * kTpr + lane) * V + j;
-                const float d = v[i][j] - mean;
-                if (c < a.cols) s += d * d;
+                const int c = (i * kTpr + lane) * V + (kWhole ? 0 : j);
+                v[i][j] -= mean;
+                s += c < cols ? v[i][j] * v[i][j] : 0.0f;
             }
         const float rstd = 1.0f / sqrtf(row_sum<kTpr>(s, buf[1]) * inv + a.eps);
         if (there) {
+            if constexpr (kNv > 2) ask_weights();
             if (lane == 0) {
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
@@ -77,21 +119,22 @@ template <typename T, int kTpr, int kNv> __global__ __launch_bounds__(NormGroup<
             T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
             for (int i = 0; i < kNv; ++i) {
-                const int64_t c = (int64_t)(i * kTpr + lane) * V;
-                float w[V], b[V];
+                const int c = (i * kTpr + lane) * V;
+                float wv[V], bv[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) { w[j] = 1.0f; b[j] = 0.0f; }
-                if (a.weight) load_typed<V>(a.weight, a.weight_type, c, a.cols - c, w, 1.0f);
-                if (a.bias) load_typed<V>(a.bias, a.weight_type, c, a.cols - c, b, 0.0f);
+                for (int j = 0; j < V; ++j) { wv[j] = 1.0f; bv[j] = 0.0f; }
+                if (a.weight) w[i].get(a.weight_type, c, cols, 1.0f, wv);
+                if (a.bias) b[i].get(a.weight_type, c, cols, 0.0f, bv);
 #pragma unroll
-                for (int j = 0; j < V; ++j) w[j] = (v[i][j] - mean) * rstd * w[j] + b[j];
-                store_part<T, V>(y + c, a.cols - c, w);
+                for (int j = 0; j < V; ++j) wv[j] = v[i][j] * rstd * wv[j] + bv[j];
+                if constexpr (kWhole) { if (c < cols) store_vec<T, V>(y + c, wv); }
+                else store_part<T, V>(y + c, cols - c, wv);
             }
         }
     }
 }
 
-// Rows too long for registers: three passes over them, the later two from the cache.
+// Rows too long for registers, or shorter than a vector: three passes over them, the later two from the cache.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_long(NormForward a) {
     __shared__ float buf[2][16];
     const float inv = 1.0f / (float)a.cols;
@@ -123,50 +166,65 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_lon
 constexpr int kBackBlock = 512;
 constexpr int64_t kBackBlocks = 512;       // two blocks a compute unit: 16 wavefronts
 
-template <typename T, int kTpr, int kNv> __global__ __launch_bounds__(kBackBlock) void k_norm_backward(NormBackward a) {
+template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds__(kBackBlock) void k_norm_backward(NormBackward a) {
     constexpr int V = 16 / sizeof(T);
     constexpr int kRows = kBackBlock / kTpr;
     constexpr int kCols = kTpr * kNv * V;
     __shared__ float buf[2][2][kBackBlock / 64];
     __shared__ float sums[2][kRows > 1 ? kCols : 1];
-    const int lane = threadIdx.x % kTpr;
-    const int group = threadIdx.x / kTpr;
+    const int lane = threadIdx.x % kTpr, group = threadIdx.x / kTpr, cols = (int)a.cols;
     const float inv = 1.0f / (float)a.cols;
     float w[kNv][V], dw[kNv][V], db[kNv][V];
 #pragma unroll
     for (int i = 0; i < kNv; ++i) {
-        const int64_t c = (int64_t)(i * kTpr + lane) * V;
+        const int c = (i * kTpr + lane) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) { w[i][j] = 1.0f; dw[i][j] = 0.0f; db[i][j] = 0.0f; }
-        if (a.weight) load_typed<V>(a.weight, a.weight_type, c, a.cols - c, w[i], 0.0f);
+        if (a.weight) load_typed<V>(a.weight, a.weight_type, c, cols - c, w[i], 0.0f);
     }
-    int turn = 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows, turn ^= 1) {
-        const int64_t row = row0 + group;
-        const bool there = row < a.rows;
-        const int64_t at = there ? row : a.rows - 1;
+    // A row's values are asked for while the row before it is worked on.
+    RowVec<T, V, kWhole> nx[kNv], nd[kNv];
+    float next_mean, next_rstd;
+    auto ask = [&](int64_t row) {
+        const int64_t at = row < a.rows ? row : a.rows - 1;
         const T* x = static_cast<const T*>(a.x) + at * a.x_stride;
         const T* dy = static_cast<const T*>(a.dy) + at * a.dy_stride;
-        const float mean = a.mean[at], rstd = a.rstd[at];
-        float xh[kNv][V], d[kNv][V];
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-            const int64_t c = (int64_t)(i * kTpr + lane) * V;
-            load_part<T, V>(x + c, a.cols - c, xh[i], mean);
-            load_part<T, V>(dy + c, there ? a.cols - c : 0, d[i], 0.0f);
+            nx[i].load(x, (i * kTpr + lane) * V, cols);
+            nd[i].load(dy, (i * kTpr + lane) * V, cols);
         }
+        next_mean = a.mean[at];
+        next_rstd = a.rstd[at];
+    };
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    int turn = 0;
+    constexpr bool kEarly = kNv <= 2;                      // (more vectors would not stay in registers)
+    if constexpr (kEarly) ask((int64_t)blockIdx.x * kRows + group);
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += stride, turn ^= 1) {
+        const int64_t row = row0 + group;
+        const bool there = row < a.rows;
+        if constexpr (!kEarly) ask(row);
+        const float mean = next_mean, rstd = next_rstd;
+        float xh[kNv][V], d[kNv][V];
         float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kNv; ++i) {
+            const int c = (i * kTpr + lane) * V;
+            nx[i].get(c, cols, mean, xh[i]);
+            nd[i].get(c, cols, 0.0f, d[i]);
+        }
+        if constexpr (kEarly) { if (row0 + stride < a.rows) ask(row + stride); }
 #pragma unroll
         for (int i = 0; i < kNv; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 xh[i][j] = (xh[i][j] - mean) * rstd;
                 const float t = d[i][j] * xh[i][j];
-                if (there) {                               // (a row that is not there has no part in 0 * xh either)
-                    dw[i][j] += t;
-                    db[i][j] += d[i][j];
-                }
-                s1 += d[i][j] * w[i][j];
+                dw[i][j] += there ? t : 0.0f;
+                db[i][j] += there ? d[i][j] : 0.0f;
+                d[i][j] *= w[i][j];
+                s1 += d[i][j];
                 s2 += t * w[i][j];
             }
         if (a.dx) {
@@ -190,11 +248,12 @@ template <typename T, int kTpr, int kNv> __global__ __launch_bounds__(kBackBlock
                 T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
 #pragma unroll
                 for (int i = 0; i < kNv; ++i) {
-                    const int64_t c = (int64_t)(i * kTpr + lane) * V;
+                    const int c = (i * kTpr + lane) * V;
                     float o[V];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) o[j] = rstd * (d[i][j] * w[i][j] - m1 - xh[i][j] * m2);
-                    store_part<T, V>(dx + c, a.cols - c, o);
+                    for (int j = 0; j < V; ++j) o[j] = rstd * (d[i][j] - m1 - xh[i][j] * m2);
+                    if constexpr (kWhole) { if (c < cols) store_vec<T, V>(dx + c, o); }
+                    else store_part<T, V>(dx + c, cols - c, o);
                 }
             }
         }
@@ -270,47 +329,51 @@ template <typename T> __global__ __launch_bounds__(256) void k_norm_columns_long
     line[a.cols + c] = db;
 }
 
-// dweight (blockIdx.y = 0) and dbias (1) from `lines` lines of partial sums: 32 columns a block, 32 threads a column.
+// dweight (blockIdx.y = 0) and dbias (1) from `lines` lines of partial sums: 16 columns a block, 64 threads a column.
 __global__ __launch_bounds__(1024) void k_norm_weight_grad(const float* __restrict__ partial, int64_t lines, int64_t cols, void* dweight,
                                                            void* dbias, int32_t weight_type) {
-    __shared__ float part[32][33];
+    __shared__ float part[64][17];
     void* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
-    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-    const int r = threadIdx.x >> 5;
+    const int x = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + x;
     float s = 0.0f;
     if (c < cols)
-        for (int64_t l = r; l < lines; l += 32) s += partial[(l * 2 + blockIdx.y) * cols + c];
-    part[r][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (r == 0 && c < cols) {
-        for (int q = 1; q < 32; ++q) s += part[q][threadIdx.x & 31];
-        store_typed(out, weight_type, c, s);
+#pragma unroll 8
+        for (int64_t l = r; l < lines; l += 64) s += partial[(l * 2 + blockIdx.y) * cols + c];
+    part[r][x] = s;
+    for (int d = 32; d >= 1; d >>= 1) {
+        __syncthreads();
+        if (r < d) part[r][x] += part[r + d][x];
     }
+    if (r == 0 && c < cols) store_typed(out, weight_type, c, part[0][x]);
 }
 
 template <typename T, int kTpr, int kNv> void forward_as(const NormForward& a, hipStream_t s) {
     constexpr int kRows = NormGroup<kTpr>::kRows;
-    const int64_t blocks = std::min(ceil_div(a.rows, kRows), kMaxNormBlocks);
-    k_norm_forward<T, kTpr, kNv><<<dim3((unsigned)blocks), dim3(NormGroup<kTpr>::kThreads), 0, s>>>(a);
+    const dim3 grid((unsigned)std::min(ceil_div(a.rows, kRows), kMaxNormBlocks)), block(NormGroup<kTpr>::kThreads);
+    if (a.cols % (16 / sizeof(T)) == 0) k_norm_forward<T, kTpr, kNv, true><<<grid, block, 0, s>>>(a);
+    else k_norm_forward<T, kTpr, kNv, false><<<grid, block, 0, s>>>(a);
 }
 
 template <typename T> void forward_of(const NormForward& a, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int64_t vecs = ceil_div(a.cols, V);
-    if (vecs <= 16) forward_as<T, 16, 1>(a, s);
+    if (a.cols < V || vecs > 4096) k_norm_forward_long<T><<<dim3((unsigned)std::min(a.rows, kMaxNormBlocks)), dim3(1024), 0, s>>>(a);
+    else if (vecs <= 16) forward_as<T, 16, 1>(a, s);
     else if (vecs <= 64) forward_as<T, 64, 1>(a, s);
     else if (vecs <= 128) forward_as<T, 64, 2>(a, s);
     else if (vecs <= 256) forward_as<T, 256, 1>(a, s);
     else if (vecs <= 512) forward_as<T, 256, 2>(a, s);
     else if (vecs <= 1024) forward_as<T, 256, 4>(a, s);
-    else if (vecs <= 4096) forward_as<T, 1024, 4>(a, s);
-    else k_norm_forward_long<T><<<dim3((unsigned)std::min(a.rows, kMaxNormBlocks)), dim3(1024), 0, s>>>(a);
+    else forward_as<T, 1024, 4>(a, s);
 }
 
 // Threads and vectors of a row in the backward pass; 0: too long for registers.
 struct BackShape { int tpr, nv; };
-BackShape back_shape(int64_t vecs) {
+BackShape back_shape(int64_t cols, int64_t v) {
+    const int64_t vecs = ceil_div(cols, v);
+    if (cols < v) return {0, 0};
     if (vecs <= 16) return {16, 1};
     if (vecs <= 64) return {64, 1};
     if (vecs <= 128) return {64, 2};
@@ -322,17 +385,18 @@ BackShape back_shape(int64_t vecs) {
 }
 
 template <typename T, int kTpr, int kNv> void backward_as(const NormBackward& a, int64_t blocks, hipStream_t s) {
-    k_norm_backward<T, kTpr, kNv><<<dim3((unsigned)blocks), dim3(kBackBlock), 0, s>>>(a);
+    if (a.cols % (16 / sizeof(T)) == 0) k_norm_backward<T, kTpr, kNv, true><<<dim3((unsigned)blocks), dim3(kBackBlock), 0, s>>>(a);
+    else k_norm_backward<T, kTpr, kNv, false><<<dim3((unsigned)blocks), dim3(kBackBlock), 0, s>>>(a);
 }
 
 int64_t back_blocks(int64_t rows, int64_t cols, int32_t value_bytes) {
-    const BackShape f = back_shape(ceil_div(cols, 16 / value_bytes));
+    const BackShape f = back_shape(cols, 16 / value_bytes);
     const int64_t groups = f.tpr ? ceil_div(rows, kBackBlock / f.tpr) : rows;
     return std::max<int64_t>(1, std::min(groups, kBackBlocks));
 }
 
 template <typename T> hipError_t backward_of(const NormBackward& a, hipStream_t s) {
-    const BackShape f = back_shape(ceil_div(a.cols, 16 / (int64_t)sizeof(T)));
+    const BackShape f = back_shape(a.cols, 16 / (int64_t)sizeof(T));
     const int64_t blocks = back_blocks(a.rows, a.cols, sizeof(T));
     if (a.rows > 0) {
         switch (f.tpr * 8 + f.nv) {
@@ -352,7 +416,7 @@ template <typename T> hipError_t backward_of(const NormBackward& a, hipStream_t 
         if (e != hipSuccess) return e;
     }
     if (a.partial)
-        k_norm_weight_grad<<<dim3((unsigned)ceil_div(a.cols, 32), 2), dim3(1024), 0, s>>>(a.partial, a.rows > 0 ? blocks : 0, a.cols, a.dweight, a.dbias, a.weight_type);
+        k_norm_weight_grad<<<dim3((unsigned)ceil_div(a.cols, 16), 2), dim3(1024), 0, s>>>(a.partial, a.rows > 0 ? blocks : 0, a.cols, a.dweight, a.dbias, a.weight_type);
     return hipGetLastError();
 }
 

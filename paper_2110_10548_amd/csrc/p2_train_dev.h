@@ -49,6 +49,35 @@ template <typename T, int N> __device__ __forceinline__ void store_part(T* p, in
     for (int i = 0; i < N; ++i) if (i < n) p[i] = (T)v[i];
 }
 
+// N elements of a row from column c on, of which those before `cols` count (N <= cols).  The load itself is always a whole
+// vector inside the row and depends on nothing, so that many of them are under way together: the vector that the row's end cuts
+// is read from further left and moved.  kWhole: the rows are whole vectors.
+template <typename T, int N, bool kWhole> struct RowVec {
+    vec_t<T, N> raw;
+    __device__ __forceinline__ void load(const T* row, int c, int cols) { raw = *reinterpret_cast<const vec_t<T, N>*>(row + min(c, cols - N)); }
+    __device__ __forceinline__ void get(int c, int cols, float other, float (&v)[N]) const {
+        if constexpr (kWhole) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = c < cols ? (float)raw[i] : other;
+        } else {
+            constexpr int kWords = N * (int)sizeof(T) / 4;
+            typedef uint32_t words_t __attribute__((ext_vector_type(kWords)));
+            words_t w = __builtin_bit_cast(words_t, raw);
+            const int by = max(0, c - (cols - N)) * (int)sizeof(T);            // bytes; more than there are: nothing counts
+#pragma unroll
+            for (int d = kWords / 2; d >= 1; d /= 2)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[i] = by & 4 * d ? (i + d < kWords ? w[i + d] : 0u) : w[i];
+            if constexpr (sizeof(T) == 2)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[i] = by & 2 ? w[i] >> 16 | (i + 1 < kWords ? w[i + 1] << 16 : 0u) : w[i];
+            const vec_t<T, N> r = __builtin_bit_cast(vec_t<T, N>, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = c + i < cols ? (float)r[i] : other;
+        }
+    }
+};
+
 // Weights have a type of their own, which the whole launch agrees on.
 template <int N> __device__ __forceinline__ void load_typed(const void* p, int32_t type, int64_t at, int64_t n, float (&v)[N], float other) {
     if (type == P2_F32) load_part<float, N>(static_cast<const float*>(p) + at, n, v, other);
@@ -61,16 +90,41 @@ __device__ __forceinline__ void store_typed(void* p, int32_t type, int64_t at, f
     else static_cast<half_t*>(p)[at] = (half_t)v;
 }
 
-// Sum over groups of L consecutive lanes (a power of two up to 64); every lane gets it.
-template <int L> __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int d = L / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+// A value of another lane of the same 16, without a detour through LDS: kStep 1 and 2 exchange lanes 1 and 2 apart, 4 and 8 mirror
+// groups of 8 and 16 lanes, which for a reduction over lanes that already agree in groups of 4 and 8 is as good.
+template <int kStep> __device__ __forceinline__ uint32_t neighbour(uint32_t v) {
+    constexpr int kControl = kStep == 1 ? 0xb1 : kStep == 2 ? 0x4e : kStep == 4 ? 0x141 : 0x140;
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kControl, 0xf, 0xf, true);
+}
+template <int kStep> __device__ __forceinline__ float neighbour(float v) { return __uint_as_float(neighbour<kStep>(__float_as_uint(v))); }
+template <int kStep> __device__ __forceinline__ uint64_t neighbour(uint64_t v) {
+    return (uint64_t)neighbour<kStep>((uint32_t)(v >> 32)) << 32 | neighbour<kStep>((uint32_t)v);
+}
+__device__ __forceinline__ float far_lane(float v, int d) { return __shfl_xor(v, d, 64); }
+__device__ __forceinline__ uint32_t far_lane(uint32_t v, int d) { return (uint32_t)__shfl_xor((int)v, d, 64); }
+__device__ __forceinline__ uint64_t far_lane(uint64_t v, int d) { return (uint64_t)__shfl_xor((unsigned long long)v, d, 64); }
+
+// Reduction over groups of L consecutive lanes (a power of two up to 64); every lane gets the result, always in one order.
+template <int L, typename V, typename F> __device__ __forceinline__ V group_reduce(V v, F&& f) {
+    if constexpr (L >= 2) v = f(v, neighbour<1>(v));
+    if constexpr (L >= 4) v = f(v, neighbour<2>(v));
+    if constexpr (L >= 8) v = f(v, neighbour<4>(v));
+    if constexpr (L >= 16) v = f(v, neighbour<8>(v));
+    if constexpr (L >= 32) v = f(v, far_lane(v, 16));
+    if constexpr (L >= 64) v = f(v, far_lane(v, 32));
     return v;
 }
+template <int L> __device__ __forceinline__ float group_sum(float v) {
+    return group_reduce<L>(v, [](float a, float b) { return a + b; });
+}
 template <int L> __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-    for (int d = L / 2; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+    return group_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// What the wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void wavefront_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 struct NormForward {
