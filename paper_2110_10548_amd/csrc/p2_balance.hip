@@ -20,13 +20,14 @@ constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float exp_of(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
 
 // Keys: whole numbers in the order of the logits, and of equal ones in the order of falling indexes.  A float's bits, turned
-// over where it is negative, are in its order.  16-bit logits leave the lowest 13 of them unused: the index goes there; for 32-bit
-// ones it takes 32 bits more.  -0 is 0, NaN above everything; what is not above -inf (kNone) is never chosen.
+// over where it is negative, are in its order (NaN aside: with_nan puts it above everything).  16-bit logits leave the lowest 13 of them unused: the index goes there; for 32-bit
+// ones it takes 32 bits more.  -0 is 0; what is not above -inf (kNone) is never chosen.
 __device__ __forceinline__ uint32_t ordered(float f) {
     const uint32_t b = __float_as_uint(f + 0.0f);
-    const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-    return f != f ? 0xffffffffu : o;
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+// Whether it is a NaN's: above +inf's, or below -inf's.
+__device__ __forceinline__ bool ordered_nan(uint32_t o) { return o > 0xff800000u || o < 0x007fffffu; }
 __device__ __forceinline__ float from_ordered(uint32_t o) {
     return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
@@ -35,6 +36,7 @@ template <typename T> struct Key {                     // half_t, bf16_t
     typedef uint32_t type;
     static constexpr uint32_t kLow = 0x1fffu;
     static __device__ __forceinline__ type of(float f, int e) { return (ordered(f) & ~kLow) | (kLow - (uint32_t)e); }
+    static __device__ __forceinline__ type with_nan(type k) { return ordered_nan(k | kLow) && ordered_nan(k & ~kLow) ? k | ~kLow : k; }
     static __device__ __forceinline__ bool real(type k) { return (k & ~kLow) > (kNone & ~kLow); }
     static __device__ __forceinline__ int index(type k) { return (int)(kLow - (k & kLow)); }
     static __device__ __forceinline__ float value(type k) { return from_ordered(k & 0x80000000u ? k & ~kLow : k | kLow); }
@@ -42,6 +44,7 @@ template <typename T> struct Key {                     // half_t, bf16_t
 template <> struct Key<float> {
     typedef uint64_t type;
     static __device__ __forceinline__ type of(float f, int e) { return (uint64_t)ordered(f) << 32 | (0xffffffffu - (uint32_t)e); }
+    static __device__ __forceinline__ type with_nan(type k) { return ordered_nan((uint32_t)(k >> 32)) ? k | 0xffffffff00000000ull : k; }
     static __device__ __forceinline__ bool real(type k) { return (uint32_t)(k >> 32) > kNone; }
     static __device__ __forceinline__ int index(type k) { return (int)(0xffffffffu - (uint32_t)k); }
     static __device__ __forceinline__ float value(type k) { return from_ordered((uint32_t)(k >> 32)); }
@@ -59,28 +62,45 @@ __device__ __forceinline__ float loss_of(double sum, int64_t kept, int32_t exper
     return kept > 0 ? (float)(sum * experts / ((double)k * (double)kept * (double)kept)) : 0.0f;
 }
 
-// The logits of a row as this lane's kItems, -inf where there are none.
+// This lane's kItems logits of a row, in whole vectors that are asked for without a condition (RowVec); rows shorter than a
+// vector value by value.
 template <typename T, int kLanes, int kItems> struct Row {
-    static constexpr int V = 16 / sizeof(T) < kItems ? 16 / sizeof(T) : kItems;
+    static constexpr int V = 16 / sizeof(T);
     static constexpr int kVecs = kItems / V;
+    RowVec<T, V, false> raw[kVecs];
     static __device__ __forceinline__ int at(int lane, int i) { return ((i / V) * kLanes + lane) * V + i % V; }
-    static __device__ __forceinline__ void load(const T* row, int lane, int experts, T (&z)[kItems]) {
+    __device__ __forceinline__ void load(const T* row, int lane, int experts) {
+        if (experts >= V) {
 #pragma unroll
-        for (int q = 0; q < kVecs; ++q) {
-            const int e = (q * kLanes + lane) * V;
-            if (e + V <= experts) {
-                const vec_t<T, V> r = *reinterpret_cast<const vec_t<T, V>*>(row + e);
+            for (int q = 0; q < kVecs; ++q) raw[q].load(row, (q * kLanes + lane) * V, experts);
+        } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) z[q * V + j] = r[j];
-            } else {
+            for (int j = 0; j < V; ++j) raw[0].raw[j] = row[min(j, experts - 1)];
+        }
+    }
+    // -inf where there are no experts
+    __device__ __forceinline__ void get(int lane, int experts, float (&p)[kItems]) const {
+        float v[V];
+        if (experts % V == 0) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) z[q * V + j] = e + j < experts ? row[e + j] : (T)-INFINITY;
+            for (int q = 0; q < kVecs; ++q)
+#pragma unroll
+                for (int j = 0; j < V; ++j) p[q * V + j] = (q * kLanes + lane) * V < experts ? (float)raw[q].raw[j] : -INFINITY;
+        } else if (experts > V) {
+#pragma unroll
+            for (int q = 0; q < kVecs; ++q) {
+                raw[q].get((q * kLanes + lane) * V, experts, -INFINITY, v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) p[q * V + j] = v[j];
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) p[i] = at(lane, i) < experts ? (float)raw[0].raw[i % V] : -INFINITY;
         }
     }
 };
 
-template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock) void k_balance_forward(BalanceForward a) {
+template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock, 4) void k_balance_forward(BalanceForward a) {
     typedef typename Key<T>::type K;
     typedef Row<T, kLanes, kItems> R;
     constexpr int kTokens = kBalanceBlock / kLanes;
@@ -95,21 +115,24 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     float acc[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) acc[i] = 0.0f;
-    for (int64_t t0 = (int64_t)blockIdx.x * kTokens; t0 < a.tokens; t0 += (int64_t)gridDim.x * kTokens) {
+    // A token's logits are asked for while the one before it is worked on.
+    const int64_t stride = (int64_t)gridDim.x * kTokens;
+    R next;
+    bool next_keep = false;
+    auto ask = [&](int64_t t) {
+        const int64_t at = t < a.tokens ? t : a.tokens - 1;
+        next.load(static_cast<const T*>(a.logits) + at * a.stride, lane, a.experts);
+        next_keep = t < a.tokens && (!a.keep || a.keep[at]);
+    };
+    const int64_t first = (int64_t)blockIdx.x * kTokens;
+    if (first < a.tokens) ask(first + threadIdx.x / kLanes);
+    for (int64_t t0 = first; t0 < a.tokens; t0 += stride) {
         const int64_t t = t0 + threadIdx.x / kLanes;
-        const bool there = t < a.tokens;
-        const bool keep = there && (!a.keep || a.keep[t]);
+        const bool there = t < a.tokens, keep = next_keep;
         float p[kItems];
         K key[kItems];
-        {
-            T z[kItems];
-            R::load(static_cast<const T*>(a.logits) + (there ? t : a.tokens - 1) * a.stride, lane, a.experts, z);
-#pragma unroll
-            for (int i = 0; i < kItems; ++i) {
-                p[i] = (float)z[i];
-                key[i] = Key<T>::of(p[i], R::at(lane, i));
-            }
-        }
+        next.get(lane, a.experts, p);
+        if (t0 + stride < a.tokens) ask(t + stride);
         float m = p[0];
 #pragma unroll
         for (int i = 1; i < kItems; ++i) m = fmaxf(m, p[i]);
@@ -117,35 +140,41 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            p[i] = R::at(lane, i) < a.experts ? exp_of(p[i], m) : 0.0f;
-            s += p[i];
+            key[i] = Key<T>::of(p[i], R::at(lane, i));
+            p[i] = exp_of(p[i], m);
         }
-        const float inv = 1.0f / group_sum<kLanes>(s);
+        if (kLanes * kItems != a.experts)                  // (else all of them are experts)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) p[i] = R::at(lane, i) < a.experts ? p[i] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) s += p[i];
+        s = group_sum<kLanes>(s);
+        if (__any(s != s)) {                               // a NaN, or an infinity: see which, NaN is above everything
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) key[i] = Key<T>::with_nan(key[i]);
+        }
+        const float inv = __builtin_amdgcn_rcpf(s);
         // The k best, one after the other: the next is the largest key below the last, and as whole numbers that wrap around
         // key - last is the larger the nearer the key is below.  Lane i % kLanes keeps the i-th until as many as there are lanes
         // are to be written.
-        int32_t held_expert = -1;
-        float held_gate = 0.0f;
+        K held = 0, last = 0;
         bool on = false;
-        K last = 0;
         for (int i = 0; i < a.k; ++i) {
             K best = key[0] - last;
 #pragma unroll
             for (int q = 1; q < kItems; ++q) { const K d = key[q] - last; best = d > best ? d : best; }
             best = group_reduce<kLanes>(best, [](K x, K y) { return x > y ? x : y; });
             last += best;                                  // (there are k keys at least: -inf has one, too)
-            const bool real = keep && Key<T>::real(last);
-            if (i == 0) on = real;
-            if (i % kLanes == lane) {
-                held_expert = real ? Key<T>::index(last) : -1;
-                held_gate = real ? exp_of(Key<T>::value(last), m) * inv : 0.0f;
-            }
+            if (i == 0) on = keep && Key<T>::real(last);
+            if (i % kLanes == lane) held = last;
             if ((i + 1) % kLanes == 0 || i + 1 == a.k) {
                 const int slot = i - i % kLanes + lane;
                 if (there && slot <= i) {
-                    a.expert[t * a.k + slot] = held_expert;
-                    a.gate[t * a.k + slot] = held_gate;
-                    if (held_expert >= 0) atomicAdd(&count[held_expert], 1);
+                    const bool real = keep && Key<T>::real(held);
+                    const int e = Key<T>::index(held);
+                    a.expert[t * a.k + slot] = real ? e : -1;
+                    a.gate[t * a.k + slot] = real ? exp_of(Key<T>::value(held), m) * inv : 0.0f;
+                    if (real) atomicAdd(&count[e], 1);
                 }
             }
         }
@@ -249,7 +278,7 @@ __global__ __launch_bounds__(kBalanceBlock) void k_balance_loss(const int64_t* c
 
 // Backward.  The gates' gradients of a token go to their experts' places in a row of LDS of the token's lanes, which hold zeros
 // otherwise and are cleared again after use; only the token's own lanes, which are of one wavefront, touch that row.
-template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock) void k_balance_backward(BalanceBackward a) {
+template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock, 4) void k_balance_backward(BalanceBackward a) {
     typedef Row<T, kLanes, kItems> R;
     constexpr int kTokens = kBalanceBlock / kLanes;
     constexpr int kWidth = kLanes * kItems;
@@ -265,32 +294,53 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         w[i] = e < a.experts ? (float)(c * (double)a.counts[e]) : 0.0f;
         mine[e] = 0.0f;
     }
-    for (int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes; t < a.tokens; t += (int64_t)gridDim.x * kTokens) {
-        T z[kItems];
-        R::load(static_cast<const T*>(a.logits) + t * a.stride, lane, a.experts, z);
-        const bool keep = !a.keep || a.keep[t];
+    const int64_t stride = (int64_t)gridDim.x * kTokens, start = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
+    // A token's logits, and of its choices this lane's first, are asked for while the one before it is worked on.
+    R next;
+    bool next_keep = false;
+    int32_t next_expert = -1;
+    float next_dgate = 0.0f;
+    auto ask = [&](int64_t t) {
+        const int64_t at = t < a.tokens ? t : a.tokens - 1;
+        next.load(static_cast<const T*>(a.logits) + at * a.stride, lane, a.experts);
+        next_keep = !a.keep || a.keep[at];
+        if (a.dgate && lane < a.k) {
+            next_expert = a.expert[at * a.k + lane];
+            next_dgate = a.dgate[at * a.k + lane];
+        }
+    };
+    if (a.tokens > 0) ask(start);
+    for (int64_t t = start; t < a.tokens; t += stride) {
+        const bool keep = next_keep;
+        const uint32_t expert = (uint32_t)next_expert;
+        const float dgate = next_dgate;
+        float p[kItems], m = -INFINITY;
+        next.get(lane, a.experts, p);
+        ask(t + stride);
         wavefront_exchange();                              // (the row is clear)
+        if (expert < (uint32_t)a.experts) atomicAdd(&mine[expert], dgate);
         if (a.dgate)
-            for (int i = lane; i < a.k; i += kLanes) {
+            for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
                 if (e < (uint32_t)a.experts) atomicAdd(&mine[e], a.dgate[t * a.k + i]);
             }
-        float p[kItems], m = -INFINITY, any = 0.0f;
+        bool any = false;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            p[i] = (float)z[i];
             m = fmaxf(m, p[i]);
-            any = p[i] != -INFINITY ? 1.0f : any;
+            any |= p[i] != -INFINITY;
         }
         m = group_max<kLanes>(m);
-        const bool on = keep && group_max<kLanes>(any) > 0.0f;
+        const bool on = keep && group_reduce<kLanes>((uint32_t)any, [](uint32_t x, uint32_t y) { return x | y; }) != 0;
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            p[i] = R::at(lane, i) < a.experts ? exp_of(p[i], m) : 0.0f;
-            s += p[i];
-        }
-        const float inv = 1.0f / group_sum<kLanes>(s);
+        for (int i = 0; i < kItems; ++i) p[i] = exp_of(p[i], m);
+        if (kLanes * kItems != a.experts)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) p[i] = R::at(lane, i) < a.experts ? p[i] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) s += p[i];
+        const float inv = __builtin_amdgcn_rcpf(group_sum<kLanes>(s));
         wavefront_exchange();                              // (all gradients are in the row)
         float u[kItems], dot = 0.0f;
 #pragma unroll
@@ -301,8 +351,9 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         }
         dot = group_sum<kLanes>(dot);
         wavefront_exchange();                              // (the row has been read)
+        if (expert < (uint32_t)a.experts) mine[expert] = 0.0f;
         if (a.dgate)
-            for (int i = lane; i < a.k; i += kLanes) {
+            for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
                 if (e < (uint32_t)a.experts) mine[e] = 0.0f;
             }
@@ -318,28 +369,31 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     }
 }
 
-// Lanes of a token: 16 at most up to 512 experts (reductions over 16 lanes need no LDS), and a lane's logits 8 to 32.
-int lanes_for(int32_t experts) {
-    int lanes = 1;
-    while (lanes < 16 && lanes * 8 < experts) lanes *= 2;
-    return experts <= 512 ? lanes : 64;
+// Lanes of a token and a lane's logits: 8, and from 129 experts on 16.  (A call for 131072 16-bit tokens over 256 experts takes 45 us with
+// 16 and 57 with 8, for 65536 fp32 tokens over 512 103 with either; 32 do not stay in registers with their keys and sums.)
+struct RowShape { int lanes, items; };
+RowShape row_shape(int32_t experts) {
+    RowShape r = {1, experts <= 128 ? 8 : 16};
+    while (r.lanes * r.items < experts) r.lanes *= 2;
+    return r;
 }
 int64_t balance_blocks(int64_t tokens, int32_t experts) {
-    return std::max<int64_t>(1, std::min(ceil_div(tokens, kBalanceBlock / lanes_for(experts)), kBalanceBlocks));
+    return std::max<int64_t>(1, std::min(ceil_div(tokens, kBalanceBlock / row_shape(experts).lanes), kBalanceBlocks));
 }
 
-#define P2_BALANCE_CASES(KERNEL, T)                                                                       \
-    switch (lanes_for(a.experts)) {                                                                       \
-        case 1: KERNEL<T, 1, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
-        case 2: KERNEL<T, 2, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
-        case 4: KERNEL<T, 4, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
-        case 8: KERNEL<T, 8, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;                           \
-        case 16:                                                                                          \
-            if (a.experts <= 128) KERNEL<T, 16, 8><<<grid, dim3(kBalanceBlock), 0, s>>>(a);               \
-            else if (a.experts <= 256) KERNEL<T, 16, 16><<<grid, dim3(kBalanceBlock), 0, s>>>(a);         \
-            else KERNEL<T, 16, 32><<<grid, dim3(kBalanceBlock), 0, s>>>(a);                               \
-            break;                                                                                        \
-        default: KERNEL<T, 64, 16><<<grid, dim3(kBalanceBlock), 0, s>>>(a);                               \
+#define P2_BALANCE_CASE(KERNEL, T, LANES, ITEMS) \
+    case LANES * 32 + ITEMS: KERNEL<T, LANES, ITEMS><<<grid, dim3(kBalanceBlock), 0, s>>>(a); break;
+#define P2_BALANCE_CASES(KERNEL, T)                                                     \
+    const RowShape shape = row_shape(a.experts);                                \
+    switch (shape.lanes * 32 + shape.items) {                                           \
+        P2_BALANCE_CASE(KERNEL, T, 1, 8)                                                \
+        P2_BALANCE_CASE(KERNEL, T, 2, 8)                                                \
+        P2_BALANCE_CASE(KERNEL, T, 4, 8)                                                \
+        P2_BALANCE_CASE(KERNEL, T, 8, 8)                                                \
+        P2_BALANCE_CASE(KERNEL, T, 16, 8)                                               \
+        P2_BALANCE_CASE(KERNEL, T, 16, 16)                                              \
+        P2_BALANCE_CASE(KERNEL, T, 32, 16)                                              \
+        P2_BALANCE_CASE(KERNEL, T, 64, 16)                                              \
     }
 
 }  // namespace

@@ -100,9 +100,31 @@ template <int kStep> __device__ __forceinline__ float neighbour(float v) { retur
 template <int kStep> __device__ __forceinline__ uint64_t neighbour(uint64_t v) {
     return (uint64_t)neighbour<kStep>((uint32_t)(v >> 32)) << 32 | neighbour<kStep>((uint32_t)v);
 }
-__device__ __forceinline__ float far_lane(float v, int d) { return __shfl_xor(v, d, 64); }
-__device__ __forceinline__ uint32_t far_lane(uint32_t v, int d) { return (uint32_t)__shfl_xor((int)v, d, 64); }
-__device__ __forceinline__ uint64_t far_lane(uint64_t v, int d) { return (uint64_t)__shfl_xor((unsigned long long)v, d, 64); }
+// A reduction's step over lanes 16 (32) apart: the instruction exchanges every second row of 16 lanes (half of 32) of two registers, so
+// that of a value and itself one register has the lower lanes' values twice, the other the upper lanes'.
+template <int kFar, typename F> __device__ __forceinline__ uint32_t far_step(uint32_t v, F&& f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (kFar == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return f((uint32_t)r[0], (uint32_t)r[1]);
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return f((uint32_t)r[0], (uint32_t)r[1]);
+    }
+#else
+    return f(v, v);
+#endif
+}
+template <int kFar, typename F> __device__ __forceinline__ float far_step(float v, F&& f) {
+    return __uint_as_float(far_step<kFar>(__float_as_uint(v), [&](uint32_t a, uint32_t b) { return __float_as_uint(f(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int kFar, typename F> __device__ __forceinline__ uint64_t far_step(uint64_t v, F&& f) {
+    uint32_t other_low = 0, low = 0;
+    far_step<kFar>((uint32_t)v, [&](uint32_t a, uint32_t b) { low = a; other_low = b; return a; });
+    uint32_t other_high = 0, high = 0;
+    far_step<kFar>((uint32_t)(v >> 32), [&](uint32_t a, uint32_t b) { high = a; other_high = b; return a; });
+    return f((uint64_t)high << 32 | low, (uint64_t)other_high << 32 | other_low);
+}
 
 // Reduction over groups of L consecutive lanes (a power of two up to 64); every lane gets the result, always in one order.
 template <int L, typename V, typename F> __device__ __forceinline__ V group_reduce(V v, F&& f) {
@@ -110,8 +132,8 @@ template <int L, typename V, typename F> __device__ __forceinline__ V group_redu
     if constexpr (L >= 4) v = f(v, neighbour<2>(v));
     if constexpr (L >= 8) v = f(v, neighbour<4>(v));
     if constexpr (L >= 16) v = f(v, neighbour<8>(v));
-    if constexpr (L >= 32) v = f(v, far_lane(v, 16));
-    if constexpr (L >= 64) v = f(v, far_lane(v, 32));
+    if constexpr (L >= 32) v = far_step<16>(v, f);
+    if constexpr (L >= 64) v = far_step<32>(v, f);
     return v;
 }
 template <int L> __device__ __forceinline__ float group_sum(float v) {
