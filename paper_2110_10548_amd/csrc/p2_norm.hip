@@ -73,7 +73,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     constexpr int kRows = NormGroup<kTpr>::kRows;
     __shared__ float buf[2][16];
     const int lane = threadIdx.x % kTpr, cols = (int)a.cols;
-    const float inv = 1.0f / (float)a.cols;
+    const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
     for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
         const int64_t row = row0 + threadIdx.x / kTpr;
         const bool there = row < a.rows;                   // (rows of a block's own threads: all of them, or none)
@@ -99,7 +99,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
 #pragma unroll
             for (int j = 0; j < V; ++j) s += v[i][j];
         }
-        const float mean = row_sum<kTpr>(s, buf[0]) * inv;
+        const float mean = row_sum<kTpr>(s, buf[0]) / n;
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kNv; ++i)
@@ -109,7 +109,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
                 v[i][j] -= mean;
                 s += c < cols ? v[i][j] * v[i][j] : 0.0f;
             }
-        const float rstd = 1.0f / sqrtf(row_sum<kTpr>(s, buf[1]) * inv + a.eps);
+        const float rstd = 1.0f / sqrtf(row_sum<kTpr>(s, buf[1]) / n + a.eps);
         if (there) {
             if constexpr (kNv > 2) ask_weights();
             if (lane == 0) {
@@ -137,15 +137,15 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
 // Rows too long for registers, or shorter than a vector: three passes over them, the later two from the cache.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_long(NormForward a) {
     __shared__ float buf[2][16];
-    const float inv = 1.0f / (float)a.cols;
+    const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         float s = 0.0f;
         for (int64_t c = threadIdx.x; c < a.cols; c += 1024) s += (float)x[c];
-        const float mean = row_sum<1024>(s, buf[0]) * inv;
+        const float mean = row_sum<1024>(s, buf[0]) / n;
         s = 0.0f;
         for (int64_t c = threadIdx.x; c < a.cols; c += 1024) { const float d = (float)x[c] - mean; s += d * d; }
-        const float rstd = 1.0f / sqrtf(row_sum<1024>(s, buf[1]) * inv + a.eps);
+        const float rstd = 1.0f / sqrtf(row_sum<1024>(s, buf[1]) / n + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;

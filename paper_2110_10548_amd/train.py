@@ -58,11 +58,10 @@ def _refuse(text):
 
 def _on_device(*tensors):
     """The current stream, after a look at whether all tensors are on its device."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            _refuse("tensor not on the current device")
-    return torch._C._cuda_getCurrentRawStream(here)        # (a Stream object would take 3 us to make)
+    at = {t.get_device() for t in tensors if t is not None}
+    if -1 in at or len(at) != 1 or at != {torch.cuda.current_device()}:
+        _refuse("tensors must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(at.pop())    # (a Stream object would take 3 us to make)
 
 
 def _type(t, what):
