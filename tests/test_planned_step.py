@@ -1,0 +1,18 @@
+"""The example that plans a training step's reductions and runs the operators around them."""
+import importlib.util
+import os
+
+import pytest
+
+from conftest import ROOT
+
+
+@pytest.mark.gpu
+def test_planned_step_agrees_with_one_device():
+    spec = importlib.util.spec_from_file_location("planned_step", os.path.join(ROOT, "examples", "planned_step.py"))
+    step = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(step)
+    loss, whole, off, small, large = step.main(tokens=1000, width=160, experts=24, chosen=3, say=lambda *a: None)
+    # fp32 sums of some hundred terms in another order; the update magnifies what is off by up to 485 of the norm's 1
+    assert abs(loss / whole - 1) < 1e-5 and off[0] < 1e-5 and off[1] < 5e-3
+    assert [op for op, _, _ in large.steps] != ["AllReduce"] and large.seconds < large.allreduce_seconds
