@@ -175,11 +175,11 @@ template <int kLoads> __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q come to LDS in stages of 32 values of k
-// (64 for upper halves), kStages - 1 of them under way while one is multiplied.  A row of a stage takes 128 bytes; its
+// One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q come to LDS in stages of kSub times 32
+// values of k (64 for upper halves), kStages - 1 of them under way while one is multiplied.  A row of a stage takes 128 bytes; its
 // 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
 // Rows past the end of P or Q are zeros: the loads' descriptors end with the matrix.
-template <int kTile, int kWavesM, int kWavesN, int kStages, int kTerms, int kKind>
+template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub, int kTerms, int kKind>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Product a) {
     constexpr int kWaves = kWavesM * kWavesN;
     constexpr int FM = kTile / kWavesM / 16, FN = kTile / kWavesN / 16;
@@ -188,8 +188,8 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     constexpr int kAhead = kStages - 1;
     constexpr int kPerRow = (2 * kLoads + FM - 1) / FM;    // loads issued with a row of fragments: all of them in the first half
     static_assert(kLoads * 8 * kWaves == kTile && FM * kWavesM * 16 == kTile && FN * kWavesN * 16 == kTile, "rows are dealt out evenly");
-    static_assert(2 * kLoads * (kAhead - 1) < 64, "the loads' counter");
-    __shared__ __attribute__((aligned(1024))) char lds[kStages][2][kTile * kLine];
+    static_assert(2 * kLoads * kSub * (kAhead - 1) < 64, "the loads' counter");
+    __shared__ __attribute__((aligned(1024))) char lds[kStages][kSub][2][kTile * kLine];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, of as few matrices as can be.
     int t;
@@ -224,25 +224,40 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     const Rows q = rows_of(a.q + matrix * a.q_plane, (int64_t)bj * kTile, a.cols);
     const int part = (lane & 7) ^ (lane >> 3);
     const int from = (wave * kLoads * 8 + (lane >> 3)) * (int)pitch + (kTerms == 3 ? part * 16 : (part >> 2) * kLine + (part & 3) * 16);
-    auto bring_one = [&](int stage, int l, int at) {       // the l-th load of each operand
+    auto bring_one = [&](int stage, int sub, int l, int at) {          // the l-th load of each operand
         const int src = from + l * 8 * (int)pitch;
         const int dst = (wave * kLoads + l) * 1024;
-        p.bring(&lds[stage][0][dst], src, at);
-        q.bring(&lds[stage][1][dst], src, at);
+        p.bring(&lds[stage][sub][0][dst], src, at + sub * kStepBytes);
+        q.bring(&lds[stage][sub][1][dst], src, at + sub * kStepBytes);
     };
     const int wm = wave / kWavesN, wn = wave % kWavesN;
     const int row = lane & 15, quad = lane >> 4;
     const int64_t i0 = (int64_t)bi * kTile + wm * FM * 16, j0 = (int64_t)bj * kTile + wn * FN * 16;
-    int steps = (int)(a.k / (kTerms == 3 ? 32 : 64)), begin = 0;
-    if constexpr (kKind == kPart) {                        // (every part has a step at least)
-        begin = (int)((int64_t)steps * part_of_k / a.parts);
-        steps = (int)((int64_t)steps * (part_of_k + 1) / a.parts) - begin;
+    // The result's old values are asked for first: they are there when the products are.
+    half4 high[FN], low[FN];
+    auto fetch = [&](int fi) {
+        if constexpr (kKind != kGram && kKind != kPart) {
+            if (i0 + fi * 16 >= a.rows) return;
+#pragma unroll
+            for (int fj = 0; fj < FN; ++fj) {
+                if (j0 + fj * 16 >= a.cols) continue;
+                const char* o = a.old + matrix * a.old_plane + (j0 + fj * 16 + row) * a.rows * 4 + pair_at(i0 + fi * 16 + quad * 4);
+                high[fj] = *reinterpret_cast<const half4*>(o);
+                low[fj] = *reinterpret_cast<const half4*>(o + kLine / 2);
+            }
+        }
+    };
+    fetch(0);
+    int stages = (int)(a.k / ((kTerms == 3 ? 32 : 64) * kSub)), begin = 0;
+    if constexpr (kKind == kPart) {                        // (every part has a stage at least)
+        begin = (int)((int64_t)stages * part_of_k / a.parts);
+        stages = (int)((int64_t)stages * (part_of_k + 1) / a.parts) - begin;
     }
 #pragma unroll
     for (int s = 0; s < kAhead; ++s)
-        if (s < steps)
+        if (s < stages)
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) bring_one(s, l, (begin + s) * kStepBytes);
+            for (int l = 0; l < kSub * kLoads; ++l) bring_one(s, l / kLoads, l % kLoads, (begin + s) * kSub * kStepBytes);
     float4_t acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -251,43 +266,46 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     // where this lane's 16 bytes of a row lie: highs and lows, or two pieces of highs
     const int at0 = row * kLine + (quad ^ (row & 7)) * 16, at1 = row * kLine + ((quad + 4) ^ (row & 7)) * 16;
     int stage = 0, next = kAhead;
-    for (int s = 0; s < steps; ++s) {
-        if (s + kAhead <= steps) stage_barrier<2 * kLoads * (kAhead - 1)>();
+    for (int s = 0; s < stages; ++s) {
+        if (s + kAhead <= stages) stage_barrier<2 * kLoads * kSub * (kAhead - 1)>();
         else stage_barrier<0>();
-        const bool more = s + kAhead < steps;
-        const int at = (begin + s + kAhead) * kStepBytes;
-        const char* tp = lds[stage][0] + wm * FM * 16 * kLine;
-        const char* tq = lds[stage][1] + wn * FN * 16 * kLine;
-        half8 q0[FN], q1[FN], p0, p1;
-        p0 = *reinterpret_cast<const half8*>(tp + at0);
-        p1 = *reinterpret_cast<const half8*>(tp + at1);
+        const bool more = s + kAhead < stages;
+        const int at = (begin + s + kAhead) * kSub * kStepBytes;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            q0[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at0);
-            q1[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at1);
-        }
-        // The loads of a stage to come are spread over the first rows of fragments: issued together they would hold up this
-        // stage's products for as long as the compute unit's address unit takes for all of them.
+        for (int sub = 0; sub < kSub; ++sub) {
+            const char* tp = lds[stage][sub][0] + wm * FM * 16 * kLine;
+            const char* tq = lds[stage][sub][1] + wn * FN * 16 * kLine;
+            half8 q0[FN], q1[FN], p0, p1;
+            p0 = *reinterpret_cast<const half8*>(tp + at0);
+            p1 = *reinterpret_cast<const half8*>(tp + at1);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            half8 n0, n1;
-            if (i + 1 < FM) {
-                n0 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at0);
-                n1 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at1);
+            for (int j = 0; j < FN; ++j) {
+                q0[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at0);
+                q1[j] = *reinterpret_cast<const half8*>(tq + j * 16 * kLine + at1);
             }
-            if (more)
+            // The loads of a stage to come are spread over the first rows of fragments: issued together they would hold up this
+            // stage's products for as long as the compute unit's address unit takes for all of them.
 #pragma unroll
-                for (int l = i * kPerRow; l < (i + 1) * kPerRow && l < kLoads; ++l) bring_one(next, l, at);
+            for (int i = 0; i < FM; ++i) {
+                half8 n0, n1;
+                if (i + 1 < FM) {
+                    n0 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at0);
+                    n1 = *reinterpret_cast<const half8*>(tp + (i + 1) * 16 * kLine + at1);
+                }
+                if (more)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p1, q0[j], acc[i][j]) : multiply(p0, q0[j], acc[i][j]);
+                    for (int l = i * kPerRow; l < (i + 1) * kPerRow && l < kLoads; ++l) bring_one(next, sub, l, at);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p0, q1[j], acc[i][j]) : multiply(p1, q1[j], acc[i][j]);
-            if constexpr (kTerms == 3)
+                for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p1, q0[j], acc[i][j]) : multiply(p0, q0[j], acc[i][j]);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q0[j], acc[i][j]);
-            p0 = n0;
-            p1 = n1;
-            __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p0, q1[j], acc[i][j]) : multiply(p1, q1[j], acc[i][j]);
+                if constexpr (kTerms == 3)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q0[j], acc[i][j]);
+                p0 = n0;
+                p1 = n1;
+                if constexpr (kSub == 1) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         next = stage;
         stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -310,21 +328,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     // strip goes through LDS, where a lane picks up four columns of one row.
     constexpr int kPitch = FN * 16 + 4;
     static_assert(kWaves * 16 * kPitch * 4 <= (int)sizeof(lds), "the strips fit");
-    uint32_t* strip = reinterpret_cast<uint32_t*>(&lds[0][0][0]) + wave * 16 * kPitch;
-    half4 high[FN], low[FN];
-    auto fetch = [&](int fi) {
-        if constexpr (kKind != kGram) {
-            if (i0 + fi * 16 >= a.rows) return;
-#pragma unroll
-            for (int fj = 0; fj < FN; ++fj) {
-                if (j0 + fj * 16 >= a.cols) continue;
-                const char* o = a.old + matrix * a.old_plane + (j0 + fj * 16 + row) * a.rows * 4 + pair_at(i0 + fi * 16 + quad * 4);
-                high[fj] = *reinterpret_cast<const half4*>(o);
-                low[fj] = *reinterpret_cast<const half4*>(o + kLine / 2);
-            }
-        }
-    };
-    fetch(0);
+    uint32_t* strip = reinterpret_cast<uint32_t*>(&lds[0][0][0][0]) + wave * 16 * kPitch;
 #pragma unroll
     for (int fi = 0; fi < FM; ++fi) {
         if (i0 + fi * 16 >= a.rows) break;                 // (padded sizes are whole fragments)
@@ -687,11 +691,11 @@ int64_t tiles_of(const Product& p, int64_t tile, int kind) {
     return kind == kGram || kind == kPart || kind == kPoly ? down * (down + 1) / 2 : down * across;
 }
 
-template <int kTile, int kWavesM, int kWavesN, int kStages> void product(Product p, int terms, int kind, hipStream_t s) {
+template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void product(Product p, int terms, int kind, hipStream_t s) {
     p.tiles = (int32_t)tiles_of(p, kTile, kind) * (kind == kPart ? p.parts : 1);
     const dim3 grid((unsigned)(p.tiles * p.matrices));
     const dim3 block(kWavesM * kWavesN * 64);
-#define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, TERMS, KIND><<<grid, block, 0, s>>>(p)
+#define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, TERMS == 3 ? kSub : 1, TERMS, KIND><<<grid, block, 0, s>>>(p)
     if (kind == kGram && terms == 3) P2_PRODUCT(3, kGram);
     else if (kind == kGram) P2_PRODUCT(1, kGram);
     else if (kind == kPoly) P2_PRODUCT(3, kPoly);
@@ -705,7 +709,9 @@ template <int kTile, int kWavesM, int kWavesN, int kStages> void product(Product
 // (measured, products of 1000 to 4096 rows): 256 x 256 2.45, 192 x 192 1.4, 128 x 128 0.7; of 64 x 64 several share a
 // unit's time, 0.25 for each.  Larger tiles need less of each operand's traffic and smaller ones leave fewer units idle:
 // X X^T of 4096 x 4096 takes 266 us in 136 tiles of 256, 200 in 253 of 192, 240 in 528 of 128, 340 in 2080 of 64, and B X
-// 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.
+// 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.  Where no unit has two tiles of 64 x 64 a stage's latency
+// counts: eight wavefronts and 64 values of k between barriers (updates of 512 x 512 126 us for 141, 1024 x 1024 186 for
+// 225); where units do, the LDS that this takes would keep their other tiles out (32 updates of 256 x 256 172 us for 152).
 void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     auto cost = [&](int64_t tile, double stage, bool shared) {
         const int64_t tiles = tiles_of(p, tile, kind) * p.matrices;
@@ -713,10 +719,11 @@ void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     };
     const double c64 = cost(64, 0.25, true), c128 = cost(128, 0.7, false), c192 = cost(192, 1.4, false), c256 = cost(256, 2.45, false);
     const double least = std::min({c64, c128, c192, c256});
-    if (c256 == least) product<256, 2, 4, 2>(p, terms, kind, s);
-    else if (c192 == least) product<192, 2, 4, 3>(p, terms, kind, s);
-    else if (c128 == least) product<128, 2, 4, 2>(p, terms, kind, s);
-    else product<64, 2, 2, 3>(p, terms, kind, s);
+    if (c256 == least) product<256, 2, 4, 2, 1>(p, terms, kind, s);
+    else if (c192 == least) product<192, 2, 4, 3, 1>(p, terms, kind, s);
+    else if (c128 == least) product<128, 2, 4, 2, 1>(p, terms, kind, s);
+    else if (tiles_of(p, 64, kind) * p.matrices <= kUnits) product<64, 2, 4, 3, 2>(p, terms, kind, s);
+    else product<64, 2, 2, 3, 1>(p, terms, kind, s);
 }
 
 // X X^T of a short and long X has few tiles and a long sum: it is cut into as many parts as there are compute units for, of 16
@@ -862,7 +869,7 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
         if (parts > 1) {
             p.out = sums; p.parts = (int32_t)parts;
             p.tiles = (int32_t)(tiles_of(p, 64, kPart) * parts);
-            k_newton_product<64, 2, 2, 3, 3, kPart><<<dim3((unsigned)(p.tiles * a.count)), dim3(256), 0, s>>>(p);
+            k_newton_product<64, 2, 2, 3, 2, 3, kPart><<<dim3((unsigned)(p.tiles * a.count)), dim3(256), 0, s>>>(p);
             k_newton_join<<<dim3((unsigned)tiles_of(p, 64, kPart), (unsigned)a.count), dim3(256), 0, s>>>(sums, (int32_t)parts, a.count, m, f.gram, ga, ab);
         } else {
             product_by_size(p, terms, kGram, s);
