@@ -62,40 +62,49 @@ __device__ __forceinline__ float loss_of(double sum, int64_t kept, int32_t exper
     return kept > 0 ? (float)(sum * experts / ((double)k * (double)kept * (double)kept)) : 0.0f;
 }
 
-// This lane's kItems logits of a row, in whole vectors that are asked for without a condition (RowVec); rows shorter than a
-// vector value by value.
+// This lane's kItems logits of a row, in whole vectors that are asked for without a condition (load_whole); rows shorter than a
+// vector value by value.  place(i): the expert that value i belongs to; mine(i): whether it is this lane's to count.
 template <typename T, int kLanes, int kItems> struct Row {
     static constexpr int V = 16 / sizeof(T);
     static constexpr int kVecs = kItems / V;
-    RowVec<T, V, false> raw[kVecs];
-    static __device__ __forceinline__ int at(int lane, int i) { return ((i / V) * kLanes + lane) * V + i % V; }
+    vec_t<T, V> raw[kVecs];
+    static __device__ __forceinline__ int first(int lane, int q) { return (q * kLanes + lane) * V; }
+    static __device__ __forceinline__ int place(int lane, int experts, int i) {
+        return experts >= V ? vec_at(first(lane, i / V), experts, V) + i % V : first(lane, i / V) + i % V;
+    }
+    static __device__ __forceinline__ bool mine(int lane, int experts, int i) {
+        return experts >= V ? own<V, false>(first(lane, i / V), experts, i % V) : first(lane, i / V) + i % V < experts;
+    }
     __device__ __forceinline__ void load(const T* row, int lane, int experts) {
         if (experts >= V) {
 #pragma unroll
-            for (int q = 0; q < kVecs; ++q) raw[q].load(row, (q * kLanes + lane) * V, experts);
+            for (int q = 0; q < kVecs; ++q) raw[q] = load_whole<T, V>(row, first(lane, q), experts);
         } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) raw[0].raw[j] = row[min(j, experts - 1)];
-        }
-    }
-    // -inf where there are no experts
-    __device__ __forceinline__ void get(int lane, int experts, float (&p)[kItems]) const {
-        float v[V];
-        if (experts % V == 0) {
 #pragma unroll
             for (int q = 0; q < kVecs; ++q)
 #pragma unroll
-                for (int j = 0; j < V; ++j) p[q * V + j] = (q * kLanes + lane) * V < experts ? (float)raw[q].raw[j] : -INFINITY;
-        } else if (experts > V) {
+                for (int j = 0; j < V; ++j) raw[q][j] = row[min(j, experts - 1)];
+        }
+    }
+    __device__ __forceinline__ void get(float (&p)[kItems]) const {
 #pragma unroll
-            for (int q = 0; q < kVecs; ++q) {
-                raw[q].get((q * kLanes + lane) * V, experts, -INFINITY, v);
+        for (int i = 0; i < kItems; ++i) p[i] = (float)raw[i / V][i % V];
+    }
+    // `other` in the place of values that are not this lane's to count
+    static __device__ __forceinline__ void count_once(int lane, int experts, float other, float (&p)[kItems]) {
+        if (kLanes * kItems != experts)                    // (else all of them are)
 #pragma unroll
-                for (int j = 0; j < V; ++j) p[q * V + j] = v[j];
-            }
-        } else {
+            for (int i = 0; i < kItems; ++i) p[i] = mine(lane, experts, i) ? p[i] : other;
+    }
+    __device__ __forceinline__ static void store(T* row, int lane, int experts, const float (&o)[kItems]) {
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) p[i] = at(lane, i) < experts ? (float)raw[0].raw[i % V] : -INFINITY;
+        for (int q = 0; q < kVecs; ++q) {
+            const int e = first(lane, q);
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = o[q * V + j];
+            if (experts >= V) { if (e < experts) store_vec<T, V>(row + vec_at(e, experts, V), v); }
+            else store_part<T, V>(row + e, experts - e, v);
         }
     }
 };
@@ -131,7 +140,8 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         const bool there = t < a.tokens, keep = next_keep;
         float p[kItems];
         K key[kItems];
-        next.get(lane, a.experts, p);
+        next.get(p);
+        R::count_once(lane, a.experts, -INFINITY, p);
         if (t0 + stride < a.tokens) ask(t + stride);
         float m = p[0];
 #pragma unroll
@@ -140,12 +150,10 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            key[i] = Key<T>::of(p[i], R::at(lane, i));
+            key[i] = Key<T>::of(p[i], R::place(lane, a.experts, i));
             p[i] = exp_of(p[i], m);
         }
-        if (kLanes * kItems != a.experts)                  // (else all of them are experts)
-#pragma unroll
-            for (int i = 0; i < kItems; ++i) p[i] = R::at(lane, i) < a.experts ? p[i] : 0.0f;
+        R::count_once(lane, a.experts, 0.0f, p);           // (m may be -inf)
 #pragma unroll
         for (int i = 0; i < kItems; ++i) s += p[i];
         s = group_sum<kLanes>(s);
@@ -189,7 +197,7 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     for (int i = 0; i < kItems; ++i) {
 #pragma unroll
         for (int d = kLanes; d < 64; d <<= 1) acc[i] += __shfl_xor(acc[i], d, 64);
-        if ((threadIdx.x & 63) < kLanes) sums[threadIdx.x >> 6][R::at(lane, i)] = acc[i];
+        if ((threadIdx.x & 63) < kLanes && R::mine(lane, a.experts, i)) sums[threadIdx.x >> 6][R::place(lane, a.experts, i)] = acc[i];
     }
     __syncthreads();
     const bool alone = gridDim.x == 1;
@@ -284,15 +292,15 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     constexpr int kWidth = kLanes * kItems;
     __shared__ __attribute__((aligned(16))) float extra[kTokens][kWidth];
     const int lane = threadIdx.x % kLanes;
-    float* mine = extra[threadIdx.x / kLanes];
+    float* slots = extra[threadIdx.x / kLanes];
     const double kept = (double)a.kept[0];
     const double c = kept > 0 ? (a.dloss ? (double)a.dloss[0] : 1.0) * a.experts / (a.k * kept * kept) : 0.0;
     float w[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const int e = R::at(lane, i);
+        const int e = R::place(lane, a.experts, i);
         w[i] = e < a.experts ? (float)(c * (double)a.counts[e]) : 0.0f;
-        mine[e] = 0.0f;
+        slots[R::first(lane, i / R::V) + i % R::V] = 0.0f;
     }
     const int64_t stride = (int64_t)gridDim.x * kTokens, start = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
     // A token's logits, and of its choices this lane's first, are asked for while the one before it is worked on.
@@ -315,14 +323,14 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         const uint32_t expert = (uint32_t)next_expert;
         const float dgate = next_dgate;
         float p[kItems], m = -INFINITY;
-        next.get(lane, a.experts, p);
+        next.get(p);
         ask(t + stride);
         wavefront_exchange();                              // (the row is clear)
-        if (expert < (uint32_t)a.experts) atomicAdd(&mine[expert], dgate);
+        if (expert < (uint32_t)a.experts) atomicAdd(&slots[expert], dgate);
         if (a.dgate)
             for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
-                if (e < (uint32_t)a.experts) atomicAdd(&mine[e], a.dgate[t * a.k + i]);
+                if (e < (uint32_t)a.experts) atomicAdd(&slots[e], a.dgate[t * a.k + i]);
             }
         bool any = false;
 #pragma unroll
@@ -332,40 +340,32 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         }
         m = group_max<kLanes>(m);
         const bool on = keep && group_reduce<kLanes>((uint32_t)any, [](uint32_t x, uint32_t y) { return x | y; }) != 0;
-        float s = 0.0f;
+        float s = 0.0f, counted[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) p[i] = exp_of(p[i], m);
-        if (kLanes * kItems != a.experts)
+        for (int i = 0; i < kItems; ++i) counted[i] = p[i] = exp_of(p[i], m);
+        R::count_once(lane, a.experts, 0.0f, counted);
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) p[i] = R::at(lane, i) < a.experts ? p[i] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) s += p[i];
+        for (int i = 0; i < kItems; ++i) s += counted[i];
         const float inv = __builtin_amdgcn_rcpf(group_sum<kLanes>(s));
         wavefront_exchange();                              // (all gradients are in the row)
         float u[kItems], dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            u[i] = w[i] + mine[R::at(lane, i)];
-            p[i] *= inv;
-            dot += p[i] * u[i];
+            u[i] = w[i] + slots[R::place(lane, a.experts, i)];
+            dot += counted[i] * u[i];
         }
-        dot = group_sum<kLanes>(dot);
+        dot = group_sum<kLanes>(dot) * inv;
         wavefront_exchange();                              // (the row has been read)
-        if (expert < (uint32_t)a.experts) mine[expert] = 0.0f;
+        if (expert < (uint32_t)a.experts) slots[expert] = 0.0f;
         if (a.dgate)
             for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
-                if (e < (uint32_t)a.experts) mine[e] = 0.0f;
+                if (e < (uint32_t)a.experts) slots[e] = 0.0f;
             }
-        T* out = static_cast<T*>(a.dlogits) + t * a.dlogits_stride;
+        float o[kItems];
 #pragma unroll
-        for (int q = 0; q < R::kVecs; ++q) {
-            const int e = (q * kLanes + lane) * R::V;
-            float o[R::V];
-#pragma unroll
-            for (int j = 0; j < R::V; ++j) o[j] = on ? p[q * R::V + j] * (u[q * R::V + j] - dot) : 0.0f;
-            store_part<T, R::V>(out + e, a.experts - e, o);
-        }
+        for (int i = 0; i < kItems; ++i) o[i] = on ? p[i] * inv * (u[i] - dot) : 0.0f;
+        R::store(static_cast<T*>(a.dlogits) + t * a.dlogits_stride, lane, a.experts, o);
     }
 }
 

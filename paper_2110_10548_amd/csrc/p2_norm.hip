@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kNormBlock = 256;            // threads of a block whose rows take less than a block
 constexpr int64_t kMaxNormBlocks = 1 << 20;
+constexpr int64_t kForwardThreads = 256 * 2048;          // rows beyond what fills the chip are dealt out in turn
 
 template <int kTpr> struct NormGroup {
     static constexpr int kThreads = kTpr < kNormBlock ? kNormBlock : kTpr;
@@ -37,81 +38,96 @@ template <int kTpr> __device__ __forceinline__ float row_sum(float v, float* buf
     }
 }
 
-// N weights from column c on, in whatever type they have; loaded like a row's vectors.
-template <int N, bool kWhole> struct WeightVec {
-    RowVec<float, N, kWhole> raw;              // 16-bit types: the first half of it
+// A lane's N weights, in whatever type they have; loaded like a row's vectors.
+template <int N> struct WeightVec {
+    vec_t<float, N> raw;                       // 16-bit types: the first half of it
     __device__ __forceinline__ void load(const void* p, int32_t type, int c, int cols) {
         if (type == P2_F32) {
-            raw.load(static_cast<const float*>(p), c, cols);
+            raw = load_whole<float, N>(static_cast<const float*>(p), c, cols);
         } else {
-            RowVec<half_t, N, kWhole> r;
-            r.load(static_cast<const half_t*>(p), c, cols);
             typedef float part_t __attribute__((ext_vector_type(N / 2)));
-            const part_t w = __builtin_bit_cast(part_t, r.raw);
+            const part_t w = __builtin_bit_cast(part_t, load_whole<half_t, N>(static_cast<const half_t*>(p), c, cols));
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) raw.raw[i] = w[i];
+            for (int i = 0; i < N / 2; ++i) raw[i] = w[i];
         }
     }
-    template <typename T> __device__ __forceinline__ void get_narrow(int c, int cols, float other, float (&v)[N]) const {
-        typedef float part_t __attribute__((ext_vector_type(N / 2)));
-        part_t w;
+    __device__ __forceinline__ void get(int32_t type, float (&v)[N]) const {
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) w[i] = raw.raw[i];
-        RowVec<T, N, kWhole> r;
-        r.raw = __builtin_bit_cast(decltype(r.raw), w);
-        r.get(c, cols, other, v);
-    }
-    __device__ __forceinline__ void get(int32_t type, int c, int cols, float other, float (&v)[N]) const {
-        if (type == P2_F32) raw.get(c, cols, other, v);
-        else if (type == P2_F16) get_narrow<half_t>(c, cols, other, v);
-        else get_narrow<bf16_t>(c, cols, other, v);
+        for (int i = 0; i < N; ++i) {
+            if (type == P2_F32) {
+                v[i] = raw[i];
+            } else {
+                const uint32_t w = __float_as_uint(raw[i / 2]);
+                const uint16_t h = (uint16_t)(i % 2 ? w >> 16 : w);
+                v[i] = type == P2_BF16 ? __uint_as_float((uint32_t)h << 16) : (float)__builtin_bit_cast(half_t, h);
+            }
+        }
     }
 };
 
 template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds__(NormGroup<kTpr>::kThreads) void k_norm_forward(NormForward a) {
     constexpr int V = 16 / sizeof(T);
     constexpr int kRows = NormGroup<kTpr>::kRows;
+    constexpr bool kEarly = kNv <= 2;                      // weights for all rows, and a row ahead, stay in registers
     __shared__ float buf[2][16];
-    const int lane = threadIdx.x % kTpr, cols = (int)a.cols;
+    const int lane = threadIdx.x % kTpr, group = threadIdx.x / kTpr, cols = (int)a.cols;
     const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
-    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
-        const int64_t row = row0 + threadIdx.x / kTpr;
-        const bool there = row < a.rows;                   // (rows of a block's own threads: all of them, or none)
-        const T* x = static_cast<const T*>(a.x) + (there ? row : a.rows - 1) * a.x_stride;
-        RowVec<T, V, kWhole> raw[kNv];
-        WeightVec<V, kWhole> w[kNv], b[kNv];
+    vec_t<T, V> next[kNv];
+    auto ask = [&](int64_t row) {                          // (rows of a block's own threads: all of them are there, or none)
+        const T* x = static_cast<const T*>(a.x) + (row < a.rows ? row : a.rows - 1) * a.x_stride;
 #pragma unroll
-        for (int i = 0; i < kNv; ++i) raw[i].load(x, (i * kTpr + lane) * V, cols);
-        auto ask_weights = [&] {
-            if (a.weight)
+        for (int i = 0; i < kNv; ++i) next[i] = load_whole<T, V>(x, (i * kTpr + lane) * V, cols);
+    };
+    WeightVec<V> raw_w[kNv], raw_b[kNv];
+    auto ask_weights = [&] {
+        if (a.weight)
 #pragma unroll
-                for (int i = 0; i < kNv; ++i) w[i].load(a.weight, a.weight_type, (i * kTpr + lane) * V, cols);
-            if (a.bias)
+            for (int i = 0; i < kNv; ++i) raw_w[i].load(a.weight, a.weight_type, (i * kTpr + lane) * V, cols);
+        if (a.bias)
 #pragma unroll
-                for (int i = 0; i < kNv; ++i) b[i].load(a.bias, a.weight_type, (i * kTpr + lane) * V, cols);
-        };
-        if constexpr (kNv <= 2) ask_weights();             // (there are registers to have them wait in)
+            for (int i = 0; i < kNv; ++i) raw_b[i].load(a.bias, a.weight_type, (i * kTpr + lane) * V, cols);
+    };
+    float w[kEarly ? kNv : 1][V], b[kEarly ? kNv : 1][V];
+    auto weights_of = [&](int i, float (&wv)[V], float (&bv)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) { wv[j] = 1.0f; bv[j] = 0.0f; }
+        if (a.weight) raw_w[i].get(a.weight_type, wv);
+        if (a.bias) raw_b[i].get(a.weight_type, bv);
+    };
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    if constexpr (kEarly) {
+        ask((int64_t)blockIdx.x * kRows + group);
+        ask_weights();
+#pragma unroll
+        for (int i = 0; i < kNv; ++i) weights_of(i, w[i], b[i]);
+    }
+    for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += stride) {
+        const int64_t row = row0 + group;
+        const bool there = row < a.rows;
+        if constexpr (!kEarly) ask(row);
         float v[kNv][V];
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-            raw[i].get((i * kTpr + lane) * V, cols, 0.0f, v[i]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += v[i][j];
+            for (int j = 0; j < V; ++j) {
+                v[i][j] = (float)next[i][j];
+                s += own<V, kWhole>((i * kTpr + lane) * V, cols, j) ? v[i][j] : 0.0f;
+            }
         }
+        if constexpr (kEarly) { if (row0 + stride < a.rows) ask(row + stride); }
         const float mean = row_sum<kTpr>(s, buf[0]) / n;
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < kNv; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int c = (i * kTpr + lane) * V + (kWhole ? 0 : j);
                 v[i][j] -= mean;
-                s += c < cols ? v[i][j] * v[i][j] : 0.0f;
+                s += own<V, kWhole>((i * kTpr + lane) * V, cols, j) ? v[i][j] * v[i][j] : 0.0f;
             }
         const float rstd = 1.0f / sqrtf(row_sum<kTpr>(s, buf[1]) / n + a.eps);
         if (there) {
-            if constexpr (kNv > 2) ask_weights();
+            if constexpr (!kEarly) ask_weights();
             if (lane == 0) {
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
@@ -120,15 +136,11 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
 #pragma unroll
             for (int i = 0; i < kNv; ++i) {
                 const int c = (i * kTpr + lane) * V;
-                float wv[V], bv[V];
+                if constexpr (!kEarly) weights_of(i, w[0], b[0]);
+                float o[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) { wv[j] = 1.0f; bv[j] = 0.0f; }
-                if (a.weight) w[i].get(a.weight_type, c, cols, 1.0f, wv);
-                if (a.bias) b[i].get(a.weight_type, c, cols, 0.0f, bv);
-#pragma unroll
-                for (int j = 0; j < V; ++j) wv[j] = v[i][j] * rstd * wv[j] + bv[j];
-                if constexpr (kWhole) { if (c < cols) store_vec<T, V>(y + c, wv); }
-                else store_part<T, V>(y + c, cols - c, wv);
+                for (int j = 0; j < V; ++j) o[j] = v[i][j] * rstd * w[kEarly ? i : 0][j] + b[kEarly ? i : 0][j];
+                if (c < cols) store_vec<T, V>(y + vec_at(c, cols, V), o);
             }
         }
     }
@@ -171,7 +183,8 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     constexpr int kRows = kBackBlock / kTpr;
     constexpr int kCols = kTpr * kNv * V;
     __shared__ float buf[2][2][kBackBlock / 64];
-    __shared__ float sums[2][kRows > 1 ? kCols : 1];
+    constexpr int kPart = kTpr < 64 ? 64 : kTpr;           // threads whose sums are added up before they go to LDS
+    __shared__ __attribute__((aligned(16))) float sums[kBackBlock / kPart][kRows > 1 ? kCols : 4];
     const int lane = threadIdx.x % kTpr, group = threadIdx.x / kTpr, cols = (int)a.cols;
     const float inv = 1.0f / (float)a.cols;
     float w[kNv][V], dw[kNv][V], db[kNv][V];
@@ -180,10 +193,14 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
         const int c = (i * kTpr + lane) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) { w[i][j] = 1.0f; dw[i][j] = 0.0f; db[i][j] = 0.0f; }
-        if (a.weight) load_typed<V>(a.weight, a.weight_type, c, cols - c, w[i], 0.0f);
+        if (a.weight) {
+            WeightVec<V> raw;
+            raw.load(a.weight, a.weight_type, c, cols);
+            raw.get(a.weight_type, w[i]);
+        }
     }
     // A row's values are asked for while the row before it is worked on.
-    RowVec<T, V, kWhole> nx[kNv], nd[kNv];
+    vec_t<T, V> nx[kNv], nd[kNv];
     float next_mean, next_rstd;
     auto ask = [&](int64_t row) {
         const int64_t at = row < a.rows ? row : a.rows - 1;
@@ -191,8 +208,8 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
         const T* dy = static_cast<const T*>(a.dy) + at * a.dy_stride;
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-            nx[i].load(x, (i * kTpr + lane) * V, cols);
-            nd[i].load(dy, (i * kTpr + lane) * V, cols);
+            nx[i] = load_whole<T, V>(x, (i * kTpr + lane) * V, cols);
+            nd[i] = load_whole<T, V>(dy, (i * kTpr + lane) * V, cols);
         }
         next_mean = a.mean[at];
         next_rstd = a.rstd[at];
@@ -210,9 +227,11 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-            const int c = (i * kTpr + lane) * V;
-            nx[i].get(c, cols, mean, xh[i]);
-            nd[i].get(c, cols, 0.0f, d[i]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                xh[i][j] = (float)nx[i][j];
+                d[i][j] = (float)nd[i][j];
+            }
         }
         if constexpr (kEarly) { if (row0 + stride < a.rows) ask(row + stride); }
 #pragma unroll
@@ -224,8 +243,9 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
                 dw[i][j] += there ? t : 0.0f;
                 db[i][j] += there ? d[i][j] : 0.0f;
                 d[i][j] *= w[i][j];
-                s1 += d[i][j];
-                s2 += t * w[i][j];
+                const bool mine = own<V, kWhole>((i * kTpr + lane) * V, cols, j);
+                s1 += mine ? d[i][j] : 0.0f;
+                s2 += mine ? t * w[i][j] : 0.0f;
             }
         if (a.dx) {
             // two sums at one barrier; the buffers of the next row are other ones
@@ -252,8 +272,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
                     float o[V];
 #pragma unroll
                     for (int j = 0; j < V; ++j) o[j] = rstd * (d[i][j] - m1 - xh[i][j] * m2);
-                    if constexpr (kWhole) { if (c < cols) store_vec<T, V>(dx + c, o); }
-                    else store_part<T, V>(dx + c, cols - c, o);
+                    if (c < cols) store_vec<T, V>(dx + vec_at(c, cols, V), o);
                 }
             }
         }
@@ -263,27 +282,37 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     if constexpr (kRows == 1) {
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-            const int64_t c = (int64_t)(i * kTpr + lane) * V;
-            store_part<float, V>(line + c, a.cols - c, dw[i]);
-            store_part<float, V>(line + a.cols + c, a.cols - c, db[i]);
+            const int c = (i * kTpr + lane) * V, at = vec_at(c, cols, V);
+            if (c < cols) {                                // (both lanes of a column have seen the same rows: the same sums)
+                store_vec<float, V>(line + at, dw[i]);
+                store_vec<float, V>(line + a.cols + at, db[i]);
+            }
         }
     } else {
-        for (int g = 0; g < kRows; ++g) {
-            if (group == g) {
+        // Groups of one wavefront first, then the wavefronts', side by side in LDS: a lane's values where its vectors would lie, so
+        // that column c of the vector that the row's end cuts is found further right.
+        const int cut = kWhole ? cols : (cols - 1) / V * V, further = cut - (cols - V);
 #pragma unroll
-                for (int i = 0; i < kNv; ++i)
+        for (int which = 0; which < 2; ++which) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const int c = (i * kTpr + lane) * V + j;
-                        sums[0][c] = g ? sums[0][c] + dw[i][j] : dw[i][j];
-                        sums[1][c] = g ? sums[1][c] + db[i][j] : db[i][j];
-                    }
+            for (int i = 0; i < kNv; ++i) {
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    v[j] = which ? db[i][j] : dw[i][j];
+#pragma unroll
+                    for (int d = kTpr; d < 64; d <<= 1) v[j] += __shfl_xor(v[j], d, 64);
+                }
+                if (kTpr >= 64 || (threadIdx.x & 63) < kTpr) store_vec<float, V>(&sums[threadIdx.x / kPart][(i * kTpr + lane) * V], v);
             }
             __syncthreads();
-        }
-        for (int64_t c = threadIdx.x; c < a.cols; c += kBackBlock) {
-            line[c] = sums[0][c];
-            line[a.cols + c] = sums[1][c];
+            for (int c = threadIdx.x; c < cols; c += kBackBlock) {
+                float s = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kBackBlock / kPart; ++q) s += sums[q][kWhole || c < cut ? c : c + further];
+                line[which * a.cols + c] = s;
+            }
+            __syncthreads();
         }
     }
 }
@@ -351,7 +380,7 @@ __global__ __launch_bounds__(1024) void k_norm_weight_grad(const float* __restri
 
 template <typename T, int kTpr, int kNv> void forward_as(const NormForward& a, hipStream_t s) {
     constexpr int kRows = NormGroup<kTpr>::kRows;
-    const dim3 grid((unsigned)std::min(ceil_div(a.rows, kRows), kMaxNormBlocks)), block(NormGroup<kTpr>::kThreads);
+    const dim3 grid((unsigned)std::min(ceil_div(a.rows, kRows), kForwardThreads / NormGroup<kTpr>::kThreads)), block(NormGroup<kTpr>::kThreads);
     if (a.cols % (16 / sizeof(T)) == 0) k_norm_forward<T, kTpr, kNv, true><<<grid, block, 0, s>>>(a);
     else k_norm_forward<T, kTpr, kNv, false><<<grid, block, 0, s>>>(a);
 }
@@ -365,7 +394,7 @@ template <typename T> void forward_of(const NormForward& a, hipStream_t s) {
     else if (vecs <= 128) forward_as<T, 64, 2>(a, s);
     else if (vecs <= 256) forward_as<T, 256, 1>(a, s);
     else if (vecs <= 512) forward_as<T, 256, 2>(a, s);
-    else if (vecs <= 1024) forward_as<T, 256, 4>(a, s);
+    else if (vecs <= 1024) forward_as<T, 512, 2>(a, s);
     else forward_as<T, 1024, 4>(a, s);
 }
 

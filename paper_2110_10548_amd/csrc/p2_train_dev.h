@@ -49,34 +49,18 @@ template <typename T, int N> __device__ __forceinline__ void store_part(T* p, in
     for (int i = 0; i < N; ++i) if (i < n) p[i] = (T)v[i];
 }
 
-// N elements of a row from column c on, of which those before `cols` count (N <= cols).  The load itself is always a whole
-// vector inside the row and depends on nothing, so that many of them are under way together: the vector that the row's end cuts
-// is read from further left and moved.  kWhole: the rows are whole vectors.
-template <typename T, int N, bool kWhole> struct RowVec {
-    vec_t<T, N> raw;
-    __device__ __forceinline__ void load(const T* row, int c, int cols) { raw = *reinterpret_cast<const vec_t<T, N>*>(row + min(c, cols - N)); }
-    __device__ __forceinline__ void get(int c, int cols, float other, float (&v)[N]) const {
-        if constexpr (kWhole) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = c < cols ? (float)raw[i] : other;
-        } else {
-            constexpr int kWords = N * (int)sizeof(T) / 4;
-            typedef uint32_t words_t __attribute__((ext_vector_type(kWords)));
-            words_t w = __builtin_bit_cast(words_t, raw);
-            const int by = max(0, c - (cols - N)) * (int)sizeof(T);            // bytes; more than there are: nothing counts
-#pragma unroll
-            for (int d = kWords / 2; d >= 1; d /= 2)
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[i] = by & 4 * d ? (i + d < kWords ? w[i + d] : 0u) : w[i];
-            if constexpr (sizeof(T) == 2)
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[i] = by & 2 ? w[i] >> 16 | (i + 1 < kWords ? w[i + 1] << 16 : 0u) : w[i];
-            const vec_t<T, N> r = __builtin_bit_cast(vec_t<T, N>, w);
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = c + i < cols ? (float)r[i] : other;
-        }
-    }
-};
+// A lane's N elements of a row, from column c on (N <= cols).  The load is always a whole vector inside the row and depends on
+// nothing, so that many of them are under way together.  Where the row's end cuts the vector, or lies before it, the last N elements are
+// taken instead: those before column c are another lane's, too.  They count once, for that lane; what a lane makes of them is
+// the same, so whole vectors are stored as well.
+__device__ __forceinline__ int vec_at(int c, int cols, int n) { return min(c, cols - n); }
+template <typename T, int N> __device__ __forceinline__ vec_t<T, N> load_whole(const T* row, int c, int cols) {
+    return *reinterpret_cast<const vec_t<T, N>*>(row + vec_at(c, cols, N));
+}
+// Whether element j of the vector is this lane's.  kWhole: the row is whole vectors, and the lane has all of its own or none.
+template <int N, bool kWhole> __device__ __forceinline__ bool own(int c, int cols, int j) {
+    return kWhole ? c < cols : j >= c - vec_at(c, cols, N);
+}
 
 // Weights have a type of their own, which the whole launch agrees on.
 template <int N> __device__ __forceinline__ void load_typed(const void* p, int32_t type, int64_t at, int64_t n, float (&v)[N], float other) {

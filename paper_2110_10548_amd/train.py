@@ -56,12 +56,15 @@ def _refuse(text):
     raise P2Error(P2_EINVAL, text)
 
 
-def _on_device(*tensors):
+def _on_device(first, *others):
     """The current stream, after a look at whether all tensors are on its device."""
-    at = {t.get_device() for t in tensors if t is not None}
-    if -1 in at or len(at) != 1 or at != {torch.cuda.current_device()}:
+    here = first.get_device()
+    if here < 0 or here != torch._C._cuda_getDevice():
         _refuse("tensors must be on the current device")
-    return torch._C._cuda_getCurrentRawStream(at.pop())    # (a Stream object would take 3 us to make)
+    for t in others:
+        if t is not None and t.get_device() != here:
+            _refuse("tensors must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(here)        # (a Stream object would take 3 us to make)
 
 
 def _type(t, what):
@@ -72,14 +75,22 @@ def _type(t, what):
 
 
 def _rows(t):
-    """`t` as a matrix whose rows are contiguous, and the distance between them."""
+    """(matrix whose rows are contiguous, rows, columns, distance between rows) of t [..., columns]."""
+    if t.dim() == 2:
+        n, cols = t.shape
+        stride, one = t.stride()
+        if one == 1 and stride >= cols:
+            return t, n, cols, stride
     cols = t.shape[-1]
-    if t.dim() != 2:
-        t = t.reshape(-1, cols) if cols else t.reshape(0, 0)
+    t = t.reshape(-1, cols) if cols else t.reshape(0, 0)
     n = t.shape[0]
     if (cols > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < cols):
         t = t.contiguous()
-    return t, (t.stride(0) if n > 1 else max(cols, 1))
+    return t, n, cols, (t.stride(0) if n > 1 else max(cols, 1))
+
+
+def _like(t):
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _ptr(t):
@@ -102,18 +113,17 @@ def p2_layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     if x.dim() < 1:
         _refuse("x must have at least one dimension")
     stream = _on_device(x, weight, bias)
-    kind, cols = _type(x, "x"), x.shape[-1]
+    kind = _type(x, "x")
+    rows, n, cols, stride_x = _rows(x)
     weight, bias = _vector(weight, cols, "weight"), _vector(bias, cols, "bias")
     given = weight if weight is not None else bias
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         _refuse("weight and bias must have the same type")
-    rows, stride = _rows(x)
-    n = rows.shape[0]
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _like(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    B._check(lib().p2_layer_norm_forward(rows.data_ptr(), kind, stride, _ptr(weight), _ptr(bias), kind if given is None else _type(given, "weight"),
-                                         n, cols, eps, y.data_ptr(), max(cols, 1), mean.data_ptr(), rstd.data_ptr(), stream))
+    rstd = torch.empty_like(mean)
+    B._check(lib().p2_layer_norm_forward(rows.data_ptr(), kind, stride_x, _ptr(weight), _ptr(bias), kind if given is None else _type(given, "weight"),
+                                         n, cols, eps, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), stream))
     return y, mean, rstd
 
 
@@ -122,20 +132,18 @@ def p2_layer_norm_backward(dy, x, weight, mean, rstd, dx=True, dweight=True, dbi
     if dy.shape != x.shape or dy.dtype != x.dtype or x.dim() < 1:
         _refuse("dy and x must have the same shape and type")
     stream = _on_device(dy, x, weight, mean, rstd)
-    kind, cols = _type(x, "x"), x.shape[-1]
+    kind = _type(x, "x")
+    rows, n, cols, stride_x = _rows(x)
+    drows, _, _, stride_dy = _rows(dy)
     weight = _vector(weight, cols, "weight")
-    rows, stride = _rows(x)
-    drows, dstride = _rows(dy)
-    n = rows.shape[0]
-    mean, rstd = (_vector(t.reshape(-1), n, "mean and rstd", torch.float32) for t in (mean, rstd))
-    sums = x.dtype if weight is None else weight.dtype
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx else None
-    dw = torch.empty(cols, dtype=sums, device=x.device) if dweight else None
-    db = torch.empty(cols, dtype=sums, device=x.device) if dbias else None
+    mean, rstd = _vector(mean.reshape(-1), n, "mean", torch.float32), _vector(rstd.reshape(-1), n, "rstd", torch.float32)
+    like = x if weight is None else weight
+    out = _like(x) if dx else None
+    dw = torch.empty(cols, dtype=like.dtype, device=x.device) if dweight else None
+    db = torch.empty(cols, dtype=like.dtype, device=x.device) if dbias else None
     work, size = _workspace("p2_layer_norm_backward_workspace", (n, cols), x) if dweight or dbias else (None, 0)
-    B._check(lib().p2_layer_norm_backward(drows.data_ptr(), dstride, rows.data_ptr(), stride, kind, _ptr(weight),
-                                          kind if weight is None else _type(weight, "weight"), mean.data_ptr(), rstd.data_ptr(), n, cols,
-                                          _ptr(out), max(cols, 1), _ptr(dw), _ptr(db), _ptr(work), size, stream))
+    B._check(lib().p2_layer_norm_backward(drows.data_ptr(), stride_dy, rows.data_ptr(), stride_x, kind, _ptr(weight), _type(like, "weight"),
+                                          mean.data_ptr(), rstd.data_ptr(), n, cols, _ptr(out), cols, _ptr(dw), _ptr(db), _ptr(work), size, stream))
     return out, dw, db
 
 
@@ -153,18 +161,16 @@ def p2_balance_forward(logits, k, keep=None):
     keep = _tokens(logits, keep)
     stream = _on_device(logits, keep)
     kind = _type(logits, "logits")
-    rows, stride = _rows(logits)
-    n, e = rows.shape
+    rows, n, e, stride_z = _rows(logits)
     d = logits.device
-    room = max(int(k), 0)
-    expert = torch.empty((n, room), dtype=torch.int32, device=d)
-    gate = torch.empty((n, room), dtype=torch.float32, device=d)
+    expert = torch.empty((n, max(k, 0)), dtype=torch.int32, device=d)
+    gate = torch.empty_like(expert, dtype=torch.float32)
     counts = torch.empty(e, dtype=torch.int64, device=d)
-    prob_sum = torch.empty(e, dtype=torch.float32, device=d)
+    prob_sum = torch.empty_like(counts, dtype=torch.float32)
     kept = torch.empty((), dtype=torch.int64, device=d)
-    loss = torch.empty((), dtype=torch.float32, device=d)
+    loss = torch.empty_like(kept, dtype=torch.float32)
     work, size = _workspace("p2_balance_forward_workspace", (n, e), logits)
-    B._check(lib().p2_balance_forward(rows.data_ptr(), kind, stride, _ptr(keep), n, e, k, expert.data_ptr(), gate.data_ptr(), counts.data_ptr(),
+    B._check(lib().p2_balance_forward(rows.data_ptr(), kind, stride_z, _ptr(keep), n, e, k, expert.data_ptr(), gate.data_ptr(), counts.data_ptr(),
                                       prob_sum.data_ptr(), kept.data_ptr(), loss.data_ptr(), _ptr(work), size, stream))
     return {"expert": expert, "gate": gate, "counts": counts, "prob_sum": prob_sum, "tokens": kept, "loss": loss}
 
@@ -190,8 +196,7 @@ def p2_balance_backward(logits, expert, counts, tokens, keep=None, dgate=None, d
     keep = _tokens(logits, keep)
     stream = _on_device(logits, expert, counts, tokens, keep, dgate, dloss)
     kind = _type(logits, "logits")
-    rows, stride = _rows(logits)
-    n, e = rows.shape
+    rows, n, e, stride_z = _rows(logits)
     if expert.dtype != torch.int32 or expert.dim() != 2 or expert.shape[0] != n:
         _refuse("expert must be int32 [tokens, k]")
     k = expert.shape[1]
@@ -201,8 +206,8 @@ def p2_balance_backward(logits, expert, counts, tokens, keep=None, dgate=None, d
         _refuse("dloss must be one float32")
     counts = _statistics(counts, tokens, e)
     expert, dgate = expert.contiguous(), None if dgate is None else dgate.contiguous()
-    out = torch.empty((n, e), dtype=logits.dtype, device=logits.device)
-    B._check(lib().p2_balance_backward(rows.data_ptr(), kind, stride, _ptr(keep), n, e, k, expert.data_ptr(), _ptr(dgate), counts.data_ptr(),
+    out = _like(logits)
+    B._check(lib().p2_balance_backward(rows.data_ptr(), kind, stride_z, _ptr(keep), n, e, k, expert.data_ptr(), _ptr(dgate), counts.data_ptr(),
                                        tokens.data_ptr(), _ptr(dloss), out.data_ptr(), max(e, 1), stream))
     return out
 
