@@ -62,28 +62,28 @@ __device__ __forceinline__ float loss_of(double sum, int64_t kept, int32_t exper
     return kept > 0 ? (float)(sum * experts / ((double)k * (double)kept * (double)kept)) : 0.0f;
 }
 
-// This lane's kItems logits of a row, in whole vectors that are asked for without a condition (load_whole); rows shorter than a
-// vector value by value.  place(i): the expert that value i belongs to; mine(i): whether it is this lane's to count.
+// This lane's kItems logits of a row, in whole vectors that are asked for without a condition (load_whole); a row shorter than a
+// vector, which one lane has alone, value by value.  place(i): the expert that value i belongs to; mine(i): whether it is this
+// lane's to count.
 template <typename T, int kLanes, int kItems> struct Row {
     static constexpr int V = 16 / sizeof(T);
     static constexpr int kVecs = kItems / V;
     vec_t<T, V> raw[kVecs];
+    static __device__ __forceinline__ bool is_short(int experts) { return kLanes == 1 && experts < V; }
     static __device__ __forceinline__ int first(int lane, int q) { return (q * kLanes + lane) * V; }
     static __device__ __forceinline__ int place(int lane, int experts, int i) {
-        return experts >= V ? vec_at(first(lane, i / V), experts, V) + i % V : first(lane, i / V) + i % V;
+        return is_short(experts) ? i : vec_at(first(lane, i / V), experts, V) + i % V;
     }
     static __device__ __forceinline__ bool mine(int lane, int experts, int i) {
-        return experts >= V ? own<V, false>(first(lane, i / V), experts, i % V) : first(lane, i / V) + i % V < experts;
+        return is_short(experts) ? i < experts : own<V, false>(first(lane, i / V), experts, i % V);
     }
     __device__ __forceinline__ void load(const T* row, int lane, int experts) {
-        if (experts >= V) {
+        if (!is_short(experts)) {
 #pragma unroll
             for (int q = 0; q < kVecs; ++q) raw[q] = load_whole<T, V>(row, first(lane, q), experts);
         } else {
 #pragma unroll
-            for (int q = 0; q < kVecs; ++q)
-#pragma unroll
-                for (int j = 0; j < V; ++j) raw[q][j] = row[min(j, experts - 1)];
+            for (int i = 0; i < kItems; ++i) raw[i / V][i % V] = row[min(i, experts - 1)];
         }
     }
     __device__ __forceinline__ void get(float (&p)[kItems]) const {
@@ -96,15 +96,27 @@ template <typename T, int kLanes, int kItems> struct Row {
 #pragma unroll
             for (int i = 0; i < kItems; ++i) p[i] = mine(lane, experts, i) ? p[i] : other;
     }
+    static __device__ __forceinline__ float sum_once(int lane, int experts, const float (&p)[kItems]) {
+        float s = 0.0f;
+        if (kLanes * kItems == experts) {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) s += p[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) s += mine(lane, experts, i) ? p[i] : 0.0f;
+        }
+        return s;
+    }
+    // Every lane stores all of its vectors, also where another one stores the same: with stores that depend on nothing the compiler
+    // can count what is under way, and the next row's loads need not wait for them.
     __device__ __forceinline__ static void store(T* row, int lane, int experts, const float (&o)[kItems]) {
 #pragma unroll
         for (int q = 0; q < kVecs; ++q) {
-            const int e = first(lane, q);
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = o[q * V + j];
-            if (experts >= V) { if (e < experts) store_vec<T, V>(row + vec_at(e, experts, V), v); }
-            else store_part<T, V>(row + e, experts - e, v);
+            if (!is_short(experts)) store_vec<T, V>(row + vec_at(first(lane, q), experts, V), v);
+            else store_part<T, V>(row + q * V, experts - q * V, v);
         }
     }
 };
@@ -227,31 +239,33 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     }
 }
 
-// Adds up the blocks' lines: 16 experts a block (the tokens that count are one more column), 64 threads each.  The block
-// that is done last works the loss out.
-__global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t lines) {
-    __shared__ float prob[64][17];
-    __shared__ int64_t count[64][17];
+// Adds up the blocks' lines: kWide experts a block (the tokens that count are one more column), 1024 / kWide threads each.  Where
+// one block has all of them it works the loss out, too; else the block that is done last.
+template <int kWide> __global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t lines) {
+    constexpr int kDeep = 1024 / kWide;
+    __shared__ float prob[kDeep][kWide + 1];
+    __shared__ int64_t count[kDeep][kWide + 1];
     __shared__ double buf[16];
     __shared__ bool last;
-    const int x = threadIdx.x & 15, r = threadIdx.x >> 4;
-    const int e = blockIdx.x * 16 + x;
+    const int x = threadIdx.x % kWide, r = threadIdx.x / kWide;
+    const int e = blockIdx.x * kWide + x;
     float s = 0.0f;
     int64_t n = 0;
     if (e <= a.experts) {
         const int column = min(e, a.experts - 1);
 #pragma unroll 8
-        for (int l = r; l < lines; l += 64) {
+        for (int l = r; l < lines; l += kDeep) {
             s += a.part_prob[(int64_t)l * a.experts + column];
             n += a.part_count[(int64_t)l * (a.experts + 1) + e];
         }
     }
     prob[r][x] = s;
     count[r][x] = n;
-    for (int d = 32; d >= 1; d >>= 1) {
+    for (int d = kDeep / 2; d >= 1; d >>= 1) {
         __syncthreads();
         if (r < d) { prob[r][x] += prob[r + d][x]; count[r][x] += count[r + d][x]; }
     }
+    __syncthreads();
     if (r == 0 && e <= a.experts) {
         if (e < a.experts) {
             a.prob_sum[e] = prob[0][x];
@@ -259,6 +273,13 @@ __global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t 
         } else {
             a.kept[0] = count[0][x];
         }
+    }
+    double l = 0.0;
+    if (gridDim.x == 1) {
+        if (r == 0 && e < a.experts) l = (double)prob[0][x] * (double)count[0][x];
+        l = block_sum(l, buf);
+        if (threadIdx.x == 0) a.loss[0] = loss_of(l, count[0][a.experts], a.experts, a.k);
+        return;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -269,7 +290,6 @@ __global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t 
     __syncthreads();
     if (!last) return;
     __threadfence();
-    double l = 0.0;
     for (int q = threadIdx.x; q < a.experts; q += 1024) l += (double)a.prob_sum[q] * (double)a.counts[q];
     l = block_sum(l, buf);
     if (threadIdx.x == 0) a.loss[0] = loss_of(l, a.kept[0], a.experts, a.k);
@@ -340,21 +360,21 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         }
         m = group_max<kLanes>(m);
         const bool on = keep && group_reduce<kLanes>((uint32_t)any, [](uint32_t x, uint32_t y) { return x | y; }) != 0;
-        float s = 0.0f, counted[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) counted[i] = p[i] = exp_of(p[i], m);
-        R::count_once(lane, a.experts, 0.0f, counted);
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) s += counted[i];
-        const float inv = __builtin_amdgcn_rcpf(group_sum<kLanes>(s));
+        for (int i = 0; i < kItems; ++i) p[i] = exp_of(p[i], m);
+        const float inv = __builtin_amdgcn_rcpf(group_sum<kLanes>(R::sum_once(lane, a.experts, p)));
         wavefront_exchange();                              // (all gradients are in the row)
-        float u[kItems], dot = 0.0f;
+        float u[kItems];
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) u[i] = slots[R::place(lane, a.experts, i)];
+        float pu[kItems];
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            u[i] = w[i] + slots[R::place(lane, a.experts, i)];
-            dot += counted[i] * u[i];
+            u[i] += w[i];
+            p[i] *= inv;
+            pu[i] = p[i] * u[i];
         }
-        dot = group_sum<kLanes>(dot) * inv;
+        const float dot = group_sum<kLanes>(R::sum_once(lane, a.experts, pu));
         wavefront_exchange();                              // (the row has been read)
         if (expert < (uint32_t)a.experts) slots[expert] = 0.0f;
         if (a.dgate)
@@ -364,7 +384,7 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
             }
         float o[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) o[i] = on ? p[i] * inv * (u[i] - dot) : 0.0f;
+        for (int i = 0; i < kItems; ++i) o[i] = on ? p[i] * (u[i] - dot) : 0.0f;
         R::store(static_cast<T*>(a.dlogits) + t * a.dlogits_stride, lane, a.experts, o);
     }
 }
@@ -408,7 +428,8 @@ hipError_t launch_balance_forward(const BalanceForward& a, hipStream_t s) {
     else { P2_BALANCE_CASES(k_balance_forward, half_t) }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    k_balance_sum<<<dim3((unsigned)ceil_div(a.experts + 1, 16)), dim3(1024), 0, s>>>(a, (int32_t)blocks);
+    if (a.experts < 64) k_balance_sum<64><<<dim3(1), dim3(1024), 0, s>>>(a, (int32_t)blocks);
+    else k_balance_sum<16><<<dim3((unsigned)ceil_div(a.experts + 1, 16)), dim3(1024), 0, s>>>(a, (int32_t)blocks);
     return hipGetLastError();
 }
 
