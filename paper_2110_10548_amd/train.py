@@ -120,7 +120,7 @@ def p2_layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         _refuse("weight and bias must have the same type")
     y = _like(x)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean = torch.empty(n if x.dim() == 2 else x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     B._check(lib().p2_layer_norm_forward(rows.data_ptr(), kind, stride_x, _ptr(weight), _ptr(bias), kind if given is None else _type(given, "weight"),
                                          n, cols, eps, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), stream))
