@@ -77,6 +77,13 @@ template <typename T, int kLanes, int kItems> struct Row {
     static __device__ __forceinline__ bool mine(int lane, int experts, int i) {
         return is_short(experts) ? i < experts : own<V, false>(first(lane, i / V), experts, i % V);
     }
+    // Where expert e's value lies in a row of LDS: the lanes' i-th values side by side.  Rows are kPitch apart, so that what the
+    // wavefront's lanes read at once lies in different banks.
+    static constexpr int kPitch = kLanes * (kItems + 1);
+    static __device__ __forceinline__ int slot(int e) {
+        const int v = e / V;
+        return ((v / kLanes) * V + e % V) * kLanes + v % kLanes;
+    }
     __device__ __forceinline__ void load(const T* row, int lane, int experts) {
         if (!is_short(experts)) {
 #pragma unroll
@@ -309,18 +316,19 @@ __global__ __launch_bounds__(kBalanceBlock) void k_balance_loss(const int64_t* c
 template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock, 4) void k_balance_backward(BalanceBackward a) {
     typedef Row<T, kLanes, kItems> R;
     constexpr int kTokens = kBalanceBlock / kLanes;
-    constexpr int kWidth = kLanes * kItems;
-    __shared__ __attribute__((aligned(16))) float extra[kTokens][kWidth];
+    __shared__ float extra[kTokens][R::kPitch];
     const int lane = threadIdx.x % kLanes;
     float* slots = extra[threadIdx.x / kLanes];
     const double kept = (double)a.kept[0];
     const double c = kept > 0 ? (a.dloss ? (double)a.dloss[0] : 1.0) * a.experts / (a.k * kept * kept) : 0.0;
     float w[kItems];
+    int from[kItems];                                      // this lane's values in the row
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
         const int e = R::place(lane, a.experts, i);
         w[i] = e < a.experts ? (float)(c * (double)a.counts[e]) : 0.0f;
-        slots[R::first(lane, i / R::V) + i % R::V] = 0.0f;
+        from[i] = R::slot(e);
+        slots[i * kLanes + lane] = 0.0f;
     }
     const int64_t stride = (int64_t)gridDim.x * kTokens, start = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
     // A token's logits, and of its choices this lane's first, are asked for while the one before it is worked on.
@@ -346,11 +354,11 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         next.get(p);
         ask(t + stride);
         wavefront_exchange();                              // (the row is clear)
-        if (expert < (uint32_t)a.experts) atomicAdd(&slots[expert], dgate);
+        if (expert < (uint32_t)a.experts) atomicAdd(&slots[R::slot(expert)], dgate);
         if (a.dgate)
             for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
-                if (e < (uint32_t)a.experts) atomicAdd(&slots[e], a.dgate[t * a.k + i]);
+                if (e < (uint32_t)a.experts) atomicAdd(&slots[R::slot(e)], a.dgate[t * a.k + i]);
             }
         bool any = false;
 #pragma unroll
@@ -366,7 +374,7 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         wavefront_exchange();                              // (all gradients are in the row)
         float u[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) u[i] = slots[R::place(lane, a.experts, i)];
+        for (int i = 0; i < kItems; ++i) u[i] = slots[from[i]];
         float pu[kItems];
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
@@ -376,11 +384,11 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         }
         const float dot = group_sum<kLanes>(R::sum_once(lane, a.experts, pu));
         wavefront_exchange();                              // (the row has been read)
-        if (expert < (uint32_t)a.experts) slots[expert] = 0.0f;
+        if (expert < (uint32_t)a.experts) slots[R::slot(expert)] = 0.0f;
         if (a.dgate)
             for (int i = lane + kLanes; i < a.k; i += kLanes) {
                 const uint32_t e = (uint32_t)a.expert[t * a.k + i];
-                if (e < (uint32_t)a.experts) slots[e] = 0.0f;
+                if (e < (uint32_t)a.experts) slots[R::slot(e)] = 0.0f;
             }
         float o[kItems];
 #pragma unroll
