@@ -35,7 +35,7 @@ __device__ __forceinline__ int64_t pair_at(int64_t k) { return (k >> 5) * kLine 
 __device__ __forceinline__ float4_t multiply(half8 p, half8 q, float4_t sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, sum, 0, 0, 0); }
 __device__ __forceinline__ void split(float v, half_t& high, half_t& low) {
     high = (half_t)v;
-    low = (half_t)(v - (float)high);
+    low = (half_t)fmaf((float)high, -1.0f, v);             // (one instruction with the conversion)
 }
 
 __device__ __forceinline__ uint32_t pack(float v) {
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float v = acc[fi][fj][r] * a.sum_factor;
-                if constexpr (kKind != kGram) v += ((float)high[fj][r] + (float)low[fj][r]) * a.old_factor;
+                if constexpr (kKind != kGram) v = fmaf((float)high[fj][r], a.old_factor, fmaf((float)low[fj][r], a.old_factor, v));
                 w[fj][r] = kKind == kLast ? __float_as_uint(v * a.gain) : pack(v);
             }
         if (fi + 1 < FM) fetch(fi + 1);
@@ -380,9 +380,13 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     }
 }
 
-__device__ __forceinline__ float4_t load_halves(const half_t* high, const half_t* low) {
+// v * factor + (high + low) * old_factor
+__device__ __forceinline__ float4_t add_halves(float4_t v, float factor, const half_t* high, const half_t* low, float old_factor) {
     const half4 h = *reinterpret_cast<const half4*>(high), l = *reinterpret_cast<const half4*>(low);
-    return float4_t{(float)h[0] + (float)l[0], (float)h[1] + (float)l[1], (float)h[2] + (float)l[2], (float)h[3] + (float)l[3]};
+    float4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = fmaf((float)h[i], old_factor, fmaf((float)l[i], old_factor, v[i] * factor));
+    return r;
 }
 __device__ __forceinline__ void store_halves(half_t* high, half_t* low, float4_t v) {
     half4 h, l;
@@ -553,7 +557,7 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
             for (int x = 0; x < FM; ++x)
 #pragma unroll
                 for (int y = 0; y < FN; ++y)
-                    acc[x][y] = acc[x][y] * a.poly_sum[step] + load_halves(ah + at_of(x, y), al + at_of(x, y)) * a.poly_old[step];
+                    acc[x][y] = add_halves(acc[x][y], a.poly_sum[step], ah + at_of(x, y), al + at_of(x, y), a.poly_old[step]);
         __syncthreads();                                   // everybody has read A
         place(1.0f);
         __syncthreads();
@@ -586,7 +590,7 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
 #pragma unroll
             for (int i = 0; i < 2 * kBlocks; ++i) {
                 const int at = small_at(i * 16 + row, jb + quad * 4, XP, x_mask);
-                c[i] = c[i] * a.apply_sum[step] + load_halves(xh + at, xl + at) * a.apply_old[step];
+                c[i] = add_halves(c[i], a.apply_sum[step], xh + at, xl + at, a.apply_old[step]);
             }
             wavefront_exchange();                          // (all lanes have their columns)
 #pragma unroll
