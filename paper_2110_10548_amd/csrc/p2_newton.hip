@@ -127,7 +127,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(cons
     }
 }
 
-enum : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3, kPart = 4 };
+enum : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3, kPart = 4, kLastHalf = 5 };     // kLast: fp32, of upper halves bf16; kLastHalf: fp16
 
 struct Product {
     const char* p; const char* q;              // pairs: rows of P and of Q
@@ -140,7 +140,7 @@ struct Product {
     int64_t rows, cols;                        // padded size of the result
     int64_t out_rows, out_cols, out_stride;    // kLast: the result's own, and whether it is to be written turned
     float old_factor, sum_factor, gain;        // (old * old_factor + sum * sum_factor) * gain
-    int32_t out_turned, out_type;
+    int32_t out_turned;
     int32_t tiles, parts;                      // blocks of a matrix; kPart: parts that k is cut into
     int64_t matrices;
 };
@@ -175,12 +175,17 @@ template <int kLoads> __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");
 }
 
+template <bool kFirst, typename A, typename B> struct Pick { typedef A type; };
+template <typename A, typename B> struct Pick<false, A, B> { typedef B type; };
+
 // One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q come to LDS in stages of kSub times 32
 // values of k (64 for upper halves), kStages - 1 of them under way while one is multiplied.  A row of a stage takes 128 bytes; its
 // 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
 // Rows past the end of P or Q are zeros: the loads' descriptors end with the matrix.
 template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub, int kTerms, int kKind>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Product a) {
+    constexpr bool kEnd = kKind == kLast || kKind == kLastHalf;
+    typedef typename Pick<kKind == kLastHalf, half_t, typename Pick<kTerms == 1, bf16_t, float>::type>::type Out;
     constexpr int kWaves = kWavesM * kWavesN;
     constexpr int FM = kTile / kWavesM / 16, FN = kTile / kWavesN / 16;
     constexpr int kStepBytes = kTerms == 3 ? kLine : 2 * kLine;
@@ -339,24 +344,24 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
             for (int r = 0; r < 4; ++r) {
                 float v = acc[fi][fj][r] * a.sum_factor;
                 if constexpr (kKind != kGram) v = fmaf((float)high[fj][r], a.old_factor, fmaf((float)low[fj][r], a.old_factor, v));
-                w[fj][r] = kKind == kLast ? __float_as_uint(v * a.gain) : pack(v);
+                w[fj][r] = kEnd ? __float_as_uint(v * a.gain) : pack(v);
             }
         if (fi + 1 < FM) fetch(fi + 1);
         const int64_t i = i0 + fi * 16 + quad * 4;
-        if (kKind != kLast || a.out_turned) {
-            char* t = kKind == kApply ? a.turned + matrix * a.q_plane : kKind == kLast ? nullptr : a.straight + matrix * a.old_plane;
+        if (!kEnd || a.out_turned) {
+            char* t = kKind == kApply ? a.turned + matrix * a.q_plane : kEnd ? nullptr : a.straight + matrix * a.old_plane;
 #pragma unroll
             for (int fj = 0; fj < FN; ++fj) {
                 const int64_t j = j0 + fj * 16 + row;
-                if constexpr (kKind == kLast) {
+                if constexpr (kEnd) {
                     const float f[4] = {__uint_as_float(w[fj][0]), __uint_as_float(w[fj][1]), __uint_as_float(w[fj][2]), __uint_as_float(w[fj][3])};
-                    if (j < a.out_cols) store_four(a.out, a.out_type, matrix * a.out_plane + j * a.out_stride + i, a.out_rows - i, f);
+                    if (j < a.out_cols) store_part<Out, 4>(static_cast<Out*>(a.out) + matrix * a.out_plane + j * a.out_stride + i, a.out_rows - i, f);
                 } else {
                     if (j < a.cols) store_pairs(t + j * a.rows * 4 + pair_at(i), w[fj]);
                 }
             }
         }
-        if (kKind == kApply || (kKind == kLast ? !a.out_turned : bi != bj)) {
+        if (kKind == kApply || (kEnd ? !a.out_turned : bi != bj)) {
 #pragma unroll
             for (int fj = 0; fj < FN; ++fj)
 #pragma unroll
@@ -367,9 +372,9 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
                 const int item = x * 64 + lane, si = item / (FN * 4), sj = item % (FN * 4) * 4;
                 const u32x4 u = *reinterpret_cast<const u32x4*>(strip + si * kPitch + sj);
                 const int64_t ri = i0 + fi * 16 + si, rj = j0 + sj;
-                if constexpr (kKind == kLast) {
+                if constexpr (kEnd) {
                     const float f[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-                    if (ri < a.out_rows) store_four(a.out, a.out_type, matrix * a.out_plane + ri * a.out_stride + rj, a.out_cols - rj, f);
+                    if (ri < a.out_rows) store_part<Out, 4>(static_cast<Out*>(a.out) + matrix * a.out_plane + ri * a.out_stride + rj, a.out_cols - rj, f);
                 } else if (rj < a.cols) {
                     const uint32_t f[4] = {u.x, u.y, u.z, u.w};
                     store_pairs(a.straight + matrix * a.old_plane + ri * a.cols * 4 + pair_at(rj), f);
@@ -399,6 +404,19 @@ __device__ __forceinline__ void store_halves(half_t* high, half_t* low, float4_t
     }
     *reinterpret_cast<half4*>(high) = h;
     *reinterpret_cast<half4*>(low) = l;
+}
+
+// A float's two halves in the places of a pair: the results, all 32 bits of them.
+typedef uint32_t words2 __attribute__((ext_vector_type(2), may_alias));
+__device__ __forceinline__ void store_bits(half_t* high, half_t* low, float4_t v) {
+    const uint32_t b0 = __float_as_uint(v[0]), b1 = __float_as_uint(v[1]), b2 = __float_as_uint(v[2]), b3 = __float_as_uint(v[3]);
+    *reinterpret_cast<words2*>(high) = words2{b0 >> 16 | (b1 & 0xffff0000u), b2 >> 16 | (b3 & 0xffff0000u)};
+    *reinterpret_cast<words2*>(low) = words2{(b0 & 0xffffu) | b1 << 16, (b2 & 0xffffu) | b3 << 16};
+}
+__device__ __forceinline__ float4_t load_bits(const half_t* high, const half_t* low) {
+    const words2 h = *reinterpret_cast<const words2*>(high), l = *reinterpret_cast<const words2*>(low);
+    return float4_t{__uint_as_float(h.x << 16 | (l.x & 0xffffu)), __uint_as_float((h.x & 0xffff0000u) | l.x >> 16),
+                    __uint_as_float(h.y << 16 | (l.y & 0xffffu)), __uint_as_float((h.y & 0xffff0000u) | l.y >> 16)};
 }
 
 // A matrix whose smaller side is at most 32 kBlocks (128) and which fits in LDS goes through all its steps there: one block
@@ -449,28 +467,24 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
     const int i0 = block / kAcross * FM * 16, j0 = block % kAcross * FN * 16;
     const T* g = static_cast<const T*>(a.g) + (int64_t)blockIdx.x * a.matrix_stride;
     const bool tall = a.rows > a.cols;
-    // Vectors of 16 bytes, four of a thread's under way at a time: once for the norm, once more (from the cache) for LDS.
-    constexpr int V = 16 / sizeof(T);
-    const int across = (a.cols + V - 1) / V, vecs = a.rows * across;
+    // Squares of 4 x 4 values a thread, whose four rows are under way together: once for the norm, once more (from the cache) for
+    // LDS, where four values of a row of X, which are a row or a column of the square, are written at a time.
+    const int across = (a.cols + 3) / 4, squares = (a.rows + 3) / 4 * across;
     auto each = [&](auto&& use) {
-        for (int v0 = threadIdx.x; v0 < vecs; v0 += 4 * kSmallBlock) {
-            float v[4][V];
+        for (int at = threadIdx.x; at < squares; at += kSmallBlock) {
+            const int r = at / across * 4, c = at % across * 4;
+            float v[4][4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int at = v0 + u * kSmallBlock, r = at / across, c = at % across * V;
-                load_part<T, V>(g + (int64_t)r * a.stride + c, at < vecs ? a.cols - c : 0, v[u], 0.0f);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int at = v0 + u * kSmallBlock, r = at / across, c = at % across * V;
-                if (at < vecs) use(r, c, v[u]);
-            }
+            for (int u = 0; u < 4; ++u) load_part<T, 4>(g + (int64_t)min(r + u, a.rows - 1) * a.stride + c, r + u < a.rows ? a.cols - c : 0, v[u], 0.0f);
+            use(r, c, v);
         }
     };
     double s = 0.0;
-    each([&](int, int, const float (&v)[V]) {
+    each([&](int, int, const float (&v)[4][4]) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) s += (double)v[e] * (double)v[e];
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += (double)v[u][e] * (double)v[u][e];
     });
     for (int i = threadIdx.x; i < 2 * M * XP / 8; i += kSmallBlock) reinterpret_cast<half8*>(xh)[i] = half8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
@@ -481,13 +495,15 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += buf[w];
     const double factor = scale_factor(s, a.eps, a.unit);
-    each([&](int r, int c, const float (&v)[V]) {
+    each([&](int r, int c, const float (&v)[4][4]) {       // (what lies beyond the matrix is zeros, and inside the padding)
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (c + e < a.cols) {
-                const int at = tall ? small_at(c + e, r, XP, x_mask) : small_at(r, c + e, XP, x_mask);
-                split((float)((double)v[e] * factor), xh[at], xl[at]);
-            }
+        for (int u = 0; u < 4; ++u) {
+            float4_t x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (float)((double)(tall ? v[e][u] : v[u][e]) * factor);
+            const int at = tall ? small_at(c + u, r, XP, x_mask) : small_at(r + u, c, XP, x_mask);
+            store_halves(xh + at, xl + at, x);
+        }
     });
     __syncthreads();
     for (int step = 0; step < a.steps; ++step) {
@@ -596,23 +612,26 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
 #pragma unroll
             for (int i = 0; i < 2 * kBlocks; ++i) {
                 const int ri = i * 16 + row, rj = jb + quad * 4;
-                if (!last) {
-                    const int at = small_at(ri, rj, XP, x_mask);
-                    store_halves(xh + at, xl + at, c[i]);
-                } else if (ri < (tall ? a.cols : a.rows)) {
-                    const float v[4] = {c[i][0] * a.gain, c[i][1] * a.gain, c[i][2] * a.gain, c[i][3] * a.gain};
-                    const int64_t base = (int64_t)blockIdx.x * a.out_plane;
-                    if (!tall) {
-                        store_four(a.out, a.out_type, base + ri * a.out_stride + rj, a.cols - rj, v);
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (rj + r < a.rows) store_typed(a.out, a.out_type, base + (rj + r) * a.out_stride + ri, v[r]);
-                    }
-                }
+                const int at = small_at(ri, rj, XP, x_mask);
+                if (last) store_bits(xh + at, xl + at, c[i] * a.gain);
+                else store_halves(xh + at, xl + at, c[i]);
             }
         }
         __syncthreads();
+    }
+    for (int at = threadIdx.x; at < squares; at += kSmallBlock) {
+        const int r = at / across * 4, c = at % across * 4;
+        float4_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int from = tall ? small_at(c + u, r, XP, x_mask) : small_at(r + u, c, XP, x_mask);
+            v[u] = load_bits(xh + from, xl + from);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float o[4] = {tall ? v[0][u] : v[u][0], tall ? v[1][u] : v[u][1], tall ? v[2][u] : v[u][2], tall ? v[3][u] : v[u][3]};
+            if (r + u < a.rows) store_four(a.out, a.out_type, (int64_t)blockIdx.x * a.out_plane + (r + u) * a.out_stride + c, a.cols - c, o);
+        }
     }
 }
 
@@ -704,6 +723,7 @@ template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void produ
     else if (kind == kGram) P2_PRODUCT(1, kGram);
     else if (kind == kPoly) P2_PRODUCT(3, kPoly);
     else if (kind == kApply) P2_PRODUCT(3, kApply);
+    else if (kind == kLastHalf) P2_PRODUCT(3, kLastHalf);
     else if (terms == 3) P2_PRODUCT(3, kLast);
     else P2_PRODUCT(1, kLast);
 #undef P2_PRODUCT
@@ -897,10 +917,10 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
         if (last) {
             p.out = a.out; p.out_plane = a.out_matrix_stride; p.out_stride = a.out_stride;
             p.out_rows = std::min(a.rows, a.cols); p.out_cols = std::max(a.rows, a.cols);
-            p.out_turned = tall; p.out_type = a.out_type;
+            p.out_turned = tall;
             p.gain = (float)(a.scale / f.unit);
         }
-        product_by_size(p, terms, last ? kLast : kApply, s);
+        product_by_size(p, terms, !last ? kApply : a.out_type == P2_F16 ? kLastHalf : kLast, s);
         unit = f.unit;
         e = hipGetLastError();
     }
