@@ -5,6 +5,7 @@
 // vectors); a wavefront takes 64 / kLanes tokens at a time.  Choosing goes by keys in which a larger logit, and of equal ones
 // the lower index, is the larger whole number: it is exact and does not depend on how the softmax is rounded.
 #include <algorithm>
+#include <type_traits>
 
 #include "p2_train_dev.h"
 
@@ -19,35 +20,101 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // e^(v - m), v and m finite or not; 1 ulp of 2^x and what the product rounds.
 __device__ __forceinline__ float exp_of(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
 
-// Keys: whole numbers in the order of the logits, and of equal ones in the order of falling indexes.  A float's bits, turned
-// over where it is negative, are in its order (NaN aside: with_nan puts it above everything).  16-bit logits leave the lowest 13 of them unused: the index goes there; for 32-bit
-// ones it takes 32 bits more.  -0 is 0; what is not above -inf (kNone) is never chosen.
+// Keys: whole numbers in the order of the logits, and of equal ones in the order of falling indexes; never 0.  A float's bits, turned
+// over where it is negative, are in its order (NaN aside: with_nan puts it above everything).  -0 is 0; what is not above -inf (kNone)
+// is never chosen.  16-bit logits and their indexes share 32 bits, 32-bit ones take 64.
 __device__ __forceinline__ uint32_t ordered(float f) {
     const uint32_t b = __float_as_uint(f + 0.0f);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-// Whether it is a NaN's: above +inf's, or below -inf's.
-__device__ __forceinline__ bool ordered_nan(uint32_t o) { return o > 0xff800000u || o < 0x007fffffu; }
-__device__ __forceinline__ float from_ordered(uint32_t o) {
-    return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+// Two 16-bit logits at a time: sign and magnitude become two's complement, which has one 0, and the sign is turned over.
+__device__ __forceinline__ uint32_t ordered_pair(uint32_t w) {
+    typedef int16_t short2_t __attribute__((ext_vector_type(2)));
+    const short2_t sign = __builtin_bit_cast(short2_t, w) >> 15;
+    const uint32_t turned = w ^ (__builtin_bit_cast(uint32_t, sign) | 0x80008000u);
+    return __builtin_bit_cast(uint32_t, (short2_t)(__builtin_bit_cast(short2_t, turned) - sign));
 }
-constexpr uint32_t kNone = 0x007fffffu;                // ordered(-inf)
 template <typename T> struct Key {                     // half_t, bf16_t
     typedef uint32_t type;
-    static constexpr uint32_t kLow = 0x1fffu;
-    static __device__ __forceinline__ type of(float f, int e) { return (ordered(f) & ~kLow) | (kLow - (uint32_t)e); }
-    static __device__ __forceinline__ type with_nan(type k) { return ordered_nan(k | kLow) && ordered_nan(k & ~kLow) ? k | ~kLow : k; }
-    static __device__ __forceinline__ bool real(type k) { return (k & ~kLow) > (kNone & ~kLow); }
-    static __device__ __forceinline__ int index(type k) { return (int)(kLow - (k & kLow)); }
-    static __device__ __forceinline__ float value(type k) { return from_ordered(k & 0x80000000u ? k & ~kLow : k | kLow); }
+    static constexpr uint32_t kInf = std::is_same<T, half_t>::value ? 0x7c00u : 0x7f80u;
+    static constexpr type kNone = (0x8000u - kInf) << 16;                  // -inf's, without an index
+    static __device__ __forceinline__ type with_nan(type k) { return k > ((0x8000u + kInf) << 16 | 0xffffu) || k < kNone ? k | 0xffff0000u : k; }
+    static __device__ __forceinline__ bool real(type k) { return k > (kNone | 0xffffu); }
+    static __device__ __forceinline__ int index(type k) { return (int)(0xffffu - (k & 0xffffu)); }
+    static __device__ __forceinline__ float value(type k) {
+        const int v = (int)(k >> 16) - 0x8000;
+        return (float)__builtin_bit_cast(T, (uint16_t)(v < 0 ? 0x8000 - v : v));
+    }
+    // of a vector's N values, the first of which is expert e's (N even)
+    template <int N> static __device__ __forceinline__ void of(const vec_t<T, N>& v, int e, type* key) {
+        typedef uint32_t words_t __attribute__((ext_vector_type(N / 2)));
+        const words_t w = __builtin_bit_cast(words_t, v);
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+            const uint32_t o = ordered_pair(w[j]), low = 0xffffu - (uint32_t)(e + 2 * j);
+            key[2 * j] = o << 16 | low;
+            key[2 * j + 1] = (o & 0xffff0000u) | (low - 1);
+        }
+    }
 };
 template <> struct Key<float> {
     typedef uint64_t type;
-    static __device__ __forceinline__ type of(float f, int e) { return (uint64_t)ordered(f) << 32 | (0xffffffffu - (uint32_t)e); }
-    static __device__ __forceinline__ type with_nan(type k) { return ordered_nan((uint32_t)(k >> 32)) ? k | 0xffffffff00000000ull : k; }
-    static __device__ __forceinline__ bool real(type k) { return (uint32_t)(k >> 32) > kNone; }
+    static constexpr uint32_t kBelow = 0x007fffffu;    // ordered(-inf)
+    static constexpr type kNone = (uint64_t)kBelow << 32;
+    static __device__ __forceinline__ type with_nan(type k) {
+        const uint32_t o = (uint32_t)(k >> 32);
+        return o > 0xff800000u || o < kBelow ? k | 0xffffffff00000000ull : k;
+    }
+    static __device__ __forceinline__ bool real(type k) { return (uint32_t)(k >> 32) > kBelow; }
     static __device__ __forceinline__ int index(type k) { return (int)(0xffffffffu - (uint32_t)k); }
-    static __device__ __forceinline__ float value(type k) { return from_ordered((uint32_t)(k >> 32)); }
+    static __device__ __forceinline__ float value(type k) {
+        const uint32_t o = (uint32_t)(k >> 32);
+        return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+    }
+    template <int N> static __device__ __forceinline__ void of(const vec_t<float, N>& v, int e, type* key) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) key[j] = (uint64_t)ordered(v[j]) << 32 | (0xffffffffu - (uint32_t)(e + j));
+    }
+};
+
+// A lane's kAhead largest keys in falling order; 0 where it has fewer.  insert(key, i): the lane's i-th, in the order of their experts,
+// among the first kDepth.
+template <typename K, int kAhead = 4> struct Largest { // 32 bits: the middle of three in an instruction each
+    static constexpr int kMost = kAhead;
+    K v[kAhead] = {};
+    template <int kDepth> __device__ __forceinline__ void insert(K x, int) {
+#pragma unroll
+        for (int n = kDepth - 1; n > 0; --n) v[n] = max(min(v[n - 1], v[n]), min(max(v[n - 1], v[n]), x));
+        v[0] = max(v[0], x);
+    }
+    __device__ __forceinline__ bool empty() const { return v[0] == 0; }
+    template <typename R> __device__ __forceinline__ K first(int, int) const { return v[0]; }
+    __device__ __forceinline__ void pop() {
+#pragma unroll
+        for (int n = 0; n + 1 < kAhead; ++n) v[n] = v[n + 1];
+        v[kAhead - 1] = 0;
+    }
+};
+template <> struct Largest<uint64_t> {                 // values, and which of the lane's they are: of equal ones the first
+    static constexpr int kAhead = 3, kMost = kAhead;       // (four: 4 % more time for 8 of 512 experts, registers spill)
+    Largest<uint32_t, kAhead> value;
+    uint32_t of[kAhead] = {};
+    template <int kDepth> __device__ __forceinline__ void insert(uint64_t x, int i) {
+        const uint32_t o = (uint32_t)(x >> 32);
+#pragma unroll
+        for (int n = kDepth - 1; n >= 0; --n) of[n] = n > 0 && o > value.v[n > 0 ? n - 1 : 0] ? of[n > 0 ? n - 1 : 0] : o > value.v[n] ? i : of[n];
+        value.template insert<kDepth>(o, i);
+    }
+    __device__ __forceinline__ bool empty() const { return value.empty(); }
+    template <typename R> __device__ __forceinline__ uint64_t first(int lane, int experts) const {
+        return (uint64_t)value.v[0] << 32 | (0xffffffffu - (uint32_t)R::place(lane, experts, (int)of[0]));
+    }
+    __device__ __forceinline__ void pop() {
+        value.pop();
+#pragma unroll
+        for (int n = 0; n + 1 < kAhead; ++n) of[n] = of[n + 1];
+        of[kAhead - 1] = 0;
+    }
 };
 
 __device__ __forceinline__ double block_sum(double v, double* buf) {       // thread 0 gets it
@@ -97,8 +164,13 @@ template <typename T, int kLanes, int kItems> struct Row {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) p[i] = (float)raw[i / V][i % V];
     }
+    __device__ __forceinline__ void keys(int lane, int experts, typename Key<T>::type (&key)[kItems]) const {
+#pragma unroll
+        for (int q = 0; q < kVecs; ++q) Key<T>::template of<V>(raw[q], place(lane, experts, q * V), &key[q * V]);
+        count_once(lane, experts, Key<T>::kNone, key);
+    }
     // `other` in the place of values that are not this lane's to count
-    static __device__ __forceinline__ void count_once(int lane, int experts, float other, float (&p)[kItems]) {
+    template <typename U> static __device__ __forceinline__ void count_once(int lane, int experts, U other, U (&p)[kItems]) {
         if (kLanes * kItems != experts)                    // (else all of them are)
 #pragma unroll
             for (int i = 0; i < kItems; ++i) p[i] = mine(lane, experts, i) ? p[i] : other;
@@ -147,10 +219,10 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     const int64_t stride = (int64_t)gridDim.x * kTokens;
     R next;
     bool next_keep = false;
+    auto logits_of = [&](int64_t t) { return static_cast<const T*>(a.logits) + (t < a.tokens ? t : a.tokens - 1) * a.stride; };
     auto ask = [&](int64_t t) {
-        const int64_t at = t < a.tokens ? t : a.tokens - 1;
-        next.load(static_cast<const T*>(a.logits) + at * a.stride, lane, a.experts);
-        next_keep = t < a.tokens && (!a.keep || a.keep[at]);
+        next.load(logits_of(t), lane, a.experts);
+        next_keep = t < a.tokens && (!a.keep || a.keep[t]);
     };
     const int64_t first = (int64_t)blockIdx.x * kTokens;
     if (first < a.tokens) ask(first + threadIdx.x / kLanes);
@@ -158,57 +230,97 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
         const int64_t t = t0 + threadIdx.x / kLanes;
         const bool there = t < a.tokens, keep = next_keep;
         float p[kItems];
-        K key[kItems];
         next.get(p);
-        R::count_once(lane, a.experts, -INFINITY, p);
-        if (t0 + stride < a.tokens) ask(t + stride);
-        float m = p[0];
+        auto larger = [](K x, K y) { return x > y ? x : y; };
+        Largest<K> mine;
+        {
+            K key[kItems];
+            next.keys(lane, a.experts, key);
+            if (a.k <= 2) {                                // (131072 tokens, 2 of 256 experts: 27.4 us for 28.6)
 #pragma unroll
-        for (int i = 1; i < kItems; ++i) m = fmaxf(m, p[i]);
-        m = group_max<kLanes>(m);
+                for (int i = 0; i < kItems; ++i) mine.template insert<2>(key[i], i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) mine.template insert<Largest<K>::kMost>(key[i], i);
+            }
+        }
+        if (t0 + stride < a.tokens) ask(t + stride);
+        auto best_of_all = [&] { return group_reduce<kLanes>(mine.template first<R>(lane, a.experts), larger); };
+        K best = best_of_all();
+        // e^(v - m) as 2^(v log2e - m log2e): what the rounding of the second product is off by is common to the row.
+        float m = Key<T>::value(best);
+        const float shift = m * kLog2e;
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            key[i] = Key<T>::of(p[i], R::place(lane, a.experts, i));
-            p[i] = exp_of(p[i], m);
-        }
-        R::count_once(lane, a.experts, 0.0f, p);           // (m may be -inf)
+        for (int i = 0; i < kItems; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], kLog2e, -shift));
+        R::count_once(lane, a.experts, 0.0f, p);
 #pragma unroll
         for (int i = 0; i < kItems; ++i) s += p[i];
         s = group_sum<kLanes>(s);
-        if (__any(s != s)) {                               // a NaN, or an infinity: see which, NaN is above everything
+        // Logits whose products overflow or are off by more than a factor, infinities and NaN: from the differences, NaN above everything.
+        const bool odd = !(s > 0.5f && s < 2.0f * P2_MAX_EXPERTS);
+        if (odd) {
+            mine = Largest<K>();
+            K key[kItems];
+            R again;
+            again.load(logits_of(t), lane, a.experts);
+            again.keys(lane, a.experts, key);
+            again.get(p);
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) key[i] = Key<T>::with_nan(key[i]);
+            for (int i = 0; i < kItems; ++i) mine.template insert<Largest<K>::kMost>(Key<T>::with_nan(key[i]), i);
+            best = best_of_all();
+            m = Key<T>::value(best);
+            s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) p[i] = exp_of(p[i], m);
+            R::count_once(lane, a.experts, 0.0f, p);       // (m may be -inf)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) s += p[i];
+            s = group_sum<kLanes>(s);
         }
         const float inv = __builtin_amdgcn_rcpf(s);
-        // The k best, one after the other: the next is the largest key below the last, and as whole numbers that wrap around
-        // key - last is the larger the nearer the key is below.  Lane i % kLanes keeps the i-th until as many as there are lanes
-        // are to be written.
-        K held = 0, last = 0;
-        bool on = false;
-        for (int i = 0; i < a.k; ++i) {
-            K best = key[0] - last;
-#pragma unroll
-            for (int q = 1; q < kItems; ++q) { const K d = key[q] - last; best = d > best ? d : best; }
-            best = group_reduce<kLanes>(best, [](K x, K y) { return x > y ? x : y; });
-            last += best;                                  // (there are k keys at least: -inf has one, too)
-            if (i == 0) on = keep && Key<T>::real(last);
-            if (i % kLanes == lane) held = last;
-            if ((i + 1) % kLanes == 0 || i + 1 == a.k) {
-                const int slot = i - i % kLanes + lane;
-                if (there && slot <= i) {
-                    const bool real = keep && Key<T>::real(held);
-                    const int e = Key<T>::index(held);
-                    a.expert[t * a.k + slot] = real ? e : -1;
-                    a.gate[t * a.k + slot] = real ? exp_of(Key<T>::value(held), m) * inv : 0.0f;
-                    if (real) atomicAdd(&count[e], 1);
-                }
-            }
-        }
+        const bool on = keep && Key<T>::real(best);
         if (on) {
             if (lane == 0) atomicAdd(&count[a.experts], 1);
 #pragma unroll
             for (int i = 0; i < kItems; ++i) acc[i] += p[i] * inv;
+        }
+        // The k best, one after the other: the largest of what the lanes have left.  A lane that has given all of its list looks for
+        // the next ones among its keys below the last (of 256 experts' eight best 1 token in 60 has four in one lane, 1 in 5 three).  Lane i keeps the i-th of as
+        // many as there are lanes, which are then written.
+        auto advance = [&] {
+            if (mine.template first<R>(lane, a.experts) == best) mine.pop();
+            if (__any(mine.empty())) {
+                K key[kItems];
+                R again;
+                again.load(logits_of(t), lane, a.experts);
+                again.keys(lane, a.experts, key);
+                if (mine.empty())
+#pragma unroll
+                    for (int q = 0; q < kItems; ++q) {
+                        const K x = odd ? Key<T>::with_nan(key[q]) : key[q];
+                        mine.template insert<Largest<K>::kMost>(x < best ? x : 0, q);
+                    }
+            }
+            best = best_of_all();
+        };
+        for (int base = 0; base < a.k; base += kLanes) {
+            const int n = min(a.k - base, kLanes);
+            if (base) advance();
+            K held = best;
+            for (int i = 1; i < n; ++i) {
+                advance();
+                if (lane >= i) held = best;
+            }
+            if (there && lane < n) {
+                const bool real = keep && Key<T>::real(held);
+                const int e = Key<T>::index(held);
+                const float v = Key<T>::value(held);
+                const int64_t at = t * a.k + base + lane;
+                a.expert[at] = real ? e : -1;
+                a.gate[at] = real ? (odd ? exp_of(v, m) : __builtin_amdgcn_exp2f(fmaf(v, kLog2e, -shift))) * inv : 0.0f;
+                if (real) atomicAdd(&count[e], 1);
+            }
         }
     }
     // lanes of a wavefront that hold the same experts, then the wavefronts, in a fixed order
@@ -250,8 +362,8 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
 // one block has all of them it works the loss out, too; else the block that is done last.
 template <int kWide> __global__ __launch_bounds__(1024) void k_balance_sum(BalanceForward a, int32_t lines) {
     constexpr int kDeep = 1024 / kWide;
-    __shared__ float prob[kDeep][kWide + 1];
-    __shared__ int64_t count[kDeep][kWide + 1];
+    __shared__ float prob[16][kWide];
+    __shared__ int64_t count[16][kWide], tokens;
     __shared__ double buf[16];
     __shared__ bool last;
     const int x = threadIdx.x % kWide, r = threadIdx.x / kWide;
@@ -266,37 +378,37 @@ template <int kWide> __global__ __launch_bounds__(1024) void k_balance_sum(Balan
             n += a.part_count[(int64_t)l * (a.experts + 1) + e];
         }
     }
-    prob[r][x] = s;
-    count[r][x] = n;
-    for (int d = kDeep / 2; d >= 1; d >>= 1) {
-        __syncthreads();
-        if (r < d) { prob[r][x] += prob[r + d][x]; count[r][x] += count[r + d][x]; }
-    }
+    // a wavefront's lanes of the same expert, then the wavefronts
+#pragma unroll
+    for (int d = kWide; d < 64; d <<= 1) { s += __shfl_xor(s, d, 64); n += __shfl_xor(n, d, 64); }
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) < kWide) { prob[wave][x] = s; count[wave][x] = n; }
     __syncthreads();
-    if (r == 0 && e <= a.experts) {
+    if (r == 0) {
+        s = 0.0f;
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) { s += prob[w][x]; n += count[w][x]; }
         if (e < a.experts) {
-            a.prob_sum[e] = prob[0][x];
-            a.counts[e] = count[0][x];
-        } else {
-            a.kept[0] = count[0][x];
+            a.prob_sum[e] = s;
+            a.counts[e] = n;
+        } else if (e == a.experts) {
+            a.kept[0] = n;
+            tokens = n;
         }
     }
     double l = 0.0;
     if (gridDim.x == 1) {
-        if (r == 0 && e < a.experts) l = (double)prob[0][x] * (double)count[0][x];
+        if (r == 0 && e < a.experts) l = (double)s * (double)n;
         l = block_sum(l, buf);
-        if (threadIdx.x == 0) a.loss[0] = loss_of(l, count[0][a.experts], a.experts, a.k);
+        if (threadIdx.x == 0) a.loss[0] = loss_of(l, tokens, a.experts, a.k);
         return;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        last = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
-        __threadfence();
-    }
+    // (thread 0's wavefront has written all of the block's results)
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
     __syncthreads();
     if (!last) return;
-    __threadfence();
     for (int q = threadIdx.x; q < a.experts; q += 1024) l += (double)a.prob_sum[q] * (double)a.counts[q];
     l = block_sum(l, buf);
     if (threadIdx.x == 0) a.loss[0] = loss_of(l, a.kept[0], a.experts, a.k);

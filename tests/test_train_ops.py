@@ -345,6 +345,35 @@ def test_routing_statistics_add_up_over_devices(T):
     assert torch.equal(g, T.p2_balance_backward(z, whole["expert"], whole["counts"], whole["tokens"]))
 
 
+@pytest.mark.parametrize("experts,k", [(6, 6), (16, 8), (60, 9), (64, 64), (130, 20), (256, 8), (500, 33), (1024, 64)])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_routing_of_choices_side_by_side(T, experts, k, kind):
+    """The best experts all in one place: a lane has to give far more of them than its share."""
+    up = torch.arange(experts, device="cuda", dtype=torch.float64)
+    rows = [up / 8, -up / 8, torch.zeros(experts, device="cuda"), (up % 3 == 0) * 2.0, (up // 8 % 2) * 1.0, -(up - experts // 2).abs() / 4, torch.where(up < experts // 2, up / 8, -math.inf),
+            torch.where(up % 2 == 0, math.nan, up / 8), torch.where(up < 7, torch.where(up % 2 == 0, -math.nan, math.inf), -up / 8)]
+    z = torch.stack([r.double() for r in rows]).to(kind)
+    r, want = T.p2_balance_forward(z, k), route_reference(z, None, k)
+    assert np.array_equal(r["expert"].cpu().numpy(), want["expert"]) and np.array_equal(r["counts"].cpu().numpy(), want["counts"])
+    gate = torch.from_numpy(want["gate"][:7]).cuda()
+    compare(r["gate"][:7], gate, (2 * 128 + 70) * U * gate + 2.0 ** -126, "gate")         # (z - m up to 128: what is below fp32's normal numbers may be 0)
+
+
+@pytest.mark.parametrize("offset", [1e4, -1e4, 3e7, -3e7, 3e38, -3e38])
+def test_routing_of_far_logits(T, offset):
+    """Softmax of logits a long way from zero; the steps between fp32 numbers there are 2^-10, 2 and 2^105."""
+    step = max(0.5, float(np.spacing(np.float32(abs(offset)))))
+    whole = torch.randint(-8, 8, (40, 70), generator=torch.Generator().manual_seed(3)).cuda()
+    z = (offset + step * whole.double()).float()
+    z[5, 7] = -z[5, 7]                                    # the other end, too
+    for kind in (F32, BF16):
+        r, want = T.p2_balance_forward(z.to(kind), 6), route_reference(z.to(kind), None, 6)
+        assert np.array_equal(r["expert"].cpu().numpy(), want["expert"])
+        gate = torch.from_numpy(want["gate"]).cuda()
+        compare(r["gate"], gate, (2 * 104 + 134) * U * gate + 2.0 ** -126, "gate")
+        assert abs(float(r["loss"]) / want["loss"] - 1) <= (2 * 104 + 134 + 140) * U
+
+
 def test_routing_beyond_32_bits(T):
     stride, experts = (1 << 30) + 64, 24
     wide = torch.empty(3 * stride, dtype=F16, device="cuda")
