@@ -736,6 +736,9 @@ template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void produ
 // 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.  Where no unit has two tiles of 64 x 64 a stage's latency
 // counts: eight wavefronts and 64 values of k between barriers (updates of 512 x 512 126 us for 141, 1024 x 1024 186 for
 // 225); where units do, the LDS that this takes would keep their other tiles out (32 updates of 256 x 256 172 us for 152).
+// Where the units suffice for tiles of 48 x 48, more of them have one: three wavefronts, each 16 rows of all columns, which read
+// less of LDS together, and three stages under way (updates of 1000 x 2777 288 us for 306, 1024 x 4096 351 for 367, 512 x 2048
+// 168 for 173, two of 700 x 2000 230 for 242; with two stages under way 295, 356, 167 and 233).
 void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     auto cost = [&](int64_t tile, double stage, bool shared) {
         const int64_t tiles = tiles_of(p, tile, kind) * p.matrices;
@@ -746,6 +749,7 @@ void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     if (c256 == least) product<256, 2, 4, 2, 1>(p, terms, kind, s);
     else if (c192 == least) product<192, 2, 4, 3, 1>(p, terms, kind, s);
     else if (c128 == least) product<128, 2, 4, 2, 1>(p, terms, kind, s);
+    else if (tiles_of(p, 48, kind) * p.matrices <= kUnits) product<48, 3, 1, 4, 2>(p, terms, kind, s);
     else if (tiles_of(p, 64, kind) * p.matrices <= kUnits) product<64, 2, 4, 3, 2>(p, terms, kind, s);
     else product<64, 2, 2, 3, 1>(p, terms, kind, s);
 }
@@ -810,10 +814,12 @@ bool is_small(int64_t rows, int64_t cols) {
 }
 
 template <typename T, int kBlocks> hipError_t small_as(const Small& p, int64_t count, hipStream_t s) {
-    // (once a process: a block may have all of a compute unit's LDS)
-    static const hipError_t room = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_newton_small<T, kBlocks>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
-    if (room != hipSuccess) return room;
-    k_newton_small<T, kBlocks><<<dim3((unsigned)count), dim3(kSmallBlock), (size_t)small_bytes(32 * kBlocks, p.n), s>>>(p);
+    const size_t bytes = (size_t)small_bytes(32 * kBlocks, p.n);
+    if (bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_newton_small<T, kBlocks>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
+        if (e != hipSuccess) return e;
+    }
+    k_newton_small<T, kBlocks><<<dim3((unsigned)count), dim3(kSmallBlock), bytes, s>>>(p);
     return hipGetLastError();
 }
 template <typename T> hipError_t small_of(const Small& p, int64_t count, hipStream_t s) {

@@ -136,7 +136,9 @@ def p2_layer_norm_backward(dy, x, weight, mean, rstd, dx=True, dweight=True, dbi
     rows, n, cols, stride_x = _rows(x)
     drows, _, _, stride_dy = _rows(dy)
     weight = _vector(weight, cols, "weight")
-    mean, rstd = _vector(mean.reshape(-1), n, "mean", torch.float32), _vector(rstd.reshape(-1), n, "rstd", torch.float32)
+    if mean.dim() != 1 or rstd.dim() != 1:
+        mean, rstd = mean.reshape(-1), rstd.reshape(-1)
+    mean, rstd = _vector(mean, n, "mean", torch.float32), _vector(rstd, n, "rstd", torch.float32)
     like = x if weight is None else weight
     out = _like(x) if dx else None
     dw = torch.empty(cols, dtype=like.dtype, device=x.device) if dweight else None
