@@ -61,11 +61,19 @@ __device__ __forceinline__ double block_sum_256(double s, double* buf) {
     __syncthreads();
     return (buf[0] + buf[1]) + (buf[2] + buf[3]);
 }
-// What a matrix whose squares sum to s is multiplied by; zeros stay zeros without an eps, too.
-__device__ __forceinline__ double scale_factor(double s, double eps, double unit) {
-    s = sqrt(s) + eps;
-    return s == 0.0 ? 0.0 : unit / s;
-}
+// What a matrix whose squares sum to s is multiplied by, as part * 2^power; zeros stay zeros without an eps, too.  The power of two
+// comes first, so that values of any size lose nothing, and one rounding to 32 bits is left (64-bit products took twice the time).
+struct Factor {
+    float part;
+    int power;
+    __device__ __forceinline__ Factor(double s, double eps, double unit) {
+        s = sqrt(s) + eps;
+        const double f = s == 0.0 ? 0.0 : unit / s;
+        part = (float)__builtin_amdgcn_frexp_mant(f);
+        power = __builtin_amdgcn_frexp_exp(f);
+    }
+    __device__ __forceinline__ float operator()(float v) const { return __builtin_amdgcn_ldexpf(v, power) * part; }
+};
 
 // Sum of squares, in 64 bits: entries of any size, and no overflow before the root.  `across` threads (a power of two) take a
 // row, 256 / across rows at a time.
@@ -91,7 +99,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_norm(const
 template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(const T* g, int64_t stride, int64_t matrix_stride, int64_t rows, int64_t cols,
                                                                             const double* parts, int32_t n_parts, double eps, double unit, char* straight,
                                                                             char* turned, int64_t rows_padded, int64_t cols_padded, int64_t plane) {
-    __shared__ float tile[64][65];
+    __shared__ uint32_t tile[64][65];
     __shared__ double buf[4];
     const T* m = g + (int64_t)blockIdx.z * matrix_stride;
     const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
@@ -105,15 +113,14 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(cons
     double s = 0.0;
     for (int i = threadIdx.x; i < n_parts; i += 256) s += parts[(int64_t)blockIdx.z * n_parts + i];
     s = block_sum_256(s, buf);
-    const double factor = scale_factor(s, eps, unit);
+    const Factor factor(s, eps, unit);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            v[i][j] = (float)((double)v[i][j] * factor);
-            tile[y + i * 16][x + j] = v[i][j];
-            w[j] = pack(v[i][j]);
+            w[j] = pack(factor(v[i][j]));
+            tile[y + i * 16][x + j] = w[j];
         }
         store_pairs(straight + blockIdx.z * plane + (r0 + y + i * 16) * cols_padded * 4 + pair_at(c0 + x), w);
     }
@@ -122,7 +129,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(cons
     for (int i = 0; i < 4; ++i) {
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack(tile[x + j][y + i * 16]);
+        for (int j = 0; j < 4; ++j) w[j] = tile[x + j][y + i * 16];
         store_pairs(turned + blockIdx.z * plane + (c0 + y + i * 16) * rows_padded * 4 + pair_at(r0 + x), w);
     }
 }
@@ -494,13 +501,13 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
     s = 0.0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += buf[w];
-    const double factor = scale_factor(s, a.eps, a.unit);
+    const Factor factor(s, a.eps, a.unit);
     each([&](int r, int c, const float (&v)[4][4]) {       // (what lies beyond the matrix is zeros, and inside the padding)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             float4_t x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = (float)((double)(tall ? v[e][u] : v[u][e]) * factor);
+            for (int e = 0; e < 4; ++e) x[e] = factor(tall ? v[e][u] : v[u][e]);
             const int at = tall ? small_at(c + u, r, XP, x_mask) : small_at(r + u, c, XP, x_mask);
             store_halves(xh + at, xl + at, x);
         }
