@@ -4,6 +4,10 @@
 // result are worked out from there, so that a pass moves what it cannot do without: 2 values an element forward, 3 backward.
 // Rows are dealt to groups of kTpr threads (a part of a wavefront, a wavefront, or a block), each thread holding kNv vectors
 // of 16 bytes.
+//
+// What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 24.1 us, 5.6 TB/s (part of it from the last
+// cache); backward with both sums, 16384 x 4096 bf16: 84.5 us, 4.8 TB/s, of which k_norm_weight_grad takes 7.7.  Rows with odd ends: 5003 x 1023
+// fp16 of rows 1061 apart 8 us, 2.6 TB/s.  One row: 2.3 us on the device in a call of 10.
 #include <algorithm>
 
 #include "p2_train_dev.h"
@@ -65,6 +69,7 @@ template <int N> struct WeightVec {
     }
 };
 
+// mean = sum x / n, rstd = 1 / sqrt(sum (x - mean)^2 / n + eps), y = (x - mean) rstd w + b.
 template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds__(NormGroup<kTpr>::kThreads) void k_norm_forward(NormForward a) {
     constexpr int V = 16 / sizeof(T);
     constexpr int kRows = NormGroup<kTpr>::kRows;
@@ -146,7 +151,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     }
 }
 
-// Rows too long for registers, or shorter than a vector: three passes over them, the later two from the cache.
+// Rows too long for registers (more than 4096 vectors), or shorter than a vector: three passes over them, the later two from the cache.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_long(NormForward a) {
     __shared__ float buf[2][16];
     const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
@@ -172,9 +177,10 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_lon
     }
 }
 
-// Backward.  A block takes every gridDim.x-th group of rows and keeps its columns' sums of dy * xh and dy in registers
-// the whole time; at its end they are added up over the block's row groups in a fixed order and written as one line of
-// partial sums, which k_norm_weight_grad adds up.
+// Backward.  xh = (x - mean) rstd, g = dy w, dx = rstd (g - mean(g) - xh mean(g xh)).  A block takes every gridDim.x-th group of
+// rows and keeps its columns' sums of dy * xh and dy in registers the whole time; at its end they are added up over the block's
+// row groups in a fixed order and written as one line of partial sums, which k_norm_weight_grad adds up.  Two blocks of 512 threads a
+// compute unit: in one of 1024, which would halve the lines, four rows wait for each other's barriers (16384 x 4096 231 us for 84).
 constexpr int kBackBlock = 512;
 constexpr int64_t kBackBlocks = 512;       // two blocks a compute unit: 16 wavefronts
 
