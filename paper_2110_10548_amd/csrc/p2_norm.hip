@@ -151,7 +151,7 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     }
 }
 
-// Rows too long for registers (more than 4096 vectors), or shorter than a vector: three passes over them, the later two from the cache.
+// Rows too long for registers (more than 4096 vectors): three passes over them, the later two from the cache.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_long(NormForward a) {
     __shared__ float buf[2][16];
     const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
@@ -174,6 +174,36 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_lon
             if (a.bias) load_typed<1>(a.bias, a.weight_type, c, 1, b, 0.0f);
             y[c] = (T)(((float)x[c] - mean) * rstd * w[0] + b[0]);
         }
+    }
+}
+
+// Rows shorter than a vector (three fp32 values, seven 16-bit ones): a thread each.
+constexpr int kShortBlock = 256;
+template <typename T> __global__ __launch_bounds__(kShortBlock) void k_norm_forward_short(NormForward a) {
+    constexpr int kMost = 16 / sizeof(T) - 1;
+    const int cols = (int)a.cols;
+    const float n = (float)a.cols;
+    for (int64_t row = (int64_t)blockIdx.x * kShortBlock + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * kShortBlock) {
+        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        T* y = static_cast<T*>(a.y) + row * a.y_stride;
+        float v[kMost], s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kMost; ++c) { v[c] = c < cols ? (float)x[c] : 0.0f; s += v[c]; }
+        const float mean = s / n;
+        s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kMost; ++c) { v[c] -= mean; s += c < cols ? v[c] * v[c] : 0.0f; }
+        const float rstd = 1.0f / sqrtf(s / n + a.eps);
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+        for (int c = 0; c < kMost; ++c)
+            if (c < cols) {
+                float w[1] = {1.0f}, b[1] = {0.0f};
+                if (a.weight) load_typed<1>(a.weight, a.weight_type, c, 1, w, 1.0f);
+                if (a.bias) load_typed<1>(a.bias, a.weight_type, c, 1, b, 0.0f);
+                y[c] = (T)(v[c] * rstd * w[0] + b[0]);
+            }
     }
 }
 
@@ -349,6 +379,60 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_backward_lo
     }
 }
 
+// Rows shorter than a vector: dx, and a line of partial sums a block.
+template <typename T> __global__ __launch_bounds__(kShortBlock) void k_norm_backward_short(NormBackward a) {
+    constexpr int kMost = 16 / sizeof(T) - 1, kWaves = kShortBlock / 64;
+    __shared__ float sums[kWaves][2][kMost];
+    const int cols = (int)a.cols;
+    const float inv = 1.0f / (float)a.cols;
+    float w[kMost], dw[kMost], db[kMost];
+#pragma unroll
+    for (int c = 0; c < kMost; ++c) {
+        float v[1] = {1.0f};
+        if (a.weight && c < cols) load_typed<1>(a.weight, a.weight_type, c, 1, v, 1.0f);
+        w[c] = v[0];
+        dw[c] = db[c] = 0.0f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * kShortBlock + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * kShortBlock) {
+        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float xh[kMost], d[kMost], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kMost; ++c) {
+            xh[c] = c < cols ? ((float)x[c] - mean) * rstd : 0.0f;
+            d[c] = c < cols ? (float)dy[c] : 0.0f;
+            const float t = d[c] * xh[c];
+            dw[c] += t;
+            db[c] += d[c];
+            d[c] *= w[c];
+            s1 += d[c];
+            s2 += t * w[c];
+        }
+        s1 *= inv;
+        s2 *= inv;
+        if (a.dx) {
+            T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
+#pragma unroll
+            for (int c = 0; c < kMost; ++c) if (c < cols) dx[c] = (T)(rstd * (d[c] - s1 - xh[c] * s2));
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int c = 0; c < kMost; ++c) {
+        const float p = group_sum<64>(dw[c]), q = group_sum<64>(db[c]);
+        if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6][0][c] = p; sums[threadIdx.x >> 6][1][c] = q; }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < 2 * cols) {
+        const int which = (int)threadIdx.x / cols, c = (int)threadIdx.x % cols;
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) s += sums[q][which][c];
+        a.partial[((int64_t)blockIdx.x * 2 + which) * a.cols + c] = s;
+    }
+}
+
 // Partial sums of rows too long for registers: a block takes 256 columns of every gridDim.y-th row.
 template <typename T> __global__ __launch_bounds__(256) void k_norm_columns_long(NormBackward a) {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -394,7 +478,8 @@ template <typename T, int kTpr, int kNv> void forward_as(const NormForward& a, h
 template <typename T> void forward_of(const NormForward& a, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int64_t vecs = ceil_div(a.cols, V);
-    if (a.cols < V || vecs > 4096) k_norm_forward_long<T><<<dim3((unsigned)std::min(a.rows, kMaxNormBlocks)), dim3(1024), 0, s>>>(a);
+    if (a.cols < V) k_norm_forward_short<T><<<dim3((unsigned)std::min(ceil_div(a.rows, kShortBlock), kForwardThreads / kShortBlock)), dim3(kShortBlock), 0, s>>>(a);
+    else if (vecs > 4096) k_norm_forward_long<T><<<dim3((unsigned)std::min(a.rows, kMaxNormBlocks)), dim3(1024), 0, s>>>(a);
     else if (vecs <= 16) forward_as<T, 16, 1>(a, s);
     else if (vecs <= 64) forward_as<T, 64, 1>(a, s);
     else if (vecs <= 128) forward_as<T, 64, 2>(a, s);
@@ -404,11 +489,11 @@ template <typename T> void forward_of(const NormForward& a, hipStream_t s) {
     else forward_as<T, 1024, 4>(a, s);
 }
 
-// Threads and vectors of a row in the backward pass; 0: too long for registers.
+// Threads and vectors of a row in the backward pass; 0: too long for registers; 1 thread: shorter than a vector.
 struct BackShape { int tpr, nv; };
 BackShape back_shape(int64_t cols, int64_t v) {
     const int64_t vecs = ceil_div(cols, v);
-    if (cols < v) return {0, 0};
+    if (cols < v) return {1, 0};
     if (vecs <= 16) return {16, 1};
     if (vecs <= 64) return {64, 1};
     if (vecs <= 128) return {64, 2};
@@ -426,7 +511,7 @@ template <typename T, int kTpr, int kNv> void backward_as(const NormBackward& a,
 
 int64_t back_blocks(int64_t rows, int64_t cols, int32_t value_bytes) {
     const BackShape f = back_shape(cols, 16 / value_bytes);
-    const int64_t groups = f.tpr ? ceil_div(rows, kBackBlock / f.tpr) : rows;
+    const int64_t groups = f.tpr == 1 ? ceil_div(rows, kShortBlock) : f.tpr ? ceil_div(rows, kBackBlock / f.tpr) : rows;
     return std::max<int64_t>(1, std::min(groups, kBackBlocks));
 }
 
@@ -435,6 +520,7 @@ template <typename T> hipError_t backward_of(const NormBackward& a, hipStream_t 
     const int64_t blocks = back_blocks(a.rows, a.cols, sizeof(T));
     if (a.rows > 0) {
         switch (f.tpr * 8 + f.nv) {
+            case 1 * 8: k_norm_backward_short<T><<<dim3((unsigned)blocks), dim3(kShortBlock), 0, s>>>(a); break;
             case 16 * 8 + 1: backward_as<T, 16, 1>(a, blocks, s); break;
             case 64 * 8 + 1: backward_as<T, 64, 1>(a, blocks, s); break;
             case 64 * 8 + 2: backward_as<T, 64, 2>(a, blocks, s); break;

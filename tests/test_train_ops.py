@@ -107,6 +107,13 @@ def test_layer_norm_many_rows(T, rows, cols, kind):
     test_layer_norm(T, rows, cols, kind, F32, 0)
 
 
+@pytest.mark.parametrize("cols", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("kind,pad", [(F32, 0), (BF16, 1), (F16, 0)])
+def test_layer_norm_of_few_columns(T, cols, kind, pad):
+    test_layer_norm(T, 150001, cols, kind, F32, pad)
+    test_layer_norm(T, 0, cols, kind, kind, pad)
+
+
 def test_layer_norm_gradient_is_that_of_differences(T):
     """Along a direction: the 64-bit loss at x + h v and x - h v; its own error is h^2 times a third derivative."""
     x, dy, w, b = norm_inputs(6, 40, F32, F32, 0)
