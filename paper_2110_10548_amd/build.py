@@ -10,10 +10,26 @@ SOURCES = ["p2_plan.cpp", "p2_literal.hip", "p2_compact.hip", "p2_regs.hip", "p2
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
+TENSORS = os.path.join(HERE, "_train.so")                  # extension module: the training operators on torch tensors
+
+
+def tensors_command():
+    """The host compiler's command: only torch's and Python's headers, no device code."""
+    import sysconfig
+    import torch
+    where = os.path.dirname(os.path.abspath(torch.__file__))
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            "-isystem", os.path.join(where, "include"), "-isystem", os.path.join(where, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "p2_train_tensors.cpp"), "-o", TENSORS,
+            "-L" + os.path.join(where, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
 
 def build(verbose: bool = False) -> str:
     objs = []
-    procs = []
+    cmd = tensors_command()
+    if verbose:
+        print(" ".join(cmd))
+    procs = [(subprocess.Popen(cmd), cmd)]
     for src in SOURCES:
         obj = os.path.join(CSRC, os.path.splitext(src)[0] + ".o")
         cmd = ["hipcc", "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj] + FLAGS

@@ -15,7 +15,7 @@
 //
 // What bounds it.  4096 x 4096: the matrix units; three products of 16 bits each take 3.2 ms, 1.24 to 1.30 P operations a second in the large
 // products, where a plain product of that size by the installed library reaches 1.21.  Around 1000 rows: LDS, which tiles of 48 and 64 read
-// and write for twice the time of their MFMA (2777 x 1000 fp32 294 us, 0.47 P).  Stacks of 256 x 256: launches and the first loads of
+// and write for twice the time of their MFMA (2777 x 1000 fp32 300 us, 0.47 P).  Stacks of 256 x 256: launches and the first loads of
 // each (17 in 148 us; deeper prefetch changes nothing).  Up to 128 rows: one launch, one block's chain of steps (64 x 64 17 us).
 #include <algorithm>
 #include <cmath>

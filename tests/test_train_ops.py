@@ -573,3 +573,71 @@ def test_in_a_graph(T):
         torch.cuda.synchronize()
         want = _step(T, *inputs)                          # eager work between the replays
         assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+# ------------------------------------------------------------------------------------------------ what is refused, and what is left behind
+
+def test_tensors_that_do_not_fit_are_refused(T):
+    x, w, z = draw(1, 6, 40).float(), draw(2, 40).float(), draw(3, 10, 12).float()
+    y, mean, rstd = T.p2_layer_norm_forward(x, w, w)
+    r = T.p2_balance_forward(z, 3)
+    keep, dgate = torch.ones(10, dtype=torch.bool, device="cuda"), torch.ones(10, 3, device="cuda")
+    expert, counts, prob, tokens = (r[n] for n in ("expert", "counts", "prob_sum", "tokens"))
+    refused = [
+        lambda: T.p2_layer_norm_forward(x.double(), w, w), lambda: T.p2_layer_norm_forward(x, w[:39], None), lambda: T.p2_layer_norm_forward(x, w, w.to(BF16)),
+        lambda: T.p2_layer_norm_forward(x, None, w.long()), lambda: T.p2_layer_norm_forward(x, w.cpu()), lambda: T.p2_layer_norm_forward(x, w[None]),
+        lambda: T.p2_layer_norm_forward(x, w, w, eps=-1.0), lambda: T.p2_layer_norm_forward(x[:, :0]),
+        lambda: T.p2_layer_norm_backward(x, x, w, mean[:5], rstd), lambda: T.p2_layer_norm_backward(x, x, w, mean, rstd.double()),
+        lambda: T.p2_layer_norm_backward(x.to(F16), x, w, mean, rstd), lambda: T.p2_layer_norm_backward(x, x, w, mean, rstd.cpu()),
+        lambda: T.p2_balance_forward(z, 0), lambda: T.p2_balance_forward(z, -1), lambda: T.p2_balance_forward(z, 13), lambda: T.p2_balance_forward(z, 1 << 40),
+        lambda: T.p2_balance_forward(z, 3, keep=keep[:9]), lambda: T.p2_balance_forward(z, 3, keep=keep.float()), lambda: T.p2_balance_forward(z, 3, keep=keep.cpu()),
+        lambda: T.p2_balance_forward(z[:, :0], 1), lambda: T.p2_balance_forward(z.int(), 1),
+        lambda: T.p2_balance_loss(counts.int(), prob, tokens, 3), lambda: T.p2_balance_loss(counts, prob[:11], tokens, 3), lambda: T.p2_balance_loss(counts, prob, counts, 3),
+        lambda: T.p2_balance_loss(counts, prob, tokens, 13),
+        lambda: T.p2_balance_backward(z, expert.long(), counts, tokens), lambda: T.p2_balance_backward(z, expert[:9], counts, tokens),
+        lambda: T.p2_balance_backward(z, expert, counts[:11], tokens), lambda: T.p2_balance_backward(z, expert, counts, tokens, dgate=dgate[:, :2]),
+        lambda: T.p2_balance_backward(z, expert, counts, tokens, dgate=dgate.double()), lambda: T.p2_balance_backward(z, expert, counts, tokens, dloss=dgate),
+        lambda: T.p2_balance_backward(z, expert, counts, tokens.cpu()),
+        lambda: T.p2_orthogonalize(x, steps=0), lambda: T.p2_orthogonalize(x, dtype=torch.float64), lambda: T.p2_orthogonalize(x.long()), lambda: T.p2_orthogonalize(x[:0])]
+    torch.cuda.synchronize()
+    room = torch.cuda.memory_allocated()
+    for i, call in enumerate(refused):
+        with pytest.raises(T.P2Error):
+            call()
+            pytest.fail("call %d was not refused" % i)
+    for call in (lambda: T.p2_layer_norm_forward(x, 3), lambda: T.p2_balance_forward(z, 1.5), lambda: T.p2_orthogonalize(x, steps="five"), lambda: T.p2_layer_norm_forward(x, eps=None)):
+        with pytest.raises(TypeError):
+            call()
+    assert torch.cuda.memory_allocated() == room
+
+
+def test_calls_leave_nothing_behind(T):
+    import sys
+    inputs = _step_inputs(4)
+    _step(T, *inputs)
+    torch.cuda.synchronize()
+    room, held = torch.cuda.memory_allocated(), [sys.getrefcount(t) for t in inputs]
+    for _ in range(20):
+        _step(T, *inputs)
+    assert torch.cuda.memory_allocated() == room and [sys.getrefcount(t) for t in inputs] == held
+
+
+def test_forms_of_the_arguments(T):
+    """Results have the shapes and types that the arguments call for, whatever these are laid out like."""
+    x = draw(1, 3, 5, 24).to(BF16)
+    y, mean, rstd = T.p2_layer_norm_forward(x)
+    assert y.shape == x.shape and y.dtype == BF16 and mean.shape == rstd.shape == (3, 5) and mean.dtype == F32
+    dx, dw, db = T.p2_layer_norm_backward(x, x, None, mean, rstd, dweight=False)
+    assert dx.shape == x.shape and dw is None and db.shape == (24,) and db.dtype == BF16
+    v, m, s = T.p2_layer_norm_forward(x[1, 2])
+    assert v.shape == (24,) and m.shape == s.shape == () and torch.equal(v, y[1, 2]) and torch.equal(m, mean[1, 2])
+    turned = x.permute(1, 0, 2)
+    assert torch.equal(T.p2_layer_norm_forward(turned)[0], y.permute(1, 0, 2))
+    w = torch.nn.Parameter(torch.ones(24, device="cuda"))
+    assert torch.equal(T.p2_layer_norm_forward(x, w.to(BF16))[0], y) and not T.p2_layer_norm_forward(x.float(), w)[0].requires_grad
+    z = draw(2, 24, 30).float()
+    r, t = T.p2_balance_forward(z, 2), T.p2_balance_forward(z.t().contiguous().t(), 2, keep=torch.ones(24, dtype=torch.uint8, device="cuda"))
+    assert all(torch.equal(r[n], t[n]) for n in r) and [r[n].shape for n in r] == [(24, 2), (24, 2), (30,), (30,), (), ()]
+    assert [r[n].dtype for n in r] == [torch.int32, F32, torch.int64, F32, torch.int64, F32]
+    g = T.p2_orthogonalize(x, dtype=F32)
+    assert g.shape == x.shape and g.dtype == F32 and T.p2_orthogonalize(x.transpose(1, 2)).shape == (3, 24, 5)
