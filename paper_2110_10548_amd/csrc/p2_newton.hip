@@ -14,8 +14,8 @@
 // for B X).  Sizes are padded to multiples of 64 with zeros, which stay zeros through all steps.
 //
 // What bounds it.  4096 x 4096: the matrix units; three products of 16 bits each take 3.2 ms, 1.24 to 1.30 P operations a second in the large
-// products, where a plain product of that size by the installed library reaches 1.21.  Around 1000 rows: LDS, which tiles of 48 and 64 read
-// and write for twice the time of their MFMA (2777 x 1000 fp32 300 us, 0.47 P).  Stacks of 256 x 256: launches and the first loads of
+// products, where a plain product of that size by the installed library reaches 1.21.  Around 1000 rows: the operands' way from L2 to LDS
+// (2777 x 1000 fp32 300 us; X X^T brings 267 MB there in 19.4 us, B X 369 in 28.5), or latency where larger tiles need less of it.  Stacks of 256 x 256: launches and the first loads of
 // each (17 in 148 us; deeper prefetch changes nothing).  Up to 128 rows: one launch, one block's chain of steps (64 x 64 17 us).
 #include <algorithm>
 #include <cmath>
@@ -748,8 +748,8 @@ template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void produ
 // 329, 404, 355, 460; X X^T of 1000 x 2777 takes 165, 103, 66 and 30.  Where no unit has two tiles of 64 x 64 a stage's latency
 // counts: eight wavefronts and 64 values of k between barriers (updates of 512 x 512 126 us for 141, 1024 x 1024 186 for
 // 225); where units do, the LDS that this takes would keep their other tiles out (32 updates of 256 x 256 172 us for 152).
-// Where the units suffice for tiles of 48 x 48, more of them have one: three wavefronts, each 16 rows of all columns, which read
-// less of LDS together, and three stages under way (updates of 1000 x 2777 288 us for 306, 1024 x 4096 351 for 367, 512 x 2048
+// Where the units suffice for tiles of 48 x 48, more of them have one: three wavefronts, each 16 rows of all columns, and three
+// stages under way (updates of 1000 x 2777 288 us for 306, 1024 x 4096 351 for 367, 512 x 2048
 // 168 for 173, two of 700 x 2000 230 for 242; with two stages under way 295, 356, 167 and 233).
 void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
     auto cost = [&](int64_t tile, double stage, bool shared) {
