@@ -448,24 +448,31 @@ template <typename T> __global__ __launch_bounds__(256) void k_norm_columns_long
     line[a.cols + c] = db;
 }
 
-// dweight (blockIdx.y = 0) and dbias (1) from `lines` lines of partial sums: 16 columns a block, 64 threads a column.
+// dweight (blockIdx.y = 0) and dbias (1) from `lines` lines of partial sums: 32 columns a block, whole lines of the cache (16 columns: every
+// line fetched twice, 84.4 us for 81.6 a call with 16384 x 4096), 32 threads a column.  Sums of a wavefront's threads by lane exchange, then of the
+// wavefronts in their order.
+constexpr int kSumColumns = 32;
 __global__ __launch_bounds__(1024) void k_norm_weight_grad(const float* __restrict__ partial, int64_t lines, int64_t cols, void* dweight,
                                                            void* dbias, int32_t weight_type) {
-    __shared__ float part[64][17];
+    constexpr int kWide = kSumColumns, kDeep = 1024 / kWide;
+    __shared__ float part[16][kWide];
     void* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
-    const int x = threadIdx.x & 15, r = threadIdx.x >> 4;
-    const int64_t c = (int64_t)blockIdx.x * 16 + x;
+    const int x = threadIdx.x % kWide, r = threadIdx.x / kWide;
+    const int64_t c = (int64_t)blockIdx.x * kWide + x;
     float s = 0.0f;
     if (c < cols)
 #pragma unroll 8
-        for (int64_t l = r; l < lines; l += 64) s += partial[(l * 2 + blockIdx.y) * cols + c];
-    part[r][x] = s;
-    for (int d = 32; d >= 1; d >>= 1) {
-        __syncthreads();
-        if (r < d) part[r][x] += part[r + d][x];
-    }
-    if (r == 0 && c < cols) store_typed(out, weight_type, c, part[0][x]);
+        for (int64_t l = r; l < lines; l += kDeep) s += partial[(l * 2 + blockIdx.y) * cols + c];
+#pragma unroll
+    for (int d = kWide; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
+    if ((threadIdx.x & 63) < kWide) part[threadIdx.x >> 6][x] = s;
+    __syncthreads();
+    if (r > 0 || c >= cols) return;
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += part[w][x];
+    store_typed(out, weight_type, c, s);
 }
 
 template <typename T, int kTpr, int kNv> void forward_as(const NormForward& a, hipStream_t s) {
@@ -537,7 +544,7 @@ template <typename T> hipError_t backward_of(const NormBackward& a, hipStream_t 
         if (e != hipSuccess) return e;
     }
     if (a.partial)
-        k_norm_weight_grad<<<dim3((unsigned)ceil_div(a.cols, 16), 2), dim3(1024), 0, s>>>(a.partial, a.rows > 0 ? blocks : 0, a.cols, a.dweight, a.dbias, a.weight_type);
+        k_norm_weight_grad<<<dim3((unsigned)ceil_div(a.cols, kSumColumns), 2), dim3(1024), 0, s>>>(a.partial, a.rows > 0 ? blocks : 0, a.cols, a.dweight, a.dbias, a.weight_type);
     return hipGetLastError();
 }
 
