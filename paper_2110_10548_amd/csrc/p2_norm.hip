@@ -6,7 +6,7 @@
 // of 16 bytes.
 //
 // What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 24.1 us, 5.6 TB/s (part of it from the last
-// cache); backward with both sums, 16384 x 4096 bf16: 84.4 us, 4.8 TB/s, of which k_norm_weight_grad takes 7.7.  Rows with odd ends: 5003 x 1023
+// cache); backward with both sums, 16384 x 4096 bf16: 81.1 us, 5.0 TB/s, of which k_norm_weight_grad takes 5.1.  Rows with odd ends: 5003 x 1023
 // fp16 of rows 1061 apart 8 us, 2.6 TB/s.  One row: 2.4 us on the device in a call of 6.8.
 #include <algorithm>
 
