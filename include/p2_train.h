@@ -97,8 +97,8 @@ int32_t p2_orthogonalize_workspace(int64_t count, int64_t rows, int64_t cols, in
  * (for matrices with more rows than columns on their transposes), result = scale * X.  `count` matrices of rows x cols
  * lie `matrix_stride` elements apart.  type is that of G, out_type that of the result, which is written with its own
  * strides.  A zero matrix gives zeros; one that holds an infinity or a NaN gives NaN throughout.
- * The products take each operand as a pair of 16-bit floats (22 bits) and are summed in 32 bits.  Where out_type is
- * P2_BF16 the last step takes the upper half only: nothing magnifies its rounding, which stays below that of the result.
+ * The products take each operand as a pair of 16-bit floats (22 bits) and are summed in 32 bits; the result is rounded
+ * to out_type once, at the end: for each type it is the P2_F32 result, rounded.
  * Coefficients under which singular values of X may pass 2^10 are refused (P2_EUNSUPPORTED): the bound is worked out from
  * the polynomial, starting from [0, 1].  rows and cols up to 2^17, the pairs' padded size below 2^40 bytes. */
 int32_t p2_orthogonalize(const void* g, int32_t type, int64_t stride, int64_t matrix_stride, int64_t count, int64_t rows,

@@ -2,7 +2,7 @@
 //
 // Numbers.  Small singular values of X grow by a = 3.4445 a step, 485 times over five steps, and what a step rounds off grows
 // with them: with 16-bit operands the result of a gradient of low rank is off by 4 % (fp16) or 29 % (bf16).  So a
-// matrix is kept as pairs of fp16 numbers, value = (high + low) / 2^scale, 22 bits together, and a product takes three MFMA:
+// matrix is kept as pairs of fp16 numbers, value = (high + low) / 2^scale, 22 bits together, in every step, and a product takes three MFMA:
 // high*high + high*low + low*high, summed in fp32 (low*low is below what fp32 holds).  The scales come from the bound that the
 // polynomial sets on the singular values, so that no entry passes fp16's largest number (no entry is larger than the
 // largest singular value).
@@ -139,18 +139,18 @@ template <typename T> __global__ __launch_bounds__(256) void k_newton_scale(cons
     }
 }
 
-enum : int { kGram = 0, kPoly = 1, kApply = 2, kLast = 3, kPart = 4, kLastHalf = 5 };     // kLast: fp32, of upper halves bf16; kLastHalf: fp16
+enum : int { kGram = 0, kPoly = 1, kApply = 2, kPart = 3, kLast = 4, kLastBrain = 5, kLastHalf = 6 };     // the last ones: fp32, bf16, fp16
 
 struct Product {
     const char* p; const char* q;              // pairs: rows of P and of Q
-    const char* old;                           // kPoly: A; kApply, kLast: X turned
+    const char* old;                           // kPoly: A; kApply, the last ones: X turned
     char* straight;                            // result (kGram, kPoly: the whole result)
     char* turned;
-    void* out;                                 // kLast; kPart: sums of the parts of k, [parts][matrices][rows][cols]
+    void* out;                                 // the last ones; kPart: sums of the parts of k, [parts][matrices][rows][cols]
     int64_t p_plane, q_plane, old_plane, out_plane;      // from matrix to matrix: bytes (out: elements)
     int64_t k;                                 // summed length, padded
     int64_t rows, cols;                        // padded size of the result
-    int64_t out_rows, out_cols, out_stride;    // kLast: the result's own, and whether it is to be written turned
+    int64_t out_rows, out_cols, out_stride;    // the last ones: the result's own, and whether it is to be written turned
     float old_factor, sum_factor, gain;        // (old * old_factor + sum * sum_factor) * gain
     int32_t out_turned;
     int32_t tiles, parts;                      // blocks of a matrix; kPart: parts that k is cut into
@@ -187,20 +187,20 @@ template <int kLoads> __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");
 }
 
-template <bool kFirst, typename A, typename B> struct Pick { typedef A type; };
-template <typename A, typename B> struct Pick<false, A, B> { typedef B type; };
+template <int kKind> struct Result { typedef float type; };
+template <> struct Result<kLastBrain> { typedef bf16_t type; };
+template <> struct Result<kLastHalf> { typedef half_t type; };
 
-// One tile of C = P Q^T.  kTerms 3: pairs; 1: their upper halves.  The tiles of P and Q come to LDS in stages of kSub times 32
-// values of k (64 for upper halves), kStages - 1 of them under way while one is multiplied.  A row of a stage takes 128 bytes; its
+// One tile of C = P Q^T.  The tiles of P and Q come to LDS in stages of kSub times 32 values of k, kStages - 1 of them under way while one
+// is multiplied.  A row of a stage takes 128 bytes; its
 // 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
 // Rows past the end of P or Q are zeros: the loads' descriptors end with the matrix.
-template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub, int kTerms, int kKind>
+template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub, int kKind>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Product a) {
-    constexpr bool kEnd = kKind == kLast || kKind == kLastHalf;
-    typedef typename Pick<kKind == kLastHalf, half_t, typename Pick<kTerms == 1, bf16_t, float>::type>::type Out;
+    constexpr bool kEnd = kKind >= kLast;
+    typedef typename Result<kKind>::type Out;
     constexpr int kWaves = kWavesM * kWavesN;
     constexpr int FM = kTile / kWavesM / 16, FN = kTile / kWavesN / 16;
-    constexpr int kStepBytes = kTerms == 3 ? kLine : 2 * kLine;
     constexpr int kLoads = kTile / 8 / kWaves;             // of each operand a stage; one brings 8 rows
     constexpr int kAhead = kStages - 1;
     constexpr int kPerRow = (2 * kLoads + FM - 1) / FM;    // loads issued with a row of fragments: all of them in the first half
@@ -240,12 +240,12 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     const Rows p = rows_of(a.p + matrix * a.p_plane, (int64_t)bi * kTile, a.rows);
     const Rows q = rows_of(a.q + matrix * a.q_plane, (int64_t)bj * kTile, a.cols);
     const int part = (lane & 7) ^ (lane >> 3);
-    const int from = (wave * kLoads * 8 + (lane >> 3)) * (int)pitch + (kTerms == 3 ? part * 16 : (part >> 2) * kLine + (part & 3) * 16);
+    const int from = (wave * kLoads * 8 + (lane >> 3)) * (int)pitch + part * 16;
     auto bring_one = [&](int stage, int sub, int l, int at) {          // the l-th load of each operand
         const int src = from + l * 8 * (int)pitch;
         const int dst = (wave * kLoads + l) * 1024;
-        p.bring(&lds[stage][sub][0][dst], src, at + sub * kStepBytes);
-        q.bring(&lds[stage][sub][1][dst], src, at + sub * kStepBytes);
+        p.bring(&lds[stage][sub][0][dst], src, at + sub * kLine);
+        q.bring(&lds[stage][sub][1][dst], src, at + sub * kLine);
     };
     const int wm = wave / kWavesN, wn = wave % kWavesN;
     const int row = lane & 15, quad = lane >> 4;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
         }
     };
     fetch(0);
-    int stages = (int)(a.k / ((kTerms == 3 ? 32 : 64) * kSub)), begin = 0;
+    int stages = (int)(a.k / (32 * kSub)), begin = 0;
     if constexpr (kKind == kPart) {                        // (every part has a stage at least)
         begin = (int)((int64_t)stages * part_of_k / a.parts);
         stages = (int)((int64_t)stages * (part_of_k + 1) / a.parts) - begin;
@@ -274,20 +274,20 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
     for (int s = 0; s < kAhead; ++s)
         if (s < stages)
 #pragma unroll
-            for (int l = 0; l < kSub * kLoads; ++l) bring_one(s, l / kLoads, l % kLoads, (begin + s) * kSub * kStepBytes);
+            for (int l = 0; l < kSub * kLoads; ++l) bring_one(s, l / kLoads, l % kLoads, (begin + s) * kSub * kLine);
     float4_t acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    // where this lane's 16 bytes of a row lie: highs and lows, or two pieces of highs
+    // where this lane's 16 bytes of a row lie: highs and lows
     const int at0 = row * kLine + (quad ^ (row & 7)) * 16, at1 = row * kLine + ((quad + 4) ^ (row & 7)) * 16;
     int stage = 0, next = kAhead;
     for (int s = 0; s < stages; ++s) {
         if (s + kAhead <= stages) stage_barrier<2 * kLoads * kSub * (kAhead - 1)>();
         else stage_barrier<0>();
         const bool more = s + kAhead < stages;
-        const int at = (begin + s + kAhead) * kSub * kStepBytes;
+        const int at = (begin + s + kAhead) * kSub * kLine;
 #pragma unroll
         for (int sub = 0; sub < kSub; ++sub) {
             const char* tp = lds[stage][sub][0] + wm * FM * 16 * kLine;
@@ -313,12 +313,11 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void k_newton_product(Produ
 #pragma unroll
                     for (int l = i * kPerRow; l < (i + 1) * kPerRow && l < kLoads; ++l) bring_one(next, sub, l, at);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p1, q0[j], acc[i][j]) : multiply(p0, q0[j], acc[i][j]);
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p1, q0[j], acc[i][j]);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = kTerms == 3 ? multiply(p0, q1[j], acc[i][j]) : multiply(p1, q1[j], acc[i][j]);
-                if constexpr (kTerms == 3)
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q1[j], acc[i][j]);
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q0[j], acc[i][j]);
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(p0, q0[j], acc[i][j]);
                 p0 = n0;
                 p1 = n1;
                 if constexpr (kSub == 1) __builtin_amdgcn_sched_barrier(0);
@@ -726,18 +725,17 @@ int64_t tiles_of(const Product& p, int64_t tile, int kind) {
     return kind == kGram || kind == kPart || kind == kPoly ? down * (down + 1) / 2 : down * across;
 }
 
-template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void product(Product p, int terms, int kind, hipStream_t s) {
+template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void product(Product p, int kind, hipStream_t s) {
     p.tiles = (int32_t)tiles_of(p, kTile, kind) * (kind == kPart ? p.parts : 1);
     const dim3 grid((unsigned)(p.tiles * p.matrices));
     const dim3 block(kWavesM * kWavesN * 64);
-#define P2_PRODUCT(TERMS, KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, TERMS == 3 ? kSub : 1, TERMS, KIND><<<grid, block, 0, s>>>(p)
-    if (kind == kGram && terms == 3) P2_PRODUCT(3, kGram);
-    else if (kind == kGram) P2_PRODUCT(1, kGram);
-    else if (kind == kPoly) P2_PRODUCT(3, kPoly);
-    else if (kind == kApply) P2_PRODUCT(3, kApply);
-    else if (kind == kLastHalf) P2_PRODUCT(3, kLastHalf);
-    else if (terms == 3) P2_PRODUCT(3, kLast);
-    else P2_PRODUCT(1, kLast);
+#define P2_PRODUCT(KIND) k_newton_product<kTile, kWavesM, kWavesN, kStages, kSub, KIND><<<grid, block, 0, s>>>(p)
+    if (kind == kGram) P2_PRODUCT(kGram);
+    else if (kind == kPoly) P2_PRODUCT(kPoly);
+    else if (kind == kApply) P2_PRODUCT(kApply);
+    else if (kind == kLastBrain) P2_PRODUCT(kLastBrain);
+    else if (kind == kLastHalf) P2_PRODUCT(kLastHalf);
+    else P2_PRODUCT(kLast);
 #undef P2_PRODUCT
 }
 
@@ -751,19 +749,19 @@ template <int kTile, int kWavesM, int kWavesN, int kStages, int kSub> void produ
 // Where the units suffice for tiles of 48 x 48, more of them have one: three wavefronts, each 16 rows of all columns, and three
 // stages under way (updates of 1000 x 2777 288 us for 306, 1024 x 4096 351 for 367, 512 x 2048
 // 168 for 173, two of 700 x 2000 230 for 242; with two stages under way 295, 356, 167 and 233).
-void product_by_size(const Product& p, int terms, int kind, hipStream_t s) {
+void product_by_size(const Product& p, int kind, hipStream_t s) {
     auto cost = [&](int64_t tile, double stage, bool shared) {
         const int64_t tiles = tiles_of(p, tile, kind) * p.matrices;
         return stage * (shared ? std::max(1.0, (double)tiles / kUnits) : (double)ceil_div(tiles, kUnits));
     };
     const double c64 = cost(64, 0.25, true), c128 = cost(128, 0.7, false), c192 = cost(192, 1.4, false), c256 = cost(256, 2.45, false);
     const double least = std::min({c64, c128, c192, c256});
-    if (c256 == least) product<256, 2, 4, 2, 1>(p, terms, kind, s);
-    else if (c192 == least) product<192, 2, 4, 3, 1>(p, terms, kind, s);
-    else if (c128 == least) product<128, 2, 4, 2, 1>(p, terms, kind, s);
-    else if (tiles_of(p, 48, kind) * p.matrices <= kUnits) product<48, 3, 1, 4, 2>(p, terms, kind, s);
-    else if (tiles_of(p, 64, kind) * p.matrices <= kUnits) product<64, 2, 4, 3, 2>(p, terms, kind, s);
-    else product<64, 2, 2, 3, 1>(p, terms, kind, s);
+    if (c256 == least) product<256, 2, 4, 2, 1>(p, kind, s);
+    else if (c192 == least) product<192, 2, 4, 3, 1>(p, kind, s);
+    else if (c128 == least) product<128, 2, 4, 2, 1>(p, kind, s);
+    else if (tiles_of(p, 48, kind) * p.matrices <= kUnits) product<48, 3, 1, 4, 2>(p, kind, s);
+    else if (tiles_of(p, 64, kind) * p.matrices <= kUnits) product<64, 2, 4, 3, 2>(p, kind, s);
+    else product<64, 2, 2, 3, 1>(p, kind, s);
 }
 
 // X X^T of a short and long X has few tiles and a long sum: it is cut into as many parts as there are compute units for, of 16
@@ -897,10 +895,7 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     for (int i = 0; i < a.steps && e == hipSuccess; ++i) {
         const bool last = i + 1 == a.steps;
-        // Nothing magnifies what the last step rounds off.  For a bf16 result (1.66e-3 off by its own rounding) upper halves will do
-        // for X X^T and B X: 0.7e-3 to 0.9e-3 more or less at random, 1.8e-3 together.  Not for A A: its rounding is common to all
-        // of the result (in fp16 3e-3 where there are few rows).
-        const int terms = last && a.out_type == P2_BF16 ? 1 : 3;
+        // (Pairs in the last step, too, whatever the result's type: a X and B X may cancel, and then they magnify what upper halves round off.)
         const StepFactors f = step_factors(a, i, unit);
         Product p = {};
         p.matrices = a.count;
@@ -911,10 +906,10 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
         if (parts > 1) {
             p.out = sums; p.parts = (int32_t)parts;
             p.tiles = (int32_t)(tiles_of(p, 64, kPart) * parts);
-            k_newton_product<64, 2, 2, 3, 2, 3, kPart><<<dim3((unsigned)(p.tiles * a.count)), dim3(256), 0, s>>>(p);
+            k_newton_product<64, 2, 2, 3, 2, kPart><<<dim3((unsigned)(p.tiles * a.count)), dim3(256), 0, s>>>(p);
             k_newton_join<<<dim3((unsigned)tiles_of(p, 64, kPart), (unsigned)a.count), dim3(256), 0, s>>>(sums, (int32_t)parts, a.count, m, f.gram, ga, ab);
         } else {
-            product_by_size(p, terms, kGram, s);
+            product_by_size(p, kGram, s);
         }
         p = {};
         p.matrices = a.count;
@@ -923,7 +918,7 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
         p.k = p.rows = p.cols = m;
         p.old_factor = f.poly_old;
         p.sum_factor = f.poly_sum;
-        product_by_size(p, 3, kPoly, s);
+        product_by_size(p, kPoly, s);
         p = {};
         p.matrices = a.count;
         p.p = gb; p.p_plane = ab;
@@ -938,7 +933,7 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t s) {
             p.out_turned = tall;
             p.gain = (float)(a.scale / f.unit);
         }
-        product_by_size(p, terms, !last ? kApply : a.out_type == P2_F16 ? kLastHalf : kLast, s);
+        product_by_size(p, !last ? kApply : a.out_type == P2_BF16 ? kLastBrain : a.out_type == P2_F16 ? kLastHalf : kLast, s);
         unit = f.unit;
         e = hipGetLastError();
     }

@@ -467,6 +467,33 @@ def test_update_large(T, rows, cols):
     assert float(off) <= float(bound)
 
 
+def like_a_gradient(form, rows, cols):
+    if form == "equal":
+        return torch.full((rows, cols), 0.37, dtype=torch.float64, device="cuda")
+    if form == "rank one":
+        return draw(5, rows, 1) @ draw(6, 1, cols)
+    if form == "low rank":
+        return draw(1, rows, 4) @ draw(2, 4, cols) + 1e-3 * draw(3, rows, cols)
+    return draw(4, rows, cols)
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 70), (150, 333), (200, 300), (700, 200), (1000, 2777), (2048, 2048)])
+@pytest.mark.parametrize("form", ["normal", "low rank", "rank one", "equal"])
+def test_update_is_rounded_once(T, rows, cols, form):
+    """A 16-bit result is the 32-bit one rounded, also where a X and B X cancel (and would magnify what fewer bits round off)."""
+    g = like_a_gradient(form, rows, cols).to(BF16)
+    for steps, coefficients in ((5, NS), (1, NS), (1, (100.0, -200.0, 101.0)), (1, (3.0, -4.0, 1.01)), (6, (1.875, -1.25, 0.375))):
+        full = T.p2_orthogonalize(g, steps=steps, coefficients=coefficients, dtype=F32)
+        for kind in (BF16, F16):
+            assert torch.equal(T.p2_orthogonalize(g, steps=steps, coefficients=coefficients, dtype=kind), full.to(kind)), (steps, coefficients, kind)
+        if steps == 1:
+            # X is in each term once for every power; four roundings to 22 bits each, and a rounding to 24 bits for every 32 terms of three sums
+            want, sizes = newton_schulz(g, steps=1, coefficients=coefficients)
+            a, b, c = (abs(v) for v in coefficients)
+            bound = (4 + 3 * max(rows, cols) / 32 / 4) * 2.0 ** -22 * (a + 3 * b + 5 * c) * sizes[0] / sizes[1]
+            assert torch.linalg.vector_norm(full.double() - want) <= bound * sizes[1], (coefficients, float(bound))
+
+
 @pytest.mark.parametrize("rows,cols", [(48, 80), (300, 200)])
 def test_update_forms(T, rows, cols):
     g = draw(4, rows, cols).float()
