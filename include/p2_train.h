@@ -41,7 +41,7 @@ extern "C" {
 #define P2_MAX_CHOSEN 64      /* experts that one token may choose                  */
 
 /* y = (x - mean) * rstd * weight + bias for each row of `cols` values (>= 1): mean and variance over the row (the
- * variance of all `cols` values, from centred squares), rstd = 1 / sqrt(variance + eps), eps >= 0.  `type` is that of x
+ * variance of all `cols` values, from squares of what is centred on the mean before its rounding), rstd = 1 / sqrt(variance + eps), eps >= 0.  `type` is that of x
  * and y, `weight_type` that of weight and bias; either may be NULL (1 and 0).  mean and rstd (NULL, or [rows]) are what the
  * backward pass needs.  y may be x (same stride).  rows = 0 writes nothing. */
 int32_t p2_layer_norm_forward(const void* x, int32_t type, int64_t x_stride, const void* weight, const void* bias,

@@ -1,12 +1,12 @@
 // Layer norm, forward and backward.
 //
-// A row is read once and stays in registers: its mean, the mean of its centred squares (no difference of large sums) and the
-// result are worked out from there, so that a pass moves what it cannot do without: 2 values an element forward, 3 backward.
+// A row is read once and stays in registers: its mean, with what the first sum of it rounded off, the mean of its centred squares and
+// the result are worked out from there, so that a pass moves what it cannot do without: 2 values an element forward, 3 backward.
 // Rows are dealt to groups of kTpr threads (a part of a wavefront, a wavefront, or a block), each thread holding kNv vectors
 // of 16 bytes.
 //
-// What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 24.1 us, 5.6 TB/s (part of it from the last
-// cache); backward with both sums, 16384 x 4096 bf16: 81.1 us, 5.0 TB/s, of which k_norm_weight_grad takes 5.1.  Rows with odd ends: 5003 x 1023
+// What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 26.1 us, 5.1 TB/s (part of it from the last
+// cache; 24.3 without what the first mean rounds off, which a row of 5000 fp32 values of 12345.678 pays for with results of 0.5 for 0); backward with both sums, 16384 x 4096 bf16: 81.1 us, 5.0 TB/s, of which k_norm_weight_grad takes 5.1.  Rows with odd ends: 5003 x 1023
 // fp16 of rows 1061 apart 8 us, 2.6 TB/s.  One row: 2.4 us on the device in a call of 6.8.
 #include <algorithm>
 
@@ -42,6 +42,55 @@ template <int kTpr> __device__ __forceinline__ float row_sum(float v, float* buf
     }
 }
 
+// Two of them at one barrier.
+template <int kTpr> __device__ __forceinline__ void row_sums(float& a, float& b, float* buf_a, float* buf_b) {
+    if constexpr (kTpr <= 64) {
+        a = group_sum<kTpr>(a);
+        b = group_sum<kTpr>(b);
+    } else {
+        constexpr int kWaves = kTpr / 64;
+        a = group_sum<64>(a);
+        b = group_sum<64>(b);
+        if ((threadIdx.x & 63) == 0) { buf_a[threadIdx.x >> 6] = a; buf_b[threadIdx.x >> 6] = b; }
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) { a += buf_a[(threadIdx.x / kTpr) * kWaves + w]; b += buf_b[(threadIdx.x / kTpr) * kWaves + w]; }
+    }
+}
+
+// What a row's first mean rounded off, and its spread.  A sum of n values in 32 bits rounds, so the first mean is off by some steps of its own
+// size, which may be more than the whole spread of a row that lies far from zero.  What the values' distances from it sum up to is taken off again:
+// the mean is mean + low, a centred value (x - mean) - low, the variance that of those.  It comes from the distances' squares, less low^2, as long as
+// that loses a bit at most, which two sums at one barrier suffice for; else (rows of equal values, nearly) the rest is taken off, too, and the squares
+// are summed afresh.
+// each(f): f(x - mean, whether it counts) for this thread's values.  kTpr: threads of the row, which are a block's where it has several wavefronts
+// (the barriers); buf: a line for each sum, the first of which is the mean's, so that the next row's is written when all have read this one's.
+struct Centre {
+    float low, rstd;
+    __device__ __forceinline__ float of(float d) const { return (d - low) * rstd; }
+    __device__ __forceinline__ float whole_mean(float mean) const { return low == low ? mean + low : mean; }     // (an infinity beside numbers has an infinite mean)
+};
+constexpr int kSumLines = 5;
+template <int kTpr, typename Each> __device__ __forceinline__ Centre centre_of(float n, float eps, float (*buf)[16], Each&& each) {
+    float s = 0.0f, q = 0.0f;
+    each([&](float d, bool counts) { const float v = counts ? d : 0.0f; s += v; q += v * v; });
+    row_sums<kTpr>(s, q, buf[1], buf[2]);
+    Centre c;
+    c.low = s / n;
+    const float square = c.low * c.low;
+    float variance = q / n - square;
+    if (!(variance >= square && square < INFINITY)) {      // (the same for all threads of the row)
+        s = q = 0.0f;
+        each([&](float d, bool counts) { s += counts ? d - c.low : 0.0f; });
+        c.low += row_sum<kTpr>(s, buf[3]) / n;
+        each([&](float d, bool counts) { const float v = counts ? d - c.low : 0.0f; q += v * v; });
+        variance = row_sum<kTpr>(q, buf[4]) / n;
+    }
+    c.rstd = 1.0f / sqrtf(variance + eps);
+    return c;
+}
+
 // A lane's N weights, in whatever type they have; loaded like a row's vectors.
 template <int N> struct WeightVec {
     vec_t<float, N> raw;                       // 16-bit types: the first half of it
@@ -74,9 +123,9 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
     constexpr int V = 16 / sizeof(T);
     constexpr int kRows = NormGroup<kTpr>::kRows;
     constexpr bool kEarly = kNv <= 2;                      // weights for all rows, and a row ahead, stay in registers
-    __shared__ float buf[2][16];
+    static_assert(kTpr <= 64 || kRows == 1, "rows of several wavefronts have a block each");
+    __shared__ float buf[kSumLines][16];
     const int lane = threadIdx.x % kTpr, group = threadIdx.x / kTpr, cols = (int)a.cols;
-    const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
     vec_t<T, V> next[kNv];
     auto ask = [&](int64_t row) {                          // (rows of a block's own threads: all of them are there, or none)
         const T* x = static_cast<const T*>(a.x) + (row < a.rows ? row : a.rows - 1) * a.x_stride;
@@ -111,68 +160,63 @@ template <typename T, int kTpr, int kNv, bool kWhole> __global__ __launch_bounds
         const bool there = row < a.rows;
         if constexpr (!kEarly) ask(row);
         float v[kNv][V];
-        float s = 0.0f;
+        auto each = [&](auto&& f) {
 #pragma unroll
-        for (int i = 0; i < kNv; ++i) {
+            for (int i = 0; i < kNv; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] = (float)next[i][j];
-                s += own<V, kWhole>((i * kTpr + lane) * V, cols, j) ? v[i][j] : 0.0f;
-            }
-        }
-        if constexpr (kEarly) { if (row0 + stride < a.rows) ask(row + stride); }
-        const float mean = row_sum<kTpr>(s, buf[0]) / n;
-        s = 0.0f;
+                for (int j = 0; j < V; ++j) f(v[i][j], own<V, kWhole>((i * kTpr + lane) * V, cols, j));
+        };
 #pragma unroll
         for (int i = 0; i < kNv; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] -= mean;
-                s += own<V, kWhole>((i * kTpr + lane) * V, cols, j) ? v[i][j] * v[i][j] : 0.0f;
-            }
-        const float rstd = 1.0f / sqrtf(row_sum<kTpr>(s, buf[1]) / n + a.eps);
+            for (int j = 0; j < V; ++j) v[i][j] = (float)next[i][j];
+        if constexpr (kEarly) { if (row0 + stride < a.rows) ask(row + stride); }
+        float s = 0.0f;
+        each([&](float x, bool counts) { s += counts ? x : 0.0f; });
+        const float n = (float)a.cols, mean = row_sum<kTpr>(s, buf[0]) / n;
+        each([&](float& x, bool) { x -= mean; });
+        const Centre c = centre_of<kTpr>(n, a.eps, buf, each);
         if (there) {
             if constexpr (!kEarly) ask_weights();
             if (lane == 0) {
-                if (a.mean) a.mean[row] = mean;
-                if (a.rstd) a.rstd[row] = rstd;
+                if (a.mean) a.mean[row] = c.whole_mean(mean);
+                if (a.rstd) a.rstd[row] = c.rstd;
             }
             T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
             for (int i = 0; i < kNv; ++i) {
-                const int c = (i * kTpr + lane) * V;
+                const int at = (i * kTpr + lane) * V;
                 if constexpr (!kEarly) weights_of(i, w[0], b[0]);
                 float o[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) o[j] = v[i][j] * rstd * w[kEarly ? i : 0][j] + b[kEarly ? i : 0][j];
-                if (c < cols) store_vec<T, V>(y + vec_at(c, cols, V), o);
+                for (int j = 0; j < V; ++j) o[j] = c.of(v[i][j]) * w[kEarly ? i : 0][j] + b[kEarly ? i : 0][j];
+                if (at < cols) store_vec<T, V>(y + vec_at(at, cols, V), o);
             }
         }
     }
 }
 
-// Rows too long for registers (more than 4096 vectors): three passes over them, the later two from the cache.
+// Rows too long for registers (more than 4096 vectors): three passes over them (five where the mean is taken off once more), the later ones from the cache.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_long(NormForward a) {
-    __shared__ float buf[2][16];
-    const float n = (float)a.cols;                         // (a row of equal values has exactly that mean: no product with 1 / n)
+    __shared__ float buf[kSumLines][16];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         float s = 0.0f;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 1024) s += (float)x[c];
-        const float mean = row_sum<1024>(s, buf[0]) / n;
-        s = 0.0f;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 1024) { const float d = (float)x[c] - mean; s += d * d; }
-        const float rstd = 1.0f / sqrtf(row_sum<1024>(s, buf[1]) / n + a.eps);
+        for (int64_t i = threadIdx.x; i < a.cols; i += 1024) s += (float)x[i];
+        const float n = (float)a.cols, mean = row_sum<1024>(s, buf[0]) / n;
+        const Centre c = centre_of<1024>(n, a.eps, buf, [&](auto&& f) {
+            for (int64_t i = threadIdx.x; i < a.cols; i += 1024) f((float)x[i] - mean, true);
+        });
         if (threadIdx.x == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+            if (a.mean) a.mean[row] = c.whole_mean(mean);
+            if (a.rstd) a.rstd[row] = c.rstd;
         }
         T* y = static_cast<T*>(a.y) + row * a.y_stride;
-        for (int64_t c = threadIdx.x; c < a.cols; c += 1024) {
+        for (int64_t i = threadIdx.x; i < a.cols; i += 1024) {
             float w[1] = {1.0f}, b[1] = {0.0f};
-            if (a.weight) load_typed<1>(a.weight, a.weight_type, c, 1, w, 1.0f);
-            if (a.bias) load_typed<1>(a.bias, a.weight_type, c, 1, b, 0.0f);
-            y[c] = (T)(((float)x[c] - mean) * rstd * w[0] + b[0]);
+            if (a.weight) load_typed<1>(a.weight, a.weight_type, i, 1, w, 1.0f);
+            if (a.bias) load_typed<1>(a.bias, a.weight_type, i, 1, b, 0.0f);
+            y[i] = (T)(c.of((float)x[i] - mean) * w[0] + b[0]);
         }
     }
 }
@@ -182,27 +226,28 @@ constexpr int kShortBlock = 256;
 template <typename T> __global__ __launch_bounds__(kShortBlock) void k_norm_forward_short(NormForward a) {
     constexpr int kMost = 16 / sizeof(T) - 1;
     const int cols = (int)a.cols;
-    const float n = (float)a.cols;
     for (int64_t row = (int64_t)blockIdx.x * kShortBlock + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * kShortBlock) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         T* y = static_cast<T*>(a.y) + row * a.y_stride;
         float v[kMost], s = 0.0f;
 #pragma unroll
-        for (int c = 0; c < kMost; ++c) { v[c] = c < cols ? (float)x[c] : 0.0f; s += v[c]; }
-        const float mean = s / n;
-        s = 0.0f;
+        for (int i = 0; i < kMost; ++i) { v[i] = i < cols ? (float)x[i] : 0.0f; s += v[i]; }
+        const float n = (float)a.cols, mean = s / n;
 #pragma unroll
-        for (int c = 0; c < kMost; ++c) { v[c] -= mean; s += c < cols ? v[c] * v[c] : 0.0f; }
-        const float rstd = 1.0f / sqrtf(s / n + a.eps);
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
+        for (int i = 0; i < kMost; ++i) v[i] -= mean;
+        const Centre c = centre_of<1>(n, a.eps, nullptr, [&](auto&& f) {
 #pragma unroll
-        for (int c = 0; c < kMost; ++c)
-            if (c < cols) {
+            for (int i = 0; i < kMost; ++i) f(v[i], i < cols);
+        });
+        if (a.mean) a.mean[row] = c.whole_mean(mean);
+        if (a.rstd) a.rstd[row] = c.rstd;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i)
+            if (i < cols) {
                 float w[1] = {1.0f}, b[1] = {0.0f};
-                if (a.weight) load_typed<1>(a.weight, a.weight_type, c, 1, w, 1.0f);
-                if (a.bias) load_typed<1>(a.bias, a.weight_type, c, 1, b, 0.0f);
-                y[c] = (T)(v[c] * rstd * w[0] + b[0]);
+                if (a.weight) load_typed<1>(a.weight, a.weight_type, i, 1, w, 1.0f);
+                if (a.bias) load_typed<1>(a.bias, a.weight_type, i, 1, b, 0.0f);
+                y[i] = (T)(c.of(v[i]) * w[0] + b[0]);
             }
     }
 }

@@ -195,6 +195,56 @@ def test_layer_norm_values_at_the_edge(T):
     assert dx[1].isnan().all() and torch.isfinite(dx[0]).all() and torch.isfinite(dx[3]).all() and (db == 4).all()
 
 
+FAR = [(300, 2), (300, 3), (300, 7), (9, 64), (3, 100), (2, 512), (4, 1023), (3, 2048), (2, 4096), (2, 5000), (2, 8192), (2, 9001), (2, 16384), (1, 40000)]
+
+
+@pytest.mark.parametrize("rows,cols", FAR)
+@pytest.mark.parametrize("kind,values", [(F32, (12345.678, 1000.1, -3.3e8, 0.1, 1e30)), (F16, (1000.5, 0.1, -999.0)), (BF16, (1000.0, -3.3e8, 0.1))])
+def test_layer_norm_of_equal_values(T, rows, cols, kind, values):
+    """Distances from a first mean are whole steps of the value, and what is left of their sum tells how many: nothing remains."""
+    for value in values:
+        x = torch.full((rows, cols), value, dtype=kind, device="cuda")
+        y, mean, rstd = T.p2_layer_norm_forward(x)
+        assert not y.any() and torch.equal(mean, x[:, 0].float()), (value, float(y.float().abs().max()), float(mean[0]))
+        assert float((rstd.double() * math.sqrt(1e-5) - 1).abs().max()) <= 4 * U
+
+
+@pytest.mark.parametrize("rows,cols", FAR)
+@pytest.mark.parametrize("kind,offset", [(F32, 1e6), (F32, -3e4), (F16, 2000.0)])
+def test_layer_norm_of_rows_far_from_zero(T, rows, cols, kind, offset):
+    """The first mean is off by up to 70 roundings of the offset, which is taken off again: what remains is off by as many of the distances."""
+    x = (offset + draw(cols, rows, cols)).to(kind)
+    y, mean, rstd = T.p2_layer_norm_forward(x, eps=1e-12)
+    ry, rmean, rr, xh = norm_reference(x, None, None, 1e-12)
+    there = torch.isfinite(rr) & (rr < 1e5)               # (two values may be the same)
+    low = 70 * U * abs(offset)
+    compare(mean[there], rmean[there], (70 * U * (1 / rr + low))[there], "mean")
+    compare(rstd[there], rr[there], 200 * U * rr[there], "rstd")
+    compare(y[there], ry[there], U * (70 * (1 + low * rr[:, None]) + 300 * (1 + xh.abs()))[there], "y")
+
+
+@pytest.mark.parametrize("rows,cols", FAR)
+def test_layer_norm_of_nearly_equal_values(T, rows, cols):
+    """One value a step away from the others: the variance is far below the square of what the first mean is off by."""
+    x = torch.full((rows, cols), 12345.678, device="cuda")
+    x[:, cols // 2] = torch.nextafter(x[0, 0], x.new_tensor(math.inf))
+    y, mean, rstd = T.p2_layer_norm_forward(x, eps=1e-15)
+    ry, rmean, rr, xh = norm_reference(x, None, None, 1e-15)
+    compare(rstd, rr, 200 * U * rr, "rstd")
+    # the taken-off part of the mean is rounded to 24 bits itself, in units of a step over sqrt(cols)
+    compare(y, ry, (300 + 35 * math.sqrt(cols)) * U * (1 + xh.abs()), "y")
+    compare(mean, rmean, 70 * U / rr, "mean")
+
+
+def test_layer_norm_statistics_of_what_is_no_number(T):
+    for cols in (3, 100, 2048, 5000, 40000):
+        x = draw(cols, 4, cols).float()
+        x[0, 1], x[1, 2], x[2, 0] = math.inf, -math.inf, math.nan
+        y, mean, rstd = T.p2_layer_norm_forward(x)
+        assert mean[0] == math.inf and mean[1] == -math.inf and mean[2].isnan() and rstd[:3].isnan().all() and y[:3].isnan().all()
+        assert torch.isfinite(y[3]).all()
+
+
 def test_layer_norm_beyond_32_bits(T):
     """Rows further apart than 2^31 values."""
     stride, cols = (1 << 30) + 8, 264
