@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -81,6 +82,18 @@ void on_device(const at::Tensor& first, std::initializer_list<const at::Tensor*>
         if (t->defined() && t->device() != first.device()) refuse("tensors must be on the current device");
 }
 
+// A result has no history: a warning, from where the call stands, where an argument is to have a gradient that would never come.
+void not_recorded(const char* call, std::initializer_list<const at::Tensor*> arguments) {
+    if (!at::GradMode::is_enabled()) return;
+    for (const at::Tensor* t : arguments)
+        if (t->defined() && t->requires_grad()) {
+            const std::string text = std::string(call) + ": an argument requires a gradient, but nothing is recorded for autograd and the result has no history; call it "
+                                     "under torch.no_grad(), or in an autograd function whose backward makes the gradient's call";
+            if (PyErr_WarnEx(PyExc_UserWarning, text.c_str(), 2) < 0) throw Refused();
+            return;
+        }
+}
+
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
 // A matrix of t's rows, contiguous each.
@@ -144,6 +157,7 @@ PyObject* layer_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const double eps = number(a[3]);
         void* stream = stream_of(a[4]);
         on_device(x, {&weight, &bias});
+        not_recorded("p2_layer_norm_forward", {&x, &weight, &bias});
         const int32_t type = type_of(x, "x");
         const Rows r = rows_of(x);
         weight = vector_of(std::move(weight), r.cols, "weight", false);
@@ -172,6 +186,7 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         }
         void* stream = stream_of(a[8]);
         on_device(x, {&dy, &weight, &mean, &rstd});
+        not_recorded("p2_layer_norm_backward", {&dy, &x, &weight, &mean, &rstd});
         const int32_t type = type_of(x, "x");
         const Rows r = rows_of(x), d = rows_of(dy);
         weight = vector_of(std::move(weight), r.cols, "weight", false);
@@ -207,6 +222,7 @@ PyObject* balance_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         void* stream = stream_of(a[3]);
         const at::Tensor keep = keep_of(logits, optional(a[2], "keep"));
         on_device(logits, {&keep});
+        not_recorded("p2_balance_forward", {&logits});
         const int32_t type = type_of(logits, "logits");
         const Rows r = rows_of(logits);
         const int32_t experts = (int32_t)std::min<int64_t>(r.cols, std::numeric_limits<int32_t>::max());
@@ -239,6 +255,7 @@ PyObject* balance_loss(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const at::Tensor counts = counts_of(first, kept, first.dim() == 1 ? first.size(0) : -1);
         const at::Tensor prob_sum = vector_of(tensor(a[1], "prob_sum"), counts.size(0), "prob_sum", true);
         on_device(counts, {&prob_sum, &kept});
+        not_recorded("p2_balance_loss", {&prob_sum});
         const int32_t experts = (int32_t)std::min<int64_t>(counts.size(0), std::numeric_limits<int32_t>::max());
         at::Tensor loss = at::empty({}, prob_sum.options());
         check(calls.balance_loss((const int64_t*)ptr(counts), (const float*)ptr(prob_sum), (const int64_t*)ptr(kept), experts, k, (float*)ptr(loss), stream));
@@ -254,6 +271,7 @@ PyObject* balance_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         void* stream = stream_of(a[7]);
         const at::Tensor keep = keep_of(logits, optional(a[4], "keep"));
         on_device(logits, {&chosen, &counts, &kept, &keep, &dgate, &dloss});
+        not_recorded("p2_balance_backward", {&logits, &dgate, &dloss});
         const int32_t type = type_of(logits, "logits");
         const Rows r = rows_of(logits);
         if (chosen.scalar_type() != at::kInt || chosen.dim() != 2 || chosen.size(0) != r.n) refuse("expert must be int32 [tokens, k]");
@@ -279,6 +297,7 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const double coefficients[3] = {number(a[2]), number(a[3]), number(a[4])}, eps = number(a[5]), scale = number(a[6]);
         const int64_t asked = whole(a[7]);
         void* stream = stream_of(a[8]);
+        not_recorded("p2_orthogonalize", {&g});
         const int32_t type = type_of(g, "g"), out_type = asked < 0 ? type : (int32_t)asked;
         at::Tensor out = at::empty(g.sizes(), g.options().dtype(scalar_of(out_type)));
         const int64_t rows = g.size(-2), cols = g.size(-1);

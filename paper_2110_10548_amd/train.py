@@ -3,7 +3,7 @@ by a small extension module (csrc/p2_train_tensors.cpp), which calls the library
 
 Tensors live on the current device and are worked on in the current stream; results and workspaces come from torch's
 allocator, so calls may be captured into a graph.  Nothing here is recorded for autograd: the gradients are calls of their
-own.  Rows whose last dimension is not contiguous, or whose leading dimensions have no common stride, are copied first.
+own, and where autograd records and an argument requires a gradient a UserWarning says so.  Rows whose last dimension is not contiguous, or whose leading dimensions have no common stride, are copied first.
 """
 import ctypes as C
 

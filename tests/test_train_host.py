@@ -2,6 +2,7 @@
 import ctypes as C
 import os
 import re
+import warnings
 
 import pytest
 import torch
@@ -146,3 +147,30 @@ def test_tensors_elsewhere_or_of_other_types_are_refused(T):
         with pytest.raises(T.P2Error) as e:
             call()
         assert e.value.code == EINVAL
+
+
+def test_arguments_that_require_a_gradient_bring_a_warning(T):
+    """No rows: nothing is queued, so the extension module's calls need no GPU (the entry points look at the device first)."""
+    calls = T._native_calls()
+    x, w, g = torch.zeros(0, 8), torch.ones(8), torch.zeros(0, 5, 7)
+    m, expert, counts, tokens = torch.zeros(0), torch.zeros(0, 2, dtype=torch.int32), torch.zeros(8, dtype=torch.int64), torch.zeros((), dtype=torch.int64)
+    one = torch.ones(())
+
+    def all_of(grad):
+        p = {n: t.clone().requires_grad_(n == grad) for n, t in dict(x=x, w=w, g=g, one=one).items()}
+        calls.layer_norm_forward(p["x"], p["w"], None, 1e-5, 0)
+        calls.layer_norm_backward(p["x"], p["x"], p["w"], m, m, True, False, False, 0)
+        calls.balance_backward(p["x"], expert, counts, tokens, None, None, p["one"], 0)
+        calls.orthogonalize(p["g"], 5, *T.NEWTON_SCHULZ, 1e-7, 1.0, -1, 0)
+
+    for grad, count in (("x", 3), ("w", 2), ("g", 1), ("one", 1), (None, 0)):
+        with warnings.catch_warnings(record=True) as caught:
+            warnings.simplefilter("always")
+            all_of(grad)
+        assert [c.category for c in caught] == [UserWarning] * count and all("autograd" in str(c.message) for c in caught)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with torch.no_grad():
+            all_of("x")
+        with pytest.raises(UserWarning):                   # (a warning that is an error is one here, too)
+            all_of("x")

@@ -5,6 +5,7 @@ terms one after the other is off by at most d 2^-24 of the sum of their absolute
 together add more than 64 terms a row in sequence here (rows of up to 32768), or 64 + rows / 512 a column.
 """
 import math
+import warnings
 
 import numpy as np
 import pytest
@@ -718,3 +719,22 @@ def test_forms_of_the_arguments(T):
     assert [r[n].dtype for n in r] == [torch.int32, F32, torch.int64, F32, torch.int64, F32]
     g = T.p2_orthogonalize(x, dtype=F32)
     assert g.shape == x.shape and g.dtype == F32 and T.p2_orthogonalize(x.transpose(1, 2)).shape == (3, 24, 5)
+
+
+def test_a_parameter_that_would_not_train_is_warned_of(T):
+    x, z, g = draw(1, 6, 40).float(), draw(2, 10, 12).float(), draw(3, 20, 30).float()
+    w = torch.nn.Parameter(torch.ones(40, device="cuda"))
+    y, mean, rstd = T.p2_layer_norm_forward(x, w.detach())
+    r = T.p2_balance_forward(z, 3)
+    zp, gp, prob = (t.clone().requires_grad_() for t in (z, g, r["prob_sum"]))
+    calls = (lambda: T.p2_layer_norm_forward(x, w), lambda: T.p2_layer_norm_backward(x, x, w, mean, rstd), lambda: T.p2_balance_forward(zp, 3),
+             lambda: T.p2_balance_loss(r["counts"], prob, r["tokens"], 3), lambda: T.p2_balance_backward(zp, r["expert"], r["counts"], r["tokens"]),
+             lambda: T.p2_orthogonalize(gp))
+    for call in calls:
+        with pytest.warns(UserWarning, match="nothing is recorded for autograd") as caught:
+            call()
+        assert len(caught) == 1 and caught[0].filename == __file__
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            with torch.no_grad():
+                call()
