@@ -1,4 +1,8 @@
-"""Build libp2.so (HIP kernels + C ABI) for gfx950, in-tree."""
+"""Build libp2.so (HIP kernels + C ABI) for gfx950, in-tree, and _train.so (the training operators on torch tensors).
+
+The library needs hipcc alone; the extension module needs torch's and Python's headers and is built apart from it.
+"""
+import importlib.util
 import os
 import subprocess
 
@@ -26,10 +30,7 @@ def tensors_command():
 
 def build(verbose: bool = False) -> str:
     objs = []
-    cmd = tensors_command()
-    if verbose:
-        print(" ".join(cmd))
-    procs = [(subprocess.Popen(cmd), cmd)]
+    procs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, os.path.splitext(src)[0] + ".o")
         cmd = ["hipcc", "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj] + FLAGS
@@ -47,5 +48,19 @@ def build(verbose: bool = False) -> str:
     return LIB
 
 
+def build_tensors(verbose: bool = False):
+    """The extension module's path, or None where there is no torch to build it for."""
+    if importlib.util.find_spec("torch") is None:
+        print("torch is not installed: libp2.so is complete, the training operators on torch tensors are left out")
+        return None
+    cmd = tensors_command()
+    if verbose:
+        print(" ".join(cmd))
+    if subprocess.run(cmd).returncode != 0:
+        raise RuntimeError("compile failed: " + " ".join(cmd))
+    return TENSORS
+
+
 if __name__ == "__main__":
     print(build(verbose=True))
+    print(build_tensors(verbose=True))
