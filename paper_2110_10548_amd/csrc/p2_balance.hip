@@ -429,7 +429,10 @@ __global__ __launch_bounds__(kBalanceBlock) void k_balance_loss(const int64_t* c
 }
 
 // Backward.  u = dloss experts / (k kept^2) counts + the choices' dgate, dlogits = p (u - sum p u).  The gates' gradients of a token go to their experts' places in a row of LDS of the token's lanes, which hold zeros
-// otherwise and are cleared again after use; only the token's own lanes, which are of one wavefront, touch that row.
+// otherwise and are cleared again after use; only the token's own lanes, which are of one wavefront, touch that row.  Where a caller's choices name
+// an expert more than once (the forward pass never does) its gradients are added one by one in the order of the choices: instructions of one wavefront
+// follow each other, and an instruction's additions to one place are made in the order of the lanes, which a test of sums that cancel only in that
+// order holds to.
 template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBalanceBlock, 4) void k_balance_backward(BalanceBackward a) {
     typedef Row<T, kLanes, kItems> R;
     constexpr int kTokens = kBalanceBlock / kLanes;

@@ -346,6 +346,28 @@ def test_routing_gradient_is_that_of_differences(T):
     assert abs((loss(h) - loss(-h)) / (2 * h) - float((got.double() * v).sum())) <= 600 * U * size + 1e-8 * size
 
 
+@pytest.mark.parametrize("tokens,experts,k", [(5, 4, 4), (40, 12, 8), (70, 64, 6), (33, 256, 8), (20, 300, 40), (9, 1024, 64)])
+def test_routing_gradient_of_experts_named_twice(T, tokens, experts, k):
+    """Not what the forward pass chooses: the gates' gradients of such an expert are added in their order (another order would leave 1 or 2 here)."""
+    rng = np.random.RandomState(tokens + k)
+    z = draw(tokens, tokens, experts).float()
+    expert = rng.randint(-1, 3, (tokens, k)).astype(np.int32)
+    values = rng.choice([2.0 ** 24, -2.0 ** 24, 1.0, 1.0, 0.0], (tokens, k)).astype(np.float32)
+    expert[0, :], values[0, :4] = 1, (2.0 ** 24, 1.0, 1.0, -2.0 ** 24)
+    values[0, 4:] = 0.0
+    u = np.zeros((tokens, experts + 1), np.float32)
+    for i in range(k):
+        u[np.arange(tokens), expert[:, i]] += values[:, i]
+    u = torch.from_numpy(u[:, :experts]).double().cuda()
+    p = torch.softmax(z.double(), 1)
+    counts, kept = torch.zeros(experts, dtype=torch.int64, device="cuda"), torch.tensor(tokens, device="cuda")
+    want, size = p * (u - (p * u).sum(1, keepdim=True)), p * (u.abs() + (p * u.abs()).sum(1, keepdim=True))
+    args = (z, torch.from_numpy(expert).cuda(), counts, kept, None, torch.from_numpy(values).cuda())
+    got = T.p2_balance_backward(*args)
+    compare(got, want, 540 * U * size, "dlogits")
+    assert not got[0].any() and all(torch.equal(got, T.p2_balance_backward(*args)) for _ in range(5))
+
+
 @pytest.mark.parametrize("kind", [F32, BF16, F16])
 def test_routing_of_equal_extreme_and_masked_logits(T, kind):
     lowest, inf, nan = torch.finfo(kind).min, math.inf, math.nan
