@@ -116,7 +116,7 @@ def main(tokens=16384, width=1024, experts=64, chosen=4, say=print):
     layer = Layer(width, experts, chosen)
     x = torch.randn(tokens, width, device="cuda") * torch.exp(0.5 * torch.randn(tokens, 1, device="cuda"))
     dout, dgate = torch.randn(tokens, width, device="cuda") / tokens, torch.randn(tokens, chosen, device="cuda") / tokens
-    shares = torch.arange(tokens, device="cuda").chunk(devices)
+    shares = torch.arange(tokens, device="cuda").tensor_split(devices)      # (as many for every device, or one more; few tokens: none for some)
 
     small = Program((2 * experts + 1) * 8)
     large = Program((2 * width + width * experts + width * width) * 4)

@@ -16,3 +16,14 @@ def test_planned_step_agrees_with_one_device():
     # fp32 sums of some hundred terms in another order; the update magnifies what is off by up to 485 of the norm's 1
     assert abs(loss / whole - 1) < 1e-5 and off[0] < 1e-5 and off[1] < 5e-3
     assert [op for op, _, _ in large.steps] != ["AllReduce"] and large.seconds < large.allreduce_seconds
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [20, 1001, 5])
+def test_planned_step_of_batches_that_do_not_divide(tokens):
+    """Every device has its share, some of them one token less, or none at all."""
+    spec = importlib.util.spec_from_file_location("planned_step", os.path.join(ROOT, "examples", "planned_step.py"))
+    step = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(step)
+    loss, whole, off, _, _ = step.main(tokens=tokens, width=160, experts=24, chosen=3, say=lambda *a: None)
+    assert abs(loss / whole - 1) < 1e-5 and off[0] < 1e-5 and off[1] < 5e-3
