@@ -659,6 +659,22 @@ def test_another_stream(T):
     assert all(torch.equal(p, q) for p, q in zip(want, got))
 
 
+def test_two_streams_at_once(T):
+    """Calls under way together share nothing: statistics over several blocks, partial sums and updates too large for LDS, alternately, with no wait between."""
+    inputs = [_step_inputs(40 + i) for i in range(4)]
+    want = [_step(T, *i) for i in inputs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for turn in range(6):
+        for i, x in enumerate(inputs):
+            with torch.cuda.stream(streams[(turn + i) % 2]):
+                got.append((i, _step(T, *x)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for i, one in got for p, q in zip(want[i], one))
+
+
 def test_in_a_graph(T):
     inputs = _step_inputs(3)
     _step(T, *inputs)                                     # first calls load kernels
