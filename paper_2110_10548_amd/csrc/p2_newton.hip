@@ -38,7 +38,13 @@ constexpr int64_t kMostNormParts = 1024;       // blocks that a matrix's norm is
 // Byte of the high half of pair k in a row; its low half is 64 further.
 __device__ __forceinline__ int64_t pair_at(int64_t k) { return (k >> 5) * kLine + (k & 31) * 2; }
 __device__ __forceinline__ float4_t multiply(half8 p, half8 q, float4_t sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, sum, 0, 0, 0); }
+// v as a sum of two.  The compiler may make `high` twice, once for its store and once for `low`, and where v is a product round it to 32 bits first in
+// only one of the two: next to a tie they differ by a step of 11 bits (one entry in some thousand).  After the empty statement v is a number in
+// 32 bits, whose halves come out the same however often they are made.
 __device__ __forceinline__ void split(float v, half_t& high, half_t& low) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm("" : "+v"(v));
+#endif
     high = (half_t)v;
     low = (half_t)fmaf((float)high, -1.0f, v);             // (one instruction with the conversion)
 }

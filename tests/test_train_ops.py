@@ -540,6 +540,25 @@ def test_update_large(T, rows, cols):
     assert float(off) <= float(bound)
 
 
+@pytest.mark.parametrize("count,rows,cols", [(64, 16, 16), (64, 60, 100), (64, 100, 100), (64, 128, 90), (32, 200, 200), (8, 300, 500), (2, 1100, 900)])
+def test_update_operands_have_22_bits(T, count, rows, cols):
+    """Entry by entry: X alone (the coefficients 1, 0, 0), and of diagonal matrices, whose sums have one term each, its powers by way of A and B."""
+    g = draw(rows, count, rows, cols).float()
+    x = g.double() / torch.linalg.vector_norm(g.double(), dim=(-2, -1), keepdim=True)
+    got = T.p2_orthogonalize(g, steps=1, coefficients=(1.0, 0.0, 0.0), eps=0.0).double()
+    # a pair is off by half a step of its lower half at most (2^-23; below fp16's normal numbers 2^-25 of 2^-15); the factor, its product, the gain's and the
+    # result are rounded to 24 bits
+    assert ((got - x).abs() <= 3 * 2.0 ** -23 * x.abs() + 2.0 ** -39).all(), float(((got - x) / x).abs().max())
+    n = min(rows, cols)
+    g = torch.zeros(count, rows, cols, device="cuda")
+    g[:, range(n), range(n)] = 0.5 + torch.rand(count, n, generator=torch.Generator().manual_seed(rows)).cuda()
+    x = g.double() / torch.linalg.vector_norm(g.double(), dim=(-2, -1), keepdim=True)
+    for power, coefficients in ((3, (0.0, 1.0, 0.0)), (5, (0.0, 0.0, 1.0))):
+        got = T.p2_orthogonalize(g, steps=1, coefficients=coefficients, eps=0.0).double()
+        # X's pairs and factor in every place, A twice, A A or B, the products' lowest terms (2^-22 each) and the same roundings at the end
+        assert ((got - x ** power).abs() <= 20 * 2.0 ** -22 * x.abs() ** power + 2.0 ** -39 * x.abs()).all(), (power, float((got / x ** power - 1).abs().nan_to_num().max()))
+
+
 def like_a_gradient(form, rows, cols):
     if form == "equal":
         return torch.full((rows, cols), 0.37, dtype=torch.float64, device="cuda")
