@@ -3,7 +3,7 @@
 // Numbers.  Small singular values of X grow by a = 3.4445 a step, 485 times over five steps, and what a step rounds off grows
 // with them: with 16-bit operands the result of a gradient of low rank is off by 4 % (fp16) or 29 % (bf16).  So a
 // matrix is kept as pairs of fp16 numbers, value = (high + low) / 2^scale, 22 bits together, in every step, and a product takes three MFMA:
-// high*high + high*low + low*high, summed in fp32 (low*low is below what fp32 holds).  The scales come from the bound that the
+// high*high + high*low + low*high, summed in fp32 (low*low is below what sums of more than 64 terms round off).  The scales come from the bound that the
 // polynomial sets on the singular values, so that no entry passes fp16's largest number (no entry is larger than the
 // largest singular value).
 //
@@ -471,6 +471,10 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
     constexpr int FM = kBlocks < 3 ? 1 : 2, FN = kBlocks < 3 ? 2 : kBlocks;
     constexpr int kAcross = M / (16 * FN), kAll = M / (16 * FM) * kAcross, kSplit = kBlocks == 1 ? kWaves / kAll : 1;
     constexpr int AP = small_pitch(M), kAMask = small_mask(AP);
+    // Low times low is 2^-22 of a term at most, 2^-24 as a rule.  Of few rows the sums have so few roundings of their own that it counts: off by (mean of
+    // forty normal matrices; without it / with it / products in 32 bits) 5 x 7 1.04 / 0.78 / 0.69e-6, 33 x 90 1.63 / 1.31 / 1.24e-6, 64 x 200 1.59 / 1.30 /
+    // 1.43e-6, but 96 x 120 1.00 / 0.94 / 1.36e-6, where it would take 13 % of the time of 128 x 128 (of 64 x 64 5 %).
+    constexpr bool kLowest = kBlocks <= 2;
     extern __shared__ __attribute__((aligned(16))) char small_lds[];
     const int XP = a.n, x_mask = small_mask(a.n);
     half_t* xh = reinterpret_cast<half_t*>(small_lds + kSmallSpare);
@@ -549,7 +553,10 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
 #pragma unroll
                     for (int x = 0; x < FM; ++x)
 #pragma unroll
-                        for (int y = 0; y < FN; ++y) acc[x][y] = multiply(p1[x], q0[y], acc[x][y]);
+                        for (int y = 0; y < FN; ++y) {
+                            if constexpr (kLowest) acc[x][y] = multiply(p1[x], q1[y], acc[x][y]);
+                            acc[x][y] = multiply(p1[x], q0[y], acc[x][y]);
+                        }
 #pragma unroll
                     for (int x = 0; x < FM; ++x)
 #pragma unroll
@@ -614,6 +621,7 @@ template <typename T, int kBlocks> __global__ __launch_bounds__(kSmallBlock) voi
                 for (int k = 0; k < kBlocks; ++k) {
                     const int at = small_at(i * 16 + row, k * 32 + quad * 8, AP, kAMask);
                     const half8 p0 = *reinterpret_cast<const half8*>(ah + at), p1 = *reinterpret_cast<const half8*>(al + at);
+                    if constexpr (kLowest) c[i] = multiply(q1[k], p1, c[i]);
                     c[i] = multiply(q0[k], p1, c[i]);
                     c[i] = multiply(q1[k], p0, c[i]);
                     c[i] = multiply(q0[k], p0, c[i]);

@@ -540,6 +540,22 @@ def test_update_large(T, rows, cols):
     assert float(off) <= float(bound)
 
 
+@pytest.mark.parametrize("rows,cols", [(5, 7), (16, 16), (16, 60), (80, 20), (24, 24), (32, 128), (33, 90), (64, 200), (100, 100), (130, 200), (700, 300)])
+def test_update_is_as_exact_as_products_in_32_bits(T, rows, cols):
+    """On the average of forty matrices, a tenth for what these differ by."""
+    a, b, c = NS
+    g = draw(rows * cols, 40, rows, cols).float()
+    want, sizes = newton_schulz(g)
+    x = g if rows <= cols else g.transpose(1, 2).contiguous()
+    x = (x.double() / (torch.linalg.vector_norm(x.double(), dim=(-2, -1), keepdim=True) + 1e-7)).float()
+    for _ in range(5):
+        m = x @ x.transpose(1, 2).contiguous()
+        x = a * x + (b * m + c * (m @ m)) @ x
+    plain = x if rows <= cols else x.transpose(1, 2)
+    off = [float((torch.linalg.vector_norm(v.double() - want, dim=(-2, -1)) / sizes[-1]).mean()) for v in (T.p2_orthogonalize(g), plain)]
+    assert off[0] <= 1.1 * off[1], off
+
+
 @pytest.mark.parametrize("count,rows,cols", [(64, 16, 16), (64, 60, 100), (64, 100, 100), (64, 128, 90), (32, 200, 200), (8, 300, 500), (2, 1100, 900)])
 def test_update_operands_have_22_bits(T, count, rows, cols):
     """Entry by entry: X alone (the coefficients 1, 0, 0), and of diagonal matrices, whose sums have one term each, its powers by way of A and B."""
