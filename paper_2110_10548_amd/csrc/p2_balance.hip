@@ -21,7 +21,12 @@ constexpr int kBalanceBlock = 512;
 constexpr int64_t kBalanceBlocks = 512;                // two blocks a compute unit
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// e^(v - m), v and m finite or not; 1 ulp of 2^x and what the product rounds.
+// Exponentials and inverses of sums are the instructions for 2^x and 1 / x, which are off by a step of 32 bits at most; a library's exponential and a
+// division, by half a step each, would take several times their instructions in kernels that vector instructions bound (and half a step of a sum is
+// what adding it up rounds off anyway).  Gates are off by 6.8e-8 to 7.2e-8 of their value (root mean square; logits of a spread of 1.5, 8 to 256 experts),
+// with these 5.0e-8 to 5.4e-8; probability sums of 20000 tokens by 2.2e-7 at most, with these 3.6e-7 (torch's order of sums).
+
+// e^(v - m), v and m finite or not.
 __device__ __forceinline__ float exp_of(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
 
 // Keys: whole numbers in the order of the logits, and of equal ones in the order of falling indexes; never 0.  A float's bits, turned
@@ -517,8 +522,11 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBala
     }
 }
 
-// Lanes of a token and a lane's logits: 8, and from 129 experts on 16.  (Measured while choices were made without lists: 131072 16-bit tokens
-// over 256 experts 45 us with 16 and 57 with 8, 65536 fp32 tokens over 512 103 with either; 32 do not stay in registers with their sums.)
+// Lanes of a token and a lane's logits: 8, and from 129 experts on 16, in both passes (us of the forward pass / of the gradient, with 8 against 16 logits
+// a lane): 131072 tokens over 64 experts, bf16 and two choices 16 / 11 against 16 / 14, eight 21 / 12 against 27 / 17, fp32 35 / 14 against 50 / 18;
+// over 128, eight choices, bf16 28 / 18 against 28 / 19, fp32 48 / 26 against 64 / 28; over 160 bf16 50 / 32 against 38 / 29; over 256 bf16 49 / 32
+// against 37 / 29, fp32 81 / 46 against 81 / 46 (two choices 46 / 46 against 56 / 45: the one kind that 8 would suit better); 65536 over 512 bf16
+// 53 / 33 against 38 / 30, fp32 88 / 46 against 75 / 46.
 struct RowShape { int lanes, items; };
 RowShape row_shape(int32_t experts) {
     RowShape r = {1, experts <= 128 ? 8 : 16};
