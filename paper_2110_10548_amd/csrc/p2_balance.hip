@@ -5,9 +5,9 @@
 // vectors); a wavefront takes 64 / kLanes tokens at a time.  Choosing goes by keys in which a larger logit, and of equal ones
 // the lower index, is the larger whole number: it is exact and does not depend on how the softmax is rounded.
 //
-// What bounds it: the gradient, memory (131072 bf16 tokens over 256 experts 29.4 us, 4.8 TB/s; a copy of 4 GiB reaches 4.84).  The choice,
-// vector instructions: 395 of them and 16 exponentials for four tokens, 24 of 33 us at eight choices of 256 (75 MB: 2.1 TB/s), 6 more for the sums
-// over blocks; a call 35.6.  One token: 4.8 us on the device in a call of 9.2.
+// What bounds it: the gradient, memory (131072 bf16 tokens over 256 experts 29.9 us, 4.8 TB/s; a copy of 4 GiB reaches 4.84).  The choice,
+// vector instructions: 395 of them and 16 exponentials for four tokens, 24 of 31.5 us at eight choices of 256 (75 MB: 2.4 TB/s), 6.4 more for the sums
+// over blocks (both under the profiler); a call 35.8.  One token: 4.9 us on the device in a call of 9.1.
 #include <algorithm>
 #include <type_traits>
 

@@ -13,10 +13,11 @@
 // tiles on and below the diagonal are computed, and written to both sides.  X is kept in both orders (m x n for X X^T, n x m
 // for B X).  Sizes are padded to multiples of 64 with zeros, which stay zeros through all steps.
 //
-// What bounds it.  4096 x 4096: the matrix units; three products of 16 bits each take 3.2 ms, 1.24 to 1.30 P operations a second in the large
-// products, where a plain product of that size by the installed library reaches 1.21.  Around 1000 rows: the operands' way from L2 to LDS
-// (2777 x 1000 fp32 300 us; X X^T brings 267 MB there in 19.4 us, B X 369 in 28.5), or latency where larger tiles need less of it.  Stacks of 256 x 256: launches and the first loads of
-// each (17 in 148 us; deeper prefetch changes nothing).  Up to 128 rows: one launch, one block's chain of steps (64 x 64 17 us).
+// What it reaches, and what bounds it as far as counters show.  4096 x 4096 3.48 ms: the large products do 1.21 to 1.27 P operations a second (the last one, which writes one
+// order alone, 1.38), all three terms of the tiles computed, where the installed library's plain 16-bit product of that size does 1.24 to 1.27; the matrix units are busy
+// for half of the time at 2.4 GHz.  Around 1000 rows (2777 x 1000 fp32 313 us) neither they (13 to 27 %) nor one wait alone: wavefronts wait 26 to 41 % of their
+// time, and for an instruction 16 to 48 %; L2 is read at 12.0 TB/s by X X^T (255 MB in 21.2 us) and 13.3 by B X (392 in 29.5).  Stacks of 256 x 256: launches and the first
+// loads of each (17 in 155 us; deeper prefetch changes nothing).  Up to 128 rows: one launch, one block's chain of steps (64 x 64 18 us).
 #include <algorithm>
 #include <cmath>
 

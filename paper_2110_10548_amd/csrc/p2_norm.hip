@@ -5,9 +5,10 @@
 // Rows are dealt to groups of kTpr threads (a part of a wavefront, a wavefront, or a block), each thread holding kNv vectors
 // of 16 bytes.
 //
-// What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 26.1 us, 5.1 TB/s (part of it from the last
-// cache; 24.3 without what the first mean rounds off, which a row of 5000 fp32 values of 12345.678 pays for with results of 0.5 for 0); backward with both sums, 16384 x 4096 bf16: 81.1 us, 5.0 TB/s, of which k_norm_weight_grad takes 5.1.  Rows with odd ends: 5003 x 1023
-// fp16 of rows 1061 apart 8 us, 2.6 TB/s.  One row: 2.4 us on the device in a call of 6.8.
+// What bounds it: memory.  A copy of 4 GiB reaches 4.84 TB/s here; forward, 8192 x 4096 bf16: 25.9 us, 5.2 TB/s (part of it from the last
+// cache; 24 without what the first mean rounds off, which a row of 5000 fp32 values of 12345.678 pays for with results of 0.5 for 0); backward with both sums,
+// 16384 x 4096 bf16: 80.9 us, 5.0 TB/s, of which k_norm_weight_grad takes 4.9.  Rows with odd ends: 5003 x 1023 fp16 of rows 1061 apart 8 us, 2.6 TB/s.  One
+// row: 2.4 us on the device in a call of 6.7.
 #include <algorithm>
 
 #include "p2_train_dev.h"
