@@ -8,7 +8,13 @@
  *  - the balance of a router over experts: counts and probability sums per expert are sums over the device's
  *    tokens; the loss of the whole batch and its gradient need them reduced in between, hence three calls;
  *  - orthogonalised updates: a reduced weight gradient goes through Newton-Schulz products, which need the whole
- *    matrix on the device.
+ *    matrix on the device;
+ *  - routing to experts by scores, biases and groups: counts per expert are sums over the device's tokens, and the biases
+ *    that balance the experts follow from the counts of the whole batch;
+ *  - AdamW over many tensors: the sum of the gradients' squares is a sum over the devices' shares, and the step is what is done with a
+ *    reduced gradient, or with a device's part of it, whose new weights' copy is then gathered;
+ *  - matrix products with bias, activation and residual: a weight's gradient is a sum over the device's rows, and a
+ *    device's part of the inner dimension gives a part of the sum over the tensor axis.
  *
  * Conventions (those of p2.h, except where this says otherwise)
  *  - Every function returns an int32 status: P2_OK or a negative error; p2_last_error() returns the text.
@@ -105,6 +111,113 @@ int32_t p2_orthogonalize(const void* g, int32_t type, int64_t stride, int64_t ma
                          int64_t cols, int32_t steps, const double* coefficients, double eps, double scale, void* out,
                          int32_t out_type, int64_t out_stride, int64_t out_matrix_stride, void* workspace,
                          int64_t workspace_bytes, void* stream);
+
+#define P2_SOFTMAX 0
+#define P2_SIGMOID 1
+#define P2_MAX_GROUPS 64      /* groups that a router's experts are in */
+
+int32_t p2_route_forward_workspace(int64_t tokens, int32_t experts, int32_t k, int32_t groups, int64_t* bytes);
+
+/* Routes each token to k experts by scores: s = softmax of its logits, or their sigmoids; v = s + bias (NULL: 0), compared in 64 bits, is
+ * what is chosen by, and s what the gates are made of.  An expert whose logit or bias is -inf is not on offer; NaN counts as larger
+ * than every number.  (A softmax over a logit of NaN or +inf is NaN throughout.)
+ *   The experts are in `groups` groups of equal size, one after the other.  A group's value is the sum of its group_best (1 or 2) largest
+ *   v (of as many as are on offer), and the choice is made within the group_limit groups of the largest values.
+ *   expert[t][i] = the i-th best of those; gate[t][i] = scale * s, or with `renormalise` scale * s / (sum of the chosen experts' s), which
+ *   keeps its digits where all of them are tiny.  Ties, of groups and of experts: the lowest index.  Where a token has fewer than k
+ *   experts on offer the rest is -1 and 0.
+ *   counts[e] = how often expert e was chosen; kept[0] = tokens that count: those with a logit above -inf (or NaN) whose keep[t] is not 0 (keep may
+ *   be NULL).  The others choose nothing, and their logits are not looked at.
+ * 1 <= k <= min(experts, P2_MAX_CHOSEN), experts a multiple of groups, 1 <= group_limit <= groups. */
+int32_t p2_route_forward(const void* logits, int32_t type, int64_t stride, const uint8_t* keep, const float* bias, int64_t tokens,
+                         int32_t experts, int32_t k, int32_t score, int32_t groups, int32_t group_limit, int32_t group_best,
+                         int32_t renormalise, double scale, int32_t* expert, float* gate, int64_t* counts, int64_t* kept,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradient of  sum dgate * gate  with respect to the logits (the choice itself has none); score, renormalise and scale are those of
+ * the forward call.  Choices of -1 count for nothing, and a token of these alone gets zeros.  Where a token names an expert twice both count.
+ * dlogits has the logits' type and may be the logits themselves (same stride). */
+int32_t p2_route_backward(const void* logits, int32_t type, int64_t stride, int64_t tokens, int32_t experts, int32_t k, int32_t score,
+                          int32_t renormalise, double scale, const int32_t* expert, const float* dgate, void* dlogits,
+                          int64_t dlogits_stride, void* stream);
+
+/* out[e] = bias[e] + rate * sign(mean(counts) - counts[e]): an expert that was chosen less often than the mean is liked better next
+ * time.  counts are those of the whole batch.  out may be bias. */
+int32_t p2_route_bias(const float* bias, const int64_t* counts, int32_t experts, double rate, float* out, void* stream);
+
+int32_t p2_square_sum_workspace(int64_t n, int64_t* bytes);
+
+/* out[0] = sum of the squares of all values of n tensors of one type, in 64 bits.  `tensors` and `counts` (values of each) are HOST arrays, which are
+ * read before the call returns. */
+int32_t p2_square_sum(const void* const* tensors, const int64_t* counts, int64_t n, int32_t type, double* out, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+#define P2_STATE_BLOCK 256    /* values that share a scale of an 8-bit state */
+
+/* One tensor of an AdamW step, `count` values one after the other.  copy: NULL, or where the new weights go in copy_type, too.
+ * 32 bits: mean and square are float[count].  8 bits: int8_t[count] and uint8_t[count], with a scale for each P2_STATE_BLOCK values
+ * (the last block may be shorter).  A block's scale is its largest absolute value; with q the stored number
+ *   mean = scale * (q / 127) * |q / 127|,   square = scale * (q / 255)^4,
+ * the nearest q is stored (of a square other than 0 at least 1), and a block that holds nothing of 2^-100 or more is held as zeros.  A block that
+ * holds an infinity or a NaN becomes NaN throughout. */
+typedef struct p2_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* copy;
+    void* mean;
+    void* square;
+    float* mean_scale;
+    float* square_scale;
+    int64_t count;
+} p2_adamw_tensor;
+
+int32_t p2_adamw_workspace(int64_t* bytes);
+
+/* One step over n tensors (a HOST array, read before the call returns), t = step[0] + 1 being its number:
+ *   g = grad * grad_factor * min(1, max_norm / (grad_factor * sqrt(square_sum[0])))
+ *   mean = beta1 mean + (1 - beta1) g,  square = beta2 square + (1 - beta2) g^2
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * mean / (sqrt(square / (1 - beta2^t)) + eps)
+ * with lr = lr * rate[0] (a float on the device; NULL: 1), so that a captured step may follow a schedule.  The new weights are worked out from
+ * mean and square before these are rounded to 8 bits; without a 32-bit copy of its own a 16-bit param is rounded to nearest each step.
+ * square_sum (device; NULL: no clipping, every step is made) is what p2_square_sum gave, of all devices' gradients where they share a norm.  Where it
+ * is not finite the step is left out: nothing is changed, step[0] neither.  Else step[0] (device) becomes t.  max_norm may be infinity: only
+ * this check.  state_bits: 32 or 8; 8 takes eps >= 1e-12 (smaller squares would be held as 0).  No two tensors may overlap. */
+int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_t grad_type, int32_t copy_type, int32_t state_bits,
+                 int64_t* step, const float* rate, double lr, double beta1, double beta2, double eps, double weight_decay,
+                 double grad_factor, const double* square_sum, double max_norm, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The values that 8-bit states stand for: of each tensor mean, mean_scale, square, square_scale and count are read (8 bits), and
+ * mean_out[i], square_out[i] (HOST arrays of device pointers to float[count]; an entry may be NULL) written. */
+int32_t p2_adamw_values(const p2_adamw_tensor* tensors, int64_t n, float* const* mean_out, float* const* square_out, void* stream);
+
+#define P2_NO_ACTIVATION 0
+#define P2_RELU 1
+#define P2_GELU 2             /* z (1 + erf(z / sqrt 2)) / 2                                    */
+#define P2_GELU_TANH 3        /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2              */
+#define P2_SILU 4             /* z / (1 + e^-z)                                                 */
+
+/* Takes the arguments of the call that it is for (pointers are looked at for their alignment alone). */
+int32_t p2_linear_forward_workspace(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t type,
+                                    int64_t rows, int64_t inner, int64_t outer, int64_t* bytes);
+
+/* y = activation(z) + residual with z = x weight^T + bias:  x [rows][inner], weight [outer][inner], y, z and residual [rows][outer], bias
+ * [outer], all of one type.  bias, residual and z (not kept) may be NULL.  y may be residual (same stride).  Products are summed, and
+ * everything up to y worked out, in 32 bits: y goes by the z that has not been rounded yet. */
+int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, const void* bias,
+                          const void* residual, int64_t residual_stride, int32_t type, int32_t activation, int64_t rows,
+                          int64_t inner, int64_t outer, void* y, int64_t y_stride, void* z, int64_t z_stride, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+
+int32_t p2_linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer, int64_t* bytes);
+
+/* With dz = dy * activation'(z):  dx = dz weight, dweight = dz^T x, dbias = sum over rows of dz; dx, dweight and dbias may each be NULL: not asked
+ * for.  z is what the forward pass kept (NULL without an activation); at 0 the slope of P2_RELU is 0.  The residual's gradient is dy.  dweight and
+ * dbias have `weight_type`, all else `type`.  dz is rounded to `type` for the products (dbias adds up what has not been rounded).
+ * rows = 0 writes zeros to dweight and dbias.  */
+int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int64_t z_stride, const void* x, int64_t x_stride,
+                           const void* weight, int64_t weight_stride, int32_t type, int32_t activation, int64_t rows, int64_t inner,
+                           int64_t outer, void* dx, int64_t dx_stride, void* dweight, int64_t dweight_stride, void* dbias,
+                           int32_t weight_type, void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

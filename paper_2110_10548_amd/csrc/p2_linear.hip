@@ -1,0 +1,540 @@
+// Matrix products of a layer: y = activation(x W^T + bias) + residual, and its gradients dx = dz W, dW = dz^T x, dbias = sum dz with
+// dz = dy * activation'(z).
+//
+// Every product is rows times rows, C[j][i] = sum_k A[i][k] B[j][k], with the summed index contiguous in both: the forward pass takes weight
+// and x as they are, and for the gradients weight, x and dz are written turned first.  A tile of C comes from stages of 128 bytes of
+// each row (64 values of 16 bits, 32 of 32) that are brought to LDS straight from memory while the stage before is multiplied.  The MFMA's rows
+// are A's: a lane has four neighbouring columns of one row of C.
+#include <algorithm>
+
+#include "p2_train_dev.h"
+
+namespace p2 {
+
+namespace {
+
+typedef half_t half8 __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kLine = 128;                     // bytes of a row in a stage
+constexpr int64_t kUnits = 256;                // compute units
+constexpr float kLog2e = 1.44269504088896340736f;
+
+int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
+
+// ---------------------------------------------------------------------------------------------- activations
+
+__device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
+
+// (z (1 + tanh u) / 2 = z sigmoid(2 u))
+__device__ __forceinline__ float activate(float z, int32_t activation) {
+    switch (activation) {
+        case P2_RELU: return z < 0.0f ? 0.0f : z;
+        case P2_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
+        case P2_GELU_TANH: return z * sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+        case P2_SILU: return z * sigmoid_of(z);
+        default: return z;
+    }
+}
+__device__ __forceinline__ float slope_of(float z, int32_t activation) {
+    switch (activation) {
+        case P2_RELU: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+        case P2_GELU: return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
+        case P2_GELU_TANH: {
+            const float p = sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+            return p + p * (1.0f - p) * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
+        }
+        case P2_SILU: {
+            const float p = sigmoid_of(z);
+            return p * (1.0f + z * (1.0f - p));
+        }
+        default: return 1.0f;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ results
+
+// What becomes of a sum: C's row j, column i.
+struct Result {
+    const void* bias; const void* residual; void* y; void* z;
+    int64_t residual_stride, y_stride, z_stride;
+    int32_t y_type, activation;        // (bias, residual and z have the operands' type)
+};
+template <typename T> __device__ __forceinline__ void finish(const Result& r, int64_t j, int64_t i, int64_t n, float (&v)[4]) {
+    if (r.bias) {
+        float b[4];
+        load_part<T, 4>(static_cast<const T*>(r.bias) + i, n, b, 0.0f);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += b[q];
+    }
+    if (r.z) store_part<T, 4>(static_cast<T*>(r.z) + j * r.z_stride + i, n, v);
+    if (r.activation != P2_NO_ACTIVATION)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = activate(v[q], r.activation);
+    if (r.residual) {
+        float b[4];
+        load_part<T, 4>(static_cast<const T*>(r.residual) + j * r.residual_stride + i, n, b, 0.0f);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += b[q];
+    }
+    if (r.y_type == P2_F32) store_part<float, 4>(static_cast<float*>(r.y) + j * r.y_stride + i, n, v);
+    else if (r.y_type == P2_BF16) store_part<bf16_t, 4>(static_cast<bf16_t*>(r.y) + j * r.y_stride + i, n, v);
+    else store_part<half_t, 4>(static_cast<half_t*>(r.y) + j * r.y_stride + i, n, v);
+}
+
+// ------------------------------------------------------------------------------------------------ products
+
+struct Product {
+    const char* a; const char* b;      // rows, 16-byte aligned
+    int64_t a_pitch, b_pitch;          // bytes from row to row, multiples of 16
+    int64_t a_rows, b_rows, length;    // length: bytes of a row, a multiple of 16
+    float* sums;                       // more than one part: [parts][b_rows][a_rows]
+    int32_t across, down, parts;       // tiles of A's and of B's rows, parts of the length
+    Result r;
+};
+
+// 16 bytes of a row a lane: products of what 16 lanes x 4 have.
+__device__ __forceinline__ void multiply(const half8& p, const half8& q, float4_t& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, c, 0, 0, 0); }
+__device__ __forceinline__ void multiply(const bf16x8& p, const bf16x8& q, float4_t& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0); }
+__device__ __forceinline__ void multiply(const float4_t& p, const float4_t& q, float4_t& c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], q[i], c, 0, 0, 0);
+}
+template <typename T> struct Fragment;
+template <> struct Fragment<half_t> { typedef half8 type; };
+template <> struct Fragment<bf16_t> { typedef bf16x8 type; };
+template <> struct Fragment<float> { typedef float4_t type; };
+
+// Rows of an operand and 16 bytes a lane of them to LDS (`to`: the wavefront's, lanes one after the other); what lies past `bytes` comes as
+// zeros.  Only the device's compiler knows the descriptor's type.
+struct Rows {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __amdgpu_buffer_rsrc_t at;
+    __device__ __forceinline__ Rows(const char* p, int bytes) : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, bytes, 0x00027000)) {}
+    __device__ __forceinline__ void bring(char* to, int lane_offset, int offset) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(at, (__attribute__((address_space(3))) void*)to, 16, lane_offset, offset, 0, 0);
+    }
+#else
+    __device__ Rows(const char*, int) {}
+    __device__ void bring(char*, int, int) const {}
+#endif
+};
+
+// Waits until at most kLoads of this wavefront's loads are under way (and all its LDS reads are done), then for the others.
+template <int kLoads> __device__ __forceinline__ void stage_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((kLoads & 15) | (kLoads >> 4) << 14 | 0x70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+constexpr int kPastEnd = 0x7ffffff0;           // an offset that no descriptor reaches
+
+template <typename T, int kTileA, int kTileB, int kWavesA, int kWavesB, int kStages>
+__global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_product(Product a) {
+    typedef typename Fragment<T>::type F;
+    constexpr int kWaves = kWavesA * kWavesB;
+    constexpr int FA = kTileA / kWavesA / 16, FB = kTileB / kWavesB / 16;
+    constexpr int kLoadsA = kTileA / 8 / kWaves, kLoadsB = kTileB / 8 / kWaves;        // of a stage; one brings 8 rows
+    constexpr int kAhead = kStages - 1;
+    static_assert(kLoadsA * 8 * kWaves == kTileA && kLoadsB * 8 * kWaves == kTileB, "rows are dealt out evenly");
+    static_assert((kLoadsA + kLoadsB) * (kAhead - 1) < 64, "the loads' counter");
+    __shared__ __attribute__((aligned(1024))) char lds[kStages][(kTileA + kTileB) * kLine];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours.
+    int t;
+    {
+        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = blockIdx.x & 7;
+        t = die * whole + min(die, rest) + (blockIdx.x >> 3);
+    }
+    const int tiles = a.across * a.down, part = t / tiles;
+    t %= tiles;
+    int ti, tj;                                            // column by column of four rows of tiles
+    {
+        const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
+        tj = first + in % high;
+        ti = in / high;
+    }
+    const auto rows_of = [&](const char* p, int64_t pitch, int64_t first, int64_t rows, int tile) {
+        const int64_t n = min(rows - first, (int64_t)tile);
+        return Rows(p + first * pitch, (int)((n - 1) * pitch + a.length));
+    };
+    const Rows ra = rows_of(a.a, a.a_pitch, (int64_t)ti * kTileA, a.a_rows, kTileA);
+    const Rows rb = rows_of(a.b, a.b_pitch, (int64_t)tj * kTileB, a.b_rows, kTileB);
+    // A row's 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int from_a = (wave * kLoadsA * 8 + (lane >> 3)) * (int)a.a_pitch + piece, from_b = (wave * kLoadsB * 8 + (lane >> 3)) * (int)a.b_pitch + piece;
+    const int all = (int)((a.length + kLine - 1) / kLine);
+    const int begin = (int)((int64_t)all * part / a.parts), stages = (int)((int64_t)all * (part + 1) / a.parts) - begin;
+    const auto bring = [&](int stage, int s) {
+        const int at = (begin + s) * kLine;
+        const bool inside = at + piece < a.length;         // (zeros past the row's end)
+#pragma unroll
+        for (int l = 0; l < kLoadsA; ++l)
+            ra.bring(&lds[stage][(wave * kLoadsA + l) * 1024], inside ? from_a + l * 8 * (int)a.a_pitch : kPastEnd, at);
+#pragma unroll
+        for (int l = 0; l < kLoadsB; ++l)
+            rb.bring(&lds[stage][kTileA * kLine + (wave * kLoadsB + l) * 1024], inside ? from_b + l * 8 * (int)a.b_pitch : kPastEnd, at);
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+        if (s < stages) bring(s, s);
+    float4_t acc[FA][FB];
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) acc[i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
+    int stage = 0, next = kAhead % kStages;
+    for (int s = 0; s < stages; ++s) {
+        if (s + kAhead <= stages) stage_barrier<(kLoadsA + kLoadsB) * (kAhead - 1)>();
+        else stage_barrier<0>();
+        if (s + kAhead < stages) bring(next, s + kAhead);
+        const char* pa = lds[stage] + wa * FA * 16 * kLine;
+        const char* pb = lds[stage] + kTileA * kLine + wb * FB * 16 * kLine;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int at = row * kLine + ((half * 4 + quad) ^ (row & 7)) * 16;
+            F fa[FA], fb[FB];
+#pragma unroll
+            for (int j = 0; j < FB; ++j) fb[j] = *reinterpret_cast<const F*>(pb + j * 16 * kLine + at);
+#pragma unroll
+            for (int i = 0; i < FA; ++i) fa[i] = *reinterpret_cast<const F*>(pa + i * 16 * kLine + at);
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int j = 0; j < FB; ++j) multiply(fa[i], fb[j], acc[i][j]);
+        }
+        next = stage;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    const int64_t i0 = (int64_t)ti * kTileA + wa * FA * 16 + quad * 4, j0 = (int64_t)tj * kTileB + wb * FB * 16 + row;
+#pragma unroll
+    for (int fj = 0; fj < FB; ++fj) {
+        const int64_t j = j0 + fj * 16;
+        if (j >= a.b_rows) continue;
+#pragma unroll
+        for (int fi = 0; fi < FA; ++fi) {
+            const int64_t i = i0 + fi * 16;
+            if (i >= a.a_rows) continue;
+            float v[4] = {acc[fi][fj][0], acc[fi][fj][1], acc[fi][fj][2], acc[fi][fj][3]};
+            if (a.parts > 1) store_part<float, 4>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
+            else finish<T>(a.r, j, i, a.a_rows - i, v);
+        }
+    }
+}
+
+// Parts of sums added up, in their order.
+template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Product a) {
+    const int64_t quads = (a.a_rows + 3) / 4, items = quads * a.b_rows, plane = a.a_rows * a.b_rows;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < items; x += (int64_t)gridDim.x * 256) {
+        const int64_t j = x / quads, i = x % quads * 4, n = a.a_rows - i;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < a.parts; ++p) {
+            float w[4];
+            load_part<float, 4>(a.sums + p * plane + j * a.a_rows + i, n, w, 0.0f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += w[q];
+        }
+        finish<T>(a.r, j, i, n, v);
+    }
+}
+
+// A few rows of x against all of the weight's, which are read once: a wavefront takes kEach of them at a time.
+template <typename T, int kRows, int kEach> __global__ __launch_bounds__(256) void k_linear_rows(const T* x, int64_t x_stride, const T* weight, int64_t weight_stride, int64_t inner,
+                                                                                                 int64_t outer, Result r) {
+    constexpr int V = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    const int64_t i0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kEach;
+    if (i0 >= outer) return;
+    float sum[kRows][kEach] = {};
+    for (int64_t k = lane * V; k < inner; k += 64 * V) {
+        float p[kRows][V], q[kEach][V];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) load_part<T, V>(weight + min(i0 + e, outer - 1) * weight_stride + k, inner - k, q[e], 0.0f);
+#pragma unroll
+        for (int m = 0; m < kRows; ++m) load_part<T, V>(x + m * x_stride + k, inner - k, p[m], 0.0f);
+#pragma unroll
+        for (int m = 0; m < kRows; ++m)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e)
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[m][e] = fmaf(p[m][v], q[e][v], sum[m][e]);
+    }
+#pragma unroll
+    for (int m = 0; m < kRows; ++m) {
+        float v[4] = {};
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] = group_sum<64>(sum[m][e]);
+        if (lane == m) finish<T>(r, m, i0, min((int64_t)kEach, outer - i0), v);
+    }
+}
+
+// ------------------------------------------------------------------------------------- operands in order
+
+// A matrix as a product takes it: straight, turned, or both, with zeros from its end to whole stages.  With z the values are dy activation'(z), and
+// each tile's sums over its rows go to sums[tile][cols].
+struct Pack {
+    const void* from; const void* z; char* straight; char* turned; float* sums;
+    int64_t from_stride, z_stride, straight_pitch, turned_pitch;       // pitches in bytes
+    int64_t rows, cols;
+    int32_t activation;
+};
+template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Pack a) {
+    __shared__ float tile[64][65];
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + y + i * 16, c = c0 + x, n = r < a.rows ? a.cols - c : 0;
+        float v[4];
+        load_part<T, 4>(static_cast<const T*>(a.from) + r * a.from_stride + c, n, v, 0.0f);
+        if (a.z) {
+            float z[4];
+            load_part<T, 4>(static_cast<const T*>(a.z) + r * a.z_stride + c, n, z, 0.0f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = q < n ? v[q] * slope_of(z[q], a.activation) : 0.0f;
+        }
+        if (a.straight && r < a.rows) store_part<T, 4>(reinterpret_cast<T*>(a.straight + r * a.straight_pitch) + c, a.straight_pitch / (int)sizeof(T) - c, v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tile[y + i * 16][x + q] = v[q];
+    }
+    if (!a.turned && !a.sums) return;
+    __syncthreads();
+    if (a.turned) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t c = c0 + y + i * 16, r = r0 + x;
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = tile[x + q][y + i * 16];
+            if (c < a.cols) store_part<T, 4>(reinterpret_cast<T*>(a.turned + c * a.turned_pitch) + r, a.turned_pitch / (int)sizeof(T) - r, v);
+        }
+    }
+    if (a.sums && threadIdx.x < 64 && c0 + threadIdx.x < a.cols) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s += tile[i][threadIdx.x];
+        a.sums[(int64_t)blockIdx.y * a.cols + c0 + threadIdx.x] = s;
+    }
+}
+
+// Adds up the tiles' lines: 64 columns a block, 16 threads each.
+__global__ __launch_bounds__(1024) void k_linear_sums(const float* lines, int64_t n, int64_t cols, void* out, int32_t type) {
+    __shared__ float part[16][64];
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + x;
+    float s = 0.0f;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t l = y; l < n; l += 16) s += lines[l * cols + c];
+    part[y][x] = s;
+    __syncthreads();
+    if (y > 0 || c >= cols) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += part[i][x];
+    store_typed(out, type, c, s);
+}
+
+__global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, int64_t stride, int64_t rows, int64_t cols) {
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < rows * cols; x += (int64_t)gridDim.x * 256) store_typed(out, type, x / cols * stride + x % cols, 0.0f);
+}
+
+// ------------------------------------------------------------------------------------------------- plans
+
+struct Plan { int32_t tile, parts; };
+// How a product of these sizes is cut: large tiles where there are enough of them for the compute units, else smaller ones and parts of the sum.
+Plan plan_of(int64_t a_rows, int64_t b_rows, int64_t length) {
+    const auto tiles = [&](int64_t t) { return ceil_div(a_rows, t) * ceil_div(b_rows, t); };
+    if (tiles(256) >= 192) return {256, 1};
+    Plan p = {b_rows <= 64 || a_rows <= 64 ? 64 : 128, 1};
+    const int64_t n = tiles(p.tile), stages = ceil_div(length, kLine);
+    if (n < kUnits) p.parts = (int32_t)std::max<int64_t>(1, std::min({ceil_div(kUnits, n), stages / 4, (int64_t)32}));
+    return p;
+}
+int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) { return p.parts > 1 ? round_up(p.parts * a_rows * b_rows * 4, 256) : 0; }
+
+template <typename T> hipError_t multiply_rows(Product p, const Plan& plan, hipStream_t s) {
+    p.across = (int32_t)ceil_div(p.a_rows, plan.tile);
+    p.down = (int32_t)ceil_div(p.b_rows, plan.tile);
+    p.parts = plan.parts;
+    const dim3 grid((unsigned)((int64_t)p.across * p.down * p.parts));
+    if (plan.tile == 256) k_linear_product<T, 256, 256, 2, 4, 2><<<grid, dim3(512), 0, s>>>(p);
+    else if (plan.tile == 128) k_linear_product<T, 128, 128, 2, 2, 3><<<grid, dim3(256), 0, s>>>(p);
+    else k_linear_product<T, 64, 64, 2, 2, 4><<<grid, dim3(256), 0, s>>>(p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.parts == 1) return e;
+    const int64_t items = ceil_div(p.a_rows, 4) * p.b_rows;
+    k_linear_join<T><<<dim3((unsigned)std::min<int64_t>(ceil_div(items, 256), 4096)), dim3(256), 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t pack(const Pack& a, hipStream_t s) {
+    const int64_t cols = a.straight ? std::max<int64_t>(a.cols, a.straight_pitch / sizeof(T)) : a.cols, rows = a.turned ? std::max<int64_t>(a.rows, a.turned_pitch / sizeof(T)) : a.rows;
+    k_linear_pack<T><<<dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64)), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// Whether rows can be brought to LDS as they are.
+bool in_order(const void* p, int64_t stride, int32_t type, int64_t cols) {
+    const int64_t size = (int64_t)type_bytes(type);
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && cols * size % 16 == 0 && stride * size <= ((int64_t)1 << 22);
+}
+bool few_rows(int64_t rows) { return rows <= 4; }
+
+struct ForwardRoom { bool pack_x, pack_weight; Plan plan; int64_t length, x, weight, sums, bytes; };
+ForwardRoom forward_room(const LinearForward& a) {
+    ForwardRoom r = {};
+    if (few_rows(a.rows)) return r;
+    const int64_t size = (int64_t)type_bytes(a.type), padded = round_up(a.inner * size, kLine);
+    r.pack_x = !in_order(a.x, a.x_stride, a.type, a.inner);
+    r.pack_weight = !in_order(a.weight, a.weight_stride, a.type, a.inner);
+    r.length = r.pack_x && r.pack_weight ? padded : round_up(a.inner * size, 16);
+    r.plan = plan_of(a.outer, a.rows, r.length);
+    r.x = 0;
+    r.weight = r.x + (r.pack_x ? round_up(a.rows * padded, 256) : 0);
+    r.sums = r.weight + (r.pack_weight ? round_up(a.outer * padded, 256) : 0);
+    r.bytes = r.sums + sums_bytes(r.plan, a.outer, a.rows);
+    return r;
+}
+
+struct BackwardRoom { Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, bytes; };
+BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
+    const int64_t size = (int64_t)type_bytes(type);
+    BackwardRoom r = {};
+    r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
+    r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
+    r.dx = plan_of(inner, rows, r.along);
+    r.dweight = plan_of(inner, outer, r.deep);
+    r.dz = 0;
+    r.dz_turned = r.dz + round_up(rows * r.along, 256);
+    r.x_turned = r.dz_turned + round_up(outer * r.deep, 256);
+    r.weight_turned = r.x_turned + round_up(inner * r.deep, 256);
+    r.lines = r.weight_turned + round_up(inner * r.along, 256);
+    r.sums = r.lines + round_up(ceil_div(rows, 64) * outer * 4, 256);
+    r.bytes = r.sums + std::max(sums_bytes(r.dx, inner, rows), sums_bytes(r.dweight, inner, outer));
+    return r;
+}
+
+template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) {
+    Result r = {};
+    r.bias = a.bias; r.residual = a.residual; r.y = a.y; r.z = a.z;
+    r.residual_stride = a.residual_stride; r.y_stride = a.y_stride; r.z_stride = a.z_stride;
+    r.y_type = a.type; r.activation = a.activation;
+    if (few_rows(a.rows)) {
+        const T* x = static_cast<const T*>(a.x);
+        const T* w = static_cast<const T*>(a.weight);
+        const dim3 grid((unsigned)ceil_div(a.outer, 8)), block(256);
+        if (a.rows == 1) k_linear_rows<T, 1, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        else if (a.rows == 2) k_linear_rows<T, 2, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        else if (a.rows == 3) k_linear_rows<T, 3, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        else k_linear_rows<T, 4, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        return hipGetLastError();
+    }
+    const ForwardRoom room = forward_room(a);
+    const int64_t padded = round_up(a.inner * (int64_t)sizeof(T), kLine);
+    Product p = {};
+    p.a = static_cast<const char*>(a.weight);
+    p.a_pitch = a.weight_stride * (int64_t)sizeof(T);
+    p.b = static_cast<const char*>(a.x);
+    p.b_pitch = a.x_stride * (int64_t)sizeof(T);
+    Pack k = {};
+    k.straight_pitch = padded;
+    k.cols = a.inner;
+    if (room.pack_x) {
+        k.from = a.x; k.from_stride = a.x_stride; k.rows = a.rows; k.straight = a.workspace + room.x;
+        const hipError_t e = pack<T>(k, s);
+        if (e != hipSuccess) return e;
+        p.b = k.straight;
+        p.b_pitch = padded;
+    }
+    if (room.pack_weight) {
+        k.from = a.weight; k.from_stride = a.weight_stride; k.rows = a.outer; k.straight = a.workspace + room.weight;
+        const hipError_t e = pack<T>(k, s);
+        if (e != hipSuccess) return e;
+        p.a = k.straight;
+        p.a_pitch = padded;
+    }
+    p.a_rows = a.outer; p.b_rows = a.rows; p.length = room.length;
+    p.sums = reinterpret_cast<float*>(a.workspace + room.sums);
+    p.r = r;
+    return multiply_rows<T>(p, room.plan, s);
+}
+
+template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s) {
+    const BackwardRoom room = backward_room(a.type, a.rows, a.inner, a.outer);
+    const bool own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
+    hipError_t e = hipSuccess;
+    Pack k = {};
+    k.from = a.dy; k.from_stride = a.dy_stride;
+    if (a.activation != P2_NO_ACTIVATION) { k.z = a.z; k.z_stride = a.z_stride; }
+    k.rows = a.rows; k.cols = a.outer; k.activation = a.activation;
+    if (a.dx && own_dz) { k.straight = a.workspace + room.dz; k.straight_pitch = room.along; }
+    if (a.dweight) { k.turned = a.workspace + room.dz_turned; k.turned_pitch = room.deep; }
+    if (a.dbias) k.sums = reinterpret_cast<float*>(a.workspace + room.lines);
+    if (k.straight || k.turned || k.sums) e = pack<T>(k, s);
+    if (e != hipSuccess) return e;
+    if (a.dbias) {
+        k_linear_sums<<<dim3((unsigned)ceil_div(a.outer, 64)), dim3(1024), 0, s>>>(k.sums, ceil_div(a.rows, 64), a.outer, a.dbias, a.weight_type);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    Product p = {};
+    p.sums = reinterpret_cast<float*>(a.workspace + room.sums);
+    if (a.dx) {
+        Pack w = {};
+        w.from = a.weight; w.from_stride = a.weight_stride; w.rows = a.outer; w.cols = a.inner;
+        w.turned = a.workspace + room.weight_turned; w.turned_pitch = room.along;
+        e = pack<T>(w, s);
+        if (e != hipSuccess) return e;
+        p.a = w.turned; p.a_pitch = room.along; p.a_rows = a.inner;
+        p.b = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
+        p.b_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
+        p.b_rows = a.rows;
+        p.length = own_dz ? room.along : a.outer * (int64_t)sizeof(T);
+        p.r = {};
+        p.r.y = a.dx; p.r.y_stride = a.dx_stride; p.r.y_type = a.type;
+        e = multiply_rows<T>(p, room.dx, s);
+        if (e != hipSuccess) return e;
+    }
+    if (a.dweight) {
+        Pack x = {};
+        x.from = a.x; x.from_stride = a.x_stride; x.rows = a.rows; x.cols = a.inner;
+        x.turned = a.workspace + room.x_turned; x.turned_pitch = room.deep;
+        e = pack<T>(x, s);
+        if (e != hipSuccess) return e;
+        p.a = x.turned; p.a_pitch = room.deep; p.a_rows = a.inner;
+        p.b = a.workspace + room.dz_turned; p.b_pitch = room.deep; p.b_rows = a.outer;
+        p.length = room.deep;
+        p.r = {};
+        p.r.y = a.dweight; p.r.y_stride = a.dweight_stride; p.r.y_type = a.weight_type;
+        e = multiply_rows<T>(p, room.dweight, s);
+    }
+    return e;
+}
+
+}  // namespace
+
+int64_t linear_forward_workspace(const LinearForward& a) { return a.rows ? forward_room(a).bytes : 0; }
+int64_t linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer) { return rows ? backward_room(type, rows, inner, outer).bytes : 0; }
+
+hipError_t launch_linear_forward(const LinearForward& a, hipStream_t s) {
+    return a.type == P2_F32 ? forward<float>(a, s) : a.type == P2_BF16 ? forward<bf16_t>(a, s) : forward<half_t>(a, s);
+}
+
+hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t s) {
+    if (a.rows == 0) {
+        if (a.dweight) {
+            k_linear_zero<<<dim3((unsigned)std::min<int64_t>(ceil_div(a.outer * a.inner, 256), 65536)), dim3(256), 0, s>>>(a.dweight, a.weight_type, a.dweight_stride, a.outer, a.inner);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (!a.dbias) return hipSuccess;
+        k_linear_zero<<<dim3((unsigned)ceil_div(a.outer, 256)), dim3(256), 0, s>>>(a.dbias, a.weight_type, a.outer, 1, a.outer);
+        return hipGetLastError();
+    }
+    return a.type == P2_F32 ? backward<float>(a, s) : a.type == P2_BF16 ? backward<bf16_t>(a, s) : backward<half_t>(a, s);
+}
+
+}  // namespace p2

@@ -3,6 +3,8 @@
 #include <cmath>
 #include <exception>
 #include <limits>
+#include <utility>
+#include <vector>
 
 #include "p2_train_dev.h"
 
@@ -63,6 +65,48 @@ int32_t check_matrices(int64_t count, int64_t rows, int64_t cols) {
     if (rows > kMostSide || cols > kMostSide || count > kMostMatrices) return api_fail(P2_EUNSUPPORTED, "sides longer than 2^17, or more than 65535 matrices");
     if ((double)orthogonalize_workspace(1, rows, cols) * (double)std::max<int64_t>(count, 1) >= std::ldexp(1.0, 40))
         return api_fail(P2_EUNSUPPORTED, "a workspace of 2^40 bytes or more");
+    return P2_OK;
+}
+
+int32_t check_route(int64_t tokens, int32_t experts, int32_t k, int32_t groups) {
+    int32_t rc = check_balance(tokens, experts, k);
+    if (rc != P2_OK) return rc;
+    if (groups < 1 || experts % groups) return api_fail(P2_EINVAL, "experts must be a multiple of groups");
+    if (groups > P2_MAX_GROUPS) return api_fail(P2_EUNSUPPORTED, "more than 64 groups");
+    return P2_OK;
+}
+int64_t route_room(int64_t tokens, int32_t experts, int32_t k, int32_t groups) {
+    const int64_t lines = route_forward_blocks(tokens, experts, k, groups);
+    return lines == 1 ? 0 : round256(lines * (experts + 1) * 4);
+}
+
+// Tensors of a call over many: as many and as long as the kernels count.
+constexpr int64_t kMostTensors = (int64_t)1 << 20, kMostValues = (int64_t)1 << 40;
+template <typename F> int32_t check_tensors(int64_t n, F&& count) {
+    if (n < 0) return api_fail(P2_EINVAL, "n < 0");
+    if (n > kMostTensors) return api_fail(P2_EUNSUPPORTED, "more than 2^20 tensors");
+    int64_t all = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (count(i) < 0) return api_fail(P2_EINVAL, "a tensor's count < 0");
+        if (count(i) > kMostValues || (all += count(i)) > kMostValues) return api_fail(P2_EUNSUPPORTED, "more than 2^40 values");
+    }
+    return P2_OK;
+}
+
+// Whether some of these ranges, all of which are written, overlap.
+typedef std::pair<const char*, const char*> Range;
+bool overlap(std::vector<Range>& ranges) {
+    std::sort(ranges.begin(), ranges.end());
+    for (size_t i = 1; i < ranges.size(); ++i)
+        if (ranges[i].first < ranges[i - 1].second) return true;
+    return false;
+}
+
+constexpr int64_t kMostLinear = (int64_t)1 << 20;
+int32_t check_linear(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
+    if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
+    if (rows < 0 || inner < 1 || outer < 1) return api_fail(P2_EINVAL, "rows < 0, inner < 1 or outer < 1");
+    if (rows > kMostLinear || inner > kMostLinear || outer > kMostLinear) return api_fail(P2_EUNSUPPORTED, "rows, inner or outer more than 2^20");
     return P2_OK;
 }
 
@@ -254,6 +298,244 @@ int32_t p2_orthogonalize(const void* g, int32_t type, int64_t stride, int64_t ma
         if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
         return launched(launch_orthogonalize(a, (hipStream_t)stream), "orthogonalize");
+    });
+}
+
+int32_t p2_route_forward_workspace(int64_t tokens, int32_t experts, int32_t k, int32_t groups, int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_route(tokens, experts, k, groups);
+        if (rc != P2_OK) return rc;
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        *bytes = route_room(tokens, experts, k, groups);
+        return P2_OK;
+    });
+}
+
+int32_t p2_route_forward(const void* logits, int32_t type, int64_t stride, const uint8_t* keep, const float* bias, int64_t tokens, int32_t experts,
+                         int32_t k, int32_t score, int32_t groups, int32_t group_limit, int32_t group_best, int32_t renormalise, double scale,
+                         int32_t* expert, float* gate, int64_t* counts, int64_t* kept, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&]() -> int32_t {
+        if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
+        int32_t rc = check_route(tokens, experts, k, groups);
+        if (rc != P2_OK) return rc;
+        if (score != P2_SOFTMAX && score != P2_SIGMOID) return api_fail(P2_EINVAL, "unknown score");
+        if (group_limit < 1 || group_limit > groups) return api_fail(P2_EINVAL, "group_limit outside 1 to groups");
+        if (group_best != 1 && group_best != 2) return api_fail(P2_EINVAL, "group_best must be 1 or 2");
+        if (!std::isfinite(scale)) return api_fail(P2_EINVAL, "scale must be finite");
+        if (const char* bad = bad_rows(logits, type, stride, tokens, experts)) return api_fail(P2_EINVAL, bad);
+        if ((tokens > 0 && (!expert || !gate)) || !counts || !kept) return api_fail(P2_EINVAL, "null argument");
+        if (!aligned_to(bias, 4) || !aligned_to(expert, 4) || !aligned_to(gate, 4) || !aligned_to(counts, 8) || !aligned_to(kept, 8))
+            return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        const int64_t room = route_room(tokens, experts, k, groups);
+        if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
+        RouteForward a = {};
+        a.logits = logits; a.keep = keep; a.bias = bias; a.expert = expert; a.gate = gate; a.counts = counts; a.kept = kept;
+        a.part_count = static_cast<int32_t*>(workspace);
+        a.stride = stride; a.tokens = tokens; a.scale = (float)scale; a.experts = experts; a.k = k; a.type = type; a.score = score;
+        a.groups = groups; a.group_limit = group_limit; a.group_best = group_best; a.renormalise = renormalise != 0;
+        return launched(launch_route_forward(a, (hipStream_t)stream), "route");
+    });
+}
+
+int32_t p2_route_backward(const void* logits, int32_t type, int64_t stride, int64_t tokens, int32_t experts, int32_t k, int32_t score,
+                          int32_t renormalise, double scale, const int32_t* expert, const float* dgate, void* dlogits, int64_t dlogits_stride, void* stream) {
+    return guarded([&]() -> int32_t {
+        if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
+        int32_t rc = check_balance(tokens, experts, k);
+        if (rc != P2_OK) return rc;
+        if (score != P2_SOFTMAX && score != P2_SIGMOID) return api_fail(P2_EINVAL, "unknown score");
+        if (!std::isfinite(scale)) return api_fail(P2_EINVAL, "scale must be finite");
+        for (const char* bad : {bad_rows(logits, type, stride, tokens, experts), bad_rows(dlogits, type, dlogits_stride, tokens, experts)})
+            if (bad) return api_fail(P2_EINVAL, bad);
+        if (tokens > 0 && (!expert || !dgate)) return api_fail(P2_EINVAL, "null argument");
+        if (dlogits == logits && tokens > 1 && dlogits_stride != stride) return api_fail(P2_EINVAL, "dlogits are the logits with another stride");
+        if (!aligned_to(expert, 4) || !aligned_to(dgate, 4)) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        RouteBackward a = {};
+        a.logits = logits; a.expert = expert; a.dgate = dgate; a.dlogits = dlogits; a.stride = stride; a.dlogits_stride = dlogits_stride;
+        a.tokens = tokens; a.scale = (float)scale; a.experts = experts; a.k = k; a.type = type; a.score = score; a.renormalise = renormalise != 0;
+        return launched(launch_route_backward(a, (hipStream_t)stream), "route's gradient");
+    });
+}
+
+int32_t p2_route_bias(const float* bias, const int64_t* counts, int32_t experts, double rate, float* out, void* stream) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_balance(0, experts, 1);
+        if (rc != P2_OK) return rc;
+        if (!std::isfinite(rate)) return api_fail(P2_EINVAL, "rate must be finite");
+        if (!bias || !counts || !out) return api_fail(P2_EINVAL, "null argument");
+        if (!aligned_to(bias, 4) || !aligned_to(counts, 8) || !aligned_to(out, 4)) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        return launched(launch_route_bias(bias, counts, experts, (float)rate, out, (hipStream_t)stream), "route's biases");
+    });
+}
+
+int32_t p2_square_sum_workspace(int64_t n, int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_tensors(n, [](int64_t) { return 0; });
+        if (rc != P2_OK) return rc;
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        *bytes = round256(square_sum_parts(n) * 8);
+        return P2_OK;
+    });
+}
+
+int32_t p2_square_sum(const void* const* tensors, const int64_t* counts, int64_t n, int32_t type, double* out, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&]() -> int32_t {
+        if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
+        if (n > 0 && (!tensors || !counts)) return api_fail(P2_EINVAL, "null argument");
+        int32_t rc = check_tensors(n, [&](int64_t i) { return counts[i]; });
+        if (rc != P2_OK) return rc;
+        for (int64_t i = 0; i < n; ++i) {
+            if (counts[i] > 0 && !tensors[i]) return api_fail(P2_EINVAL, "null argument");
+            if (!aligned_to(tensors[i], type_bytes(type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        }
+        if (!out) return api_fail(P2_EINVAL, "null argument");
+        if (!aligned_to(out, 8)) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < round256(square_sum_parts(n) * 8)) return api_fail(P2_ENOSPC, "workspace too small");
+        return launched(launch_square_sum(tensors, counts, n, type, out, static_cast<double*>(workspace), (hipStream_t)stream), "sum of squares");
+    });
+}
+
+int32_t p2_adamw_workspace(int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        *bytes = 256;
+        return P2_OK;
+    });
+}
+
+int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_t grad_type, int32_t copy_type, int32_t state_bits, int64_t* step,
+                 const float* rate, double lr, double beta1, double beta2, double eps, double weight_decay, double grad_factor, const double* square_sum,
+                 double max_norm, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&]() -> int32_t {
+        if (!known_type(type) || !known_type(grad_type) || !known_type(copy_type)) return api_fail(P2_EINVAL, "unknown element type");
+        if (state_bits != 32 && state_bits != 8) return api_fail(P2_EINVAL, "states have 32 or 8 bits");
+        if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return api_fail(P2_EINVAL, "betas must be in [0, 1)");
+        if (!std::isfinite(lr) || !std::isfinite(weight_decay)) return api_fail(P2_EINVAL, "lr and weight_decay must be finite");
+        if (!(eps >= 0.0) || std::isinf(eps)) return api_fail(P2_EINVAL, "eps must be >= 0");
+        if (state_bits == 8 && eps < 1e-12) return api_fail(P2_EUNSUPPORTED, "8-bit states take eps >= 1e-12");
+        if (!(grad_factor > 0.0) || std::isinf(grad_factor)) return api_fail(P2_EINVAL, "grad_factor must be > 0");
+        if (square_sum && !(max_norm > 0.0)) return api_fail(P2_EINVAL, "max_norm must be > 0");
+        if (n > 0 && !tensors) return api_fail(P2_EINVAL, "null argument");
+        int32_t rc = check_tensors(n, [&](int64_t i) { return tensors[i].count; });
+        if (rc != P2_OK) return rc;
+        const size_t size = type_bytes(type), state = state_bits == 8 ? 1 : 4;
+        std::vector<Range> written;
+        written.reserve((size_t)n * 4);
+        for (int64_t i = 0; i < n; ++i) {
+            const p2_adamw_tensor& t = tensors[i];
+            if (t.count == 0) continue;
+            if (!t.param || !t.grad || !t.mean || !t.square) return api_fail(P2_EINVAL, "null argument");
+            if (state_bits == 8 && (!t.mean_scale || !t.square_scale)) return api_fail(P2_EINVAL, "8-bit states need their scales");
+            if (!aligned_to(t.param, size) || !aligned_to(t.grad, type_bytes(grad_type)) || !aligned_to(t.copy, type_bytes(copy_type)) || !aligned_to(t.mean, state) ||
+                !aligned_to(t.square, state) || !aligned_to(t.mean_scale, 4) || !aligned_to(t.square_scale, 4))
+                return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+            const auto add = [&](const void* p, size_t bytes) { written.emplace_back(static_cast<const char*>(p), static_cast<const char*>(p) + (size_t)t.count * bytes); };
+            add(t.param, size);
+            add(t.mean, state);
+            add(t.square, state);
+            if (t.copy) add(t.copy, type_bytes(copy_type));
+        }
+        if (overlap(written)) return api_fail(P2_EINVAL, "tensors overlap");
+        if (!step || !aligned_to(step, 8) || !aligned_to(rate, 4) || !aligned_to(square_sum, 8)) return api_fail(P2_EINVAL, "step null, or pointer not aligned to its elements");
+        if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < 256) return api_fail(P2_ENOSPC, "workspace too small");
+        Adamw a = {};
+        a.tensors = tensors; a.n = n; a.step = step; a.rate = rate; a.square_sum = square_sum; a.numbers = static_cast<AdamwStep*>(workspace);
+        a.lr = lr; a.beta1 = beta1; a.beta2 = beta2; a.eps = eps; a.weight_decay = weight_decay; a.grad_factor = grad_factor; a.max_norm = max_norm;
+        a.type = type; a.grad_type = grad_type; a.copy_type = copy_type; a.state_bits = state_bits;
+        return launched(launch_adamw(a, (hipStream_t)stream), "AdamW");
+    });
+}
+
+int32_t p2_adamw_values(const p2_adamw_tensor* tensors, int64_t n, float* const* mean_out, float* const* square_out, void* stream) {
+    return guarded([&]() -> int32_t {
+        if (n > 0 && !tensors) return api_fail(P2_EINVAL, "null argument");
+        int32_t rc = check_tensors(n, [&](int64_t i) { return tensors[i].count; });
+        if (rc != P2_OK) return rc;
+        for (int64_t i = 0; i < n; ++i) {
+            const p2_adamw_tensor& t = tensors[i];
+            const float *m = mean_out ? mean_out[i] : nullptr, *s = square_out ? square_out[i] : nullptr;
+            if (t.count > 0 && ((m && (!t.mean || !t.mean_scale)) || (s && (!t.square || !t.square_scale)))) return api_fail(P2_EINVAL, "null argument");
+            if (!aligned_to(m, 4) || !aligned_to(s, 4) || !aligned_to(t.mean_scale, 4) || !aligned_to(t.square_scale, 4))
+                return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        }
+        return launched(launch_adamw_values(tensors, n, mean_out, square_out, (hipStream_t)stream), "AdamW's values");
+    });
+}
+
+int32_t p2_linear_forward_workspace(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t type, int64_t rows, int64_t inner,
+                                    int64_t outer, int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_linear(type, rows, inner, outer);
+        if (rc != P2_OK) return rc;
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        LinearForward a = {};
+        a.x = x; a.x_stride = x_stride; a.weight = weight; a.weight_stride = weight_stride; a.type = type; a.rows = rows; a.inner = inner; a.outer = outer;
+        *bytes = linear_forward_workspace(a);
+        return P2_OK;
+    });
+}
+
+int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, const void* bias, const void* residual,
+                          int64_t residual_stride, int32_t type, int32_t activation, int64_t rows, int64_t inner, int64_t outer, void* y, int64_t y_stride,
+                          void* z, int64_t z_stride, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_linear(type, rows, inner, outer);
+        if (rc != P2_OK) return rc;
+        if (activation < P2_NO_ACTIVATION || activation > P2_SILU) return api_fail(P2_EINVAL, "unknown activation");
+        for (const char* bad : {bad_rows(x, type, x_stride, rows, inner), bad_rows(weight, type, weight_stride, outer, inner), bad_rows(y, type, y_stride, rows, outer),
+                                residual ? bad_rows(residual, type, residual_stride, rows, outer) : nullptr, z ? bad_rows(z, type, z_stride, rows, outer) : nullptr})
+            if (bad) return api_fail(P2_EINVAL, bad);
+        if (!aligned_to(bias, type_bytes(type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        if (y && y == residual && rows > 1 && y_stride != residual_stride) return api_fail(P2_EINVAL, "y is residual with another stride");
+        if (y && (y == x || y == z || y == weight)) return api_fail(P2_EINVAL, "y is an input, or z");
+        LinearForward a = {};
+        a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z; a.workspace = static_cast<char*>(workspace);
+        a.x_stride = x_stride; a.weight_stride = weight_stride; a.residual_stride = residual_stride; a.y_stride = y_stride; a.z_stride = z_stride;
+        a.rows = rows; a.inner = inner; a.outer = outer; a.type = type; a.activation = activation;
+        const int64_t room = linear_forward_workspace(a);
+        if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
+        if (rows == 0) return P2_OK;
+        return launched(launch_linear_forward(a, (hipStream_t)stream), "linear");
+    });
+}
+
+int32_t p2_linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer, int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_linear(type, rows, inner, outer);
+        if (rc != P2_OK) return rc;
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        *bytes = linear_backward_workspace(type, rows, inner, outer);
+        return P2_OK;
+    });
+}
+
+int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int64_t z_stride, const void* x, int64_t x_stride, const void* weight,
+                           int64_t weight_stride, int32_t type, int32_t activation, int64_t rows, int64_t inner, int64_t outer, void* dx, int64_t dx_stride,
+                           void* dweight, int64_t dweight_stride, void* dbias, int32_t weight_type, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_linear(type, rows, inner, outer);
+        if (rc != P2_OK) return rc;
+        if (!known_type(weight_type)) return api_fail(P2_EINVAL, "unknown element type");
+        if (activation < P2_NO_ACTIVATION || activation > P2_SILU) return api_fail(P2_EINVAL, "unknown activation");
+        const bool slope = activation != P2_NO_ACTIVATION;
+        for (const char* bad : {bad_rows(dy, type, dy_stride, rows, outer), slope ? bad_rows(z, type, z_stride, rows, outer) : nullptr,
+                                dweight ? bad_rows(x, type, x_stride, rows, inner) : nullptr, dx ? bad_rows(weight, type, weight_stride, outer, inner) : nullptr,
+                                dx ? bad_rows(dx, type, dx_stride, rows, inner) : nullptr, dweight ? bad_rows(dweight, weight_type, dweight_stride, outer, inner) : nullptr})
+            if (bad) return api_fail(P2_EINVAL, bad);
+        if (!aligned_to(dbias, type_bytes(weight_type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
+        if (dx && (dx == dy || dx == x || dx == weight || dx == z || dx == dweight)) return api_fail(P2_EINVAL, "dx is an input, or dweight");
+        const int64_t room = linear_backward_workspace(type, rows, inner, outer);
+        if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
+        LinearBackward a = {};
+        a.dy = dy; a.z = z; a.x = x; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.workspace = static_cast<char*>(workspace);
+        a.dy_stride = dy_stride; a.z_stride = z_stride; a.x_stride = x_stride; a.weight_stride = weight_stride; a.dx_stride = dx_stride;
+        a.dweight_stride = dweight_stride; a.rows = rows; a.inner = inner; a.outer = outer; a.type = type; a.activation = activation; a.weight_type = weight_type;
+        return launched(launch_linear_backward(a, (hipStream_t)stream), "linear's gradients");
     });
 }
 

@@ -182,4 +182,57 @@ bool orthogonalize_bounds(const Orthogonalize& a, double* bounds);
 int64_t orthogonalize_workspace(int64_t count, int64_t rows, int64_t cols);
 hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t stream);
 
+struct RouteForward {
+    const void* logits; const uint8_t* keep; const float* bias; int32_t* expert; float* gate; int64_t* counts; int64_t* kept;
+    int32_t* part_count;              // [blocks][experts + 1], the last one: tokens that count; unused where one block has all of them
+    int64_t stride, tokens;
+    float scale;
+    int32_t experts, k, type, score, groups, group_limit, group_best, renormalise;
+};
+int64_t route_forward_blocks(int64_t tokens, int32_t experts, int32_t k, int32_t groups);
+hipError_t launch_route_forward(const RouteForward& a, hipStream_t stream);
+
+struct RouteBackward {
+    const void* logits; const int32_t* expert; const float* dgate; void* dlogits;
+    int64_t stride, dlogits_stride, tokens;
+    float scale;
+    int32_t experts, k, type, score, renormalise;
+};
+hipError_t launch_route_backward(const RouteBackward& a, hipStream_t stream);
+hipError_t launch_route_bias(const float* bias, const int64_t* counts, int32_t experts, float rate, float* out, hipStream_t stream);
+
+int64_t square_sum_parts(int64_t n);
+hipError_t launch_square_sum(const void* const* tensors, const int64_t* counts, int64_t n, int32_t type, double* out, double* parts, hipStream_t stream);
+
+// A step's numbers, worked out on the device.
+struct AdamwStep {
+    float factor, rate, root, shrink;     // of the gradient; lr / (1 - beta1^t); 1 / sqrt(1 - beta2^t); 1 - lr weight_decay
+    int32_t left_out;
+};
+struct Adamw {
+    const p2_adamw_tensor* tensors;
+    int64_t n;
+    int64_t* step; const float* rate; const double* square_sum; AdamwStep* numbers;
+    double lr, beta1, beta2, eps, weight_decay, grad_factor, max_norm;
+    int32_t type, grad_type, copy_type, state_bits;
+};
+hipError_t launch_adamw(const Adamw& a, hipStream_t stream);
+hipError_t launch_adamw_values(const p2_adamw_tensor* tensors, int64_t n, float* const* mean_out, float* const* square_out, hipStream_t stream);
+
+struct LinearForward {
+    const void* x; const void* weight; const void* bias; const void* residual; void* y; void* z; char* workspace;
+    int64_t x_stride, weight_stride, residual_stride, y_stride, z_stride, rows, inner, outer;
+    int32_t type, activation;
+};
+int64_t linear_forward_workspace(const LinearForward& a);
+hipError_t launch_linear_forward(const LinearForward& a, hipStream_t stream);
+
+struct LinearBackward {
+    const void* dy; const void* z; const void* x; const void* weight; void* dx; void* dweight; void* dbias; char* workspace;
+    int64_t dy_stride, z_stride, x_stride, weight_stride, dx_stride, dweight_stride, rows, inner, outer;
+    int32_t type, activation, weight_type;
+};
+int64_t linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer);
+hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream);
+
 }  // namespace p2

@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <limits>
+#include <vector>
 
 #include "../../include/p2_train.h"
 
@@ -25,6 +26,19 @@ struct Calls {
     decltype(&p2_balance_backward) balance_backward;
     decltype(&p2_orthogonalize_workspace) orthogonalize_workspace;
     decltype(&p2_orthogonalize) orthogonalize;
+    decltype(&p2_route_forward_workspace) route_forward_workspace;
+    decltype(&p2_route_forward) route_forward;
+    decltype(&p2_route_backward) route_backward;
+    decltype(&p2_route_bias) route_bias;
+    decltype(&p2_square_sum_workspace) square_sum_workspace;
+    decltype(&p2_square_sum) square_sum;
+    decltype(&p2_adamw_workspace) adamw_workspace;
+    decltype(&p2_adamw) adamw;
+    decltype(&p2_adamw_values) adamw_values;
+    decltype(&p2_linear_forward_workspace) linear_forward_workspace;
+    decltype(&p2_linear_forward) linear_forward;
+    decltype(&p2_linear_backward_workspace) linear_backward_workspace;
+    decltype(&p2_linear_backward) linear_backward;
 } calls;
 PyObject* raise_status = nullptr;              // (status): raises the library's last error
 PyObject* raise_refusal = nullptr;             // (text)
@@ -314,6 +328,285 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t given) {
     });
 }
 
+bool truth(PyObject* o) {
+    const int t = PyObject_IsTrue(o);
+    if (t < 0) throw Refused();
+    return t;
+}
+
+// (logits, k, score, bias, keep, groups, group_limit, group_best, renormalise, scale, stream) -> expert, gate, counts, tokens
+PyObject* route_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 11, [&] {
+        const at::Tensor& logits = tensor(a[0], "logits");
+        const int32_t k = whole32(a[1]), score = whole32(a[2]), groups = whole32(a[5]), limit = whole32(a[6]), best = whole32(a[7]);
+        const bool renormalise = truth(a[8]);
+        const double scale = number(a[9]);
+        void* stream = stream_of(a[10]);
+        const at::Tensor keep = keep_of(logits, optional(a[4], "keep"));
+        at::Tensor bias = optional(a[3], "bias");
+        on_device(logits, {&keep, &bias});
+        not_recorded("p2_route_forward", {&logits, &bias});
+        const int32_t type = type_of(logits, "logits");
+        const Rows r = rows_of(logits);
+        bias = vector_of(std::move(bias), r.cols, "bias", true);
+        const int32_t experts = (int32_t)std::min<int64_t>(r.cols, std::numeric_limits<int32_t>::max());
+        int64_t bytes = 0;
+        check(calls.route_forward_workspace(r.n, experts, k, groups, &bytes));         // (refuses another k, too)
+        const auto options = logits.options();
+        at::Tensor expert = at::empty({r.n, k}, options.dtype(at::kInt)), gate = at::empty({r.n, k}, options.dtype(at::kFloat));
+        at::Tensor counts = at::empty({r.cols}, options.dtype(at::kLong)), kept = at::empty({}, options.dtype(at::kLong));
+        const at::Tensor work = workspace(bytes, logits);
+        check(calls.route_forward(ptr(r.t), type, r.stride, (const uint8_t*)ptr(keep), (const float*)ptr(bias), r.n, experts, k, score, groups, limit, best, renormalise,
+                                  scale, (int32_t*)ptr(expert), (float*)ptr(gate), (int64_t*)ptr(counts), (int64_t*)ptr(kept), ptr(work), bytes, stream));
+        return results(expert, gate, counts, kept);
+    });
+}
+
+// (logits, expert, dgate, score, renormalise, scale, stream) -> dlogits
+PyObject* route_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 7, [&] {
+        const at::Tensor &logits = tensor(a[0], "logits"), &chosen = tensor(a[1], "expert"), &given_dgate = tensor(a[2], "dgate");
+        const int32_t score = whole32(a[3]);
+        const bool renormalise = truth(a[4]);
+        const double scale = number(a[5]);
+        void* stream = stream_of(a[6]);
+        on_device(logits, {&chosen, &given_dgate});
+        not_recorded("p2_route_backward", {&logits, &given_dgate});
+        const int32_t type = type_of(logits, "logits");
+        const Rows r = rows_of(logits);
+        if (chosen.scalar_type() != at::kInt || chosen.dim() != 2 || chosen.size(0) != r.n) refuse("expert must be int32 [tokens, k]");
+        if (given_dgate.scalar_type() != at::kFloat || given_dgate.sizes() != chosen.sizes()) refuse("dgate must be float32 [tokens, k]");
+        const int32_t most = std::numeric_limits<int32_t>::max();
+        const int32_t experts = (int32_t)std::min<int64_t>(r.cols, most), k = (int32_t)std::min<int64_t>(chosen.size(1), most);
+        const at::Tensor expert = chosen.contiguous(), dgate = given_dgate.contiguous();
+        at::Tensor out = like(logits);
+        check(calls.route_backward(ptr(r.t), type, r.stride, r.n, experts, k, score, renormalise, scale, (const int32_t*)ptr(expert), (const float*)ptr(dgate), ptr(out),
+                                   std::max<int64_t>(r.cols, 1), stream));
+        return result(out);
+    });
+}
+
+// (bias, counts, rate, stream) -> the new bias
+PyObject* route_bias(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 4, [&] {
+        const at::Tensor &first = tensor(a[0], "bias"), &second = tensor(a[1], "counts");
+        const double rate = number(a[2]);
+        void* stream = stream_of(a[3]);
+        on_device(first, {&second});
+        not_recorded("p2_route_bias", {&first});
+        const at::Tensor bias = vector_of(first, first.dim() == 1 ? first.size(0) : -1, "bias", true);
+        if (second.scalar_type() != at::kLong || second.dim() != 1 || second.size(0) != bias.size(0)) refuse("counts must be int64 [experts]");
+        const at::Tensor counts = second.contiguous();
+        const int32_t experts = (int32_t)std::min<int64_t>(bias.size(0), std::numeric_limits<int32_t>::max());
+        at::Tensor out = like(bias);
+        check(calls.route_bias((const float*)ptr(bias), (const int64_t*)ptr(counts), experts, rate, (float*)ptr(out), stream));
+        return result(out);
+    });
+}
+
+// Lists of tensors: all of one type and on one device.
+std::vector<at::Tensor> tensors_of(PyObject* o, const char* what, bool same_type = true) {
+    PyObject* all = PySequence_Fast(o, what);
+    if (!all) throw Refused();
+    std::vector<at::Tensor> v;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(all);
+    v.reserve(n);
+    try {
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            v.push_back(tensor(PySequence_Fast_GET_ITEM(all, i), what));
+            if (v.back().device() != v[0].device()) refuse("tensors must be on the current device");
+            if (same_type && v.back().scalar_type() != v[0].scalar_type()) refuse(std::string(what) + " must have one type");
+        }
+    } catch (...) {
+        Py_DECREF(all);
+        throw;
+    }
+    Py_DECREF(all);
+    return v;
+}
+// What a call writes, or reads with its like: as many as the parameters, of their numbers of values, without gaps.
+void matching(const std::vector<at::Tensor>& v, const std::vector<at::Tensor>& params, const char* what, at::ScalarType type, int64_t each = 1) {
+    if (v.size() != params.size()) refuse(std::string(what) + ": as many as tensors");
+    for (size_t i = 0; i < v.size(); ++i) {
+        if (v[i].device() != params[i].device()) refuse("tensors must be on the current device");
+        if (v[i].scalar_type() != type) refuse(std::string(what) + " must be " + c10::toString(type));
+        if (v[i].numel() != (params[i].numel() + each - 1) / each || (each == 1 && v[i].sizes() != params[i].sizes())) refuse(std::string(what) + " must have its tensor's shape" + (each > 1 ? ", or a scale for each block" : ""));
+        if (!v[i].is_contiguous()) refuse(std::string(what) + " must be contiguous");
+    }
+}
+
+// (tensors, stream) -> the sum
+PyObject* square_sum(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 2, [&] {
+        std::vector<at::Tensor> t = tensors_of(a[0], "tensors");
+        void* stream = stream_of(a[1]);
+        if (t.empty()) refuse("no tensors");
+        const int32_t type = type_of(t[0], "tensors");
+        std::vector<const void*> p(t.size());
+        std::vector<int64_t> n(t.size());
+        for (size_t i = 0; i < t.size(); ++i) {
+            not_recorded("p2_square_sum", {&t[i]});
+            if (!t[i].is_non_overlapping_and_dense()) t[i] = t[i].contiguous();        // (in whatever order)
+            p[i] = ptr(t[i]);
+            n[i] = t[i].numel();
+        }
+        int64_t bytes = 0;
+        check(calls.square_sum_workspace((int64_t)t.size(), &bytes));
+        const at::Tensor work = workspace(bytes, t[0]);
+        at::Tensor out = at::empty({}, t[0].options().dtype(at::kDouble));
+        check(calls.square_sum(p.data(), n.data(), (int64_t)t.size(), type, (double*)ptr(out), ptr(work), bytes, stream));
+        return result(out);
+    });
+}
+
+// (params, grads, means, squares, step, mean_scales, square_scales, copies, rate, lr, beta1, beta2, eps, weight_decay, grad_factor, square_sum, max_norm, stream)
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 18, [&]() -> PyObject* {
+        const std::vector<at::Tensor> params = tensors_of(a[0], "params");
+        std::vector<at::Tensor> grads = tensors_of(a[1], "grads");
+        const std::vector<at::Tensor> means = tensors_of(a[2], "means"), squares = tensors_of(a[3], "squares");
+        const at::Tensor& step = tensor(a[4], "step");
+        std::vector<at::Tensor> mean_scales, square_scales, copies;
+        if (a[5] != Py_None) mean_scales = tensors_of(a[5], "mean_scales");
+        if (a[6] != Py_None) square_scales = tensors_of(a[6], "square_scales");
+        if (a[7] != Py_None) copies = tensors_of(a[7], "copies");
+        const at::Tensor rate = optional(a[8], "rate"), square_sum = optional(a[15], "square_sum");
+        const double lr = number(a[9]), beta1 = number(a[10]), beta2 = number(a[11]), eps = number(a[12]), decay = number(a[13]), factor = number(a[14]), most = number(a[16]);
+        void* stream = stream_of(a[17]);
+        if (params.empty()) refuse("no tensors");
+        const bool small = a[5] != Py_None || a[6] != Py_None;
+        on_device(params[0], {&step, &rate, &square_sum});
+        if (step.scalar_type() != at::kLong || step.numel() != 1) refuse("step must be one int64");
+        if (rate.defined() && (rate.scalar_type() != at::kFloat || rate.numel() != 1)) refuse("rate must be one float32");
+        if (square_sum.defined() && (square_sum.scalar_type() != at::kDouble || square_sum.numel() != 1)) refuse("square_sum must be one float64");
+        const int32_t type = type_of(params[0], "params");
+        matching(params, params, "params", params[0].scalar_type());
+        if (grads.size() != params.size()) refuse("grads: as many as tensors");
+        const int32_t grad_type = type_of(grads[0], "grads");
+        for (size_t i = 0; i < grads.size(); ++i) {
+            if (grads[i].device() != params[i].device() || grads[i].sizes() != params[i].sizes()) refuse("grads must have their tensors' shapes");
+            if (!grads[i].is_contiguous()) grads[i] = grads[i].contiguous();
+        }
+        matching(means, params, "means", small ? at::kChar : at::kFloat);
+        matching(squares, params, "squares", small ? at::kByte : at::kFloat);
+        if (small) {
+            matching(mean_scales, params, "mean_scales", at::kFloat, P2_STATE_BLOCK);
+            matching(square_scales, params, "square_scales", at::kFloat, P2_STATE_BLOCK);
+        }
+        int32_t copy_type = P2_F32;
+        if (!copies.empty()) {
+            copy_type = type_of(copies[0], "copies");
+            matching(copies, params, "copies", copies[0].scalar_type());
+        }
+        std::vector<p2_adamw_tensor> t(params.size());
+        for (size_t i = 0; i < t.size(); ++i)
+            t[i] = {ptr(params[i]), ptr(grads[i]), copies.empty() ? nullptr : ptr(copies[i]), ptr(means[i]), ptr(squares[i]), small ? (float*)ptr(mean_scales[i]) : nullptr,
+                    small ? (float*)ptr(square_scales[i]) : nullptr, params[i].numel()};
+        int64_t bytes = 0;
+        check(calls.adamw_workspace(&bytes));
+        const at::Tensor work = workspace(bytes, params[0]);
+        check(calls.adamw(t.data(), (int64_t)t.size(), type, grad_type, copy_type, small ? 8 : 32, (int64_t*)ptr(step), (const float*)ptr(rate), lr, beta1, beta2, eps, decay,
+                          factor, (const double*)ptr(square_sum), most, ptr(work), bytes, stream));
+        Py_RETURN_NONE;
+    });
+}
+
+// (means, squares, mean_scales, square_scales, stream) -> lists of their values
+PyObject* adamw_values(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 5, [&]() -> PyObject* {
+        const std::vector<at::Tensor> means = tensors_of(a[0], "means"), squares = tensors_of(a[1], "squares"), mean_scales = tensors_of(a[2], "mean_scales"),
+                                      square_scales = tensors_of(a[3], "square_scales");
+        void* stream = stream_of(a[4]);
+        matching(means, means, "means", at::kChar);
+        matching(squares, means, "squares", at::kByte);
+        matching(mean_scales, means, "mean_scales", at::kFloat, P2_STATE_BLOCK);
+        matching(square_scales, means, "square_scales", at::kFloat, P2_STATE_BLOCK);
+        std::vector<p2_adamw_tensor> t(means.size());
+        std::vector<float*> mean_out(means.size()), square_out(means.size());
+        PyObject* lists[2] = {PyList_New((Py_ssize_t)t.size()), PyList_New((Py_ssize_t)t.size())};
+        try {
+            for (size_t i = 0; i < t.size(); ++i) {
+                t[i] = {nullptr, nullptr, nullptr, ptr(means[i]), ptr(squares[i]), (float*)ptr(mean_scales[i]), (float*)ptr(square_scales[i]), means[i].numel()};
+                for (int k = 0; k < 2; ++k) {
+                    const at::Tensor out = at::empty(means[i].sizes(), means[i].options().dtype(at::kFloat));
+                    (k ? square_out : mean_out)[i] = (float*)ptr(out);
+                    PyObject* o = result(out);
+                    if (!lists[k] || !o) throw Refused();
+                    PyList_SET_ITEM(lists[k], (Py_ssize_t)i, o);
+                }
+            }
+            check(calls.adamw_values(t.data(), (int64_t)t.size(), mean_out.data(), square_out.data(), stream));
+        } catch (...) {
+            Py_XDECREF(lists[0]);
+            Py_XDECREF(lists[1]);
+            throw;
+        }
+        return Py_BuildValue("(NN)", lists[0], lists[1]);
+    });
+}
+
+// (x, weight, bias, activation, residual, keep, stream) -> y, z
+PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 7, [&] {
+        const at::Tensor &x = tensor(a[0], "x"), &weight = tensor(a[1], "weight");
+        at::Tensor bias = optional(a[2], "bias"), residual = optional(a[4], "residual");
+        const int32_t activation = whole32(a[3]);
+        const bool keep = truth(a[5]);
+        void* stream = stream_of(a[6]);
+        on_device(x, {&weight, &bias, &residual});
+        not_recorded("p2_linear_forward", {&x, &weight, &bias, &residual});
+        const int32_t type = type_of(x, "x");
+        if (weight.dim() != 2 || weight.size(1) != x.size(-1) || weight.scalar_type() != x.scalar_type()) refuse("weight must be [outer, inner] and have x's type");
+        const Rows r = rows_of(x), w = rows_of(weight);
+        bias = vector_of(std::move(bias), w.n, "bias", false);
+        if (bias.defined() && bias.scalar_type() != x.scalar_type()) refuse("bias must have x's type");
+        std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = w.n;
+        if (residual.defined() && (residual.sizes() != at::IntArrayRef(shape) || residual.scalar_type() != x.scalar_type())) refuse("residual must have the result's shape and type");
+        const Rows s = residual.defined() ? rows_of(residual) : Rows{at::Tensor(), 0, 0, 0};
+        at::Tensor y = at::empty(shape, x.options()), z = keep ? at::empty(shape, x.options()) : at::Tensor();
+        int64_t bytes = 0;
+        check(calls.linear_forward_workspace(ptr(r.t), r.stride, ptr(w.t), w.stride, type, r.n, r.cols, w.n, &bytes));
+        const at::Tensor work = workspace(bytes, x);
+        check(calls.linear_forward(ptr(r.t), r.stride, ptr(w.t), w.stride, ptr(bias), ptr(s.t), s.stride, type, activation, r.n, r.cols, w.n, ptr(y), w.n, ptr(z), w.n, ptr(work),
+                                   bytes, stream));
+        return results(y, z);
+    });
+}
+
+// (dy, x, weight, z, activation, dx, dweight, dbias, type of the weight's gradients or -1, stream) -> dx, dweight, dbias
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 10, [&] {
+        const at::Tensor &dy = tensor(a[0], "dy"), &x = tensor(a[1], "x"), &weight = tensor(a[2], "weight");
+        const at::Tensor z = optional(a[3], "z");
+        const int32_t activation = whole32(a[4]);
+        const bool wanted[3] = {truth(a[5]), truth(a[6]), truth(a[7])};
+        const int64_t asked = whole(a[8]);
+        void* stream = stream_of(a[9]);
+        on_device(x, {&dy, &weight, &z});
+        not_recorded("p2_linear_backward", {&dy, &x, &weight, &z});
+        const int32_t type = type_of(x, "x"), weight_type = asked < 0 ? type : (int32_t)asked;
+        if (weight.dim() != 2 || weight.size(1) != x.size(-1) || weight.scalar_type() != x.scalar_type()) refuse("weight must be [outer, inner] and have x's type");
+        std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = weight.size(0);
+        if (dy.sizes() != at::IntArrayRef(shape) || dy.scalar_type() != x.scalar_type()) refuse("dy must have the result's shape and x's type");
+        if (activation != P2_NO_ACTIVATION && !z.defined()) refuse("z is what the forward pass kept: with an activation it is needed");
+        if (z.defined() && (z.sizes() != dy.sizes() || z.scalar_type() != x.scalar_type())) refuse("z must have dy's shape and type");
+        const Rows r = rows_of(x), w = rows_of(weight), d = rows_of(dy), s = z.defined() ? rows_of(z) : Rows{at::Tensor(), 0, 0, 0};
+        at::Tensor dx, dweight, dbias;
+        const auto options = x.options().dtype(scalar_of(weight_type));
+        if (wanted[0]) dx = like(x);
+        if (wanted[1]) dweight = at::empty({w.n, r.cols}, options);
+        if (wanted[2]) dbias = at::empty({w.n}, options);
+        int64_t bytes = 0;
+        check(calls.linear_backward_workspace(type, r.n, r.cols, w.n, &bytes));
+        const at::Tensor work = workspace(bytes, x);
+        check(calls.linear_backward(ptr(d.t), d.stride, ptr(s.t), s.stride, ptr(r.t), r.stride, ptr(w.t), w.stride, type, activation, r.n, r.cols, w.n, ptr(dx), r.cols,
+                                    ptr(dweight), r.cols, ptr(dbias), weight_type, ptr(work), bytes, stream));
+        return results(dx, dweight, dbias);
+    });
+}
+
 // (addresses of the C ABI in the order of Calls, raise_status, raise_refusal)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given) {
     constexpr Py_ssize_t n = sizeof(Calls) / sizeof(void*);
@@ -329,7 +622,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t given) {
 
 #define P2_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {P2_METHOD(bind), P2_METHOD(layer_norm_forward), P2_METHOD(layer_norm_backward), P2_METHOD(balance_forward), P2_METHOD(balance_loss),
-                         P2_METHOD(balance_backward), P2_METHOD(orthogonalize), {nullptr, nullptr, 0, nullptr}};
+                         P2_METHOD(balance_backward), P2_METHOD(orthogonalize), P2_METHOD(route_forward), P2_METHOD(route_backward), P2_METHOD(route_bias),
+                         P2_METHOD(square_sum), P2_METHOD(adamw), P2_METHOD(adamw_values), P2_METHOD(linear_forward), P2_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
