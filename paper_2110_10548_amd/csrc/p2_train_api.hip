@@ -75,9 +75,12 @@ int32_t check_route(int64_t tokens, int32_t experts, int32_t k, int32_t groups) 
     if (groups > P2_MAX_GROUPS) return api_fail(P2_EUNSUPPORTED, "more than 64 groups");
     return P2_OK;
 }
-int64_t route_room(int64_t tokens, int32_t experts, int32_t k, int32_t groups) {
+struct RouteRoom { int64_t again, bytes; };
+RouteRoom route_room(int64_t tokens, int32_t experts, int32_t k, int32_t groups) {
     const int64_t lines = route_forward_blocks(tokens, experts, k, groups);
-    return lines == 1 ? 0 : round256(lines * (experts + 1) * 4);
+    if (lines == 1) return {};
+    const int64_t again = round256(lines * (experts + 1) * 4);
+    return {again, again + round256(tokens)};
 }
 
 // Tensors of a call over many: as many and as long as the kernels count.
@@ -306,7 +309,7 @@ int32_t p2_route_forward_workspace(int64_t tokens, int32_t experts, int32_t k, i
         int32_t rc = check_route(tokens, experts, k, groups);
         if (rc != P2_OK) return rc;
         if (!bytes) return api_fail(P2_EINVAL, "null argument");
-        *bytes = route_room(tokens, experts, k, groups);
+        *bytes = route_room(tokens, experts, k, groups).bytes;
         return P2_OK;
     });
 }
@@ -326,12 +329,13 @@ int32_t p2_route_forward(const void* logits, int32_t type, int64_t stride, const
         if ((tokens > 0 && (!expert || !gate)) || !counts || !kept) return api_fail(P2_EINVAL, "null argument");
         if (!aligned_to(bias, 4) || !aligned_to(expert, 4) || !aligned_to(gate, 4) || !aligned_to(counts, 8) || !aligned_to(kept, 8))
             return api_fail(P2_EINVAL, "pointer not aligned to its elements");
-        const int64_t room = route_room(tokens, experts, k, groups);
-        if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
-        if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
+        const RouteRoom room = route_room(tokens, experts, k, groups);
+        if (room.bytes && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
+        if (workspace_bytes < room.bytes) return api_fail(P2_ENOSPC, "workspace too small");
         RouteForward a = {};
         a.logits = logits; a.keep = keep; a.bias = bias; a.expert = expert; a.gate = gate; a.counts = counts; a.kept = kept;
         a.part_count = static_cast<int32_t*>(workspace);
+        a.again = static_cast<uint8_t*>(workspace) + room.again;
         a.stride = stride; a.tokens = tokens; a.scale = (float)scale; a.experts = experts; a.k = k; a.type = type; a.score = score;
         a.groups = groups; a.group_limit = group_limit; a.group_best = group_best; a.renormalise = renormalise != 0;
         return launched(launch_route_forward(a, (hipStream_t)stream), "route");

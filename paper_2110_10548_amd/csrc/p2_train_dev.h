@@ -184,7 +184,8 @@ hipError_t launch_orthogonalize(const Orthogonalize& a, hipStream_t stream);
 
 struct RouteForward {
     const void* logits; const uint8_t* keep; const float* bias; int32_t* expert; float* gate; int64_t* counts; int64_t* kept;
-    int32_t* part_count;              // [blocks][experts + 1], the last one: tokens that count; unused where one block has all of them
+    int32_t* part_count;              // [blocks][experts + 1], the last one: tokens that count; this and `again` are unused where one block has all of them
+    uint8_t* again;                   // [tokens]: to be chosen for in 64 bits
     int64_t stride, tokens;
     float scale;
     int32_t experts, k, type, score, groups, group_limit, group_best, renormalise;
