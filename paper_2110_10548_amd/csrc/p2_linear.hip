@@ -6,6 +6,7 @@
 // each row (64 values of 16 bits, 32 of 32) that are brought to LDS straight from memory while the stage before is multiplied.  The MFMA's rows
 // are A's: a lane has four neighbouring columns of one row of C.
 #include <algorithm>
+#include <type_traits>
 
 #include "p2_train_dev.h"
 
@@ -61,26 +62,26 @@ struct Result {
     int64_t residual_stride, y_stride, z_stride;
     int32_t y_type, activation;        // (bias, residual and z have the operands' type)
 };
-template <typename T> __device__ __forceinline__ void finish(const Result& r, int64_t j, int64_t i, int64_t n, float (&v)[4]) {
+template <typename T, int N> __device__ __forceinline__ void finish(const Result& r, int64_t j, int64_t i, int64_t n, float (&v)[N]) {
     if (r.bias) {
-        float b[4];
-        load_part<T, 4>(static_cast<const T*>(r.bias) + i, n, b, 0.0f);
+        float b[N];
+        load_part<T, N>(static_cast<const T*>(r.bias) + i, n, b, 0.0f);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += b[q];
+        for (int q = 0; q < N; ++q) v[q] += b[q];
     }
-    if (r.z) store_part<T, 4>(static_cast<T*>(r.z) + j * r.z_stride + i, n, v);
+    if (r.z) store_part<T, N>(static_cast<T*>(r.z) + j * r.z_stride + i, n, v);
     if (r.activation != P2_NO_ACTIVATION)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = activate(v[q], r.activation);
+        for (int q = 0; q < N; ++q) v[q] = activate(v[q], r.activation);
     if (r.residual) {
-        float b[4];
-        load_part<T, 4>(static_cast<const T*>(r.residual) + j * r.residual_stride + i, n, b, 0.0f);
+        float b[N];
+        load_part<T, N>(static_cast<const T*>(r.residual) + j * r.residual_stride + i, n, b, 0.0f);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += b[q];
+        for (int q = 0; q < N; ++q) v[q] += b[q];
     }
-    if (r.y_type == P2_F32) store_part<float, 4>(static_cast<float*>(r.y) + j * r.y_stride + i, n, v);
-    else if (r.y_type == P2_BF16) store_part<bf16_t, 4>(static_cast<bf16_t*>(r.y) + j * r.y_stride + i, n, v);
-    else store_part<half_t, 4>(static_cast<half_t*>(r.y) + j * r.y_stride + i, n, v);
+    if (r.y_type == P2_F32) store_part<float, N>(static_cast<float*>(r.y) + j * r.y_stride + i, n, v);
+    else if (r.y_type == P2_BF16) store_part<bf16_t, N>(static_cast<bf16_t*>(r.y) + j * r.y_stride + i, n, v);
+    else store_part<half_t, N>(static_cast<half_t*>(r.y) + j * r.y_stride + i, n, v);
 }
 
 // ------------------------------------------------------------------------------------------------ products
@@ -220,9 +221,192 @@ __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_product(Produ
             if (i >= a.a_rows) continue;
             float v[4] = {acc[fi][fj][0], acc[fi][fj][1], acc[fi][fj][2], acc[fi][fj][3]};
             if (a.parts > 1) store_part<float, 4>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
-            else finish<T>(a.r, j, i, a.a_rows - i, v);
+            else finish<T, 4>(a.r, j, i, a.a_rows - i, v);
         }
     }
+}
+
+// The same for large tiles.  A's and B's rows of a tile come in halves of kWavesA * FA * 16 and kWavesB * FB * 16, and a stage is multiplied in four
+// phases, half by half, A0 B0, A0 B1, A1 B1, A1 B0, so that each phase's fragments are read from LDS while the one before is multiplied, six
+// reads of a fragment with every 16 MFMA, and a half's place in LDS is free for the stage after the next two phases after it has been
+// read: loads have five to six phases to arrive.  Two barriers a stage.
+template <typename T, int kWavesA, int kWavesB, int FA, int FB> struct Tile {
+    typedef typename Fragment<T>::type F;
+    static constexpr int kWaves = kWavesA * kWavesB;
+    static constexpr int kHalfA = kWavesA * FA * 16, kHalfB = kWavesB * FB * 16;       // rows of a half
+    static constexpr int kLoadsA = kHalfA / 8 / kWaves, kLoadsB = kHalfB / 8 / kWaves; // of a half by a wavefront; one brings 8 rows
+    static constexpr int kBuffer = 2 * (kHalfA + kHalfB) * kLine;
+    static constexpr int kPitch = FA * 16 + 4;                                         // of a strip of results in LDS, in floats
+    static_assert(kLoadsA * 8 * kWaves == kHalfA && kLoadsB * 8 * kWaves == kHalfB, "rows are dealt out evenly");
+    static_assert(kWaves * 16 * kPitch * 4 <= 2 * kBuffer, "the strips fit");
+};
+// Eight rows from `first` on, of which those past the matrix's end are zeros.
+__device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t first, int64_t rows, int length) {
+    const int64_t n = min(rows - first, (int64_t)8);
+    return Rows(p + (n > 0 ? first : 0) * pitch, n > 0 ? (int)((n - 1) * pitch) + length : 0);
+}
+__device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
+
+template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Product a) {
+    typedef Tile<T, kWavesA, kWavesB, FA, FB> S;
+    typedef typename S::F F;
+    constexpr int LA = S::kLoadsA, LB = S::kLoadsB, kBoth = 2 * (LA + LB);
+    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];                // two stages of A0, A1, B0, B1
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours.
+    int t;
+    {
+        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = blockIdx.x & 7;
+        t = die * whole + min(die, rest) + (blockIdx.x >> 3);
+    }
+    const int tiles = a.across * a.down, part = t / tiles;
+    t %= tiles;
+    int ti, tj;                                            // column by column of four rows of tiles
+    {
+        const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
+        tj = first + in % high;
+        ti = in / high;
+    }
+    const int length = (int)a.length;
+    const int all = (length + kLine - 1) / kLine;
+    const int begin = (int)((int64_t)all * part / a.parts), stages = (int)((int64_t)all * (part + 1) / a.parts) - begin;
+    // A row's 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int from_a = (lane >> 3) * (int)a.a_pitch + piece, from_b = (lane >> 3) * (int)a.b_pitch + piece;
+    // Every load of a stage has a descriptor of its own, which begins with its first row: lanes' offsets are the same for all of them.
+    const auto a_rows = [&](int half, int l) { return rows_from(a.a, a.a_pitch, (int64_t)ti * 2 * S::kHalfA + half * S::kHalfA + (wave * LA + l) * 8, a.a_rows, length); };
+    const auto b_rows = [&](int half, int l) { return rows_from(a.b, a.b_pitch, (int64_t)tj * 2 * S::kHalfB + half * S::kHalfB + (wave * LB + l) * 8, a.b_rows, length); };
+    const Rows ra[2][2] = {{a_rows(0, 0), a_rows(0, LA - 1)}, {a_rows(1, 0), a_rows(1, LA - 1)}}, rb[2][2] = {{b_rows(0, 0), b_rows(0, LB - 1)}, {b_rows(1, 0), b_rows(1, LB - 1)}};
+    static_assert(LA <= 2 && LB <= 2, "descriptors");
+    // the l-th load of a half of stage s; `last` may be the row's last stage, whose rest is zeros
+    const auto bring_a = [&](auto last, int half, int s, int l) {
+        const int at = (begin + s) * kLine;
+        ra[half][l].bring(&lds[(s & 1) * S::kBuffer + half * S::kHalfA * kLine + (wave * LA + l) * 1024], !decltype(last)::value || at + piece < length ? from_a : kPastEnd, at);
+    };
+    const auto bring_b = [&](auto last, int half, int s, int l) {
+        const int at = (begin + s) * kLine;
+        rb[half][l].bring(&lds[(s & 1) * S::kBuffer + (2 * S::kHalfA + half * S::kHalfB) * kLine + (wave * LB + l) * 1024],
+                          !decltype(last)::value || at + piece < length ? from_b : kPastEnd, at);
+    };
+    const auto bring_stage = [&](int s) {
+#pragma unroll
+        for (int l = 0; l < LA; ++l) bring_a(std::true_type(), 0, s, l);
+#pragma unroll
+        for (int l = 0; l < LB; ++l) bring_b(std::true_type(), 0, s, l);
+#pragma unroll
+        for (int l = 0; l < LB; ++l) bring_b(std::true_type(), 1, s, l);
+#pragma unroll
+        for (int l = 0; l < LA; ++l) bring_a(std::true_type(), 1, s, l);
+    };
+    const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
+    const int slot[2] = {row * kLine + (quad ^ (row & 7)) * 16, row * kLine + ((4 + quad) ^ (row & 7)) * 16};
+    const auto read_a = [&](int s, int half, int i, F (&f)[2]) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wa * FA * 16 * kLine + (half * S::kHalfA + i * 16) * kLine);
+    };
+    const auto read_b = [&](int s, int half, int j, F (&f)[2]) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wb * FB * 16 * kLine + (2 * S::kHalfA + half * S::kHalfB + j * 16) * kLine);
+    };
+    float4_t acc[2][2][FA][FB];
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[h >> 1][h & 1][i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    F a0[FA][2], a1[FA][2], bx[FB][2], by[FB][2];
+    // One phase: the products of two halves, and between them `reads` (the r-th of kReads) and `loads` (the l-th of kLoads).
+    const auto phase = [&](float4_t (&c)[FA][FB], const F (&fa)[FA][2], const F (&fb)[FB][2], auto reads_n, auto&& reads, auto loads_n, auto&& loads) {
+        constexpr int kReads = decltype(reads_n)::value, kLoads = decltype(loads_n)::value, kProducts = FA * FB * 2;
+#pragma unroll
+        for (int n = 0; n < kProducts; ++n) {
+            const int k = n / (FA * FB), i = n / FB % FA, j = n % FB;
+            multiply(fa[i][k], fb[j][k], c[i][j]);
+            // reads first, loads after them
+            constexpr int kEvery = kReads + kLoads > 0 ? kReads + kLoads : 1;
+#pragma unroll
+            for (int x = n * kEvery / kProducts; x < (n + 1) * kEvery / kProducts; ++x) {
+                if (x < kReads) reads(x);
+                else if (x - kReads < kLoads) loads(x - kReads);
+            }
+            in_this_order();
+        }
+    };
+    // kEnd: one of the last stages, after which fewer are left to bring.
+    const auto step = [&](auto end, int s, F (&b0)[FB][2], F (&b1)[FB][2]) {
+        constexpr bool kEnd = decltype(end)::value;
+        const bool next = !kEnd || s + 1 < stages, after = !kEnd || s + 2 < stages;
+        constexpr int kFew = FA >= 4 ? 1 : 0;              // fragments of A1 read in the first phase, of A0 in the last
+        if (next) stage_barrier<kBoth>();
+        else stage_barrier<0>();
+        phase(acc[0][0], a0, b0, std::integral_constant<int, FB + kFew>(), [&](int x) { if (x < FB) read_b(s, 1, x, b1[x < FB ? x : 0]); else read_a(s, 1, x - FB, a1[x >= FB ? x - FB : 0]); },
+              std::integral_constant<int, LA>(), [&](int l) { if (after) bring_a(end, 0, s + 2, l); });
+        phase(acc[0][1], a0, b1, std::integral_constant<int, FA - kFew>(), [&](int x) { read_a(s, 1, x + kFew, a1[x + kFew]); },
+              std::integral_constant<int, LB>(), [&](int l) { if (after) bring_b(end, 0, s + 2, l); });
+        if (after) stage_barrier<kBoth>();
+        else if (next) stage_barrier<LA + LB>();
+        else stage_barrier<0>();
+        phase(acc[1][1], a1, b1, std::integral_constant<int, FA - kFew>(), [&](int x) { if (next) read_a(s + 1, 0, x, a0[x]); },
+              std::integral_constant<int, LB>(), [&](int l) { if (after) bring_b(end, 1, s + 2, l); });
+        phase(acc[1][0], a1, b0, std::integral_constant<int, FB + kFew>(),
+              [&](int x) { if (next) { if (x < FB) read_b(s + 1, 0, x, b1[x < FB ? x : 0]); else read_a(s + 1, 0, FA - 1, a0[FA - 1]); } },
+              std::integral_constant<int, LA>(), [&](int l) { if (after) bring_a(end, 1, s + 2, l); });
+    };
+    bring_stage(0);
+    if (stages > 1) {
+        bring_stage(1);
+        stage_barrier<kBoth + LA + LB>();
+    } else {
+        stage_barrier<LA + LB>();
+    }
+#pragma unroll
+    for (int i = 0; i < FA; ++i) read_a(0, 0, i, a0[i]);
+#pragma unroll
+    for (int j = 0; j < FB; ++j) read_b(0, 0, j, bx[j]);
+    int s = 0;
+    for (; s + 4 < stages; s += 2) {
+        step(std::false_type(), s, bx, by);
+        step(std::false_type(), s + 1, by, bx);
+    }
+    for (; s + 1 < stages; s += 2) {
+        step(std::true_type(), s, bx, by);
+        step(std::true_type(), s + 1, by, bx);
+    }
+    if (s < stages) step(std::true_type(), s, bx, by);
+    // A lane has four neighbouring columns of a row of C.  Strips of 16 rows go through LDS, where a lane picks up eight.
+    stage_barrier<0>();
+    constexpr int kAcross = FA * 2;                        // lanes to a row of a strip
+    float* strip = reinterpret_cast<float*>(lds) + wave * 16 * S::kPitch;
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+        for (int fj = 0; fj < FB; ++fj) {
+            const int64_t j0 = (int64_t)tj * 2 * S::kHalfB + hb * S::kHalfB + (wb * FB + fj) * 16;
+            if (j0 >= a.b_rows) continue;
+#pragma unroll
+            for (int ha = 0; ha < 2; ++ha) {
+                const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
+                if (i0 >= a.a_rows) continue;
+#pragma unroll
+                for (int fi = 0; fi < FA; ++fi) *reinterpret_cast<float4_t*>(strip + row * S::kPitch + fi * 16 + quad * 4) = acc[ha][hb][fi][fj];
+                wavefront_exchange();
+#pragma unroll
+                for (int x = 0; x < 16 * kAcross / 64; ++x) {
+                    const int sr = (x * 64 + lane) / kAcross, sc = (x * 64 + lane) % kAcross * 8;
+                    float v[8];
+                    load_vec<float, 8>(strip + sr * S::kPitch + sc, v);
+                    const int64_t j = j0 + sr, i = i0 + sc;
+                    if (j < a.b_rows && i < a.a_rows) {
+                        if (a.parts > 1) store_part<float, 8>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
+                        else finish<T, 8>(a.r, j, i, a.a_rows - i, v);
+                    }
+                }
+                wavefront_exchange();
+            }
+        }
 }
 
 // Parts of sums added up, in their order.
@@ -237,7 +421,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Produ
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] += w[q];
         }
-        finish<T>(a.r, j, i, n, v);
+        finish<T, 4>(a.r, j, i, n, v);
     }
 }
 
@@ -267,7 +451,7 @@ template <typename T, int kRows, int kEach> __global__ __launch_bounds__(256) vo
         float v[4] = {};
 #pragma unroll
         for (int e = 0; e < kEach; ++e) v[e] = group_sum<64>(sum[m][e]);
-        if (lane == m) finish<T>(r, m, i0, min((int64_t)kEach, outer - i0), v);
+        if (lane == m) finish<T, 4>(r, m, i0, min((int64_t)kEach, outer - i0), v);
     }
 }
 
@@ -360,8 +544,8 @@ template <typename T> hipError_t multiply_rows(Product p, const Plan& plan, hipS
     p.down = (int32_t)ceil_div(p.b_rows, plan.tile);
     p.parts = plan.parts;
     const dim3 grid((unsigned)((int64_t)p.across * p.down * p.parts));
-    if (plan.tile == 256) k_linear_product<T, 256, 256, 2, 4, 2><<<grid, dim3(512), 0, s>>>(p);
-    else if (plan.tile == 128) k_linear_product<T, 128, 128, 2, 2, 3><<<grid, dim3(256), 0, s>>>(p);
+    if (plan.tile == 256) k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(p);
+    else if (plan.tile == 128) k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p);
     else k_linear_product<T, 64, 64, 2, 2, 4><<<grid, dim3(256), 0, s>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
