@@ -26,32 +26,55 @@ int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 
 // ---------------------------------------------------------------------------------------------- activations
 
-__device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
+// (The instructions for 2^x and 1 / x, which are off by a step of 32 bits: a division would take ten times as long, and the epilogue of a large product
+// has nothing to hide behind.)
+__device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
 
-// (z (1 + tanh u) / 2 = z sigmoid(2 u))
-__device__ __forceinline__ float activate(float z, int32_t activation) {
-    switch (activation) {
-        case P2_RELU: return z < 0.0f ? 0.0f : z;
-        case P2_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
-        case P2_GELU_TANH: return z * sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
-        case P2_SILU: return z * sigmoid_of(z);
-        default: return z;
+template <int kActivation> __device__ __forceinline__ float activated(float z) {
+    if constexpr (kActivation == P2_RELU) return z < 0.0f ? 0.0f : z;
+    else if constexpr (kActivation == P2_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    // (z (1 + tanh u) / 2 = z sigmoid(2 u))
+    else if constexpr (kActivation == P2_GELU_TANH) return z * sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+    else if constexpr (kActivation == P2_SILU) return z * sigmoid_of(z);
+    else return z;
+}
+template <int kActivation> __device__ __forceinline__ float slope(float z) {
+    if constexpr (kActivation == P2_RELU) {
+        return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    } else if constexpr (kActivation == P2_GELU) {
+        return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
+    } else if constexpr (kActivation == P2_GELU_TANH) {
+        const float p = sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+        return p + p * (1.0f - p) * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
+    } else if constexpr (kActivation == P2_SILU) {
+        const float p = sigmoid_of(z);
+        return p * (1.0f + z * (1.0f - p));
+    } else {
+        return 1.0f;
     }
 }
-__device__ __forceinline__ float slope_of(float z, int32_t activation) {
+// One jump for all of v.
+template <int N, typename F> __device__ __forceinline__ void with_activation(int32_t activation, F&& f) {
     switch (activation) {
-        case P2_RELU: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-        case P2_GELU: return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
-        case P2_GELU_TANH: {
-            const float p = sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
-            return p + p * (1.0f - p) * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
-        }
-        case P2_SILU: {
-            const float p = sigmoid_of(z);
-            return p * (1.0f + z * (1.0f - p));
-        }
-        default: return 1.0f;
+        case P2_RELU: f(std::integral_constant<int, P2_RELU>()); break;
+        case P2_GELU: f(std::integral_constant<int, P2_GELU>()); break;
+        case P2_GELU_TANH: f(std::integral_constant<int, P2_GELU_TANH>()); break;
+        case P2_SILU: f(std::integral_constant<int, P2_SILU>()); break;
+        default: break;
     }
+}
+template <int N> __device__ __forceinline__ void activate(float (&v)[N], int32_t activation) {
+    with_activation<N>(activation, [&](auto kind) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = activated<decltype(kind)::value>(v[q]);
+    });
+}
+// v * activation'(z)
+template <int N> __device__ __forceinline__ void times_slope(float (&v)[N], const float (&z)[N], int32_t activation) {
+    with_activation<N>(activation, [&](auto kind) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] *= slope<decltype(kind)::value>(z[q]);
+    });
 }
 
 // ------------------------------------------------------------------------------------------------ results
@@ -70,9 +93,7 @@ template <typename T, int N> __device__ __forceinline__ void finish(const Result
         for (int q = 0; q < N; ++q) v[q] += b[q];
     }
     if (r.z) store_part<T, N>(static_cast<T*>(r.z) + j * r.z_stride + i, n, v);
-    if (r.activation != P2_NO_ACTIVATION)
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = activate(v[q], r.activation);
+    activate(v, r.activation);
     if (r.residual) {
         float b[N];
         load_part<T, N>(static_cast<const T*>(r.residual) + j * r.residual_stride + i, n, b, 0.0f);
@@ -477,8 +498,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Pack 
         if (a.z) {
             float z[4];
             load_part<T, 4>(static_cast<const T*>(a.z) + r * a.z_stride + c, n, z, 0.0f);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = q < n ? v[q] * slope_of(z[q], a.activation) : 0.0f;
+            times_slope(v, z, a.activation);               // (past the matrix's end 0 times the slope at 0)
         }
         if (a.straight && r < a.rows) store_part<T, 4>(reinterpret_cast<T*>(a.straight + r * a.straight_pitch) + c, a.straight_pitch / (int)sizeof(T) - c, v);
 #pragma unroll
