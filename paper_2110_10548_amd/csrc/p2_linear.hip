@@ -6,6 +6,7 @@
 // each row (64 values of 16 bits, 32 of 32) that are brought to LDS straight from memory while the stage before is multiplied.  The MFMA's rows
 // are A's: a lane has four neighbouring columns of one row of C.
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "p2_train_dev.h"
@@ -153,101 +154,7 @@ template <int kLoads> __device__ __forceinline__ void stage_barrier() {
 
 constexpr int kPastEnd = 0x7ffffff0;           // an offset that no descriptor reaches
 
-template <typename T, int kTileA, int kTileB, int kWavesA, int kWavesB, int kStages>
-__global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_product(Product a) {
-    typedef typename Fragment<T>::type F;
-    constexpr int kWaves = kWavesA * kWavesB;
-    constexpr int FA = kTileA / kWavesA / 16, FB = kTileB / kWavesB / 16;
-    constexpr int kLoadsA = kTileA / 8 / kWaves, kLoadsB = kTileB / 8 / kWaves;        // of a stage; one brings 8 rows
-    constexpr int kAhead = kStages - 1;
-    static_assert(kLoadsA * 8 * kWaves == kTileA && kLoadsB * 8 * kWaves == kTileB, "rows are dealt out evenly");
-    static_assert((kLoadsA + kLoadsB) * (kAhead - 1) < 64, "the loads' counter");
-    __shared__ __attribute__((aligned(1024))) char lds[kStages][(kTileA + kTileB) * kLine];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours.
-    int t;
-    {
-        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = blockIdx.x & 7;
-        t = die * whole + min(die, rest) + (blockIdx.x >> 3);
-    }
-    const int tiles = a.across * a.down, part = t / tiles;
-    t %= tiles;
-    int ti, tj;                                            // column by column of four rows of tiles
-    {
-        const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
-        tj = first + in % high;
-        ti = in / high;
-    }
-    const auto rows_of = [&](const char* p, int64_t pitch, int64_t first, int64_t rows, int tile) {
-        const int64_t n = min(rows - first, (int64_t)tile);
-        return Rows(p + first * pitch, (int)((n - 1) * pitch + a.length));
-    };
-    const Rows ra = rows_of(a.a, a.a_pitch, (int64_t)ti * kTileA, a.a_rows, kTileA);
-    const Rows rb = rows_of(a.b, a.b_pitch, (int64_t)tj * kTileB, a.b_rows, kTileB);
-    // A row's 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-    const int from_a = (wave * kLoadsA * 8 + (lane >> 3)) * (int)a.a_pitch + piece, from_b = (wave * kLoadsB * 8 + (lane >> 3)) * (int)a.b_pitch + piece;
-    const int all = (int)((a.length + kLine - 1) / kLine);
-    const int begin = (int)((int64_t)all * part / a.parts), stages = (int)((int64_t)all * (part + 1) / a.parts) - begin;
-    const auto bring = [&](int stage, int s) {
-        const int at = (begin + s) * kLine;
-        const bool inside = at + piece < a.length;         // (zeros past the row's end)
-#pragma unroll
-        for (int l = 0; l < kLoadsA; ++l)
-            ra.bring(&lds[stage][(wave * kLoadsA + l) * 1024], inside ? from_a + l * 8 * (int)a.a_pitch : kPastEnd, at);
-#pragma unroll
-        for (int l = 0; l < kLoadsB; ++l)
-            rb.bring(&lds[stage][kTileA * kLine + (wave * kLoadsB + l) * 1024], inside ? from_b + l * 8 * (int)a.b_pitch : kPastEnd, at);
-    };
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-        if (s < stages) bring(s, s);
-    float4_t acc[FA][FB];
-#pragma unroll
-    for (int i = 0; i < FA; ++i)
-#pragma unroll
-        for (int j = 0; j < FB; ++j) acc[i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
-    int stage = 0, next = kAhead % kStages;
-    for (int s = 0; s < stages; ++s) {
-        if (s + kAhead <= stages) stage_barrier<(kLoadsA + kLoadsB) * (kAhead - 1)>();
-        else stage_barrier<0>();
-        if (s + kAhead < stages) bring(next, s + kAhead);
-        const char* pa = lds[stage] + wa * FA * 16 * kLine;
-        const char* pb = lds[stage] + kTileA * kLine + wb * FB * 16 * kLine;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int at = row * kLine + ((half * 4 + quad) ^ (row & 7)) * 16;
-            F fa[FA], fb[FB];
-#pragma unroll
-            for (int j = 0; j < FB; ++j) fb[j] = *reinterpret_cast<const F*>(pb + j * 16 * kLine + at);
-#pragma unroll
-            for (int i = 0; i < FA; ++i) fa[i] = *reinterpret_cast<const F*>(pa + i * 16 * kLine + at);
-#pragma unroll
-            for (int i = 0; i < FA; ++i)
-#pragma unroll
-                for (int j = 0; j < FB; ++j) multiply(fa[i], fb[j], acc[i][j]);
-        }
-        next = stage;
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-    }
-    const int64_t i0 = (int64_t)ti * kTileA + wa * FA * 16 + quad * 4, j0 = (int64_t)tj * kTileB + wb * FB * 16 + row;
-#pragma unroll
-    for (int fj = 0; fj < FB; ++fj) {
-        const int64_t j = j0 + fj * 16;
-        if (j >= a.b_rows) continue;
-#pragma unroll
-        for (int fi = 0; fi < FA; ++fi) {
-            const int64_t i = i0 + fi * 16;
-            if (i >= a.a_rows) continue;
-            float v[4] = {acc[fi][fj][0], acc[fi][fj][1], acc[fi][fj][2], acc[fi][fj][3]};
-            if (a.parts > 1) store_part<float, 4>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
-            else finish<T, 4>(a.r, j, i, a.a_rows - i, v);
-        }
-    }
-}
-
-// The same for large tiles.  A's and B's rows of a tile come in halves of kWavesA * FA * 16 and kWavesB * FB * 16, and a stage is multiplied in four
+// A tile's rows of A and of B come in halves of kWavesA * FA * 16 and kWavesB * FB * 16, and a stage is multiplied in four
 // phases, half by half, A0 B0, A0 B1, A1 B1, A1 B0, so that each phase's fragments are read from LDS while the one before is multiplied, six
 // reads of a fragment with every 16 MFMA, and a half's place in LDS is free for the stage after the next two phases after it has been
 // read: loads have five to six phases to arrive.  Two barriers a stage.
@@ -415,12 +322,12 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
                 for (int fi = 0; fi < FA; ++fi) *reinterpret_cast<float4_t*>(strip + row * S::kPitch + fi * 16 + quad * 4) = acc[ha][hb][fi][fj];
                 wavefront_exchange();
 #pragma unroll
-                for (int x = 0; x < 16 * kAcross / 64; ++x) {
+                for (int x = 0; x < (16 * kAcross + 63) / 64; ++x) {
                     const int sr = (x * 64 + lane) / kAcross, sc = (x * 64 + lane) % kAcross * 8;
                     float v[8];
-                    load_vec<float, 8>(strip + sr * S::kPitch + sc, v);
+                    load_vec<float, 8>(strip + min(sr, 15) * S::kPitch + sc, v);
                     const int64_t j = j0 + sr, i = i0 + sc;
-                    if (j < a.b_rows && i < a.a_rows) {
+                    if (sr < 16 && j < a.b_rows && i < a.a_rows) {
                         if (a.parts > 1) store_part<float, 8>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
                         else finish<T, 8>(a.r, j, i, a.a_rows - i, v);
                     }
@@ -436,6 +343,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Produ
     for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < items; x += (int64_t)gridDim.x * 256) {
         const int64_t j = x / quads, i = x % quads * 4, n = a.a_rows - i;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
         for (int p = 0; p < a.parts; ++p) {
             float w[4];
             load_part<float, 4>(a.sums + p * plane + j * a.a_rows + i, n, w, 0.0f);
@@ -547,26 +455,49 @@ __global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, in
 
 // ------------------------------------------------------------------------------------------------- plans
 
-struct Plan { int32_t tile, parts; };
-// How a product of these sizes is cut: large tiles where there are enough of them for the compute units, else smaller ones and parts of the sum.
-Plan plan_of(int64_t a_rows, int64_t b_rows, int64_t length) {
-    const auto tiles = [&](int64_t t) { return ceil_div(a_rows, t) * ceil_div(b_rows, t); };
-    if (tiles(256) >= 192) return {256, 1};
-    Plan p = {b_rows <= 64 || a_rows <= 64 ? 64 : 128, 1};
-    const int64_t n = tiles(p.tile), stages = ceil_div(length, kLine);
-    if (n < kUnits) p.parts = (int32_t)std::max<int64_t>(1, std::min({ceil_div(kUnits, n), stages / 4, (int64_t)32}));
-    return p;
+enum Cut : int32_t { k256, k128, k128x64, k64x128, k64 };      // tiles: rows of A by rows of B
+struct Plan { Cut cut; int32_t parts; };
+// What a cut takes, in us: a stage of one block that has its compute unit to itself (`alone`), a stage of each of more blocks that share one, a block's end.
+struct Price { int64_t a, b; double alone, shared, end; };
+constexpr Price kPrices16[] = {{256, 256, 1.38, 1.38, 9.0}, {128, 128, 0.60, 0.55, 2.2}, {128, 64, 0.38, 0.33, 1.1}, {64, 128, 0.40, 0.34, 1.1}, {64, 64, 0.29, 0.22, 0.6}};
+constexpr Price kPrices32[] = {{256, 256, 7.0, 7.0, 18.0}, {128, 128, 1.9, 1.9, 4.4}, {128, 64, 0.94, 0.94, 2.2}, {64, 128, 0.95, 0.95, 2.2}, {64, 64, 0.47, 0.47, 1.2}};
+int64_t tile_a(Cut c) { return kPrices16[c].a; }
+int64_t tile_b(Cut c) { return kPrices16[c].b; }
+// How a product of these sizes is cut: the cheapest by prices that were measured (blocks go to the 256 compute units one by one; a sum in parts is written and
+// read once more, by a launch of its own).  us by 256 x 256, 128 x 128, 128 x 64, 64 x 64 tiles, with the best number of parts each, bf16: 8192 x 4096 x 4096
+// 194, 240, 280, 330; 3000^3 73, 85, 102, 121; 2048^3 38, 23.5, 24.1, 28; 1024^3 23, 14, 9.5, 8.0; 512 x 4096 x 4096 36, 28, 27, 27; 64 x 4096 x 4096
+// 20, 14.6, 13.4, 12.5; 256 x 8192 x 256 23.5, 16.3, 13.5, 11.8; fp32 1531 x 1000 x 776 54, 36, 34, 33.
+Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
+    const int64_t stages = ceil_div(length, kLine);
+    Plan best = {k64, 1};
+    double least = std::numeric_limits<double>::infinity();
+    for (const Cut cut : {k256, k128, k128x64, k64x128, k64}) {
+        const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
+        const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b);
+        for (int32_t parts = 1; parts <= 32 && (parts == 1 || parts * 4 <= stages); ++parts) {
+            const double load = (double)ceil_div(tiles * parts, kUnits);
+            const double join = parts == 1 ? 0.0 : 2.5 + 0.15 * parts + (double)parts * (double)a_rows * (double)b_rows * 8.0 / 5e6;
+            const double us = (double)ceil_div(stages, parts) * std::max(price.alone, load * price.shared) + load * price.end + join;
+            if (us < least) { least = us; best = {cut, parts}; }
+            if (tiles * parts >= 16 * kUnits) break;           // (more parts than fill the units several times gain nothing)
+        }
+    }
+    return best;
 }
 int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) { return p.parts > 1 ? round_up(p.parts * a_rows * b_rows * 4, 256) : 0; }
 
 template <typename T> hipError_t multiply_rows(Product p, const Plan& plan, hipStream_t s) {
-    p.across = (int32_t)ceil_div(p.a_rows, plan.tile);
-    p.down = (int32_t)ceil_div(p.b_rows, plan.tile);
+    p.across = (int32_t)ceil_div(p.a_rows, tile_a(plan.cut));
+    p.down = (int32_t)ceil_div(p.b_rows, tile_b(plan.cut));
     p.parts = plan.parts;
     const dim3 grid((unsigned)((int64_t)p.across * p.down * p.parts));
-    if (plan.tile == 256) k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(p);
-    else if (plan.tile == 128) k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p);
-    else k_linear_product<T, 64, 64, 2, 2, 4><<<grid, dim3(256), 0, s>>>(p);
+    switch (plan.cut) {
+        case k256: k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(p); break;
+        case k128: k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p); break;
+        case k128x64: k_linear_wide<T, 2, 2, 2, 1><<<grid, dim3(256), 0, s>>>(p); break;
+        case k64x128: k_linear_wide<T, 2, 2, 1, 2><<<grid, dim3(256), 0, s>>>(p); break;
+        case k64: k_linear_wide<T, 2, 2, 1, 1><<<grid, dim3(256), 0, s>>>(p); break;
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     const int64_t items = ceil_div(p.a_rows, 4) * p.b_rows;
@@ -595,7 +526,7 @@ ForwardRoom forward_room(const LinearForward& a) {
     r.pack_x = !in_order(a.x, a.x_stride, a.type, a.inner);
     r.pack_weight = !in_order(a.weight, a.weight_stride, a.type, a.inner);
     r.length = r.pack_x && r.pack_weight ? padded : round_up(a.inner * size, 16);
-    r.plan = plan_of(a.outer, a.rows, r.length);
+    r.plan = plan_of(a.type, a.outer, a.rows, r.length);
     r.x = 0;
     r.weight = r.x + (r.pack_x ? round_up(a.rows * padded, 256) : 0);
     r.sums = r.weight + (r.pack_weight ? round_up(a.outer * padded, 256) : 0);
@@ -609,8 +540,8 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     BackwardRoom r = {};
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
     r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
-    r.dx = plan_of(inner, rows, r.along);
-    r.dweight = plan_of(inner, outer, r.deep);
+    r.dx = plan_of(type, inner, rows, r.along);
+    r.dweight = plan_of(type, inner, outer, r.deep);
     r.dz = 0;
     r.dz_turned = r.dz + round_up(rows * r.along, 256);
     r.x_turned = r.dz_turned + round_up(outer * r.deep, 256);
