@@ -16,7 +16,7 @@ constexpr int kEach = 8;                       // values of a thread; 32 threads
 constexpr int kChunk = kBlock * kEach;
 constexpr int kTensors = 48;                   // kernel arguments are 4 KiB at most
 constexpr int kSumTensors = 160;
-constexpr int kSumBlocks = 1024;
+constexpr int kSumBlocks = 2048, kSumChunk = kBlock * 32, kSumAlone = 32;     // (kSumAlone chunks at most: one block of 1024 threads has them)
 static_assert(P2_STATE_BLOCK == 32 * kEach, "half a wavefront has a block of states");
 
 template <int kMost, typename Entry> struct Table {
@@ -24,14 +24,16 @@ template <int kMost, typename Entry> struct Table {
     int32_t begin[kMost + 1];                  // the first chunk of each; the last one: all of them
     int32_t n;
 };
-template <typename Tab> __device__ __forceinline__ int tensor_of(const Tab& t, int chunk) {
-    int low = 0, high = t.n - 1;
-    while (low < high) {
-        const int mid = (low + high + 1) >> 1;
-        if (t.begin[mid] <= chunk) low = mid;
-        else high = mid - 1;
+// The tensor of a chunk, the same for the whole wavefront: a look at all of them at once (a search would wait for six loads, one after the other).
+template <int kMost> __device__ __forceinline__ int tensor_of(const int32_t* begin, int n, int chunk) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int base = 0; base < kMost; base += 64) {
+        const int i = base + lane;
+        before += __popcll(__ballot(i < n && begin[min(i, n)] <= chunk));
     }
-    return low;
+    return __builtin_amdgcn_readfirstlane(before - 1);
 }
 
 struct SumEntry { const void* p; int64_t count; };
@@ -47,18 +49,55 @@ __device__ __forceinline__ double block_sum(double v, double* buf) {       // th
     return v;
 }
 
-// Squares are added up in 64 bits: gradients of any size, and no overflow before the root.
-template <typename T> __global__ __launch_bounds__(kBlock) void k_square_sum(SumTable table, double* parts) {
-    __shared__ double buf[kBlock / 64];
+// Squares are added up in 64 bits: gradients of any size, and no overflow before the root.  A block of kThreads takes chunks of kSumChunk values, four vectors a thread
+// at a time.  Where one block has all of them it writes the sum itself.
+template <typename T, int kThreads> __global__ __launch_bounds__(kThreads) void k_square_sum(SumTable table, double* parts) {
+    constexpr int V = kSumChunk / kBlock / 4;
+    __shared__ double buf[kThreads / 64];
+    // (looked up in LDS: a load from memory would have to wait for the values asked for before it)
+    __shared__ int32_t begins[kSumTensors + 1];
+    for (int i = threadIdx.x; i <= table.n; i += kThreads) begins[i] = table.begin[i];
+    __syncthreads();
     double s = 0.0;
-    const int chunks = table.begin[table.n];
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int i = tensor_of(table, c);
-        const int64_t at = (int64_t)(c - table.begin[i]) * kChunk + threadIdx.x * kEach;
-        float v[kEach];
-        load_part<T, kEach>(static_cast<const T*>(table.tensor[i].p) + at, table.tensor[i].count - at, v, 0.0f);
+    const int chunks = table.begin[table.n], each = kThreads / kBlock, x = threadIdx.x % kBlock;
+    // A chunk is asked for while the one before it is added up.
+    vec_t<T, V> next[4] = {};
+    const auto ask = [&](int c) {
+        const int i = tensor_of<kSumTensors>(begins, table.n, c);
+        const int64_t at = (int64_t)(c - table.begin[i]) * kSumChunk, left = table.tensor[i].count - at;
+        const T* p = static_cast<const T*>(table.tensor[i].p) + at;
+        if (left >= kSumChunk) {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) s += (double)v[j] * (double)v[j];
+            for (int q = 0; q < 4; ++q) next[q] = *reinterpret_cast<const vec_t<T, V>*>(p + (q * kBlock + x) * V);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t e = (q * kBlock + x) * V;
+                if (left - e >= V) {
+                    next[q] = *reinterpret_cast<const vec_t<T, V>*>(p + e);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) next[q][j] = (T)0.0f;
+                    for (int j = 0; e + j < left; ++j)
+#pragma unroll
+                        for (int w = 0; w < V; ++w)
+                            if (w == j) next[q][w] = p[e + j];
+                }
+            }
+        }
+    };
+    int c = blockIdx.x * each + threadIdx.x / kBlock;
+    if (c < chunks) ask(c);
+    while (c < chunks) {
+        vec_t<T, V> v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = next[q];
+        c += gridDim.x * each;
+        if (c < chunks) ask(c);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < V; ++j) s = fma((double)(float)v[q][j], (double)(float)v[q][j], s);
     }
     s = block_sum(s, buf);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -95,15 +134,6 @@ __global__ void k_adamw_numbers(Adamw a) {
 // follows the formula in 32 bits has the same one.
 constexpr float kLeast = 0x1p-100f;
 
-__device__ __forceinline__ float mean_of(int q, float scale) {
-#pragma clang fp contract(off)
-    return (float)(q * abs(q)) * (scale * (1.0f / 16129.0f));
-}
-__device__ __forceinline__ float square_of(int q, float scale) {
-#pragma clang fp contract(off)
-    const float r = (float)(q * q);
-    return (r * (scale * (1.0f / 65025.0f))) * (r * (1.0f / 65025.0f));
-}
 // The largest absolute value of half a wavefront's, which is a block: NaN and infinities above everything.
 __device__ __forceinline__ float block_scale(const float (&v)[kEach]) {
     uint32_t m = 0;
@@ -113,50 +143,87 @@ __device__ __forceinline__ float block_scale(const float (&v)[kEach]) {
     const float s = __uint_as_float(m);
     return s < kLeast ? 0.0f : m >= 0x7f800000u ? __builtin_nanf("") : s;
 }
-__device__ __forceinline__ int mean_stored(float v, float inverse) {
+// The number to store: the nearest one to 127 sqrt(|v| / scale) and 255 (v / scale)^(1/4), each root and product rounded to 32 bits.  The instruction for the root is
+// off by a step at most where the function's is by half of one, so that the places differ by 127 * 2.5 * 2^-23 = 3.8e-5 and 255 * 3.25 * 2^-23 = 9.9e-5 at most; where that
+// could matter, next to the middle of two numbers (one value in some 10000 and one in 4000), the wavefront works its roots out as they are defined (sqrtf: ten instructions).
+constexpr float kNearMean = 0.5f - 4e-5f, kNearSquare = 0.5f - 1.1e-4f;
+
+template <bool kExact> __device__ __forceinline__ float root_of(float v) { return kExact ? sqrtf(v) : __builtin_amdgcn_sqrtf(v); }
+template <bool kSquare, bool kExact> __device__ __forceinline__ float place_of(float v, float inverse) {
 #pragma clang fp contract(off)
-    const float q = rintf(127.0f * sqrtf(fabsf(v) * inverse));
-    return v < 0.0f ? -(int)q : (int)q;
+    const float x = fabsf(v) * inverse;
+    return kSquare ? 255.0f * root_of<kExact>(root_of<kExact>(x)) : 127.0f * root_of<kExact>(x);
 }
-__device__ __forceinline__ int square_stored(float v, float inverse) {
-#pragma clang fp contract(off)
-    const int q = (int)rintf(255.0f * sqrtf(sqrtf(v * inverse)));
-    return v > 0.0f && inverse > 0.0f ? max(q, 1) : q;
+// The numbers of eight values as bytes.
+typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(1)));
+template <bool kSquare> __device__ __forceinline__ words2 stored(const float (&v)[kEach], float inverse) {
+    float q[kEach];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const float place = place_of<kSquare, false>(v[i], inverse);
+        q[i] = __builtin_rintf(place);
+        near |= fabsf(place - q[i]) > (kSquare ? kNearSquare : kNearMean);
+    }
+    if (__any(near))
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) q[i] = __builtin_rintf(place_of<kSquare, true>(v[i], inverse));
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (kSquare) q[i] = v[i] > 0.0f ? fmaxf(q[i], 1.0f) : q[i];
+        else q[i] = copysignf(q[i], v[i]) + 128.0f;        // (bytes without a sign are made in one instruction)
+#if defined(__HIP_DEVICE_COMPILE__)
+        w[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(q[i], i % 4, w[i / 4]);
+#endif
+    }
+    const uint32_t sign = kSquare ? 0u : 0x80808080u;
+    return inverse > 0.0f ? words2{w[0] ^ sign, w[1] ^ sign} : words2{0, 0};
 }
 __device__ __forceinline__ float inverse_of(float scale) { return scale > 0.0f ? 1.0f / scale : 0.0f; }      // (0, too, where it is NaN)
 
 typedef Table<kTensors, p2_adamw_tensor> AdamwTable;
 struct AdamwConstants { float beta1, beta2, rest1, rest2, eps; int32_t copy_type; };
 
-typedef uint8_t bytes8 __attribute__((ext_vector_type(8), aligned(1)));
-
-__device__ __forceinline__ void load_bytes(const uint8_t* p, int64_t n, uint8_t (&v)[kEach]) {
-    if (n >= kEach) {
-        const bytes8 r = *reinterpret_cast<const bytes8*>(p);
+// Eight stored numbers: bytes, as two words.  Means are stored as they are, of squares without a sign.
+__device__ __forceinline__ words2 load_bytes(const void* p, int64_t n) {
+    if (n >= kEach) return *static_cast<const words2*>(p);
+    words2 r = {0, 0};
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = r[i];
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = i < n ? p[i] : 0;
+    for (int i = 0; i < kEach; ++i)
+        if (i < n) r[i / 4] |= (uint32_t)static_cast<const uint8_t*>(p)[i] << i % 4 * 8;
+    return r;
 }
-__device__ __forceinline__ void store_bytes(uint8_t* p, int64_t n, const uint8_t (&v)[kEach]) {
-    if (n >= kEach) {
-        bytes8 r;
+__device__ __forceinline__ void store_bytes(void* p, int64_t n, words2 v) {
+    if (n >= kEach) { *static_cast<words2*>(p) = v; return; }
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) r[i] = v[i];
-        *reinterpret_cast<bytes8*>(p) = r;
-        return;
+    for (int i = 0; i < kEach; ++i)
+        if (i < n) static_cast<uint8_t*>(p)[i] = (uint8_t)(v[i / 4] >> i % 4 * 8);
+}
+__device__ __forceinline__ void means_of(words2 q, float scale, float (&v)[kEach]) {
+#pragma clang fp contract(off)
+    const float unit = scale * (1.0f / 16129.0f);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const float f = (float)((q[i / 4] ^ 0x80808080u) >> i % 4 * 8 & 0xffu) - 128.0f;       // (an unsigned byte is converted in one instruction)
+        v[i] = f * fabsf(f) * unit;
     }
+}
+__device__ __forceinline__ void squares_of(words2 q, float scale, float (&v)[kEach]) {
+#pragma clang fp contract(off)
+    const float unit = scale * (1.0f / 65025.0f);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) if (i < n) p[i] = v[i];
+    for (int i = 0; i < kEach; ++i) {
+        const float f = (float)(q[i / 4] >> i % 4 * 8 & 0xffu), r = f * f;
+        v[i] = (r * unit) * (r * (1.0f / 65025.0f));
+    }
 }
 
 template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock) void k_adamw(AdamwTable table, AdamwConstants c, const AdamwStep* numbers) {
 #pragma clang fp contract(off)
     const AdamwStep step = numbers[0];
     if (step.left_out) return;
-    const int i = tensor_of(table, blockIdx.x);
+    const int i = tensor_of<kTensors>(table.begin, table.n, blockIdx.x);
     const p2_adamw_tensor& t = table.tensor[i];
     const int64_t at = (int64_t)((int)blockIdx.x - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
     float p[kEach], g[kEach], m[kEach], v[kEach];
@@ -164,26 +231,31 @@ template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock
     load_part<G, kEach>(static_cast<const G*>(t.grad) + at, left, g, 0.0f);
     const int64_t block = at / P2_STATE_BLOCK;
     if constexpr (kBits == 8) {
-        uint8_t q[kEach], r[kEach];
-        load_bytes(static_cast<const uint8_t*>(t.mean) + at, left, q);
-        load_bytes(static_cast<const uint8_t*>(t.square) + at, left, r);
+        const words2 q = load_bytes(static_cast<const uint8_t*>(t.mean) + at, left), r = load_bytes(static_cast<const uint8_t*>(t.square) + at, left);
         const float ms = left > 0 ? t.mean_scale[block] : 0.0f, ss = left > 0 ? t.square_scale[block] : 0.0f;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            m[j] = mean_of((int8_t)q[j], ms);
-            v[j] = square_of(r[j], ss);
-        }
+        means_of(q, ms, m);
+        squares_of(r, ss, v);
     } else {
         load_part<float, kEach>(static_cast<const float*>(t.mean) + at, left, m, 0.0f);
         load_part<float, kEach>(static_cast<const float*>(t.square) + at, left, v, 0.0f);
     }
+    float update[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const float d = g[j] * step.factor;
         m[j] = c.beta1 * m[j] + c.rest1 * d;
         v[j] = c.beta2 * v[j] + c.rest2 * (d * d);
-        p[j] = p[j] * step.shrink - step.rate * (m[j] / (sqrtf(v[j]) * step.root + c.eps));
     }
+    // The instructions for the root and 1 / x are off by a step each, 2^-22 of the update; they take numbers below 2^-126 for 0, which an eps makes no matter.
+    if (c.eps >= 1e-15f) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) update[j] = m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * step.root + c.eps);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) update[j] = m[j] / (sqrtf(v[j]) * step.root + c.eps);
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) p[j] = p[j] * step.shrink - step.rate * update[j];
     store_part<P, kEach>(static_cast<P*>(t.param) + at, left, p);
     if (t.copy) {
         if (c.copy_type == P2_F32) store_part<float, kEach>(static_cast<float*>(t.copy) + at, left, p);
@@ -193,12 +265,7 @@ template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock
     if constexpr (kBits == 8) {
         // (values past the tensor's end are zeros still)
         const float ms = block_scale(m), ss = block_scale(v), mi = inverse_of(ms), si = inverse_of(ss);
-        uint8_t q[kEach], r[kEach];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            q[j] = mi > 0.0f ? (uint8_t)mean_stored(m[j], mi) : 0;
-            r[j] = si > 0.0f ? (uint8_t)square_stored(v[j], si) : 0;
-        }
+        const words2 q = stored<false>(m, mi), r = stored<true>(v, si);
         store_bytes(static_cast<uint8_t*>(t.mean) + at, left, q);
         store_bytes(static_cast<uint8_t*>(t.square) + at, left, r);
         if (threadIdx.x % 32 == 0 && left > 0) { t.mean_scale[block] = ms; t.square_scale[block] = ss; }
@@ -209,25 +276,18 @@ template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock
 }
 
 __global__ __launch_bounds__(kBlock) void k_adamw_values(AdamwTable table) {
-    const int i = tensor_of(table, blockIdx.x);
+    const int i = tensor_of<kTensors>(table.begin, table.n, blockIdx.x);
     const p2_adamw_tensor& t = table.tensor[i];            // (param and copy: where the values go)
     const int64_t at = (int64_t)((int)blockIdx.x - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
     if (left <= 0) return;
     const int64_t block = at / P2_STATE_BLOCK;
-    uint8_t q[kEach];
     float x[kEach];
     if (t.param) {
-        load_bytes(static_cast<const uint8_t*>(t.mean) + at, left, q);
-        const float s = t.mean_scale[block];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) x[j] = mean_of((int8_t)q[j], s);
+        means_of(load_bytes(static_cast<const uint8_t*>(t.mean) + at, left), t.mean_scale[block], x);
         store_part<float, kEach>(static_cast<float*>(t.param) + at, left, x);
     }
     if (t.copy) {
-        load_bytes(static_cast<const uint8_t*>(t.square) + at, left, q);
-        const float s = t.square_scale[block];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) x[j] = square_of(q[j], s);
+        squares_of(load_bytes(static_cast<const uint8_t*>(t.square) + at, left), t.square_scale[block], x);
         store_part<float, kEach>(static_cast<float*>(t.copy) + at, left, x);
     }
 }
@@ -268,24 +328,29 @@ template <typename P> void step_launch(const AdamwTable& table, const AdamwConst
 
 int64_t square_sum_parts(int64_t n) { return std::max<int64_t>(1, ceil_div(n, kSumTensors)) * kSumBlocks; }
 
-hipError_t launch_square_sum(const void* const* tensors, const int64_t* counts, int64_t n, int32_t type, double* out, double* parts, hipStream_t s) {
-    int64_t lines = 0;
+template <typename T> static hipError_t square_sum(const void* const* tensors, const int64_t* counts, int64_t n, double* out, double* parts, hipStream_t s) {
+    int64_t lines = 0, chunks = 0;
+    for (int64_t i = 0; i < n; ++i) chunks += ceil_div(counts[i], kSumChunk);
+    const bool alone = chunks > 0 && chunks <= kSumAlone && n <= kSumTensors;
     const hipError_t e = in_tables<SumTable>(
         n, kSumTensors,
         [&](int64_t i, SumEntry& t) {
             t = {tensors[i], counts[i]};
-            return ceil_div(counts[i], kChunk);
+            return ceil_div(counts[i], kSumChunk);
         },
         [&](const SumTable& table) {
-            const int blocks = std::min(table.begin[table.n], kSumBlocks);
-            if (type == P2_F32) k_square_sum<float><<<dim3(blocks), dim3(kBlock), 0, s>>>(table, parts + lines);
-            else if (type == P2_BF16) k_square_sum<bf16_t><<<dim3(blocks), dim3(kBlock), 0, s>>>(table, parts + lines);
-            else k_square_sum<half_t><<<dim3(blocks), dim3(kBlock), 0, s>>>(table, parts + lines);
+            const int blocks = alone ? 1 : std::min(table.begin[table.n], kSumBlocks);
+            if (alone) k_square_sum<T, 1024><<<dim3(1), dim3(1024), 0, s>>>(table, out);
+            else k_square_sum<T, kBlock><<<dim3(blocks), dim3(kBlock), 0, s>>>(table, parts + lines);
             lines += blocks;
         });
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || alone) return e;
     k_square_join<<<dim3(1), dim3(1024), 0, s>>>(parts, lines, out);
     return hipGetLastError();
+}
+
+hipError_t launch_square_sum(const void* const* tensors, const int64_t* counts, int64_t n, int32_t type, double* out, double* parts, hipStream_t s) {
+    return type == P2_F32 ? square_sum<float>(tensors, counts, n, out, parts, s) : type == P2_BF16 ? square_sum<bf16_t>(tensors, counts, n, out, parts, s) : square_sum<half_t>(tensors, counts, n, out, parts, s);
 }
 
 hipError_t launch_adamw(const Adamw& a, hipStream_t s) {

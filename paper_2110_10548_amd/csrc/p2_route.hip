@@ -12,7 +12,7 @@ namespace p2 {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int64_t kRouteBlocks = 768;
+constexpr int64_t kRouteBlocks = 768, kBackwardBlocks = 2048;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // How a token's lanes and their values are dealt out.
@@ -543,57 +543,110 @@ template <typename T> __global__ __launch_bounds__(kBlock) void k_route_finish(R
     }
 }
 
-// The gradient.  Only the chosen experts' logits have one, but for a softmax that is not renormalised.  A token's row is put together in LDS.
-template <typename T> __global__ __launch_bounds__(64) void k_route_backward(RouteBackward a) {
-    __shared__ float row[P2_MAX_EXPERTS];
-    const int lane = threadIdx.x;
-    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
-        const T* logits = static_cast<const T*>(a.logits) + t * a.stride;
-        for (int e = lane; e < a.experts; e += 64) row[e] = 0.0f;
-        int expert = lane < a.k ? a.expert[t * a.k + lane] : -1;
-        if ((uint32_t)expert >= (uint32_t)a.experts) expert = -1;
+// The gradient.  But for a softmax that is not renormalised only the chosen experts' logits have one, and only these are read.  The choices' parts go to their
+// experts' places in a row of LDS of the token's lanes, which holds zeros otherwise and is cleared again after use; only the token's own lanes, which are of one
+// wavefront, touch that row.  (Where a token names an expert more than once its parts are added by one instruction, in the order of the lanes.)
+template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBlock) void k_route_backward(RouteBackward a, int32_t pitch) {
+    typedef Part<T, kItems> P;
+    constexpr int kTokens = kBlock / kLanes;
+    extern __shared__ float rows[];                            // [kTokens][pitch]
+    const int lane = threadIdx.x % kLanes;
+    float* slots = rows + threadIdx.x / kLanes * pitch;
+    P part;
+    part.first = 0;
+    part.size = a.experts;
+    part.lane = lane;
+    part.lanes = kLanes;
+    part.there = true;
+    const bool dense = a.score == P2_SOFTMAX && !a.renormalise;
+    for (int e = lane; e < a.experts; e += kLanes) slots[e] = 0.0f;
+    wavefront_exchange();
+    const int64_t stride = (int64_t)gridDim.x * kTokens;
+    // A token's choices, and the row where it is needed, are asked for while the one before it is worked on.
+    int next_expert = -1;
+    float next_dgate = 0.0f, next_z = 0.0f;
+    const auto row_of = [&](int64_t t) { return static_cast<const T*>(a.logits) + t * a.stride; };
+    const auto ask = [&](int64_t t) {
+        const int64_t at = min(t, a.tokens - 1) * a.k + min(lane, a.k - 1);
+        const int e = a.expert[at];
+        next_expert = lane < a.k && (uint32_t)e < (uint32_t)a.experts ? e : -1;
+        next_dgate = a.dgate[at];
+        if (dense) part.load(row_of(min(t, a.tokens - 1)));
+    };
+    const auto ask_logit = [&](int64_t t) { next_z = (float)row_of(min(t, a.tokens - 1))[max(next_expert, 0)]; };
+    const int64_t start = (int64_t)blockIdx.x * kTokens + threadIdx.x / kLanes;
+    if (start - threadIdx.x / kLanes >= a.tokens) return;
+    ask(start);
+    ask_logit(start);
+    for (int64_t t0 = start - threadIdx.x / kLanes; t0 < a.tokens; t0 += stride) {
+        const int64_t t = t0 + threadIdx.x / kLanes;
+        const int expert = next_expert;
         const bool valid = expert >= 0;
-        const bool on = __any(valid);
-        const float z = valid ? (float)logits[expert] : -INFINITY;
-        float d = valid ? a.dgate[t * a.k + lane] * a.scale : 0.0f;
-        T* out = static_cast<T*>(a.dlogits) + t * a.dlogits_stride;
-        __syncthreads();
-        if (a.score == P2_SOFTMAX && !a.renormalise) {
-            float m = -INFINITY, s = 0.0f;
-            for (int e = lane; e < a.experts; e += 64) m = fmaxf(m, (float)logits[e]);
-            m = group_max<64>(m);
-            for (int e = lane; e < a.experts; e += 64) s += expf((float)logits[e] - m);
-            s = group_sum<64>(s);
-            if (valid) atomicAdd(&row[expert], d);
-            const float dot = group_sum<64>(valid ? expf(z - m) / s * d : 0.0f);
-            __syncthreads();
-            for (int e = lane; e < a.experts; e += 64) {
-                const float p = expf((float)logits[e] - m) / s;
-                out[e] = (T)(on ? p * (row[e] - dot) : 0.0f);
+        const float z = valid ? next_z : -INFINITY;
+        float d = valid ? next_dgate * a.scale : 0.0f;
+        float o[kItems];
+        if (dense)
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) o[i] = (float)part.raw[i / P::V][i % P::V];
+        if (t0 + stride < a.tokens) ask(t + stride);
+        float dot = 0.0f, add = d;
+        if (dense) {
+            // e^(v - m) as 2^(v log2e - m log2e): what the rounding of the second product is off by is common to the row
+            float m = o[0], s = 0.0f;
+#pragma unroll
+            for (int i = 1; i < kItems; ++i) m = fmaxf(m, o[i]);
+            m = group_max<kLanes>(m);
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                o[i] = __builtin_amdgcn_exp2f((o[i] - m) * kLog2e);
+                s += part.mine(i) ? o[i] : 0.0f;
             }
+            const float inv = 1.0f / group_sum<kLanes>(s);
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) o[i] *= inv;
+            dot = group_sum<kLanes>(valid ? __builtin_amdgcn_exp2f((z - m) * kLog2e) * inv * d : 0.0f);
         } else {
             float w = 1.0f, slope = 1.0f;
+            const float far = expf(-fabsf(z)), base = __builtin_amdgcn_rcpf(1.0f + far);
             if (a.score == P2_SIGMOID) {
-                const float far = expf(-fabsf(z)), base = 1.0f / (1.0f + far);
-                slope = z > 0.0f ? far * base : base;           // 1 - s
-                w = z > 0.0f ? base : far * base;               // s
-                if (a.renormalise) {
-                    const float m = group_max<64>(fminf(z, 0.0f));
-                    w = expf(fminf(z, 0.0f) - m) * base;
-                }
-            } else {
-                w = expf(z - group_max<64>(z));
+                slope = z > 0.0f ? far * base : base;          // 1 - s
+                w = z > 0.0f ? base : far * base;              // s
             }
-            if (!valid) w = 0.0f;
-            if (a.renormalise && on) {
-                w = w / group_sum<64>(w);
-                d -= group_sum<64>(w * d);
+            if (a.renormalise) {
+                const float under = a.score == P2_SIGMOID ? fminf(z, 0.0f) : z, m = group_max<kLanes>(under);
+                w = valid ? expf(under - m) * (a.score == P2_SIGMOID ? base : 1.0f) : 0.0f;
+                const float sum = group_sum<kLanes>(w);
+                w = w / (sum == 0.0f ? 1.0f : sum);            // (no choices: 0)
+                d -= group_sum<kLanes>(w * d);
             }
-            if (valid) atomicAdd(&row[expert], w * slope * d);
-            __syncthreads();
-            for (int e = lane; e < a.experts; e += 64) out[e] = (T)row[e];
+            add = w * slope * d;
         }
-        __syncthreads();
+        if (valid) atomicAdd(&slots[expert], add);
+        wavefront_exchange();
+        const bool on = group_reduce<kLanes>((uint32_t)valid, most_of) != 0;
+        if (t0 + stride < a.tokens) ask_logit(t + stride);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const float u = slots[min(part.place(i), a.experts - 1)];
+            o[i] = dense ? (on ? o[i] * (u - dot) : 0.0f) : u;
+        }
+        wavefront_exchange();
+        if (valid) slots[expert] = 0.0f;
+        wavefront_exchange();
+        if (t < a.tokens) {
+            T* out = static_cast<T*>(a.dlogits) + t * a.dlogits_stride;
+#pragma unroll
+            for (int q = 0; q < kItems / P::V; ++q) {
+                float v[P::V];
+#pragma unroll
+                for (int j = 0; j < P::V; ++j) v[j] = o[q * P::V + j];
+                if (a.experts >= P::V) {
+                    if (part.at(q * P::V) < a.experts) store_vec<T, P::V>(out + part.place(q * P::V), v);
+                } else {
+                    store_part<T, P::V>(out + part.at(q * P::V), a.experts - part.at(q * P::V), v);
+                }
+            }
+        }
     }
 }
 
@@ -649,6 +702,23 @@ template <typename T> hipError_t route(const RouteForward& a, const Shape& shape
     return hipGetLastError();
 }
 
+#define P2_ROUTE_BACKWARD_CASE(LANES, ITEMS) \
+    case LANES * 64 + ITEMS: k_route_backward<T, LANES, ITEMS><<<grid, dim3(kBlock), room, s>>>(a, pitch); break;
+template <typename T> void backward(const RouteBackward& a, const Shape& shape, dim3 grid, size_t room, int32_t pitch, hipStream_t s) {
+    switch (shape.lanes * 64 + shape.items) {                  // (what shape_of gives for one group)
+        P2_ROUTE_BACKWARD_CASE(1, 8)
+        P2_ROUTE_BACKWARD_CASE(2, 8)
+        P2_ROUTE_BACKWARD_CASE(4, 8)
+        P2_ROUTE_BACKWARD_CASE(8, 8)
+        P2_ROUTE_BACKWARD_CASE(16, 8)
+        P2_ROUTE_BACKWARD_CASE(32, 8)
+        P2_ROUTE_BACKWARD_CASE(64, 8)
+        P2_ROUTE_BACKWARD_CASE(16, 16)
+        P2_ROUTE_BACKWARD_CASE(32, 16)
+        P2_ROUTE_BACKWARD_CASE(64, 16)
+    }
+}
+
 }  // namespace
 
 int64_t route_forward_blocks(int64_t tokens, int32_t experts, int32_t k, int32_t groups) { return blocks_of(tokens, shape_of(experts, k, groups)); }
@@ -661,10 +731,13 @@ hipError_t launch_route_forward(const RouteForward& a, hipStream_t s) {
 
 hipError_t launch_route_backward(const RouteBackward& a, hipStream_t s) {
     if (a.tokens == 0) return hipSuccess;
-    const dim3 grid((unsigned)std::min<int64_t>(a.tokens, 8192));
-    if (a.type == P2_F32) k_route_backward<float><<<grid, dim3(64), 0, s>>>(a);
-    else if (a.type == P2_BF16) k_route_backward<bf16_t><<<grid, dim3(64), 0, s>>>(a);
-    else k_route_backward<half_t><<<grid, dim3(64), 0, s>>>(a);
+    const Shape shape = shape_of(a.experts, a.k, 1);
+    const int32_t pitch = a.experts + 4;
+    const dim3 grid((unsigned)std::min(ceil_div(a.tokens, kBlock / shape.lanes), kBackwardBlocks));
+    const size_t room = (size_t)(kBlock / shape.lanes) * pitch * sizeof(float);
+    if (a.type == P2_F32) backward<float>(a, shape, grid, room, pitch, s);
+    else if (a.type == P2_BF16) backward<bf16_t>(a, shape, grid, room, pitch, s);
+    else backward<half_t>(a, shape, grid, room, pitch, s);
     return hipGetLastError();
 }
 
