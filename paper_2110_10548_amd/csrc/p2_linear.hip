@@ -46,7 +46,8 @@ template <int kActivation> __device__ __forceinline__ float slope(float z) {
         return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
     } else if constexpr (kActivation == P2_GELU_TANH) {
         const float p = sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
-        return p + p * (1.0f - p) * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
+        const float flat = p * (1.0f - p);                 // (0 far out, where what it is multiplied by may be infinite)
+        return flat == 0.0f ? p : p + flat * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
     } else if constexpr (kActivation == P2_SILU) {
         const float p = sigmoid_of(z);
         return p * (1.0f + z * (1.0f - p));
@@ -116,6 +117,8 @@ struct Product {
     int32_t across, down, parts;       // tiles of A's and of B's rows, parts of the length
     Result r;
 };
+// Products of one launch: the first has the first `blocks` blocks.
+struct Products { Product p[2]; int32_t blocks; };
 
 // 16 bytes of a row a lane: products of what 16 lanes x 4 have.
 __device__ __forceinline__ void multiply(const half8& p, const half8& q, float4_t& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, c, 0, 0, 0); }
@@ -175,7 +178,10 @@ __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t 
 }
 __device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 
-template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Product a) {
+template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
+    const bool second = (int)blockIdx.x >= all_of.blocks;
+    const Product& a = all_of.p[__builtin_amdgcn_readfirstlane(second ? 1 : 0)];
+    const int block = (int)blockIdx.x - (second ? all_of.blocks : 0), blocks = second ? (int)gridDim.x - all_of.blocks : all_of.blocks;
     typedef Tile<T, kWavesA, kWavesB, FA, FB> S;
     typedef typename S::F F;
     constexpr int LA = S::kLoadsA, LB = S::kLoadsB, kBoth = 2 * (LA + LB);
@@ -184,8 +190,8 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours.
     int t;
     {
-        const int whole = gridDim.x / 8, rest = gridDim.x % 8, die = blockIdx.x & 7;
-        t = die * whole + min(die, rest) + (blockIdx.x >> 3);
+        const int whole = blocks / 8, rest = blocks % 8, die = block & 7;
+        t = die * whole + min(die, rest) + (block >> 3);
     }
     const int tiles = a.across * a.down, part = t / tiles;
     t %= tiles;
@@ -337,21 +343,51 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
         }
 }
 
-// Parts of sums added up, in their order.
-template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Product a) {
-    const int64_t quads = (a.a_rows + 3) / 4, items = quads * a.b_rows, plane = a.a_rows * a.b_rows;
-    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < items; x += (int64_t)gridDim.x * 256) {
-        const int64_t j = x / quads, i = x % quads * 4, n = a.a_rows - i;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int p = 0; p < a.parts; ++p) {
-            float w[4];
-            load_part<float, 4>(a.sums + p * plane + j * a.a_rows + i, n, w, 0.0f);
+// What is left of a call's products: parts of sums added up, in their order, and the tiles' lines of dbias, 16 columns a block and 16 threads a column.
+struct Join {
+    Product p[2];
+    const float* lines; void* out;             // [n][cols]
+    int64_t n, cols;
+    int32_t blocks[2];                         // of each product
+    int32_t type;
+};
+template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Join all) {
+    __shared__ float part[16][17];
+    int block = blockIdx.x;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] += w[q];
+    for (int which = 0; which < 2; ++which) {
+        const Product& a = all.p[which];
+        const int blocks = all.blocks[which];
+        if (block < blocks) {
+            const int64_t quads = (a.a_rows + 3) / 4, items = quads * a.b_rows, plane = a.a_rows * a.b_rows;
+            for (int64_t x = (int64_t)block * 256 + threadIdx.x; x < items; x += (int64_t)blocks * 256) {
+                const int64_t j = x / quads, i = x % quads * 4, n = a.a_rows - i;
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                for (int p = 0; p < a.parts; ++p) {
+                    float w[4];
+                    load_part<float, 4>(a.sums + p * plane + j * a.a_rows + i, n, w, 0.0f);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] += w[q];
+                }
+                finish<T, 4>(a.r, j, i, n, v);
+            }
+            return;
         }
-        finish<T, 4>(a.r, j, i, n, v);
+        block -= blocks;
     }
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int64_t c = (int64_t)block * 16 + x;
+    float s = 0.0f;
+    if (c < all.cols)
+#pragma unroll 4
+        for (int64_t l = y; l < all.n; l += 16) s += all.lines[l * all.cols + c];
+    part[y][x] = s;
+    __syncthreads();
+    if (y > 0 || c >= all.cols) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += part[i][x];
+    store_typed(all.out, all.type, c, s);
 }
 
 // A few rows of x against all of the weight's, which are read once: a wavefront takes kEach of them at a time.
@@ -394,9 +430,14 @@ struct Pack {
     int64_t rows, cols;
     int32_t activation;
 };
-template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Pack a) {
+// Several matrices in one launch: the m-th has the blocks from begin[m] on, across[m] of them side by side.
+struct Packs { Pack p[3]; int32_t begin[4], across[3]; };
+template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs all) {
     __shared__ float tile[64][65];
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int m = (int)blockIdx.x >= all.begin[2] ? 2 : (int)blockIdx.x >= all.begin[1] ? 1 : 0;
+    const Pack& a = all.p[__builtin_amdgcn_readfirstlane(m)];
+    const int block = (int)blockIdx.x - all.begin[m], line = block / all.across[m];
+    const int64_t r0 = (int64_t)line * 64, c0 = (int64_t)(block % all.across[m]) * 64;
     const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -428,25 +469,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Pack 
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < 64; ++i) s += tile[i][threadIdx.x];
-        a.sums[(int64_t)blockIdx.y * a.cols + c0 + threadIdx.x] = s;
+        a.sums[(int64_t)line * a.cols + c0 + threadIdx.x] = s;
     }
-}
-
-// Adds up the tiles' lines: 64 columns a block, 16 threads each.
-__global__ __launch_bounds__(1024) void k_linear_sums(const float* lines, int64_t n, int64_t cols, void* out, int32_t type) {
-    __shared__ float part[16][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + x;
-    float s = 0.0f;
-    if (c < cols)
-#pragma unroll 4
-        for (int64_t l = y; l < n; l += 16) s += lines[l * cols + c];
-    part[y][x] = s;
-    __syncthreads();
-    if (y > 0 || c >= cols) return;
-#pragma unroll
-    for (int i = 1; i < 16; ++i) s += part[i][x];
-    store_typed(out, type, c, s);
 }
 
 __global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, int64_t stride, int64_t rows, int64_t cols) {
@@ -456,6 +480,7 @@ __global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, in
 // ------------------------------------------------------------------------------------------------- plans
 
 enum Cut : int32_t { k256, k128, k128x64, k64x128, k64 };      // tiles: rows of A by rows of B
+constexpr Cut kCuts[] = {k256, k128, k128x64, k64x128, k64};
 struct Plan { Cut cut; int32_t parts; };
 // What a cut takes, in us: a stage of one block that has its compute unit to itself (`alone`), a stage of each of more blocks that share one, a block's end.
 struct Price { int64_t a, b; double alone, shared, end; };
@@ -467,47 +492,90 @@ int64_t tile_b(Cut c) { return kPrices16[c].b; }
 // read once more, by a launch of its own).  us by 256 x 256, 128 x 128, 128 x 64, 64 x 64 tiles, with the best number of parts each, bf16: 8192 x 4096 x 4096
 // 194, 240, 280, 330; 3000^3 73, 85, 102, 121; 2048^3 38, 23.5, 24.1, 28; 1024^3 23, 14, 9.5, 8.0; 512 x 4096 x 4096 36, 28, 27, 27; 64 x 4096 x 4096
 // 20, 14.6, 13.4, 12.5; 256 x 8192 x 256 23.5, 16.3, 13.5, 11.8; fp32 1531 x 1000 x 776 54, 36, 34, 33.
-Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
+struct Offer { double us; int32_t parts; };
+Offer offer_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
     const int64_t stages = ceil_div(length, kLine);
-    Plan best = {k64, 1};
-    double least = std::numeric_limits<double>::infinity();
-    for (const Cut cut : {k256, k128, k128x64, k64x128, k64}) {
-        const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
-        const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b);
-        for (int32_t parts = 1; parts <= 32 && (parts == 1 || parts * 4 <= stages); ++parts) {
-            const double load = (double)ceil_div(tiles * parts, kUnits);
-            const double join = parts == 1 ? 0.0 : 2.5 + 0.15 * parts + (double)parts * (double)a_rows * (double)b_rows * 8.0 / 5e6;
-            const double us = (double)ceil_div(stages, parts) * std::max(price.alone, load * price.shared) + load * price.end + join;
-            if (us < least) { least = us; best = {cut, parts}; }
-            if (tiles * parts >= 16 * kUnits) break;           // (more parts than fill the units several times gain nothing)
-        }
+    const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
+    const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b);
+    Offer best = {std::numeric_limits<double>::infinity(), 1};
+    for (int32_t parts = 1; parts <= 32 && (parts == 1 || parts * 4 <= stages); ++parts) {
+        const double load = (double)ceil_div(tiles * parts, kUnits);
+        const double join = parts == 1 ? 0.0 : 2.5 + 0.15 * parts + (double)parts * (double)a_rows * (double)b_rows * 8.0 / 5e6;
+        const double us = (double)ceil_div(stages, parts) * std::max(price.alone, load * price.shared) + load * price.end + join;
+        if (us < best.us) best = {us, parts};
+        if (tiles * parts >= 16 * kUnits) break;               // (more parts than fill the units several times gain nothing)
     }
     return best;
 }
+Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
+    Plan best = {k64, 1};
+    double least = std::numeric_limits<double>::infinity();
+    for (const Cut cut : kCuts) {
+        const Offer o = offer_of(cut, type, a_rows, b_rows, length);
+        if (o.us < least) { least = o.us; best = {cut, o.parts}; }
+    }
+    return best;
+}
+// Two products of one launch have one cut.
+void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1, int64_t b1, int64_t length1, Plan& p0, Plan& p1) {
+    double least = std::numeric_limits<double>::infinity();
+    for (const Cut cut : kCuts) {
+        const Offer o = offer_of(cut, type, a0, b0, length0), q = offer_of(cut, type, a1, b1, length1);
+        if (o.us + q.us < least) { least = o.us + q.us; p0 = {cut, o.parts}; p1 = {cut, q.parts}; }
+    }
+}
 int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) { return p.parts > 1 ? round_up(p.parts * a_rows * b_rows * 4, 256) : 0; }
 
-template <typename T> hipError_t multiply_rows(Product p, const Plan& plan, hipStream_t s) {
-    p.across = (int32_t)ceil_div(p.a_rows, tile_a(plan.cut));
-    p.down = (int32_t)ceil_div(p.b_rows, tile_b(plan.cut));
-    p.parts = plan.parts;
-    const dim3 grid((unsigned)((int64_t)p.across * p.down * p.parts));
-    switch (plan.cut) {
-        case k256: k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(p); break;
-        case k128: k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p); break;
-        case k128x64: k_linear_wide<T, 2, 2, 2, 1><<<grid, dim3(256), 0, s>>>(p); break;
-        case k64x128: k_linear_wide<T, 2, 2, 1, 2><<<grid, dim3(256), 0, s>>>(p); break;
-        case k64: k_linear_wide<T, 2, 2, 1, 1><<<grid, dim3(256), 0, s>>>(p); break;
+// One product, or two of one cut; and the columns' sums of `join` where it has lines.
+template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int n, Join join, hipStream_t s) {
+    Products all = {};
+    int64_t blocks = 0, joined = 0;
+    for (int i = 0; i < n; ++i) {
+        p[i].across = (int32_t)ceil_div(p[i].a_rows, tile_a(plan[i].cut));
+        p[i].down = (int32_t)ceil_div(p[i].b_rows, tile_b(plan[i].cut));
+        p[i].parts = plan[i].parts;
+        all.p[i] = p[i];
+        blocks += (int64_t)p[i].across * p[i].down * p[i].parts;
+        if (i == 0) all.blocks = (int32_t)blocks;
+        if (p[i].parts > 1) {
+            join.p[i] = p[i];
+            join.blocks[i] = (int32_t)std::min<int64_t>(ceil_div(ceil_div(p[i].a_rows, 4) * p[i].b_rows, 256), 4096);
+            joined += join.blocks[i];
+        }
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.parts == 1) return e;
-    const int64_t items = ceil_div(p.a_rows, 4) * p.b_rows;
-    k_linear_join<T><<<dim3((unsigned)std::min<int64_t>(ceil_div(items, 256), 4096)), dim3(256), 0, s>>>(p);
+    if (n > 0) {
+        const dim3 grid((unsigned)blocks);
+        switch (plan[0].cut) {
+            case k256: k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(all); break;
+            case k128: k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(all); break;
+            case k128x64: k_linear_wide<T, 2, 2, 2, 1><<<grid, dim3(256), 0, s>>>(all); break;
+            case k64x128: k_linear_wide<T, 2, 2, 1, 2><<<grid, dim3(256), 0, s>>>(all); break;
+            case k64: k_linear_wide<T, 2, 2, 1, 1><<<grid, dim3(256), 0, s>>>(all); break;
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (join.lines) joined += ceil_div(join.cols, 16);
+    if (joined == 0) return hipSuccess;
+    k_linear_join<T><<<dim3((unsigned)joined), dim3(256), 0, s>>>(join);
     return hipGetLastError();
 }
 
-template <typename T> hipError_t pack(const Pack& a, hipStream_t s) {
-    const int64_t cols = a.straight ? std::max<int64_t>(a.cols, a.straight_pitch / sizeof(T)) : a.cols, rows = a.turned ? std::max<int64_t>(a.rows, a.turned_pitch / sizeof(T)) : a.rows;
-    k_linear_pack<T><<<dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64)), dim3(256), 0, s>>>(a);
+// Up to three matrices.
+template <typename T> hipError_t pack(const Pack* a, int n, hipStream_t s) {
+    Packs all = {};
+    int64_t blocks = 0;
+    for (int m = 0; m < 3; ++m) {
+        all.begin[m] = (int32_t)blocks;
+        if (m >= n) continue;
+        const int64_t cols = a[m].straight ? std::max<int64_t>(a[m].cols, a[m].straight_pitch / sizeof(T)) : a[m].cols;
+        const int64_t rows = a[m].turned ? std::max<int64_t>(a[m].rows, a[m].turned_pitch / sizeof(T)) : a[m].rows;
+        all.p[m] = a[m];
+        all.across[m] = (int32_t)ceil_div(cols, 64);
+        blocks += all.across[m] * ceil_div(rows, 64);
+    }
+    if (blocks == 0) return hipSuccess;
+    k_linear_pack<T><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(all);
     return hipGetLastError();
 }
 
@@ -534,21 +602,21 @@ ForwardRoom forward_room(const LinearForward& a) {
     return r;
 }
 
-struct BackwardRoom { Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, bytes; };
+struct BackwardRoom { Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
 BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     const int64_t size = (int64_t)type_bytes(type);
     BackwardRoom r = {};
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
     r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
-    r.dx = plan_of(type, inner, rows, r.along);
-    r.dweight = plan_of(type, inner, outer, r.deep);
+    plan_both(type, inner, rows, r.along, inner, outer, r.deep, r.dx, r.dweight);
     r.dz = 0;
     r.dz_turned = r.dz + round_up(rows * r.along, 256);
     r.x_turned = r.dz_turned + round_up(outer * r.deep, 256);
     r.weight_turned = r.x_turned + round_up(inner * r.deep, 256);
     r.lines = r.weight_turned + round_up(inner * r.along, 256);
     r.sums = r.lines + round_up(ceil_div(rows, 64) * outer * 4, 256);
-    r.bytes = r.sums + std::max(sums_bytes(r.dx, inner, rows), sums_bytes(r.dweight, inner, outer));
+    r.more_sums = r.sums + sums_bytes(r.dx, inner, rows);
+    r.bytes = r.more_sums + sums_bytes(r.dweight, inner, outer);
     return r;
 }
 
@@ -574,79 +642,79 @@ template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) 
     p.a_pitch = a.weight_stride * (int64_t)sizeof(T);
     p.b = static_cast<const char*>(a.x);
     p.b_pitch = a.x_stride * (int64_t)sizeof(T);
-    Pack k = {};
-    k.straight_pitch = padded;
-    k.cols = a.inner;
+    Pack k[2] = {};
+    int packs = 0;
     if (room.pack_x) {
-        k.from = a.x; k.from_stride = a.x_stride; k.rows = a.rows; k.straight = a.workspace + room.x;
-        const hipError_t e = pack<T>(k, s);
-        if (e != hipSuccess) return e;
-        p.b = k.straight;
+        k[packs].from = a.x; k[packs].from_stride = a.x_stride; k[packs].rows = a.rows;
+        p.b = k[packs++].straight = a.workspace + room.x;
         p.b_pitch = padded;
     }
     if (room.pack_weight) {
-        k.from = a.weight; k.from_stride = a.weight_stride; k.rows = a.outer; k.straight = a.workspace + room.weight;
-        const hipError_t e = pack<T>(k, s);
-        if (e != hipSuccess) return e;
-        p.a = k.straight;
+        k[packs].from = a.weight; k[packs].from_stride = a.weight_stride; k[packs].rows = a.outer;
+        p.a = k[packs++].straight = a.workspace + room.weight;
         p.a_pitch = padded;
     }
+    for (int i = 0; i < packs; ++i) { k[i].straight_pitch = padded; k[i].cols = a.inner; }
+    const hipError_t e = pack<T>(k, packs, s);
+    if (e != hipSuccess) return e;
     p.a_rows = a.outer; p.b_rows = a.rows; p.length = room.length;
     p.sums = reinterpret_cast<float*>(a.workspace + room.sums);
     p.r = r;
-    return multiply_rows<T>(p, room.plan, s);
+    return multiply_rows<T>(&p, &room.plan, 1, Join(), s);
 }
 
 template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s) {
     const BackwardRoom room = backward_room(a.type, a.rows, a.inner, a.outer);
     const bool own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
-    hipError_t e = hipSuccess;
-    Pack k = {};
-    k.from = a.dy; k.from_stride = a.dy_stride;
-    if (a.activation != P2_NO_ACTIVATION) { k.z = a.z; k.z_stride = a.z_stride; }
-    k.rows = a.rows; k.cols = a.outer; k.activation = a.activation;
-    if (a.dx && own_dz) { k.straight = a.workspace + room.dz; k.straight_pitch = room.along; }
-    if (a.dweight) { k.turned = a.workspace + room.dz_turned; k.turned_pitch = room.deep; }
-    if (a.dbias) k.sums = reinterpret_cast<float*>(a.workspace + room.lines);
-    if (k.straight || k.turned || k.sums) e = pack<T>(k, s);
-    if (e != hipSuccess) return e;
-    if (a.dbias) {
-        k_linear_sums<<<dim3((unsigned)ceil_div(a.outer, 64)), dim3(1024), 0, s>>>(k.sums, ceil_div(a.rows, 64), a.outer, a.dbias, a.weight_type);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    Product p = {};
-    p.sums = reinterpret_cast<float*>(a.workspace + room.sums);
+    Pack k[3] = {};
+    int packs = 0;
+    Pack& dz = k[packs];
+    dz.from = a.dy; dz.from_stride = a.dy_stride;
+    if (a.activation != P2_NO_ACTIVATION) { dz.z = a.z; dz.z_stride = a.z_stride; }
+    dz.rows = a.rows; dz.cols = a.outer; dz.activation = a.activation;
+    if (a.dx && own_dz) { dz.straight = a.workspace + room.dz; dz.straight_pitch = room.along; }
+    if (a.dweight) { dz.turned = a.workspace + room.dz_turned; dz.turned_pitch = room.deep; }
+    if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + room.lines);
+    if (dz.straight || dz.turned || dz.sums) ++packs;
+    Product p[2] = {};
+    Plan plan[2];
+    int products = 0;
     if (a.dx) {
-        Pack w = {};
+        Pack& w = k[packs++];
+        w = Pack();
         w.from = a.weight; w.from_stride = a.weight_stride; w.rows = a.outer; w.cols = a.inner;
         w.turned = a.workspace + room.weight_turned; w.turned_pitch = room.along;
-        e = pack<T>(w, s);
-        if (e != hipSuccess) return e;
-        p.a = w.turned; p.a_pitch = room.along; p.a_rows = a.inner;
-        p.b = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
-        p.b_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
-        p.b_rows = a.rows;
-        p.length = own_dz ? room.along : a.outer * (int64_t)sizeof(T);
-        p.r = {};
-        p.r.y = a.dx; p.r.y_stride = a.dx_stride; p.r.y_type = a.type;
-        e = multiply_rows<T>(p, room.dx, s);
-        if (e != hipSuccess) return e;
+        Product& q = p[products];
+        q.a = w.turned; q.a_pitch = room.along; q.a_rows = a.inner;
+        q.b = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
+        q.b_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
+        q.b_rows = a.rows;
+        q.length = own_dz ? room.along : a.outer * (int64_t)sizeof(T);
+        q.sums = reinterpret_cast<float*>(a.workspace + room.sums);
+        q.r.y = a.dx; q.r.y_stride = a.dx_stride; q.r.y_type = a.type;
+        plan[products++] = room.dx;
     }
     if (a.dweight) {
-        Pack x = {};
+        Pack& x = k[packs++];
+        x = Pack();
         x.from = a.x; x.from_stride = a.x_stride; x.rows = a.rows; x.cols = a.inner;
         x.turned = a.workspace + room.x_turned; x.turned_pitch = room.deep;
-        e = pack<T>(x, s);
-        if (e != hipSuccess) return e;
-        p.a = x.turned; p.a_pitch = room.deep; p.a_rows = a.inner;
-        p.b = a.workspace + room.dz_turned; p.b_pitch = room.deep; p.b_rows = a.outer;
-        p.length = room.deep;
-        p.r = {};
-        p.r.y = a.dweight; p.r.y_stride = a.dweight_stride; p.r.y_type = a.weight_type;
-        e = multiply_rows<T>(p, room.dweight, s);
+        Product& q = p[products];
+        q.a = x.turned; q.a_pitch = room.deep; q.a_rows = a.inner;
+        q.b = a.workspace + room.dz_turned; q.b_pitch = room.deep; q.b_rows = a.outer;
+        q.length = room.deep;
+        q.sums = reinterpret_cast<float*>(a.workspace + room.more_sums);
+        q.r.y = a.dweight; q.r.y_stride = a.dweight_stride; q.r.y_type = a.weight_type;
+        plan[products++] = room.dweight;
     }
-    return e;
+    const hipError_t e = pack<T>(k, packs, s);
+    if (e != hipSuccess) return e;
+    Join join = {};
+    if (a.dbias) {
+        join.lines = dz.sums; join.n = ceil_div(a.rows, 64); join.cols = a.outer;
+        join.out = a.dbias; join.type = a.weight_type;
+    }
+    return multiply_rows<T>(p, plan, products, join, s);
 }
 
 }  // namespace
