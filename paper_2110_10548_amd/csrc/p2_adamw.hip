@@ -219,13 +219,11 @@ __device__ __forceinline__ void squares_of(words2 q, float scale, float (&v)[kEa
     }
 }
 
-template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock) void k_adamw(AdamwTable table, AdamwConstants c, const AdamwStep* numbers) {
+template <typename P, typename G, int kBits> __device__ __forceinline__ void adamw_chunk(const AdamwTable& table, const AdamwConstants& c, const AdamwStep& step, int chunk) {
 #pragma clang fp contract(off)
-    const AdamwStep step = numbers[0];
-    if (step.left_out) return;
-    const int i = tensor_of<kTensors>(table.begin, table.n, blockIdx.x);
+    const int i = tensor_of<kTensors>(table.begin, table.n, chunk);
     const p2_adamw_tensor& t = table.tensor[i];
-    const int64_t at = (int64_t)((int)blockIdx.x - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
+    const int64_t at = (int64_t)(chunk - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
     float p[kEach], g[kEach], m[kEach], v[kEach];
     load_part<P, kEach>(static_cast<const P*>(t.param) + at, left, p, 0.0f);
     load_part<G, kEach>(static_cast<const G*>(t.grad) + at, left, g, 0.0f);
@@ -275,10 +273,16 @@ template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock
     }
 }
 
-__global__ __launch_bounds__(kBlock) void k_adamw_values(AdamwTable table) {
-    const int i = tensor_of<kTensors>(table.begin, table.n, blockIdx.x);
+template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock) void k_adamw(AdamwTable table, AdamwConstants c, const AdamwStep* numbers) {
+    const AdamwStep step = numbers[0];
+    if (step.left_out) return;
+    for (int chunk = blockIdx.x; chunk < table.begin[table.n]; chunk += gridDim.x) adamw_chunk<P, G, kBits>(table, c, step, chunk);
+}
+
+__device__ __forceinline__ void values_of_chunk(const AdamwTable& table, int chunk) {
+    const int i = tensor_of<kTensors>(table.begin, table.n, chunk);
     const p2_adamw_tensor& t = table.tensor[i];            // (param and copy: where the values go)
-    const int64_t at = (int64_t)((int)blockIdx.x - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
+    const int64_t at = (int64_t)(chunk - table.begin[i]) * kChunk + threadIdx.x * kEach, left = t.count - at;
     if (left <= 0) return;
     const int64_t block = at / P2_STATE_BLOCK;
     float x[kEach];
@@ -291,6 +295,13 @@ __global__ __launch_bounds__(kBlock) void k_adamw_values(AdamwTable table) {
         store_part<float, kEach>(static_cast<float*>(t.copy) + at, left, x);
     }
 }
+
+__global__ __launch_bounds__(kBlock) void k_adamw_values(AdamwTable table) {
+    for (int chunk = blockIdx.x; chunk < table.begin[table.n]; chunk += gridDim.x) values_of_chunk(table, chunk);
+}
+
+// (a launch has less than 2^32 threads)
+dim3 chunks_of(const AdamwTable& table) { return dim3((unsigned)std::min(table.begin[table.n], 1 << 23)); }
 
 // Fills tables with the tensors that have values, and launches each.  (2^40 values are the most that a call takes: their chunks can be counted.)
 template <typename Tab, typename Get, typename Launch> hipError_t in_tables(int64_t n, int most, Get&& get, Launch&& launch) {
@@ -314,7 +325,7 @@ template <typename Tab, typename Get, typename Launch> hipError_t in_tables(int6
 }
 
 template <typename P, typename G> void step_launch(const AdamwTable& table, const AdamwConstants& c, int32_t bits, const AdamwStep* numbers, hipStream_t s) {
-    const dim3 grid((unsigned)table.begin[table.n]);
+    const dim3 grid = chunks_of(table);
     if (bits == 8) k_adamw<P, G, 8><<<grid, dim3(kBlock), 0, s>>>(table, c, numbers);
     else k_adamw<P, G, 32><<<grid, dim3(kBlock), 0, s>>>(table, c, numbers);
 }
@@ -380,7 +391,7 @@ hipError_t launch_adamw_values(const p2_adamw_tensor* tensors, int64_t n, float*
             t.copy = square_out ? square_out[i] : nullptr;
             return t.param || t.copy ? ceil_div(t.count, kChunk) : 0;
         },
-        [&](const AdamwTable& table) { k_adamw_values<<<dim3((unsigned)table.begin[table.n]), dim3(kBlock), 0, s>>>(table); });
+        [&](const AdamwTable& table) { k_adamw_values<<<chunks_of(table), dim3(kBlock), 0, s>>>(table); });
 }
 
 }  // namespace p2

@@ -321,9 +321,8 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
 #pragma unroll
             for (int i = 1; i < kItems; ++i) most = fmaxf(most, z[i]);
             most = group_max<kLanes>(most);
-            const float shift = most * kLog2e;
 #pragma unroll
-            for (int i = 0; i < kItems; ++i) { e[i] = __builtin_amdgcn_exp2f(fmaf(z[i], kLog2e, -shift)); s += e[i]; }
+            for (int i = 0; i < kItems; ++i) { e[i] = __builtin_amdgcn_exp2f((z[i] - most) * kLog2e); s += e[i]; }
             s = group_sum<kLanes>(s);
             inv = __builtin_amdgcn_rcpf(s);
             if constexpr (kBiased)
@@ -385,7 +384,9 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
             const bool taken = rank < a.group_limit && value;
             if (!kExact || a.group_best == 2) {
                 const uint32_t last = ~group_reduce<kLanes>(taken ? ~value : 0u, most_of), left = group_reduce<kLanes>(taken ? 0u : value, most_of);
-                if (a.group_best == 2) odd |= left && !(__uint_as_float(last) - __uint_as_float(left) > apart_sum);
+                // (a softmax's scores go by differences of logits, of which the lowest bits are off by steps of the logits' size)
+                const float size = !kBiased && !kExact && a.score == P2_SOFTMAX ? 4.0f * kItems * 0x1p-23f * fabsf(most) : 0.0f;
+                if (a.group_best == 2) odd |= left && !(__uint_as_float(last) - __uint_as_float(left) > apart_sum + size);
                 else odd |= left && last - left <= apart + kLanes;
             }
             if (!taken) list = List<kDepth>();

@@ -148,6 +148,20 @@ def test_route_far_and_odd_logits(T, score, kind):
     assert abs(float(got["gate"].sum(1).double().mean()) - 1) < 1e-6
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("offset", [1000.0, -30000.0])
+def test_route_of_logits_far_from_zero(T, score, offset):
+    """A softmax goes by differences alone: gates are off by what the logits' own steps allow, not by their size."""
+    z = (draw(10, 300, 96).float() * 2 + offset).to(F32)
+    if score == "sigmoid":
+        z = z - offset + 4 * math.copysign(1, offset)
+    for bias in (None, draw(11, 96, scale=0.01).float()):
+        for kw in (dict(), dict(groups=8, group_limit=3, group_best=2), dict(groups=8, group_limit=3, group_best=1)):
+            got, want = T.p2_route_forward(z, 6, score=score, bias=bias, **kw), route_reference(z, 6, score=score, bias=bias, **kw)
+            assert torch.equal(got["expert"], want["expert"])
+            compare(got["gate"], want["gate"], (2 * 40 + 40) * 2 * U * want["gate"], "gate")
+
+
 def test_route_with_infinities_and_nan(T):
     nan = math.nan
     z = torch.tensor([[1.0, nan, 3.0, -INF, 2.0, 0.0], [INF, 1.0, 2.0, INF, -INF, 0.0], [-INF] * 6, [nan] * 6, [1.0, 2.0, 3.0, 4.0, 5.0, 6.0]], device="cuda")
@@ -463,6 +477,14 @@ def test_adamw_leaves_what_is_between_tensors(T):
         inside[a:a + n] = True
     for t in (flat, m, v):
         assert (t[~inside] == 7).all() and (t[inside] != 7).all()
+
+
+def test_what_autograd_saved_of_a_parameter_is_out_of_date_after_a_step(T):
+    p = torch.nn.Parameter(torch.ones(8, device="cuda"))
+    loss = (p * p).sum()
+    T.p2_adamw([p], [torch.ones(8, device="cuda")], **T.p2_adamw_state([p]))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
 
 
 def test_adamw_of_more_values_than_32_bits_count(T):
