@@ -5,7 +5,7 @@ Eight devices (2 nodes of 4) hold a layer norm, a router over experts and a weig
   1. layer norm and routing of the device's own tokens; what they sum up over them are the messages;
   2. the routing statistics are summed over the devices, by the cheapest program for so few bytes;
   3. with the whole batch's statistics the backward pass; its gradients are summed by the cheapest program for their size;
-  4. the weight's update: the reduced gradient orthogonalised.
+  4. the updates: the weight's reduced gradient orthogonalised; layer norm's and the router's by AdamW, clipped by the norm of their reduced gradients.
 
 The planner (p2_search_placements) chooses the programs and predicts their times on the system described; here all eight devices'
 parts run one after the other on the one GPU, and the programs' instructions are carried out on their messages in its memory.
@@ -82,25 +82,25 @@ class Layer:
     def __init__(self, width, experts, chosen):
         self.chosen = chosen
         self.weight, self.bias = torch.ones(width, device="cuda"), torch.zeros(width, device="cuda")
-        self.router = torch.randn(width, experts, device="cuda") / width ** 0.5
+        self.router = torch.randn(experts, width, device="cuda") / width ** 0.5
         self.matrix = torch.randn(width, width, device="cuda") / width ** 0.5
 
     def forward(self, x):
         y, mean, rstd = train.p2_layer_norm_forward(x, self.weight, self.bias)
-        route = train.p2_balance_forward(y @ self.router, self.chosen)
-        return y, mean, rstd, route
+        logits, _ = train.p2_linear_forward(y, self.router)
+        return y, mean, rstd, logits, train.p2_balance_forward(logits, self.chosen)
 
     def statistics(self, route):
         return torch.cat([route["counts"].double(), route["prob_sum"].double(), route["tokens"].double()[None]])
 
     def backward(self, x, dout, dgate, kept, statistics):
-        y, mean, rstd, route = kept
-        e = self.router.shape[1]
+        y, mean, rstd, logits, route = kept
+        e = len(self.router)
         counts, tokens = statistics[:e].long(), statistics[2 * e].long()
-        dlogits = train.p2_balance_backward(y @ self.router, route["expert"], counts, tokens, dgate=dgate)
-        dmatrix, drouter = y.t() @ dout, y.t() @ dlogits
-        dy = dout @ self.matrix.t() + dlogits @ self.router.t()
-        _, dweight, dbias = train.p2_layer_norm_backward(dy, x, self.weight, mean, rstd)
+        dlogits = train.p2_balance_backward(logits, route["expert"], counts, tokens, dgate=dgate)
+        by_router, drouter, _ = train.p2_linear_backward(dlogits, y, self.router, dbias=False)
+        by_matrix, dmatrix, _ = train.p2_linear_backward(dout, y, self.matrix, dbias=False)
+        _, dweight, dbias = train.p2_layer_norm_backward(by_router + by_matrix, x, self.weight, mean, rstd)
         return torch.cat([g.reshape(-1) for g in (dweight, dbias, drouter, dmatrix)])
 
     def update(self, gradients, rate=0.02):
@@ -108,6 +108,14 @@ class Layer:
         rows, cols = self.matrix.shape
         dmatrix = gradients[-rows * cols:].view(rows, cols)
         return self.matrix - rate * train.p2_orthogonalize(dmatrix, scale=max(1.0, rows / cols) ** 0.5)
+
+    def adamw(self, gradients):
+        """Layer norm's weight and bias and the router after a first AdamW step, as one vector."""
+        params = [p.clone() for p in (self.weight, self.bias, self.router)]
+        grads = [g.view_as(p) for g, p in zip(gradients[:sum(p.numel() for p in params)].split([p.numel() for p in params]), params)]
+        total = train.p2_square_sum(grads)
+        train.p2_adamw(params, grads, **train.p2_adamw_state(params), lr=1e-3, weight_decay=0.01, square_sum=total, max_norm=1.0)
+        return torch.cat([p.reshape(-1) for p in params])
 
 
 def main(tokens=16384, width=1024, experts=64, chosen=4, say=print):
@@ -124,17 +132,18 @@ def main(tokens=16384, width=1024, experts=64, chosen=4, say=print):
     say("gradients: ", large)
 
     kept = [layer.forward(x[s]) for s in shares]
-    statistics = small.run([layer.statistics(k[3]) for k in kept])
+    statistics = small.run([layer.statistics(k[4]) for k in kept])
     loss = train.p2_balance_loss(statistics[:experts].long(), statistics[experts:2 * experts].float(), statistics[2 * experts].long(), chosen)
     gradients = large.run([layer.backward(x[s], dout[s], dgate[s], k, statistics) for s, k in zip(shares, kept)])
     matrix = layer.update(gradients)
 
     one = layer.forward(x)                                  # a single device with the whole batch
-    whole = layer.backward(x, dout, dgate, one, layer.statistics(one[3]))
-    off = [float((a - b).norm() / b.norm()) for a, b in ((gradients, whole), (matrix - layer.matrix, layer.update(whole) - layer.matrix))]
-    say("balance loss %.6f (whole batch at once: %.6f)" % (float(loss), float(one[3]["loss"])))
-    say("off a single device: gradients %.1e, update %.1e" % tuple(off))
-    return float(loss), float(one[3]["loss"]), off, small, large
+    whole = layer.backward(x, dout, dgate, one, layer.statistics(one[4]))
+    off = [float((a - b).norm() / b.norm()) for a, b in ((gradients, whole), (matrix - layer.matrix, layer.update(whole) - layer.matrix),
+                                                         (layer.adamw(gradients), layer.adamw(whole)))]
+    say("balance loss %.6f (whole batch at once: %.6f)" % (float(loss), float(one[4]["loss"])))
+    say("off a single device: gradients %.1e, update %.1e, AdamW's weights %.1e" % tuple(off))
+    return float(loss), float(one[4]["loss"]), off, small, large
 
 
 if __name__ == "__main__":
