@@ -167,9 +167,8 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> struct Tile {
     static constexpr int kHalfA = kWavesA * FA * 16, kHalfB = kWavesB * FB * 16;       // rows of a half
     static constexpr int kLoadsA = kHalfA / 8 / kWaves, kLoadsB = kHalfB / 8 / kWaves; // of a half by a wavefront; one brings 8 rows
     static constexpr int kBuffer = 2 * (kHalfA + kHalfB) * kLine;
-    static constexpr int kPitch = FA * 16 + 4;                                         // of a strip of results in LDS, in floats
     static_assert(kLoadsA * 8 * kWaves == kHalfA && kLoadsB * 8 * kWaves == kHalfB, "rows are dealt out evenly");
-    static_assert(kWaves * 16 * kPitch * 4 <= 2 * kBuffer, "the strips fit");
+    static_assert(kWaves * 2 * FB * 16 * FA * 64 <= 2 * kBuffer, "half of the results fit");
 };
 // Eight rows from `first` on, of which those past the matrix's end are zeros.
 __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t first, int64_t rows, int length) {
@@ -208,9 +207,10 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     const int from_a = (lane >> 3) * (int)a.a_pitch + piece, from_b = (lane >> 3) * (int)a.b_pitch + piece;
     // Every load of a stage has a descriptor of its own, which begins with its first row: lanes' offsets are the same for all of them.
-    const auto a_rows = [&](int half, int l) { return rows_from(a.a, a.a_pitch, (int64_t)ti * 2 * S::kHalfA + half * S::kHalfA + (wave * LA + l) * 8, a.a_rows, length); };
-    const auto b_rows = [&](int half, int l) { return rows_from(a.b, a.b_pitch, (int64_t)tj * 2 * S::kHalfB + half * S::kHalfB + (wave * LB + l) * 8, a.b_rows, length); };
-    const Rows ra[2][2] = {{a_rows(0, 0), a_rows(0, LA - 1)}, {a_rows(1, 0), a_rows(1, LA - 1)}}, rb[2][2] = {{b_rows(0, 0), b_rows(0, LB - 1)}, {b_rows(1, 0), b_rows(1, LB - 1)}};
+    const auto rows_of_a = [&](int half, int l) { return rows_from(a.a, a.a_pitch, (int64_t)ti * 2 * S::kHalfA + half * S::kHalfA + (wave * LA + l) * 8, a.a_rows, length); };
+    const auto rows_of_b = [&](int half, int l) { return rows_from(a.b, a.b_pitch, (int64_t)tj * 2 * S::kHalfB + half * S::kHalfB + (wave * LB + l) * 8, a.b_rows, length); };
+    const Rows ra[2][2] = {{rows_of_a(0, 0), rows_of_a(0, LA - 1)}, {rows_of_a(1, 0), rows_of_a(1, LA - 1)}},
+               rb[2][2] = {{rows_of_b(0, 0), rows_of_b(0, LB - 1)}, {rows_of_b(1, 0), rows_of_b(1, LB - 1)}};
     static_assert(LA <= 2 && LB <= 2, "descriptors");
     // the l-th load of a half of stage s; `last` may be the row's last stage, whose rest is zeros
     const auto bring_a = [&](auto last, int half, int s, int l) {
@@ -310,37 +310,43 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
         step(std::true_type(), s + 1, by, bx);
     }
     if (s < stages) step(std::true_type(), s, bx, by);
-    // A lane has four neighbouring columns of a row of C.  Strips of 16 rows go through LDS, where a lane picks up eight.
+    // A lane has four neighbouring columns of a row of C.  A wavefront's results go through LDS, half of the columns at a time, where a lane picks up eight.  A row's
+    // 16-byte parts are exchanged by the row's number.  (One loop, not unrolled: a copy of the activations for each strip would not stay in the instruction cache.)
     stage_barrier<0>();
-    constexpr int kAcross = FA * 2;                        // lanes to a row of a strip
-    float* strip = reinterpret_cast<float*>(lds) + wave * 16 * S::kPitch;
+    constexpr int kParts = FA * 4, kAcross = FA * 2, kRow = FA * 64;                    // of a row in LDS: 16-byte parts, lanes, bytes
+    const Result result = a.r;
+    const int64_t a_rows = a.a_rows, b_rows = a.b_rows;
+    float* const sums = a.parts > 1 ? a.sums + (int64_t)part * b_rows * a_rows : nullptr;
+    char* mine = lds + wave * 2 * FB * 16 * kRow;
 #pragma unroll
-    for (int hb = 0; hb < 2; ++hb)
+    for (int ha = 0; ha < 2; ++ha) {
 #pragma unroll
-        for (int fj = 0; fj < FB; ++fj) {
-            const int64_t j0 = (int64_t)tj * 2 * S::kHalfB + hb * S::kHalfB + (wb * FB + fj) * 16;
-            if (j0 >= a.b_rows) continue;
+        for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-            for (int ha = 0; ha < 2; ++ha) {
-                const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
-                if (i0 >= a.a_rows) continue;
+            for (int fj = 0; fj < FB; ++fj)
 #pragma unroll
-                for (int fi = 0; fi < FA; ++fi) *reinterpret_cast<float4_t*>(strip + row * S::kPitch + fi * 16 + quad * 4) = acc[ha][hb][fi][fj];
-                wavefront_exchange();
+                for (int fi = 0; fi < FA; ++fi)
+                    *reinterpret_cast<float4_t*>(mine + ((hb * FB + fj) * 16 + row) * kRow + ((fi * 4 + quad) ^ (row & (kParts - 1))) * 16) = acc[ha][hb][fi][fj];
+        wavefront_exchange();
+        const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
+#pragma unroll 1
+        for (int x = 0; x < FA * FB; ++x) {
+            const int r = (x * 64 + lane) / kAcross, c = (x * 64 + lane) % kAcross, h = r / (16 * FB);
+            const int64_t j = (int64_t)tj * 2 * S::kHalfB + h * S::kHalfB + wb * FB * 16 + r % (16 * FB), i = i0 + c * 8;
+            float v[8];
 #pragma unroll
-                for (int x = 0; x < (16 * kAcross + 63) / 64; ++x) {
-                    const int sr = (x * 64 + lane) / kAcross, sc = (x * 64 + lane) % kAcross * 8;
-                    float v[8];
-                    load_vec<float, 8>(strip + min(sr, 15) * S::kPitch + sc, v);
-                    const int64_t j = j0 + sr, i = i0 + sc;
-                    if (sr < 16 && j < a.b_rows && i < a.a_rows) {
-                        if (a.parts > 1) store_part<float, 8>(a.sums + ((int64_t)part * a.b_rows + j) * a.a_rows + i, a.a_rows - i, v);
-                        else finish<T, 8>(a.r, j, i, a.a_rows - i, v);
-                    }
-                }
-                wavefront_exchange();
+            for (int q = 0; q < 2; ++q) {
+                const float4_t f = *reinterpret_cast<const float4_t*>(mine + r * kRow + ((c * 2 + q) ^ (r & 15 & (kParts - 1))) * 16);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[q * 4 + w] = f[w];
+            }
+            if (j < b_rows && i < a_rows) {
+                if (sums) store_part<float, 8>(sums + j * a_rows + i, a_rows - i, v);
+                else finish<T, 8>(result, j, i, a_rows - i, v);
             }
         }
+        wavefront_exchange();
+    }
 }
 
 // What is left of a call's products: parts of sums added up, in their order, and the tiles' lines of dbias, 16 columns a block and 16 threads a column.
