@@ -177,6 +177,61 @@ __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t 
 }
 __device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// A tile's results: `acc` of this wavefront, tile (ti, tj) and `part` of the length.  LDS is free for them.
+template <typename S, typename T, int kWavesB, int FA, int FB>
+__device__ __forceinline__ void write_results(const Product& a, int ti, int tj, int part, char* lds, const float4_t (&acc)[2][2][FA][FB]) {
+    // A lane has four neighbouring columns of a row of C.  A wavefront's results go through LDS, half of the columns at a time, where a lane picks up eight.  A row's
+    // 16-byte parts are exchanged by the row's number.  (One loop, not unrolled: a copy of the activations for each strip would not stay in the instruction cache.)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
+    constexpr int kParts = FA * 4, kAcross = FA * 2, kRow = FA * 64;                    // of a row in LDS: 16-byte parts, lanes, bytes
+    const Result result = a.r;
+    const int64_t a_rows = a.a_rows, b_rows = a.b_rows;
+    float* const sums = a.parts > 1 ? a.sums + (int64_t)part * b_rows * a_rows : nullptr;
+    char* mine = lds + wave * 2 * FB * 16 * kRow;
+#pragma unroll
+    for (int ha = 0; ha < 2; ++ha) {
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int fj = 0; fj < FB; ++fj)
+#pragma unroll
+                for (int fi = 0; fi < FA; ++fi)
+                    *reinterpret_cast<float4_t*>(mine + ((hb * FB + fj) * 16 + row) * kRow + ((fi * 4 + quad) ^ (row & (kParts - 1))) * 16) = acc[ha][hb][fi][fj];
+        wavefront_exchange();
+        const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
+#pragma unroll 1
+        for (int x = 0; x < FA * FB; ++x) {
+            const int r = (x * 64 + lane) / kAcross, c = (x * 64 + lane) % kAcross, h = r / (16 * FB);
+            const int64_t j = (int64_t)tj * 2 * S::kHalfB + h * S::kHalfB + wb * FB * 16 + r % (16 * FB), i = i0 + c * 8;
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float4_t f = *reinterpret_cast<const float4_t*>(mine + r * kRow + ((c * 2 + q) ^ (r & 15 & (kParts - 1))) * 16);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[q * 4 + w] = f[w];
+            }
+            if (j < b_rows && i < a_rows) {
+                if (sums) store_part<float, 8>(sums + j * a_rows + i, a_rows - i, v);
+                else finish<T, 8>(result, j, i, a_rows - i, v);
+            }
+        }
+        wavefront_exchange();
+    }
+}
+
+// Which tile, and which part of the length, a block has.  Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, column by
+// column of four rows of tiles.
+struct Place { int ti, tj, part; };
+__device__ __forceinline__ Place place_of(const Product& a, int block, int blocks) {
+    const int whole = blocks / 8, rest = blocks % 8, die = block & 7, tiles = a.across * a.down;
+    int t = die * whole + min(die, rest) + (block >> 3);
+    const int part = t / tiles;
+    t %= tiles;
+    const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
+    return {in / high, first + in % high, part};
+}
+
 template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
     const bool second = (int)blockIdx.x >= all_of.blocks;
     const Product& a = all_of.p[__builtin_amdgcn_readfirstlane(second ? 1 : 0)];
@@ -186,20 +241,8 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     constexpr int LA = S::kLoadsA, LB = S::kLoadsB, kBoth = 2 * (LA + LB);
     __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];                // two stages of A0, A1, B0, B1
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    // Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours.
-    int t;
-    {
-        const int whole = blocks / 8, rest = blocks % 8, die = block & 7;
-        t = die * whole + min(die, rest) + (block >> 3);
-    }
-    const int tiles = a.across * a.down, part = t / tiles;
-    t %= tiles;
-    int ti, tj;                                            // column by column of four rows of tiles
-    {
-        const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
-        tj = first + in % high;
-        ti = in / high;
-    }
+    const Place place = place_of(a, block, blocks);
+    const int ti = place.ti, tj = place.tj, part = place.part;
     const int length = (int)a.length;
     const int all = (length + kLine - 1) / kLine;
     const int begin = (int)((int64_t)all * part / a.parts), stages = (int)((int64_t)all * (part + 1) / a.parts) - begin;
@@ -310,43 +353,101 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
         step(std::true_type(), s + 1, by, bx);
     }
     if (s < stages) step(std::true_type(), s, bx, by);
-    // A lane has four neighbouring columns of a row of C.  A wavefront's results go through LDS, half of the columns at a time, where a lane picks up eight.  A row's
-    // 16-byte parts are exchanged by the row's number.  (One loop, not unrolled: a copy of the activations for each strip would not stay in the instruction cache.)
     stage_barrier<0>();
-    constexpr int kParts = FA * 4, kAcross = FA * 2, kRow = FA * 64;                    // of a row in LDS: 16-byte parts, lanes, bytes
-    const Result result = a.r;
-    const int64_t a_rows = a.a_rows, b_rows = a.b_rows;
-    float* const sums = a.parts > 1 ? a.sums + (int64_t)part * b_rows * a_rows : nullptr;
-    char* mine = lds + wave * 2 * FB * 16 * kRow;
+    write_results<S, T, kWavesB, FA, FB>(a, ti, tj, part, lds, acc);
+}
+
+// The same for rows that cannot be brought to LDS as they are: of any alignment and length.  A stage's values are asked for while the one before is multiplied, and put
+// into LDS after that; what lies past a row's end is zeros.  Rows past the matrix's end are the last one again, whose results nobody writes.
+template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_any(Product a) {
+    typedef Tile<T, kWavesA, kWavesB, FA, FB> S;
+    typedef typename S::F F;
+    constexpr int V = 16 / sizeof(T), kLine16 = kLine / 16;
+    constexpr int kRowsA = 2 * S::kHalfA, kRowsB = 2 * S::kHalfB, kThreads = S::kWaves * 64;
+    constexpr int LA = kRowsA * kLine16 / kThreads, LB = kRowsB * kLine16 / kThreads;      // 16-byte parts of a stage a thread
+    __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const Place place = place_of(a, blockIdx.x, gridDim.x);
+    const int64_t k = a.length / (int64_t)sizeof(T);       // (here the row's own length)
+    const int all = (int)((a.length + kLine - 1) / kLine);
+    const int begin = (int)((int64_t)all * place.part / a.parts), stages = (int)((int64_t)all * (place.part + 1) / a.parts) - begin;
+    const int piece = threadIdx.x % kLine16, first = threadIdx.x / kLine16;                // this thread's part of a row, its first row
+    const auto row_of = [&](const char* p, int64_t pitch, int64_t r, int64_t rows) { return reinterpret_cast<const T*>(p + min(r, rows - 1) * pitch) + piece * V; };
+    const T *pa[LA], *pb[LB];
 #pragma unroll
-    for (int ha = 0; ha < 2; ++ha) {
+    for (int l = 0; l < LA; ++l) pa[l] = row_of(a.a, a.a_pitch, (int64_t)place.ti * kRowsA + first + l * (kThreads / kLine16), a.a_rows);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+    for (int l = 0; l < LB; ++l) pb[l] = row_of(a.b, a.b_pitch, (int64_t)place.tj * kRowsB + first + l * (kThreads / kLine16), a.b_rows);
+    vec_t<T, V> va[LA], vb[LB];
+    const auto ask = [&](int s) {
+        const int64_t at = (int64_t)(begin + s) * (kLine / (int)sizeof(T)), left = k - at - piece * V;
+        if ((begin + s + 1) * (int64_t)kLine <= a.length) {
 #pragma unroll
-            for (int fj = 0; fj < FB; ++fj)
+            for (int l = 0; l < LA; ++l) va[l] = *reinterpret_cast<const vec_t<T, V>*>(pa[l] + at);
 #pragma unroll
-                for (int fi = 0; fi < FA; ++fi)
-                    *reinterpret_cast<float4_t*>(mine + ((hb * FB + fj) * 16 + row) * kRow + ((fi * 4 + quad) ^ (row & (kParts - 1))) * 16) = acc[ha][hb][fi][fj];
-        wavefront_exchange();
-        const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
-#pragma unroll 1
-        for (int x = 0; x < FA * FB; ++x) {
-            const int r = (x * 64 + lane) / kAcross, c = (x * 64 + lane) % kAcross, h = r / (16 * FB);
-            const int64_t j = (int64_t)tj * 2 * S::kHalfB + h * S::kHalfB + wb * FB * 16 + r % (16 * FB), i = i0 + c * 8;
-            float v[8];
+            for (int l = 0; l < LB; ++l) vb[l] = *reinterpret_cast<const vec_t<T, V>*>(pb[l] + at);
+        } else {                                           // the rows' last stage
+            const auto some = [&](const T* p) {
+                vec_t<T, V> v;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const float4_t f = *reinterpret_cast<const float4_t*>(mine + r * kRow + ((c * 2 + q) ^ (r & 15 & (kParts - 1))) * 16);
+                for (int j = 0; j < V; ++j) v[j] = j < left ? p[at + j] : (T)0.0f;
+                return v;
+            };
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v[q * 4 + w] = f[w];
-            }
-            if (j < b_rows && i < a_rows) {
-                if (sums) store_part<float, 8>(sums + j * a_rows + i, a_rows - i, v);
-                else finish<T, 8>(result, j, i, a_rows - i, v);
-            }
+            for (int l = 0; l < LA; ++l) va[l] = some(pa[l]);
+#pragma unroll
+            for (int l = 0; l < LB; ++l) vb[l] = some(pb[l]);
         }
-        wavefront_exchange();
+    };
+    const auto put = [&](int s) {
+        char* to = lds + (s & 1) * S::kBuffer;
+#pragma unroll
+        for (int l = 0; l < LA; ++l) {
+            const int r = first + l * (kThreads / kLine16);
+            *reinterpret_cast<F*>(to + r * kLine + (piece ^ (r & 7)) * 16) = __builtin_bit_cast(F, va[l]);
+        }
+#pragma unroll
+        for (int l = 0; l < LB; ++l) {
+            const int r = first + l * (kThreads / kLine16);
+            *reinterpret_cast<F*>(to + (kRowsA + r) * kLine + (piece ^ (r & 7)) * 16) = __builtin_bit_cast(F, vb[l]);
+        }
+    };
+    float4_t acc[2][2][FA][FB];
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[h >> 1][h & 1][i][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
+    ask(0);
+    put(0);
+    __syncthreads();
+    for (int s = 0; s < stages; ++s) {
+        if (s + 1 < stages) ask(s + 1);
+        const char* from = lds + (s & 1) * S::kBuffer;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int at = row * kLine + ((c * 4 + quad) ^ (row & 7)) * 16;
+            F fa[2][FA], fb[2][FB];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < FA; ++i) fa[h][i] = *reinterpret_cast<const F*>(from + (h * S::kHalfA + (wa * FA + i) * 16) * kLine + at);
+#pragma unroll
+                for (int j = 0; j < FB; ++j) fb[h][j] = *reinterpret_cast<const F*>(from + (kRowsA + h * S::kHalfB + (wb * FB + j) * 16) * kLine + at);
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) multiply(fa[h >> 1][i], fb[h & 1][j], acc[h >> 1][h & 1][i][j]);
+        }
+        if (s + 1 < stages) put(s + 1);                    // (the other half of LDS: everyone has left it before the last barrier)
+        __syncthreads();
     }
+    write_results<S, T, kWavesB, FA, FB>(a, place.ti, place.tj, place.part, lds, acc);
 }
 
 // What is left of a call's products: parts of sums added up, in their order, and the tiles' lines of dbias, 16 columns a block and 16 threads a column.
@@ -498,6 +599,9 @@ int64_t tile_b(Cut c) { return kPrices16[c].b; }
 // read once more, by a launch of its own).  us by 256 x 256, 128 x 128, 128 x 64, 64 x 64 tiles, with the best number of parts each, bf16: 8192 x 4096 x 4096
 // 194, 240, 280, 330; 3000^3 73, 85, 102, 121; 2048^3 38, 23.5, 24.1, 28; 1024^3 23, 14, 9.5, 8.0; 512 x 4096 x 4096 36, 28, 27, 27; 64 x 4096 x 4096
 // 20, 14.6, 13.4, 12.5; 256 x 8192 x 256 23.5, 16.3, 13.5, 11.8; fp32 1531 x 1000 x 776 54, 36, 34, 33.
+// k_linear_any takes some half more (us, as they are against put in order first, bf16: 700 x 701 x 703 10.4 against 12.8, 100 x 5001 x 9001 50 against 67, 2000 x 1001 x 4001 32 against 36,
+// 4085 x 2093 x 367 34 against 29; fp32 440 x 111 x 78 7.1 against 11.1, 3001 x 2001 x 1003 114 against 108).
+constexpr double kAny = 1.5;
 struct Offer { double us; int32_t parts; };
 Offer offer_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
     const int64_t stages = ceil_div(length, kLine);
@@ -513,13 +617,15 @@ Offer offer_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t le
     }
     return best;
 }
-Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
+Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length, bool small, double* us) {
     Plan best = {k64, 1};
     double least = std::numeric_limits<double>::infinity();
     for (const Cut cut : kCuts) {
+        if (small && cut == k256) continue;
         const Offer o = offer_of(cut, type, a_rows, b_rows, length);
         if (o.us < least) { least = o.us; best = {cut, o.parts}; }
     }
+    if (us) *us = least;
     return best;
 }
 // Two products of one launch have one cut.
@@ -532,8 +638,8 @@ void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1
 }
 int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) { return p.parts > 1 ? round_up(p.parts * a_rows * b_rows * 4, 256) : 0; }
 
-// One product, or two of one cut; and the columns' sums of `join` where it has lines.
-template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int n, Join join, hipStream_t s) {
+// One product, or two of one cut; and the columns' sums of `join` where it has lines.  `any`: rows of any alignment, one product.
+template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int n, Join join, bool any, hipStream_t s) {
     Products all = {};
     int64_t blocks = 0, joined = 0;
     for (int i = 0; i < n; ++i) {
@@ -551,7 +657,12 @@ template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int
     }
     if (n > 0) {
         const dim3 grid((unsigned)blocks);
-        switch (plan[0].cut) {
+        if (any) switch (plan[0].cut) {
+            case k256: case k128: k_linear_any<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p[0]); break;      // (k256: never planned)
+            case k128x64: k_linear_any<T, 2, 2, 2, 1><<<grid, dim3(256), 0, s>>>(p[0]); break;
+            case k64x128: k_linear_any<T, 2, 2, 1, 2><<<grid, dim3(256), 0, s>>>(p[0]); break;
+            case k64: k_linear_any<T, 2, 2, 1, 1><<<grid, dim3(256), 0, s>>>(p[0]); break;
+        } else switch (plan[0].cut) {
             case k256: k_linear_wide<T, 2, 4, 4, 2><<<grid, dim3(512), 0, s>>>(all); break;
             case k128: k_linear_wide<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(all); break;
             case k128x64: k_linear_wide<T, 2, 2, 2, 1><<<grid, dim3(256), 0, s>>>(all); break;
@@ -592,7 +703,7 @@ bool in_order(const void* p, int64_t stride, int32_t type, int64_t cols) {
 }
 bool few_rows(int64_t rows) { return rows <= 4; }
 
-struct ForwardRoom { bool pack_x, pack_weight; Plan plan; int64_t length, x, weight, sums, bytes; };
+struct ForwardRoom { bool pack_x, pack_weight, any; Plan plan; int64_t length, x, weight, sums, bytes; };
 ForwardRoom forward_room(const LinearForward& a) {
     ForwardRoom r = {};
     if (few_rows(a.rows)) return r;
@@ -600,7 +711,19 @@ ForwardRoom forward_room(const LinearForward& a) {
     r.pack_x = !in_order(a.x, a.x_stride, a.type, a.inner);
     r.pack_weight = !in_order(a.weight, a.weight_stride, a.type, a.inner);
     r.length = r.pack_x && r.pack_weight ? padded : round_up(a.inner * size, 16);
-    r.plan = plan_of(a.type, a.outer, a.rows, r.length);
+    double us = 0.0, any_us = 0.0;
+    r.plan = plan_of(a.type, a.outer, a.rows, r.length, false, &us);
+    if (r.pack_x || r.pack_weight) {
+        // rows that are not in order are put in order first, or multiplied as they are, by whichever takes less
+        const Plan any = plan_of(a.type, a.outer, a.rows, a.inner * size, true, &any_us);
+        us += 4.0 + ((r.pack_x ? a.rows : 0) + (r.pack_weight ? a.outer : 0)) * (double)a.inner * size * 2.0 / 3.5e6;
+        if (any_us * kAny < us) {
+            r.plan = any;
+            r.any = true;
+            r.pack_x = r.pack_weight = false;
+            r.length = a.inner * size;
+        }
+    }
     r.x = 0;
     r.weight = r.x + (r.pack_x ? round_up(a.rows * padded, 256) : 0);
     r.sums = r.weight + (r.pack_weight ? round_up(a.outer * padded, 256) : 0);
@@ -666,7 +789,7 @@ template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) 
     p.a_rows = a.outer; p.b_rows = a.rows; p.length = room.length;
     p.sums = reinterpret_cast<float*>(a.workspace + room.sums);
     p.r = r;
-    return multiply_rows<T>(&p, &room.plan, 1, Join(), s);
+    return multiply_rows<T>(&p, &room.plan, 1, Join(), room.any, s);
 }
 
 template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s) {
@@ -720,7 +843,7 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
         join.lines = dz.sums; join.n = ceil_div(a.rows, 64); join.cols = a.outer;
         join.out = a.dbias; join.type = a.weight_type;
     }
-    return multiply_rows<T>(p, plan, products, join, s);
+    return multiply_rows<T>(p, plan, products, join, false, s);
 }
 
 }  // namespace
