@@ -494,24 +494,27 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
     }
 }
 
-// What is left after the first kernel.  The first blocks add up its lines: 16 experts each (the tokens that count are one more column), 16 threads an expert.  The
+// What is left after the first kernel.  The first blocks add up its lines: four experts each (the tokens that count are one more column), 64 threads an expert.  The
 // others choose in 64 bits for the tokens that it has marked, a wavefront each.  Both add whole numbers to counts, in whatever order.
 template <typename T> __global__ __launch_bounds__(kBlock) void k_route_finish(RouteForward a, int32_t lines, int32_t sum_blocks, int32_t exact_lanes) {
     extern __shared__ uint64_t keys[];                         // [wavefronts][experts]
-    __shared__ int64_t part[16][16];
+    __shared__ int64_t part[kBlock / 4][4];
     __shared__ int slots[kBlock / 64][P2_MAX_CHOSEN];
     if ((int)blockIdx.x < sum_blocks) {
-        const int x = threadIdx.x % 16, r = threadIdx.x / 16;
-        const int e = blockIdx.x * 16 + x;
+        const int x = threadIdx.x % 4, r = threadIdx.x / 4;
+        const int e = blockIdx.x * 4 + x;
         int64_t n = 0;
         if (e <= a.experts)
-#pragma unroll 8
-            for (int l = r; l < lines; l += 16) n += a.part_count[(int64_t)l * (a.experts + 1) + e];
+#pragma unroll 4
+            for (int l = r; l < lines; l += kBlock / 4) n += a.part_count[(int64_t)l * (a.experts + 1) + e];
         part[r][x] = n;
         __syncthreads();
-        if (r > 0 || e > a.experts) return;
+        if (r >= 4) return;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) n += part[i][x];
+        for (int i = r + 4; i < kBlock / 4; i += 4) n += part[i][x];
+        n += __shfl_xor(n, 4, 64);                             // (lanes 4 r + x)
+        n += __shfl_xor(n, 8, 64);
+        if (r > 0 || e > a.experts) return;
         atomicAdd(reinterpret_cast<unsigned long long*>(e < a.experts ? &a.counts[e] : a.kept), (unsigned long long)n);
         return;
     }
@@ -698,7 +701,7 @@ template <typename T> hipError_t route(const RouteForward& a, const Shape& shape
     else route<T, false>(a, shape, blocks, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    const int64_t sums = ceil_div(a.experts + 1, 16), others = std::min<int64_t>(ceil_div(a.tokens, kBlock / 4), 2048);
+    const int64_t sums = ceil_div(a.experts + 1, 4), others = std::min<int64_t>(ceil_div(a.tokens, kBlock / 4), 2048);
     k_route_finish<T><<<dim3((unsigned)(sums + others)), dim3(kBlock), key_bytes(a.experts), s>>>(a, (int32_t)blocks, (int32_t)sums, 64 / (shape.lanes / shape.group_lanes));
     return hipGetLastError();
 }
