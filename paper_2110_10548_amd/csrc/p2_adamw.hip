@@ -3,7 +3,7 @@
 // A launch takes up to kTensors tensors by value and one block for each kChunk values of them, so that nothing has to be copied to the device before a
 // step, and a captured step keeps its tensors.
 #include <algorithm>
-#include <cstring>
+#include <cmath>
 
 #include "p2_train_dev.h"
 
@@ -183,7 +183,7 @@ template <bool kSquare> __device__ __forceinline__ words2 stored(const float (&v
 __device__ __forceinline__ float inverse_of(float scale) { return scale > 0.0f ? 1.0f / scale : 0.0f; }      // (0, too, where it is NaN)
 
 typedef Table<kTensors, p2_adamw_tensor> AdamwTable;
-struct AdamwConstants { float beta1, beta2, rest1, rest2, eps; int32_t copy_type; };
+struct AdamwConstants { float beta1, beta2, rest1, rest2, eps; int32_t copy_type, by_instruction; };
 
 // Eight stored numbers: bytes, as two words.  Means are stored as they are, of squares without a sign.
 __device__ __forceinline__ words2 load_bytes(const void* p, int64_t n) {
@@ -244,8 +244,8 @@ template <typename P, typename G, int kBits> __device__ __forceinline__ void ada
         m[j] = c.beta1 * m[j] + c.rest1 * d;
         v[j] = c.beta2 * v[j] + c.rest2 * (d * d);
     }
-    // The instructions for the root and 1 / x are off by a step each, 2^-22 of the update; they take numbers below 2^-126 for 0, which an eps makes no matter.
-    if (c.eps >= 1e-15f) {
+    // The instructions for the root and 1 / x are off by a step each, 2^-22 of the update.
+    if (c.by_instruction) {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) update[j] = m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * step.root + c.eps);
     } else {
@@ -368,7 +368,9 @@ hipError_t launch_adamw(const Adamw& a, hipStream_t s) {
     k_adamw_numbers<<<dim3(1), dim3(1), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const AdamwConstants c = {(float)a.beta1, (float)a.beta2, (float)(1.0 - a.beta1), (float)(1.0 - a.beta2), (float)a.eps, a.copy_type};
+    // (The root's instruction takes squares below 2^-126 for 0.  Their roots are 2^-63 at most, and root is at most 1 / sqrt(1 - beta2): 2^-24 of such an eps.)
+    const bool by_instruction = a.eps * std::sqrt(1.0 - a.beta2) >= 0x1p-39;
+    const AdamwConstants c = {(float)a.beta1, (float)a.beta2, (float)(1.0 - a.beta1), (float)(1.0 - a.beta2), (float)a.eps, a.copy_type, by_instruction};
     return in_tables<AdamwTable>(
         a.n, kTensors,
         [&](int64_t i, p2_adamw_tensor& t) {

@@ -105,6 +105,13 @@ bool overlap(std::vector<Range>& ranges) {
     return false;
 }
 
+Range range_of(const void* p, int64_t n, size_t bytes) { return {static_cast<const char*>(p), static_cast<const char*>(p) + (size_t)n * bytes}; }
+// Whether one more overlaps these, which are in order and apart.
+bool overlap(const std::vector<Range>& ranges, const Range& one) {
+    const auto after = std::lower_bound(ranges.begin(), ranges.end(), Range(one.second, nullptr));       // the first that begins at its end or later
+    return after != ranges.begin() && std::prev(after)->second > one.first;
+}
+
 constexpr int64_t kMostLinear = (int64_t)1 << 20;
 int32_t check_linear(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
@@ -426,7 +433,7 @@ int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_
         if (rc != P2_OK) return rc;
         const size_t size = type_bytes(type), state = state_bits == 8 ? 1 : 4;
         std::vector<Range> written;
-        written.reserve((size_t)n * 4);
+        written.reserve((size_t)n * 6);
         for (int64_t i = 0; i < n; ++i) {
             const p2_adamw_tensor& t = tensors[i];
             if (t.count == 0) continue;
@@ -435,13 +442,22 @@ int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_
             if (!aligned_to(t.param, size) || !aligned_to(t.grad, type_bytes(grad_type)) || !aligned_to(t.copy, type_bytes(copy_type)) || !aligned_to(t.mean, state) ||
                 !aligned_to(t.square, state) || !aligned_to(t.mean_scale, 4) || !aligned_to(t.square_scale, 4))
                 return api_fail(P2_EINVAL, "pointer not aligned to its elements");
-            const auto add = [&](const void* p, size_t bytes) { written.emplace_back(static_cast<const char*>(p), static_cast<const char*>(p) + (size_t)t.count * bytes); };
-            add(t.param, size);
-            add(t.mean, state);
-            add(t.square, state);
-            if (t.copy) add(t.copy, type_bytes(copy_type));
+            const auto add = [&](const void* p, int64_t n, size_t bytes) { written.push_back(range_of(p, n, bytes)); };
+            add(t.param, t.count, size);
+            add(t.mean, t.count, state);
+            add(t.square, t.count, state);
+            if (t.copy) add(t.copy, t.count, type_bytes(copy_type));
+            if (state_bits == 8) {
+                add(t.mean_scale, ceil_div(t.count, P2_STATE_BLOCK), 4);
+                add(t.square_scale, ceil_div(t.count, P2_STATE_BLOCK), 4);
+            }
         }
         if (overlap(written)) return api_fail(P2_EINVAL, "tensors overlap");
+        for (int64_t i = 0; i < n; ++i) {
+            const p2_adamw_tensor& t = tensors[i];
+            if (t.count > 0 && !(t.grad == t.copy && grad_type == copy_type) && overlap(written, range_of(t.grad, t.count, type_bytes(grad_type))))
+                return api_fail(P2_EINVAL, "a gradient overlaps what is written");
+        }
         if (!step || !aligned_to(step, 8) || !aligned_to(rate, 4) || !aligned_to(square_sum, 8)) return api_fail(P2_EINVAL, "step null, or pointer not aligned to its elements");
         if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < 256) return api_fail(P2_ENOSPC, "workspace too small");
@@ -495,6 +511,7 @@ int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, i
         if (!aligned_to(bias, type_bytes(type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
         if (y && y == residual && rows > 1 && y_stride != residual_stride) return api_fail(P2_EINVAL, "y is residual with another stride");
         if (y && (y == x || y == z || y == weight)) return api_fail(P2_EINVAL, "y is an input, or z");
+        if (z && (z == x || z == weight || z == residual)) return api_fail(P2_EINVAL, "z is an input");
         LinearForward a = {};
         a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z; a.workspace = static_cast<char*>(workspace);
         a.x_stride = x_stride; a.weight_stride = weight_stride; a.residual_stride = residual_stride; a.y_stride = y_stride; a.z_stride = z_stride;
@@ -532,6 +549,7 @@ int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int
             if (bad) return api_fail(P2_EINVAL, bad);
         if (!aligned_to(dbias, type_bytes(weight_type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
         if (dx && (dx == dy || dx == x || dx == weight || dx == z || dx == dweight)) return api_fail(P2_EINVAL, "dx is an input, or dweight");
+        if (dweight && (dweight == dy || dweight == x || dweight == weight || dweight == z)) return api_fail(P2_EINVAL, "dweight is an input");
         const int64_t room = linear_backward_workspace(type, rows, inner, outer);
         if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");

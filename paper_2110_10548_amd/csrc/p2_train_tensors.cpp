@@ -502,14 +502,14 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t given) {
         for (size_t i = 0; i < t.size(); ++i)
             t[i] = {ptr(params[i]), ptr(grads[i]), copies.empty() ? nullptr : ptr(copies[i]), ptr(means[i]), ptr(squares[i]), small ? (float*)ptr(mean_scales[i]) : nullptr,
                     small ? (float*)ptr(square_scales[i]) : nullptr, params[i].numel()};
-        // (what autograd has saved of them is out of date)
-        for (const at::Tensor& p : params) p.unsafeGetTensorImpl()->bump_version();
-        for (const at::Tensor& p : copies) p.unsafeGetTensorImpl()->bump_version();
         int64_t bytes = 0;
         check(calls.adamw_workspace(&bytes));
         const at::Tensor work = workspace(bytes, params[0]);
         check(calls.adamw(t.data(), (int64_t)t.size(), type, grad_type, copy_type, small ? 8 : 32, (int64_t*)ptr(step), (const float*)ptr(rate), lr, beta1, beta2, eps, decay,
                           factor, (const double*)ptr(square_sum), most, ptr(work), bytes, stream));
+        // (what autograd has saved of them is out of date)
+        for (const at::Tensor& p : params) p.unsafeGetTensorImpl()->bump_version();
+        for (const at::Tensor& p : copies) p.unsafeGetTensorImpl()->bump_version();
         Py_RETURN_NONE;
     });
 }

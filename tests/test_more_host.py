@@ -8,6 +8,7 @@ import torch
 EINVAL, ENOSPC, EUNSUPPORTED = -1, -2, -3
 P, ODD, NULL = 4096, 4097, None      # an aligned pointer, one that is aligned to nothing, none
 NAN, INF = float("nan"), float("inf")
+LONG = dict(inner=8192, x_stride=8192, weight_stride=8192)      # a product whose sum is cut into parts, which need room
 
 
 @pytest.fixture(scope="module")
@@ -124,6 +125,14 @@ def test_adamw_refuses_a_tensor_that_is_listed_twice(T):
     assert _adamw(T, [_tensor(T, count=(1 << 40) + 1)]) == EUNSUPPORTED
 
 
+@pytest.mark.parametrize("tensor,more", [
+    (dict(mean_scale=1 << 19), dict(state_bits=8)), (dict(square_scale=(1 << 18) + 4, count=300), dict(state_bits=8)), (dict(mean_scale=(1 << 16) + 96), dict(state_bits=8)),
+    (dict(grad=1 << 12), {}), (dict(grad=(1 << 16) + 396), {}), (dict(grad=(1 << 16) - 4), {}), (dict(grad=(1 << 17) - 198), dict(grad_type=1)),
+    (dict(copy=(1 << 20)), dict(copy_type=1)), (dict(copy=(1 << 20) + 4), {})])
+def test_adamw_refuses_gradients_and_scales_in_what_is_written(T, tensor, more):
+    assert _adamw(T, [_tensor(T, **tensor)], **more) == EINVAL and b"overlap" in T.B.lib().p2_last_error()
+
+
 @pytest.mark.parametrize("tensor,mean,square", [(dict(mean=NULL), (P,), (P,)), (dict(square_scale=NULL), (P,), (P,)), (dict(), (ODD,), (P,)), (dict(), (P,), (4098,)),
                                                 (dict(count=-1), (P,), (P,))])
 def test_adamw_values_refuses(T, tensor, mean, square):
@@ -134,9 +143,9 @@ def test_adamw_values_refuses(T, tensor, mean, square):
     (dict(type=3), EINVAL), (dict(activation=5), EINVAL), (dict(activation=-1), EINVAL), (dict(rows=-1), EINVAL), (dict(inner=0), EINVAL), (dict(outer=0), EINVAL),
     (dict(x=NULL), EINVAL), (dict(weight=NULL), EINVAL), (dict(y=NULL), EINVAL), (dict(x=ODD), EINVAL), (dict(bias=ODD), EINVAL), (dict(x_stride=7), EINVAL),
     (dict(weight_stride=7), EINVAL), (dict(residual_stride=15), EINVAL), (dict(z_stride=15), EINVAL), (dict(y_stride=15), EINVAL), (dict(residual=3 * P, residual_stride=17), EINVAL),
-    (dict(y=P), EINVAL), (dict(y=2 * P), EINVAL), (dict(y=5 * P), EINVAL), (dict(rows=(1 << 20) + 1), EUNSUPPORTED),
+    (dict(y=P), EINVAL), (dict(y=2 * P), EINVAL), (dict(y=5 * P), EINVAL), (dict(z=P), EINVAL), (dict(z=2 * P), EINVAL), (dict(z=4 * P), EINVAL), (dict(rows=(1 << 20) + 1), EUNSUPPORTED),
     (dict(inner=(1 << 20) + 1, x_stride=1 << 21, weight_stride=1 << 21), EUNSUPPORTED), (dict(outer=(1 << 20) + 1, y_stride=1 << 21), EUNSUPPORTED),
-    (dict(inner=7, workspace=NULL), EINVAL), (dict(inner=7, workspace=P + 64), EINVAL), (dict(inner=7, workspace_bytes=100), ENOSPC)])
+    (dict(LONG, workspace=NULL), EINVAL), (dict(LONG, workspace=P + 64), EINVAL), (dict(LONG, workspace_bytes=100), ENOSPC)])
 def test_linear_forward_refuses(T, bad, code):
     assert _linear_forward(T, **bad) == code and T.B.lib().p2_last_error()
 
@@ -144,7 +153,7 @@ def test_linear_forward_refuses(T, bad, code):
 @pytest.mark.parametrize("bad,code", [
     (dict(type=3), EINVAL), (dict(weight_type=3), EINVAL), (dict(activation=7), EINVAL), (dict(rows=-1), EINVAL), (dict(dy=NULL), EINVAL), (dict(z=NULL), EINVAL),
     (dict(x=NULL), EINVAL), (dict(weight=NULL), EINVAL), (dict(dx=ODD), EINVAL), (dict(dweight=ODD), EINVAL), (dict(dbias=ODD), EINVAL), (dict(dy_stride=15), EINVAL),
-    (dict(dx_stride=7), EINVAL), (dict(dweight_stride=7), EINVAL), (dict(dx=P), EINVAL), (dict(dx=3 * P), EINVAL), (dict(dx=6 * P), EINVAL), (dict(workspace=NULL), EINVAL),
+    (dict(dx_stride=7), EINVAL), (dict(dweight_stride=7), EINVAL), (dict(dx=P), EINVAL), (dict(dx=3 * P), EINVAL), (dict(dx=6 * P), EINVAL), (dict(dweight=P), EINVAL), (dict(dweight=2 * P), EINVAL), (dict(dweight=3 * P), EINVAL), (dict(dweight=4 * P), EINVAL), (dict(workspace=NULL), EINVAL),
     (dict(workspace_bytes=100), ENOSPC), (dict(rows=(1 << 20) + 1), EUNSUPPORTED)])
 def test_linear_backward_refuses(T, bad, code):
     assert _linear_backward(T, **bad) == code and T.B.lib().p2_last_error()

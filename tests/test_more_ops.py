@@ -445,6 +445,25 @@ def test_adamw_of_zero_and_tiny_gradients(T):
     assert p[0].isfinite().all() and ((p[0] - 1).abs() < 0.5).all()
 
 
+@pytest.mark.parametrize("eps,beta2", [(1e-15, 0.999), (1e-12, 0.999999), (1e-8, 0.9999999), (1e-25, 0.9)])
+def test_adamw_of_squares_that_are_no_normal_numbers(T, eps, beta2):
+    # A gradient of 2.6e-19 sqrt(1 / (1 - beta2)) leaves (1 - beta2) g^2 = 6.8e-38 / 10 = 6.8e-39 and less, below 2^-126 = 1.2e-38, where a step is 2^-149 = 1.4e-45:
+    # rounding to it is 1.4e-45 / 2 of 6e-41 = 1.2e-5 at most, half of that in the root, and at most 20 U for the other operations.
+    g = torch.linspace(0.1, 1.0, 500, device="cuda") * (2.6e-19 * math.sqrt(0.1 / (1 - beta2)))
+    p = torch.zeros_like(g)
+    T.p2_adamw([p], [g], **T.p2_adamw_state([p]), lr=1.0, betas=(0.9, beta2), eps=eps)
+    want = -g.double() / (g.double().abs() + eps)
+    compare(p, want, (0.6e-5 + 20 * U) * want.abs(), (eps, beta2))
+
+
+def test_adamw_copies_into_the_gradients(T):
+    p, g = adam_inputs([(1000,), (3, 7)], F32, BF16, 32)
+    q, d = [t.clone() for t in p], [t.clone() for t in g]
+    T.p2_adamw(p, g, **T.p2_adamw_state(p), **HYPER, copies=g)
+    T.p2_adamw(q, d, **T.p2_adamw_state(q), **HYPER)
+    assert all(torch.equal(a, b) and torch.equal(c, b.to(BF16)) for a, b, c in zip(p, q, g))
+
+
 def test_adamw_rate_and_factor_on_the_device(T):
     one, two = (adam_inputs([(1000,)], F32, F32, 32) for _ in range(2))
     s1, s2 = T.p2_adamw_state(one[0]), T.p2_adamw_state(two[0])
@@ -485,6 +504,15 @@ def test_what_autograd_saved_of_a_parameter_is_out_of_date_after_a_step(T):
     T.p2_adamw([p], [torch.ones(8, device="cuda")], **T.p2_adamw_state([p]))
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_a_step_that_is_refused_leaves_what_autograd_saved(T):
+    p = torch.nn.Parameter(torch.full((8,), 3.0, device="cuda"))
+    loss = (p * p).sum()
+    with pytest.raises(T.P2Error):
+        T.p2_adamw([p], [torch.ones(8, device="cuda")], **T.p2_adamw_state([p]), lr=INF)
+    loss.backward()
+    assert (p.grad == 6.0).all()
 
 
 def test_adamw_of_more_values_than_32_bits_count(T):
