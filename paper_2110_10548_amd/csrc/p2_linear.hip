@@ -170,10 +170,11 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> struct Tile {
     static_assert(kLoadsA * 8 * kWaves == kHalfA && kLoadsB * 8 * kWaves == kHalfB, "rows are dealt out evenly");
     static_assert(kWaves * 2 * FB * 16 * FA * 64 <= 2 * kBuffer, "half of the results fit");
 };
-// Eight rows from `first` on, of which those past the matrix's end are zeros.
+// Eight rows from `first` on, of which those past the matrix's end are zeros; where all are, the first row again and zeros, whose results nobody writes
+// (a descriptor has to reach past the place in the row that a load adds to it).
 __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t first, int64_t rows, int length) {
     const int64_t n = min(rows - first, (int64_t)8);
-    return Rows(p + (n > 0 ? first : 0) * pitch, n > 0 ? (int)((n - 1) * pitch) + length : 0);
+    return Rows(p + (n > 0 ? first : 0) * pitch, (n > 0 ? (int)((n - 1) * pitch) : 0) + length);
 }
 __device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 
