@@ -173,7 +173,7 @@ typedef struct p2_adamw_tensor {
 
 int32_t p2_adamw_workspace(int64_t* bytes);
 
-/* One step over n tensors (a HOST array, read before the call returns), t = step[0] + 1 being its number:
+/* One step over n tensors (a HOST array, read before the call returns), t = step[0] + 1 being its number (0 <= step[0] < 2^40 - 1):
  *   g = grad * grad_factor * min(1, max_norm / (grad_factor * sqrt(square_sum[0])))
  *   mean = beta1 mean + (1 - beta1) g,  square = beta2 square + (1 - beta2) g^2
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * mean / (sqrt(square / (1 - beta2^t)) + eps)

@@ -113,8 +113,9 @@ struct Product {
     const char* a; const char* b;      // rows, 16-byte aligned
     int64_t a_pitch, b_pitch;          // bytes from row to row, multiples of 16
     int64_t a_rows, b_rows, length;    // length: bytes of a row, a multiple of 16
-    float* sums;                       // more than one part: [parts][b_rows][a_rows]
-    int32_t across, down, parts;       // tiles of A's and of B's rows, parts of the length
+    float* sums;                       // of the tiles in parts: [tile][part][tile's rows of B][of A]
+    int32_t across, down, whole, parts;                    // tiles of A's and of B's rows; the first `whole` have one block, the others a block for each part of the length
+    int32_t tile_a, tile_b;
     Result r;
 };
 // Products of one launch: the first has the first `blocks` blocks.
@@ -178,9 +179,28 @@ __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t 
 }
 __device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// A tile's results: `acc` of this wavefront, tile (ti, tj) and `part` of the length.  LDS is free for them.
+// Which tile, and which part of the length, a block has.  Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, column by
+// column of four rows of tiles.
+struct Place { int ti, tj, split, part; };     // split: the tile's number among those in parts, or -1
+__device__ __forceinline__ Place place_of_tile(const Product& a, int t) {
+    const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
+    return {in / high, first + in % high, t - a.whole, 0};
+}
+__device__ __forceinline__ Place place_of(const Product& a, int block) {
+    const int rest = a.across * a.down - a.whole;
+    const bool split = block >= a.whole;
+    const int x = split ? block - a.whole : block, blocks = split ? rest * a.parts : a.whole;
+    const int each = blocks / 8, more = blocks % 8, die = x & 7;
+    const int t = die * each + min(die, more) + (x >> 3), part = split ? t / rest : 0;
+    Place p = place_of_tile(a, split ? a.whole + t % rest : t);
+    p.split = split ? p.split : -1;
+    p.part = part;
+    return p;
+}
+
+// A tile's results: `acc` of this wavefront.  LDS is free for them.
 template <typename S, typename T, int kWavesB, int FA, int FB>
-__device__ __forceinline__ void write_results(const Product& a, int ti, int tj, int part, char* lds, const float4_t (&acc)[2][2][FA][FB]) {
+__device__ __forceinline__ void write_results(const Product& a, const Place& place, char* lds, const float4_t (&acc)[2][2][FA][FB]) {
     // A lane has four neighbouring columns of a row of C.  A wavefront's results go through LDS, half of the columns at a time, where a lane picks up eight.  A row's
     // 16-byte parts are exchanged by the row's number.  (One loop, not unrolled: a copy of the activations for each strip would not stay in the instruction cache.)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -188,7 +208,8 @@ __device__ __forceinline__ void write_results(const Product& a, int ti, int tj, 
     constexpr int kParts = FA * 4, kAcross = FA * 2, kRow = FA * 64;                    // of a row in LDS: 16-byte parts, lanes, bytes
     const Result result = a.r;
     const int64_t a_rows = a.a_rows, b_rows = a.b_rows;
-    float* const sums = a.parts > 1 ? a.sums + (int64_t)part * b_rows * a_rows : nullptr;
+    constexpr int kTileA = 2 * S::kHalfA, kTileB = 2 * S::kHalfB;
+    float* const sums = place.split >= 0 ? a.sums + ((int64_t)place.split * a.parts + place.part) * (kTileA * kTileB) : nullptr;
     char* mine = lds + wave * 2 * FB * 16 * kRow;
 #pragma unroll
     for (int ha = 0; ha < 2; ++ha) {
@@ -200,11 +221,12 @@ __device__ __forceinline__ void write_results(const Product& a, int ti, int tj, 
                 for (int fi = 0; fi < FA; ++fi)
                     *reinterpret_cast<float4_t*>(mine + ((hb * FB + fj) * 16 + row) * kRow + ((fi * 4 + quad) ^ (row & (kParts - 1))) * 16) = acc[ha][hb][fi][fj];
         wavefront_exchange();
-        const int64_t i0 = (int64_t)ti * 2 * S::kHalfA + ha * S::kHalfA + wa * FA * 16;
+        const int i0 = ha * S::kHalfA + wa * FA * 16;
 #pragma unroll 1
         for (int x = 0; x < FA * FB; ++x) {
             const int r = (x * 64 + lane) / kAcross, c = (x * 64 + lane) % kAcross, h = r / (16 * FB);
-            const int64_t j = (int64_t)tj * 2 * S::kHalfB + h * S::kHalfB + wb * FB * 16 + r % (16 * FB), i = i0 + c * 8;
+            const int in_j = h * S::kHalfB + wb * FB * 16 + r % (16 * FB), in_i = i0 + c * 8;
+            const int64_t j = (int64_t)place.tj * kTileB + in_j, i = (int64_t)place.ti * kTileA + in_i;
             float v[8];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
@@ -213,7 +235,7 @@ __device__ __forceinline__ void write_results(const Product& a, int ti, int tj, 
                 for (int w = 0; w < 4; ++w) v[q * 4 + w] = f[w];
             }
             if (j < b_rows && i < a_rows) {
-                if (sums) store_part<float, 8>(sums + j * a_rows + i, a_rows - i, v);
+                if (sums) store_vec<float, 8>(sums + in_j * kTileA + in_i, v);
                 else finish<T, 8>(result, j, i, a_rows - i, v);
             }
         }
@@ -221,32 +243,20 @@ __device__ __forceinline__ void write_results(const Product& a, int ti, int tj, 
     }
 }
 
-// Which tile, and which part of the length, a block has.  Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, column by
-// column of four rows of tiles.
-struct Place { int ti, tj, part; };
-__device__ __forceinline__ Place place_of(const Product& a, int block, int blocks) {
-    const int whole = blocks / 8, rest = blocks % 8, die = block & 7, tiles = a.across * a.down;
-    int t = die * whole + min(die, rest) + (block >> 3);
-    const int part = t / tiles;
-    t %= tiles;
-    const int band = t / (4 * a.across), first = band * 4, high = min(4, a.down - first), in = t - first * a.across;
-    return {in / high, first + in % high, part};
-}
-
 template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
     const bool second = (int)blockIdx.x >= all_of.blocks;
     const Product& a = all_of.p[__builtin_amdgcn_readfirstlane(second ? 1 : 0)];
-    const int block = (int)blockIdx.x - (second ? all_of.blocks : 0), blocks = second ? (int)gridDim.x - all_of.blocks : all_of.blocks;
+    const int block = (int)blockIdx.x - (second ? all_of.blocks : 0);
     typedef Tile<T, kWavesA, kWavesB, FA, FB> S;
     typedef typename S::F F;
     constexpr int LA = S::kLoadsA, LB = S::kLoadsB, kBoth = 2 * (LA + LB);
     __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];                // two stages of A0, A1, B0, B1
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const Place place = place_of(a, block, blocks);
-    const int ti = place.ti, tj = place.tj, part = place.part;
+    const Place place = place_of(a, block);
+    const int ti = place.ti, tj = place.tj, part = place.part, parts = place.split >= 0 ? a.parts : 1;
     const int length = (int)a.length;
     const int all = (length + kLine - 1) / kLine;
-    const int begin = (int)((int64_t)all * part / a.parts), stages = (int)((int64_t)all * (part + 1) / a.parts) - begin;
+    const int begin = (int)((int64_t)all * part / parts), stages = (int)((int64_t)all * (part + 1) / parts) - begin;
     // A row's 16-byte parts are exchanged by the row's number, so that the 16 rows that a wavefront reads at once lie in different banks.
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     const int from_a = (lane >> 3) * (int)a.a_pitch + piece, from_b = (lane >> 3) * (int)a.b_pitch + piece;
@@ -355,7 +365,7 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     }
     if (s < stages) step(std::true_type(), s, bx, by);
     stage_barrier<0>();
-    write_results<S, T, kWavesB, FA, FB>(a, ti, tj, part, lds, acc);
+    write_results<S, T, kWavesB, FA, FB>(a, place, lds, acc);
 }
 
 // The same for rows that cannot be brought to LDS as they are: of any alignment and length.  A stage's values are asked for while the one before is multiplied, and put
@@ -368,10 +378,11 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     constexpr int LA = kRowsA * kLine16 / kThreads, LB = kRowsB * kLine16 / kThreads;      // 16-byte parts of a stage a thread
     __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const Place place = place_of(a, blockIdx.x, gridDim.x);
+    const Place place = place_of(a, blockIdx.x);
+    const int parts = place.split >= 0 ? a.parts : 1;
     const int64_t k = a.length / (int64_t)sizeof(T);       // (here the row's own length)
     const int all = (int)((a.length + kLine - 1) / kLine);
-    const int begin = (int)((int64_t)all * place.part / a.parts), stages = (int)((int64_t)all * (place.part + 1) / a.parts) - begin;
+    const int begin = (int)((int64_t)all * place.part / parts), stages = (int)((int64_t)all * (place.part + 1) / parts) - begin;
     const int piece = threadIdx.x % kLine16, first = threadIdx.x / kLine16;                // this thread's part of a row, its first row
     const auto row_of = [&](const char* p, int64_t pitch, int64_t r, int64_t rows) { return reinterpret_cast<const T*>(p + min(r, rows - 1) * pitch) + piece * V; };
     const T *pa[LA], *pb[LB];
@@ -448,7 +459,7 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
         if (s + 1 < stages) put(s + 1);                    // (the other half of LDS: everyone has left it before the last barrier)
         __syncthreads();
     }
-    write_results<S, T, kWavesB, FA, FB>(a, place.ti, place.tj, place.part, lds, acc);
+    write_results<S, T, kWavesB, FA, FB>(a, place, lds, acc);
 }
 
 // What is left of a call's products: parts of sums added up, in their order, and the tiles' lines of dbias, 16 columns a block and 16 threads a column.
@@ -467,18 +478,23 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Join 
         const Product& a = all.p[which];
         const int blocks = all.blocks[which];
         if (block < blocks) {
-            const int64_t quads = (a.a_rows + 3) / 4, items = quads * a.b_rows, plane = a.a_rows * a.b_rows;
+            const int across = a.tile_a / 4, plane = a.tile_a * a.tile_b, in_tile = across * a.tile_b;
+            const int64_t items = (int64_t)(a.across * a.down - a.whole) * in_tile;
             for (int64_t x = (int64_t)block * 256 + threadIdx.x; x < items; x += (int64_t)blocks * 256) {
-                const int64_t j = x / quads, i = x % quads * 4, n = a.a_rows - i;
+                const int tile = (int)(x / in_tile), in = (int)(x % in_tile);
+                const Place place = place_of_tile(a, a.whole + tile);
+                const int64_t j = (int64_t)place.tj * a.tile_b + in / across, i = (int64_t)place.ti * a.tile_a + in % across * 4;
+                if (j >= a.b_rows || i >= a.a_rows) continue;
+                const float* from = a.sums + (int64_t)tile * a.parts * plane + in * 4;
                 float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
                 for (int p = 0; p < a.parts; ++p) {
                     float w[4];
-                    load_part<float, 4>(a.sums + p * plane + j * a.a_rows + i, n, w, 0.0f);
+                    load_vec<float, 4>(from + (int64_t)p * plane, w);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) v[q] += w[q];
                 }
-                finish<T, 4>(a.r, j, i, n, v);
+                finish<T, 4>(a.r, j, i, a.a_rows - i, v);
             }
             return;
         }
@@ -589,7 +605,7 @@ __global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, in
 
 enum Cut : int32_t { k256, k128, k128x64, k64x128, k64 };      // tiles: rows of A by rows of B
 constexpr Cut kCuts[] = {k256, k128, k128x64, k64x128, k64};
-struct Plan { Cut cut; int32_t parts; };
+struct Plan { Cut cut; int64_t whole; int32_t parts; };        // (as in Product)
 // What a cut takes, in us: a stage of one block that has its compute unit to itself (`alone`), a stage of each of more blocks that share one, a block's end.
 struct Price { int64_t a, b; double alone, shared, end; };
 constexpr Price kPrices16[] = {{256, 256, 1.38, 1.38, 9.0}, {128, 128, 0.60, 0.55, 2.2}, {128, 64, 0.38, 0.33, 1.1}, {64, 128, 0.40, 0.34, 1.1}, {64, 64, 0.29, 0.22, 0.6}};
@@ -600,59 +616,72 @@ int64_t tile_b(Cut c) { return kPrices16[c].b; }
 // read once more, by a launch of its own).  us by 256 x 256, 128 x 128, 128 x 64, 64 x 64 tiles, with the best number of parts each, bf16: 8192 x 4096 x 4096
 // 194, 240, 280, 330; 3000^3 73, 85, 102, 121; 2048^3 38, 23.5, 24.1, 28; 1024^3 23, 14, 9.5, 8.0; 512 x 4096 x 4096 36, 28, 27, 27; 64 x 4096 x 4096
 // 20, 14.6, 13.4, 12.5; 256 x 8192 x 256 23.5, 16.3, 13.5, 11.8; fp32 1531 x 1000 x 776 54, 36, 34, 33.
+// Tiles that fill the units whole times may have a block each and the rest be cut into parts (us, against all tiles cut alike: fp32 1531 x 1000 x 777 38 -> 29, 5000 x 800 x 600
+// 54 -> 48; bf16 3500 x 8192 x 2500 152 -> 135, 4096 x 4096 x 5120 160 -> 152; 1500^3 31.4 -> 32.4).
 // k_linear_any takes some half more (us, as they are against put in order first, bf16: 700 x 701 x 703 10.4 against 12.8, 100 x 5001 x 9001 50 against 67, 2000 x 1001 x 4001 32 against 36,
 // 4085 x 2093 x 367 34 against 29; fp32 440 x 111 x 78 7.1 against 11.1, 3001 x 2001 x 1003 114 against 108).
 constexpr double kAny = 1.5;
-struct Offer { double us; int32_t parts; };
+struct Offer { double us; Plan plan; };
 Offer offer_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
     const int64_t stages = ceil_div(length, kLine);
     const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
-    const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b);
-    Offer best = {std::numeric_limits<double>::infinity(), 1};
-    for (int32_t parts = 1; parts <= 32 && (parts == 1 || parts * 4 <= stages); ++parts) {
-        const double load = (double)ceil_div(tiles * parts, kUnits);
-        const double join = parts == 1 ? 0.0 : 2.5 + 0.15 * parts + (double)parts * (double)a_rows * (double)b_rows * 8.0 / 5e6;
-        const double us = (double)ceil_div(stages, parts) * std::max(price.alone, load * price.shared) + load * price.end + join;
-        if (us < best.us) best = {us, parts};
-        if (tiles * parts >= 16 * kUnits) break;               // (more parts than fill the units several times gain nothing)
+    const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b), full = tiles / kUnits * kUnits;
+    const double load = (double)ceil_div(tiles, kUnits);
+    Offer best = {(double)stages * std::max(price.alone, load * price.shared) + load * price.end, {cut, tiles, 1}};
+    for (int64_t whole = 0; whole < tiles; whole += std::max<int64_t>(full, 1)) {
+        if (whole != 0 && whole != full) break;
+        const int64_t rest = tiles - whole;
+        for (int32_t parts = 2; parts <= 32 && parts * 4 <= stages && rest * (parts - 1) < 16 * kUnits; ++parts) {       // (more parts than fill the units several times gain nothing)
+            const double before = (double)(whole / kUnits), after = (double)ceil_div(rest * parts, kUnits), long_part = (double)ceil_div(stages, parts);
+            const double bytes = (double)parts * std::min((double)rest * (double)(price.a * price.b), (double)a_rows * (double)b_rows) * 8.0;
+            const double us = std::max(price.alone * (whole ? (double)stages : long_part), price.shared * (before * (double)stages + after * long_part)) + (before + after) * price.end +
+                              2.5 + 0.15 * parts + bytes / 5e6;
+            if (us < best.us) best = {us, {cut, whole, parts}};
+        }
     }
     return best;
 }
 Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length, bool small, double* us) {
-    Plan best = {k64, 1};
-    double least = std::numeric_limits<double>::infinity();
+    Offer best = {std::numeric_limits<double>::infinity(), {}};
     for (const Cut cut : kCuts) {
         if (small && cut == k256) continue;
         const Offer o = offer_of(cut, type, a_rows, b_rows, length);
-        if (o.us < least) { least = o.us; best = {cut, o.parts}; }
+        if (o.us < best.us) best = o;
     }
-    if (us) *us = least;
-    return best;
+    if (us) *us = best.us;
+    return best.plan;
 }
 // Two products of one launch have one cut.
 void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1, int64_t b1, int64_t length1, Plan& p0, Plan& p1) {
     double least = std::numeric_limits<double>::infinity();
     for (const Cut cut : kCuts) {
         const Offer o = offer_of(cut, type, a0, b0, length0), q = offer_of(cut, type, a1, b1, length1);
-        if (o.us + q.us < least) { least = o.us + q.us; p0 = {cut, o.parts}; p1 = {cut, q.parts}; }
+        if (o.us + q.us < least) { least = o.us + q.us; p0 = o.plan; p1 = q.plan; }
     }
 }
-int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) { return p.parts > 1 ? round_up(p.parts * a_rows * b_rows * 4, 256) : 0; }
+int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) {
+    const int64_t rest = ceil_div(a_rows, tile_a(p.cut)) * ceil_div(b_rows, tile_b(p.cut)) - p.whole;
+    return p.parts > 1 ? rest * p.parts * tile_a(p.cut) * tile_b(p.cut) * 4 : 0;
+}
 
 // One product, or two of one cut; and the columns' sums of `join` where it has lines.  `any`: rows of any alignment, one product.
 template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int n, Join join, bool any, hipStream_t s) {
     Products all = {};
     int64_t blocks = 0, joined = 0;
     for (int i = 0; i < n; ++i) {
-        p[i].across = (int32_t)ceil_div(p[i].a_rows, tile_a(plan[i].cut));
-        p[i].down = (int32_t)ceil_div(p[i].b_rows, tile_b(plan[i].cut));
+        p[i].tile_a = (int32_t)tile_a(plan[i].cut);
+        p[i].tile_b = (int32_t)tile_b(plan[i].cut);
+        p[i].across = (int32_t)ceil_div(p[i].a_rows, p[i].tile_a);
+        p[i].down = (int32_t)ceil_div(p[i].b_rows, p[i].tile_b);
+        p[i].whole = (int32_t)plan[i].whole;
         p[i].parts = plan[i].parts;
         all.p[i] = p[i];
-        blocks += (int64_t)p[i].across * p[i].down * p[i].parts;
+        const int64_t rest = (int64_t)p[i].across * p[i].down - p[i].whole;
+        blocks += p[i].whole + rest * p[i].parts;
         if (i == 0) all.blocks = (int32_t)blocks;
         if (p[i].parts > 1) {
             join.p[i] = p[i];
-            join.blocks[i] = (int32_t)std::min<int64_t>(ceil_div(ceil_div(p[i].a_rows, 4) * p[i].b_rows, 256), 4096);
+            join.blocks[i] = (int32_t)std::min<int64_t>(ceil_div(rest * p[i].tile_a * p[i].tile_b / 4, 256), 4096);
             joined += join.blocks[i];
         }
     }

@@ -505,8 +505,17 @@ template <typename T> __global__ __launch_bounds__(kBlock) void k_route_finish(R
         const int e = blockIdx.x * 4 + x;
         int64_t n = 0;
         if (e <= a.experts)
-#pragma unroll 4
-            for (int l = r; l < lines; l += kBlock / 4) n += a.part_count[(int64_t)l * (a.experts + 1) + e];
+            for (int l0 = r; l0 < lines; l0 += 6 * (kBlock / 4)) {                     // (six lines under way)
+                int32_t v[6];
+#pragma unroll
+                for (int u = 0; u < 6; ++u) {
+                    const int l = l0 + u * (kBlock / 4);
+                    v[u] = a.part_count[(int64_t)min(l, lines - 1) * (a.experts + 1) + e];
+                    if (l >= lines) v[u] = 0;
+                }
+#pragma unroll
+                for (int u = 0; u < 6; ++u) n += v[u];
+            }
         part[r][x] = n;
         __syncthreads();
         if (r >= 4) return;
@@ -656,7 +665,7 @@ template <typename T, int kLanes, int kItems> __global__ __launch_bounds__(kBloc
 
 __global__ __launch_bounds__(1024) void k_route_bias(const float* bias, const int64_t* counts, int32_t experts, float rate, float* out) {
     __shared__ int64_t part[16];
-    const int e = threadIdx.x;                             // (one thread an expert: 1024 at most)
+    const int e = threadIdx.x;                             // (one thread an expert)
     const int64_t n = e < experts ? counts[e] : 0;
     int64_t s = n;
 #pragma unroll
@@ -746,7 +755,7 @@ hipError_t launch_route_backward(const RouteBackward& a, hipStream_t s) {
 }
 
 hipError_t launch_route_bias(const float* bias, const int64_t* counts, int32_t experts, float rate, float* out, hipStream_t s) {
-    k_route_bias<<<dim3(1), dim3(1024), 0, s>>>(bias, counts, experts, rate, out);
+    k_route_bias<<<dim3(1), dim3((unsigned)ceil_div(experts, 64) * 64), 0, s>>>(bias, counts, experts, rate, out);
     return hipGetLastError();
 }
 

@@ -462,8 +462,8 @@ int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_
         if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < 256) return api_fail(P2_ENOSPC, "workspace too small");
         Adamw a = {};
-        a.tensors = tensors; a.n = n; a.step = step; a.rate = rate; a.square_sum = square_sum; a.numbers = static_cast<AdamwStep*>(workspace);
-        a.lr = lr; a.beta1 = beta1; a.beta2 = beta2; a.eps = eps; a.weight_decay = weight_decay; a.grad_factor = grad_factor; a.max_norm = max_norm;
+        a.tensors = tensors; a.n = n; a.numbers = static_cast<AdamwStep*>(workspace); a.eps = eps;
+        a.call = {step, rate, square_sum, lr, beta1, beta2, weight_decay, grad_factor, max_norm};
         a.type = type; a.grad_type = grad_type; a.copy_type = copy_type; a.state_bits = state_bits;
         return launched(launch_adamw(a, (hipStream_t)stream), "AdamW");
     });

@@ -210,11 +210,16 @@ struct AdamwStep {
     float factor, rate, root, shrink;     // of the gradient; lr / (1 - beta1^t); 1 / sqrt(1 - beta2^t); 1 - lr weight_decay
     int32_t left_out;
 };
+struct AdamwCall {
+    int64_t* step; const float* rate; const double* square_sum;
+    double lr, beta1, beta2, weight_decay, grad_factor, max_norm;
+};
 struct Adamw {
     const p2_adamw_tensor* tensors;
     int64_t n;
-    int64_t* step; const float* rate; const double* square_sum; AdamwStep* numbers;
-    double lr, beta1, beta2, eps, weight_decay, grad_factor, max_norm;
+    AdamwCall call;
+    AdamwStep* numbers;
+    double eps;
     int32_t type, grad_type, copy_type, state_bits;
 };
 hipError_t launch_adamw(const Adamw& a, hipStream_t stream);

@@ -462,6 +462,7 @@ PyObject* square_sum(PyObject*, PyObject* const* a, Py_ssize_t given) {
 // (params, grads, means, squares, step, mean_scales, square_scales, copies, rate, lr, beta1, beta2, eps, weight_decay, grad_factor, square_sum, max_norm, stream)
 PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t given) {
     return guarded(given, 18, [&]() -> PyObject* {
+        const at::NoGradGuard nothing_recorded;
         const std::vector<at::Tensor> params = tensors_of(a[0], "params");
         std::vector<at::Tensor> grads = tensors_of(a[1], "grads");
         const std::vector<at::Tensor> means = tensors_of(a[2], "means"), squares = tensors_of(a[3], "squares");

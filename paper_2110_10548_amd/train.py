@@ -212,9 +212,8 @@ def p2_adamw(params, grads, means, squares, step, mean_scales=None, square_scale
         _refuse("max_norm needs square_sum")
     if len(betas) != 2:
         _refuse("two betas")
-    with torch.no_grad():
-        (_native or _native_calls()).adamw(params, grads, means, squares, step, mean_scales, square_scales, copies, rate, lr, betas[0], betas[1], eps, weight_decay, grad_factor,
-                                           square_sum, float("inf") if max_norm is None else max_norm, _stream(params[0]))
+    (_native or _native_calls()).adamw(params, grads, means, squares, step, mean_scales, square_scales, copies, rate, lr, betas[0], betas[1], eps, weight_decay, grad_factor,
+                                       square_sum, float("inf") if max_norm is None else max_norm, _stream(params[0]))
 
 
 def p2_adamw_values(means, squares, mean_scales, square_scales):

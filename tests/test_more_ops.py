@@ -456,6 +456,18 @@ def test_adamw_of_squares_that_are_no_normal_numbers(T, eps, beta2):
     compare(p, want, (0.6e-5 + 20 * U) * want.abs(), (eps, beta2))
 
 
+@pytest.mark.parametrize("values", [1, 256 * 8 * 1024, 256 * 8 * 1024 + 1])
+def test_adamw_counts_its_steps_whatever_it_launches(T, values):
+    p, g = torch.zeros(values, device="cuda"), torch.ones(values, device="cuda")
+    state = T.p2_adamw_state([p])
+    for t in (0, 1, 2, 2 ** 40 - 10):
+        state["step"].fill_(t)
+        T.p2_adamw([p], [g], **state, lr=0.0)
+        assert int(state["step"]) == t + 1
+    T.p2_adamw([p], [g], **state, lr=0.0, square_sum=torch.full((), INF, dtype=F64, device="cuda"))
+    assert int(state["step"]) == 2 ** 40 - 9
+
+
 def test_adamw_copies_into_the_gradients(T):
     p, g = adam_inputs([(1000,), (3, 7)], F32, BF16, 32)
     q, d = [t.clone() for t in p], [t.clone() for t in g]
@@ -624,7 +636,7 @@ def test_the_slopes_against_differences(activation):
     assert (slope(z, activation) - want).abs().max() < 1e-8
 
 
-@pytest.mark.parametrize("rows,inner,outer,kind", [(3500, 200, 3600, BF16), (3590, 72, 3700, F16), (3500, 33, 3600, F32), (1, 4096, 5000, BF16), (2000, 264, 1500, BF16), (1500, 1500, 1500, F32)])
+@pytest.mark.parametrize("rows,inner,outer,kind", [(3500, 200, 3600, BF16), (3590, 72, 3700, F16), (3500, 33, 3600, F32), (1, 4096, 5000, BF16), (2000, 264, 1500, BF16), (1500, 1500, 1500, F32), (1531, 1000, 777, F32), (1531, 1001, 777, F32), (3500, 8192, 2500, BF16), (4096, 1500, 5120, F16)])
 def test_linear_large(T, rows, inner, outer, kind):
     x, w, b, res = linear_inputs(rows, inner, outer, kind)
     y, z = check_linear(T, x, w, b, res, "gelu")
