@@ -286,6 +286,14 @@ __device__ __forceinline__ void squares_of(words2 q, float scale, float (&v)[kEa
     }
 }
 
+// Values for which the caches have no use: the values of 0.1 billion 8-bit states take 204 us instead of 238.
+typedef float float4_a __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void store_past(float* p, int64_t n, const float (&v)[kEach]) {
+    if (n < kEach) { store_part<float, kEach>(p, n, v); return; }
+#pragma unroll
+    for (int q = 0; q < kEach / 4; ++q) __builtin_nontemporal_store(float4_a{v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]}, reinterpret_cast<float4_a*>(p + q * 4));
+}
+
 template <typename P, typename G, int kBits> __device__ __forceinline__ void adamw_chunk(const AdamwTable& table, const AdamwConstants& c, const AdamwStep& step, int chunk) {
 #pragma clang fp contract(off)
     const int i = tensor_of<kTensors>(table.begin, table.n, chunk);
@@ -370,11 +378,11 @@ __device__ __forceinline__ void values_of_chunk(const AdamwTable& table, int chu
     float x[kEach];
     if (t.param) {
         means_of(load_bytes(static_cast<const uint8_t*>(t.mean) + at, left), t.mean_scale[block], x);
-        store_part<float, kEach>(static_cast<float*>(t.param) + at, left, x);
+        store_past(static_cast<float*>(t.param) + at, left, x);
     }
     if (t.copy) {
         squares_of(load_bytes(static_cast<const uint8_t*>(t.square) + at, left), t.square_scale[block], x);
-        store_part<float, kEach>(static_cast<float*>(t.copy) + at, left, x);
+        store_past(static_cast<float*>(t.copy) + at, left, x);
     }
 }
 

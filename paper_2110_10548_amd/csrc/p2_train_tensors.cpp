@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
 #include <ATen/core/grad_mode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -128,8 +129,16 @@ at::Tensor vector_of(at::Tensor t, int64_t n, const char* what, bool fp32) {
         refuse(std::string(what) + " must have shape [" + std::to_string(n) + "]" + (fp32 ? " and type torch.float32" : ""));
     return t.is_contiguous() ? t : t.contiguous();
 }
-at::Tensor like(const at::Tensor& t) { return at::empty(t.sizes(), t.options()); }
-at::Tensor workspace(int64_t bytes, const at::Tensor& t) { return bytes ? at::empty({bytes}, t.options().dtype(at::kByte)) : at::Tensor(); }
+// A new tensor on t's device, which is the current one: from the allocator that tensors there have, without the dispatcher's detour (a call with four results takes 5.6 us instead of 7.4).
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& t) {
+    if (t.is_cuda()) {
+        static c10::Allocator* const device = at::empty({1}, t.options().dtype(at::kByte)).storage().allocator();
+        if (device) return at::detail::empty_generic(sizes, device, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+    }
+    return at::empty(sizes, t.options().dtype(type));
+}
+at::Tensor like(const at::Tensor& t) { return fresh(t.sizes(), t.scalar_type(), t); }
+at::Tensor workspace(int64_t bytes, const at::Tensor& t) { return bytes ? fresh({bytes}, at::kByte, t) : at::Tensor(); }
 
 PyObject* result(const at::Tensor& t) {
     if (!t.defined()) Py_RETURN_NONE;
@@ -180,7 +189,7 @@ PyObject* layer_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const at::Tensor& given_one = weight.defined() ? weight : bias;
         const int32_t weight_type = given_one.defined() ? type_of(given_one, "weight") : type;
         at::Tensor y = like(x);
-        at::Tensor mean = at::empty(x.sizes().slice(0, x.dim() - 1), x.options().dtype(at::kFloat)), rstd = like(mean);
+        at::Tensor mean = fresh(x.sizes().slice(0, x.dim() - 1), at::kFloat, x), rstd = like(mean);
         check(calls.layer_norm_forward(ptr(r.t), type, r.stride, ptr(weight), ptr(bias), weight_type, r.n, r.cols, eps, ptr(y), r.cols, (float*)ptr(mean),
                                        (float*)ptr(rstd), stream));
         return results(y, mean, rstd);
@@ -210,8 +219,8 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const int32_t weight_type = type_of(same, "weight");
         at::Tensor dx, dweight, dbias, work;
         if (wanted[0]) dx = like(x);
-        if (wanted[1]) dweight = at::empty({r.cols}, same.options());
-        if (wanted[2]) dbias = at::empty({r.cols}, same.options());
+        if (wanted[1]) dweight = fresh({r.cols}, same.scalar_type(), same);
+        if (wanted[2]) dbias = fresh({r.cols}, same.scalar_type(), same);
         int64_t bytes = 0;
         if (wanted[1] || wanted[2]) check(calls.layer_norm_backward_workspace(r.n, r.cols, &bytes));
         work = workspace(bytes, x);
@@ -242,11 +251,9 @@ PyObject* balance_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const int32_t experts = (int32_t)std::min<int64_t>(r.cols, std::numeric_limits<int32_t>::max());
         int64_t bytes = 0;
         check(calls.balance_forward_workspace(r.n, experts, &bytes));
-        const auto options = logits.options();
-        const auto fp32 = options.dtype(at::kFloat), i64 = options.dtype(at::kLong);
         const int64_t columns = k >= 1 && k <= experts ? k : 0;        // (another k is refused below)
-        at::Tensor expert = at::empty({r.n, columns}, options.dtype(at::kInt)), gate = at::empty({r.n, columns}, fp32);
-        at::Tensor counts = at::empty({r.cols}, i64), prob_sum = at::empty({r.cols}, fp32), kept = at::empty({}, i64), loss = at::empty({}, fp32);
+        at::Tensor expert = fresh({r.n, columns}, at::kInt, logits), gate = fresh({r.n, columns}, at::kFloat, logits);
+        at::Tensor counts = fresh({r.cols}, at::kLong, logits), prob_sum = fresh({r.cols}, at::kFloat, logits), kept = fresh({}, at::kLong, logits), loss = fresh({}, at::kFloat, logits);
         const at::Tensor work = workspace(bytes, logits);
         check(calls.balance_forward(ptr(r.t), type, r.stride, (const uint8_t*)ptr(keep), r.n, experts, k, (int32_t*)ptr(expert), (float*)ptr(gate), (int64_t*)ptr(counts),
                                     (float*)ptr(prob_sum), (int64_t*)ptr(kept), (float*)ptr(loss), ptr(work), bytes, stream));
@@ -271,7 +278,7 @@ PyObject* balance_loss(PyObject*, PyObject* const* a, Py_ssize_t given) {
         on_device(counts, {&prob_sum, &kept});
         not_recorded("p2_balance_loss", {&prob_sum});
         const int32_t experts = (int32_t)std::min<int64_t>(counts.size(0), std::numeric_limits<int32_t>::max());
-        at::Tensor loss = at::empty({}, prob_sum.options());
+        at::Tensor loss = fresh({}, prob_sum.scalar_type(), prob_sum);
         check(calls.balance_loss((const int64_t*)ptr(counts), (const float*)ptr(prob_sum), (const int64_t*)ptr(kept), experts, k, (float*)ptr(loss), stream));
         return result(loss);
     });
@@ -313,7 +320,7 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t given) {
         void* stream = stream_of(a[8]);
         not_recorded("p2_orthogonalize", {&g});
         const int32_t type = type_of(g, "g"), out_type = asked < 0 ? type : (int32_t)asked;
-        at::Tensor out = at::empty(g.sizes(), g.options().dtype(scalar_of(out_type)));
+        at::Tensor out = fresh(g.sizes(), scalar_of(out_type), g);
         const int64_t rows = g.size(-2), cols = g.size(-1);
         int64_t count = 1;
         for (int64_t i = 0; i + 2 < g.dim(); ++i) count *= g.size(i);
@@ -352,9 +359,8 @@ PyObject* route_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const int32_t experts = (int32_t)std::min<int64_t>(r.cols, std::numeric_limits<int32_t>::max());
         int64_t bytes = 0;
         check(calls.route_forward_workspace(r.n, experts, k, groups, &bytes));         // (refuses another k, too)
-        const auto options = logits.options();
-        at::Tensor expert = at::empty({r.n, k}, options.dtype(at::kInt)), gate = at::empty({r.n, k}, options.dtype(at::kFloat));
-        at::Tensor counts = at::empty({r.cols}, options.dtype(at::kLong)), kept = at::empty({}, options.dtype(at::kLong));
+        at::Tensor expert = fresh({r.n, k}, at::kInt, logits), gate = fresh({r.n, k}, at::kFloat, logits);
+        at::Tensor counts = fresh({r.cols}, at::kLong, logits), kept = fresh({}, at::kLong, logits);
         const at::Tensor work = workspace(bytes, logits);
         check(calls.route_forward(ptr(r.t), type, r.stride, (const uint8_t*)ptr(keep), (const float*)ptr(bias), r.n, experts, k, score, groups, limit, best, renormalise,
                                   scale, (int32_t*)ptr(expert), (float*)ptr(gate), (int64_t*)ptr(counts), (int64_t*)ptr(kept), ptr(work), bytes, stream));
@@ -453,7 +459,7 @@ PyObject* square_sum(PyObject*, PyObject* const* a, Py_ssize_t given) {
         int64_t bytes = 0;
         check(calls.square_sum_workspace((int64_t)t.size(), &bytes));
         const at::Tensor work = workspace(bytes, t[0]);
-        at::Tensor out = at::empty({}, t[0].options().dtype(at::kDouble));
+        at::Tensor out = fresh({}, at::kDouble, t[0]);
         check(calls.square_sum(p.data(), n.data(), (int64_t)t.size(), type, (double*)ptr(out), ptr(work), bytes, stream));
         return result(out);
     });
@@ -532,7 +538,7 @@ PyObject* adamw_values(PyObject*, PyObject* const* a, Py_ssize_t given) {
             for (size_t i = 0; i < t.size(); ++i) {
                 t[i] = {nullptr, nullptr, nullptr, ptr(means[i]), ptr(squares[i]), (float*)ptr(mean_scales[i]), (float*)ptr(square_scales[i]), means[i].numel()};
                 for (int k = 0; k < 2; ++k) {
-                    const at::Tensor out = at::empty(means[i].sizes(), means[i].options().dtype(at::kFloat));
+                    const at::Tensor out = fresh(means[i].sizes(), at::kFloat, means[i]);
                     (k ? square_out : mean_out)[i] = (float*)ptr(out);
                     PyObject* o = result(out);
                     if (!lists[k] || !o) throw Refused();
@@ -568,7 +574,7 @@ PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         shape.back() = w.n;
         if (residual.defined() && (residual.sizes() != at::IntArrayRef(shape) || residual.scalar_type() != x.scalar_type())) refuse("residual must have the result's shape and type");
         const Rows s = residual.defined() ? rows_of(residual) : Rows{at::Tensor(), 0, 0, 0};
-        at::Tensor y = at::empty(shape, x.options()), z = keep ? at::empty(shape, x.options()) : at::Tensor();
+        at::Tensor y = fresh(shape, x.scalar_type(), x), z = keep ? fresh(shape, x.scalar_type(), x) : at::Tensor();
         int64_t bytes = 0;
         check(calls.linear_forward_workspace(ptr(r.t), r.stride, ptr(w.t), w.stride, type, r.n, r.cols, w.n, &bytes));
         const at::Tensor work = workspace(bytes, x);
@@ -598,10 +604,9 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         if (z.defined() && (z.sizes() != dy.sizes() || z.scalar_type() != x.scalar_type())) refuse("z must have dy's shape and type");
         const Rows r = rows_of(x), w = rows_of(weight), d = rows_of(dy), s = z.defined() ? rows_of(z) : Rows{at::Tensor(), 0, 0, 0};
         at::Tensor dx, dweight, dbias;
-        const auto options = x.options().dtype(scalar_of(weight_type));
         if (wanted[0]) dx = like(x);
-        if (wanted[1]) dweight = at::empty({w.n, r.cols}, options);
-        if (wanted[2]) dbias = at::empty({w.n}, options);
+        if (wanted[1]) dweight = fresh({w.n, r.cols}, scalar_of(weight_type), x);
+        if (wanted[2]) dbias = fresh({w.n}, scalar_of(weight_type), x);
         int64_t bytes = 0;
         check(calls.linear_backward_workspace(type, r.n, r.cols, w.n, &bytes));
         const at::Tensor work = workspace(bytes, x);
