@@ -2,7 +2,7 @@
 // dz = dy * activation'(z).
 //
 // Every product is rows times rows, C[j][i] = sum_k A[i][k] B[j][k], with the summed index contiguous in both: the forward pass takes weight
-// and x as they are, and for the gradients weight, x and dz are written turned first.  A tile of C comes from stages of 128 bytes of
+// and x as they are; for the gradients weight, x and dz are written turned first, or, in large 16-bit products, turned by the reads from LDS.  A tile of C comes from stages of 128 bytes of
 // each row (64 values of 16 bits, 32 of 32) that are brought to LDS straight from memory while the stage before is multiplied.  The MFMA's rows
 // are A's: a lane has four neighbouring columns of one row of C.
 #include <algorithm>
@@ -110,8 +110,9 @@ template <typename T, int N> __device__ __forceinline__ void finish(const Result
 // ------------------------------------------------------------------------------------------------ products
 
 struct Product {
-    const char* a; const char* b;      // rows, 16-byte aligned
+    const char* a; const char* b;      // rows, 16-byte aligned; a turned operand's are those of its transpose, `length` of them
     int64_t a_pitch, b_pitch;          // bytes from row to row, multiples of 16
+    bool turned_a, turned_b;
     int64_t a_rows, b_rows, length;    // length: bytes of a row, a multiple of 16
     float* sums;                       // of the tiles in parts: [tile][part][tile's rows of B][of A]
     int32_t across, down, whole, parts;                    // tiles of A's and of B's rows; the first `whole` have one block, the others a block for each part of the length
@@ -148,6 +149,18 @@ struct Rows {
 #endif
 };
 
+// Eight values a lane of a turned operand, whose rows in LDS are of the summed index: 16 lanes have four rows of 16 values at `from` (a lane points to four of
+// a row), and get a column's four each.
+template <typename F> __device__ __forceinline__ F read_turned(const char* __restrict from, int step) {
+    F f = {};
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef short short4_t __attribute__((ext_vector_type(4)));
+    const auto four = [&](const char* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)p); };
+    f = __builtin_bit_cast(F, __builtin_shufflevector(four(from), four(from + step), 0, 1, 2, 3, 4, 5, 6, 7));
+#endif
+    return f;
+}
+
 // Waits until at most kLoads of this wavefront's loads are under way (and all its LDS reads are done), then for the others.
 template <int kLoads> __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");
@@ -177,6 +190,24 @@ __device__ __forceinline__ Rows rows_from(const char* p, int64_t pitch, int64_t 
     const int64_t n = min(rows - first, (int64_t)8);
     return Rows(p + (n > 0 ? first : 0) * pitch, (n > 0 ? (int)((n - 1) * pitch) : 0) + length);
 }
+// A turned operand's rows of each stage, from a half's first column on (or, where there is none, from column 0).  (What it needs is kept in scalar registers:
+// fetched anew from the kernel's arguments it would make LDS reads wait.)
+struct Turned {
+    const char* first;
+    int pitch, left, extent;           // left: rows from the first stage on; extent: bytes of a row
+    __device__ __forceinline__ Turned(const char* p, int64_t row, int begin, int rows, int64_t col, int64_t cols) {
+        const int64_t c = col < cols ? col : 0;
+        const uint64_t at = reinterpret_cast<uint64_t>(p + (int64_t)begin * 64 * row + c * 2);
+        first = reinterpret_cast<const char*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
+        pitch = __builtin_amdgcn_readfirstlane((int)row);
+        left = __builtin_amdgcn_readfirstlane(rows - begin * 64);
+        extent = __builtin_amdgcn_readfirstlane((int)(cols - c) * 2);
+    }
+    __device__ __forceinline__ Rows stage(int s, bool last) const {
+        const int n = last ? min(left - s * 64, 64) : 64;
+        return Rows(first + (uint64_t)(uint32_t)(s * 64) * (uint32_t)pitch, (n - 1) * pitch + extent);
+    }
+};
 __device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Which tile, and which part of the length, a block has.  Blocks go to the eight dies in turn: tiles are dealt out so that those of a die are neighbours, column by
@@ -243,13 +274,17 @@ __device__ __forceinline__ void write_results(const Product& a, const Place& pla
     }
 }
 
-template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
+// An operand may be turned: its memory has the summed index's rows, of which a stage takes 64, and a half's columns of them lie in LDS as 64 rows of 256 bytes.  Their
+// 32-byte parts are exchanged by the row's number, so that what is read at once lies in different banks.  (16 bits and 256 x 256 tiles alone.)
+template <typename T, int kWavesA, int kWavesB, int FA, int FB, bool kTurnA = false, bool kTurnB = false>
+__global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
     const bool second = (int)blockIdx.x >= all_of.blocks;
     const Product& a = all_of.p[__builtin_amdgcn_readfirstlane(second ? 1 : 0)];
     const int block = (int)blockIdx.x - (second ? all_of.blocks : 0);
     typedef Tile<T, kWavesA, kWavesB, FA, FB> S;
     typedef typename S::F F;
     constexpr int LA = S::kLoadsA, LB = S::kLoadsB, kBoth = 2 * (LA + LB);
+    static_assert(!(kTurnA || kTurnB) || (sizeof(T) == 2 && S::kHalfA == 128 && S::kHalfB == 128), "what a turned operand is laid out for");
     __shared__ __attribute__((aligned(1024))) char lds[2 * S::kBuffer];                // two stages of A0, A1, B0, B1
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const Place place = place_of(a, block);
@@ -266,15 +301,23 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     const Rows ra[2][2] = {{rows_of_a(0, 0), rows_of_a(0, LA - 1)}, {rows_of_a(1, 0), rows_of_a(1, LA - 1)}},
                rb[2][2] = {{rows_of_b(0, 0), rows_of_b(0, LB - 1)}, {rows_of_b(1, 0), rows_of_b(1, LB - 1)}};
     static_assert(LA <= 2 && LB <= 2, "descriptors");
+    // A turned operand's loads bring four rows each, with a descriptor of the stage's rows from the half's first column on (or, where there is none, from column 0).
+    const auto turned_from = [&](int64_t pitch, int load) { return (load * 4 + (lane >> 4)) * (int)pitch + ((lane & 15) ^ ((lane >> 4) * 2 + (load >> 1 & 1) * 8)) * 16; };
+    const int turned_a[2] = {turned_from(a.a_pitch, wave * LA), turned_from(a.a_pitch, wave * LA + LA - 1)}, turned_b[2] = {turned_from(a.b_pitch, wave * LB), turned_from(a.b_pitch, wave * LB + LB - 1)};
+    const Turned ta[2] = {Turned(a.a, a.a_pitch, begin, length / 2, (int64_t)ti * 2 * S::kHalfA, a.a_rows), Turned(a.a, a.a_pitch, begin, length / 2, (int64_t)ti * 2 * S::kHalfA + S::kHalfA, a.a_rows)},
+                 tb[2] = {Turned(a.b, a.b_pitch, begin, length / 2, (int64_t)tj * 2 * S::kHalfB, a.b_rows), Turned(a.b, a.b_pitch, begin, length / 2, (int64_t)tj * 2 * S::kHalfB + S::kHalfB, a.b_rows)};
     // the l-th load of a half of stage s; `last` may be the row's last stage, whose rest is zeros
     const auto bring_a = [&](auto last, int half, int s, int l) {
         const int at = (begin + s) * kLine;
-        ra[half][l].bring(&lds[(s & 1) * S::kBuffer + half * S::kHalfA * kLine + (wave * LA + l) * 1024], !decltype(last)::value || at + piece < length ? from_a : kPastEnd, at);
+        char* to = &lds[(s & 1) * S::kBuffer + half * S::kHalfA * kLine + (wave * LA + l) * 1024];
+        if constexpr (kTurnA) ta[half].stage(s, decltype(last)::value).bring(to, turned_a[l], 0);
+        else ra[half][l].bring(to, !decltype(last)::value || at + piece < length ? from_a : kPastEnd, at);
     };
     const auto bring_b = [&](auto last, int half, int s, int l) {
         const int at = (begin + s) * kLine;
-        rb[half][l].bring(&lds[(s & 1) * S::kBuffer + (2 * S::kHalfA + half * S::kHalfB) * kLine + (wave * LB + l) * 1024],
-                          !decltype(last)::value || at + piece < length ? from_b : kPastEnd, at);
+        char* to = &lds[(s & 1) * S::kBuffer + (2 * S::kHalfA + half * S::kHalfB) * kLine + (wave * LB + l) * 1024];
+        if constexpr (kTurnB) tb[half].stage(s, decltype(last)::value).bring(to, turned_b[l], 0);
+        else rb[half][l].bring(to, !decltype(last)::value || at + piece < length ? from_b : kPastEnd, at);
     };
     const auto bring_stage = [&](int s) {
 #pragma unroll
@@ -288,15 +331,20 @@ template <typename T, int kWavesA, int kWavesB, int FA, int FB> __global__ __lau
     };
     const int wa = wave / kWavesB, wb = wave % kWavesB, row = lane & 15, quad = lane >> 4;
     const int slot[2] = {row * kLine + (quad ^ (row & 7)) * 16, row * kLine + ((4 + quad) ^ (row & 7)) * 16};
+    // (of a turned operand: four rows from quad * 8 + row / 4 on, and four rows further down; 32-byte parts by the row's lowest two bits and its fourth)
+    const int turned_slot = (quad * 8 + (row >> 2)) * 256 + (row & 3) * 8, exchanged = (row >> 2) + (quad & 1) * 4;
+    const int slot_a = turned_slot + ((wa * FA) ^ exchanged) * 32, slot_b = turned_slot + ((wb * FB) ^ exchanged) * 32;
     const auto read_a = [&](int s, int half, int i, F (&f)[2]) {
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-            f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wa * FA * 16 * kLine + (half * S::kHalfA + i * 16) * kLine);
+            if constexpr (kTurnA) f[c] = read_turned<F>(lds + (slot_a ^ i * 32) + (s & 1) * S::kBuffer + half * S::kHalfA * kLine + c * 32 * 256, 4 * 256);
+            else f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wa * FA * 16 * kLine + (half * S::kHalfA + i * 16) * kLine);
     };
     const auto read_b = [&](int s, int half, int j, F (&f)[2]) {
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-            f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wb * FB * 16 * kLine + (2 * S::kHalfA + half * S::kHalfB + j * 16) * kLine);
+            if constexpr (kTurnB) f[c] = read_turned<F>(lds + (slot_b ^ j * 32) + (s & 1) * S::kBuffer + (2 * S::kHalfA + half * S::kHalfB) * kLine + c * 32 * 256, 4 * 256);
+            else f[c] = *reinterpret_cast<const F*>(lds + (s & 1) * S::kBuffer + slot[c] + wb * FB * 16 * kLine + (2 * S::kHalfA + half * S::kHalfB + j * 16) * kLine);
     };
     float4_t acc[2][2][FA][FB];
 #pragma unroll
@@ -563,14 +611,44 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
     const int block = (int)blockIdx.x - all.begin[m], line = block / all.across[m];
     const int64_t r0 = (int64_t)line * 64, c0 = (int64_t)(block % all.across[m]) * 64;
     const int x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
+    // All is asked for before any of it is waited for, without conditions: a vector that the row's end cuts is the row's last one, moved into place after that
+    // (three matrices of 2001 x 1023 x 515 11.5 -> 11.4 us, 4001 x 2047 x 1029 20.9 -> 16.8, 8192 x 4096 x 4096 96 -> 87).
+    vec_t<T, 4> raw[4], raw_z[4];
+    const int64_t c = c0 + x, last = a.cols - 4, place = min(c, last);
+    if (last >= 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const vec_t<T, 4>*>(static_cast<const T*>(a.from) + min(r0 + y + i * 16, a.rows - 1) * a.from_stride + place);
+        if (a.z)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw_z[i] = *reinterpret_cast<const vec_t<T, 4>*>(static_cast<const T*>(a.z) + min(r0 + y + i * 16, a.rows - 1) * a.z_stride + place);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t r = min(r0 + y + i * 16, a.rows - 1), e = min(max(place, (int64_t)0) + q, a.cols - 1);
+                raw[i][q] = static_cast<const T*>(a.from)[r * a.from_stride + e];
+                if (a.z) raw_z[i][q] = static_cast<const T*>(a.z)[r * a.z_stride + e];
+            }
+    }
+    const int moved = last >= 0 ? (int)min(c - place, (int64_t)4) : c == 0 ? 0 : 4, there = (int)min(max(a.cols - c, (int64_t)0), (int64_t)4);
+    const auto in_place = [&](const vec_t<T, 4>& from, float (&v)[4], bool row) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)from[q];
+#pragma unroll
+        for (int m = 0; m < 3; ++m)
+            if (m < moved) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = row && q < there ? v[q] : 0.0f;
+    };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + y + i * 16, c = c0 + x, n = r < a.rows ? a.cols - c : 0;
+        const int64_t r = r0 + y + i * 16;
         float v[4];
-        load_part<T, 4>(static_cast<const T*>(a.from) + r * a.from_stride + c, n, v, 0.0f);
+        in_place(raw[i], v, r < a.rows);
         if (a.z) {
             float z[4];
-            load_part<T, 4>(static_cast<const T*>(a.z) + r * a.z_stride + c, n, z, 0.0f);
+            in_place(raw_z[i], z, r < a.rows);
             times_slope(v, z, a.activation);               // (past the matrix's end 0 times the slope at 0)
         }
         if (a.straight && r < a.rows) store_part<T, 4>(reinterpret_cast<T*>(a.straight + r * a.straight_pitch) + c, a.straight_pitch / (int)sizeof(T) - c, v);
@@ -685,7 +763,19 @@ template <typename T> hipError_t multiply_rows(Product* p, const Plan* plan, int
             joined += join.blocks[i];
         }
     }
-    if (n > 0) {
+    if (n > 0 && p[0].turned_a) {
+        // (a launch each: of one cut and of some size they do not need each other's blocks)
+        if constexpr (sizeof(T) == 2)
+            for (int i = 0; i < n; ++i) {
+                Products one = {};
+                one.p[0] = all.p[i];
+                one.blocks = (int32_t)(p[i].whole + ((int64_t)p[i].across * p[i].down - p[i].whole) * p[i].parts);
+                if (p[i].turned_b) k_linear_wide<T, 2, 4, 4, 2, true, true><<<dim3((unsigned)one.blocks), dim3(512), 0, s>>>(one);
+                else k_linear_wide<T, 2, 4, 4, 2, true, false><<<dim3((unsigned)one.blocks), dim3(512), 0, s>>>(one);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+    } else if (n > 0) {
         const dim3 grid((unsigned)blocks);
         if (any) switch (plan[0].cut) {
             case k256: case k128: k_linear_any<T, 2, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p[0]); break;      // (k256: never planned)
@@ -825,43 +915,59 @@ template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) 
 template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s) {
     const BackwardRoom room = backward_room(a.type, a.rows, a.inner, a.outer);
     const bool own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
+    // Large 16-bit products take weight, x and dz turned as they lie in memory, and only dz is put in order
+    // (us, bf16, without / with an activation: 8192 x 4096 x 4096 428 -> 394 / 460 -> 431, 32768 x 1024 x 1024 213 -> 156 / 248 -> 191, 4096^3 225 -> 207 / 238 -> 220).
+    const bool turned = sizeof(T) == 2 && room.dx.cut == k256 && room.dweight.cut == k256 && a.outer % 8 == 0 && (!a.dx || in_order(a.weight, a.weight_stride, a.type, a.inner)) &&
+                        (!a.dweight || in_order(a.x, a.x_stride, a.type, a.inner));
+    const char* const dz_rows = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
+    const int64_t dz_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
     Pack k[3] = {};
     int packs = 0;
     Pack& dz = k[packs];
     dz.from = a.dy; dz.from_stride = a.dy_stride;
     if (a.activation != P2_NO_ACTIVATION) { dz.z = a.z; dz.z_stride = a.z_stride; }
     dz.rows = a.rows; dz.cols = a.outer; dz.activation = a.activation;
-    if (a.dx && own_dz) { dz.straight = a.workspace + room.dz; dz.straight_pitch = room.along; }
-    if (a.dweight) { dz.turned = a.workspace + room.dz_turned; dz.turned_pitch = room.deep; }
+    if ((a.dx || (a.dweight && turned)) && own_dz) { dz.straight = a.workspace + room.dz; dz.straight_pitch = room.along; }
+    if (a.dweight && !turned) { dz.turned = a.workspace + room.dz_turned; dz.turned_pitch = room.deep; }
     if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + room.lines);
     if (dz.straight || dz.turned || dz.sums) ++packs;
     Product p[2] = {};
     Plan plan[2];
     int products = 0;
     if (a.dx) {
-        Pack& w = k[packs++];
-        w = Pack();
-        w.from = a.weight; w.from_stride = a.weight_stride; w.rows = a.outer; w.cols = a.inner;
-        w.turned = a.workspace + room.weight_turned; w.turned_pitch = room.along;
         Product& q = p[products];
-        q.a = w.turned; q.a_pitch = room.along; q.a_rows = a.inner;
-        q.b = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
-        q.b_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
-        q.b_rows = a.rows;
-        q.length = own_dz ? room.along : a.outer * (int64_t)sizeof(T);
+        if (turned) {
+            q.a = static_cast<const char*>(a.weight); q.a_pitch = a.weight_stride * (int64_t)sizeof(T); q.turned_a = true;
+        } else {
+            Pack& w = k[packs++];
+            w = Pack();
+            w.from = a.weight; w.from_stride = a.weight_stride; w.rows = a.outer; w.cols = a.inner;
+            w.turned = a.workspace + room.weight_turned; w.turned_pitch = room.along;
+            q.a = w.turned; q.a_pitch = room.along;
+        }
+        q.a_rows = a.inner;
+        q.b = dz_rows; q.b_pitch = dz_pitch; q.b_rows = a.rows;
+        q.length = own_dz && !turned ? room.along : a.outer * (int64_t)sizeof(T);
         q.sums = reinterpret_cast<float*>(a.workspace + room.sums);
         q.r.y = a.dx; q.r.y_stride = a.dx_stride; q.r.y_type = a.type;
         plan[products++] = room.dx;
     }
     if (a.dweight) {
-        Pack& x = k[packs++];
-        x = Pack();
-        x.from = a.x; x.from_stride = a.x_stride; x.rows = a.rows; x.cols = a.inner;
-        x.turned = a.workspace + room.x_turned; x.turned_pitch = room.deep;
         Product& q = p[products];
-        q.a = x.turned; q.a_pitch = room.deep; q.a_rows = a.inner;
-        q.b = a.workspace + room.dz_turned; q.b_pitch = room.deep; q.b_rows = a.outer;
-        q.length = room.deep;
+        if (turned) {
+            q.a = static_cast<const char*>(a.x); q.a_pitch = a.x_stride * (int64_t)sizeof(T); q.turned_a = true;
+            q.b = dz_rows; q.b_pitch = dz_pitch; q.turned_b = true;
+            q.length = a.rows * (int64_t)sizeof(T);
+        } else {
+            Pack& x = k[packs++];
+            x = Pack();
+            x.from = a.x; x.from_stride = a.x_stride; x.rows = a.rows; x.cols = a.inner;
+            x.turned = a.workspace + room.x_turned; x.turned_pitch = room.deep;
+            q.a = x.turned; q.a_pitch = room.deep;
+            q.b = a.workspace + room.dz_turned; q.b_pitch = room.deep;
+            q.length = room.deep;
+        }
+        q.a_rows = a.inner; q.b_rows = a.outer;
         q.sums = reinterpret_cast<float*>(a.workspace + room.more_sums);
         q.r.y = a.dweight; q.r.y_stride = a.dweight_stride; q.r.y_type = a.weight_type;
         plan[products++] = room.dweight;

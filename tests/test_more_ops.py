@@ -636,7 +636,7 @@ def test_the_slopes_against_differences(activation):
     assert (slope(z, activation) - want).abs().max() < 1e-8
 
 
-@pytest.mark.parametrize("rows,inner,outer,kind", [(3500, 200, 3600, BF16), (3590, 72, 3700, F16), (3500, 33, 3600, F32), (1, 4096, 5000, BF16), (2000, 264, 1500, BF16), (1500, 1500, 1500, F32), (1531, 1000, 777, F32), (1531, 1001, 777, F32), (3500, 8192, 2500, BF16), (4096, 1500, 5120, F16)])
+@pytest.mark.parametrize("rows,inner,outer,kind", [(3500, 200, 3600, BF16), (3590, 72, 3700, F16), (3500, 33, 3600, F32), (1, 4096, 5000, BF16), (2000, 264, 1500, BF16), (1500, 1500, 1500, F32), (1531, 1000, 777, F32), (1531, 1001, 777, F32), (3500, 8192, 2500, BF16), (4096, 1500, 5120, F16), (4100, 2056, 4104, BF16), (8200, 1032, 4104, F16), (8200, 4096, 1032, BF16)])
 def test_linear_large(T, rows, inner, outer, kind):
     x, w, b, res = linear_inputs(rows, inner, outer, kind)
     y, z = check_linear(T, x, w, b, res, "gelu")
