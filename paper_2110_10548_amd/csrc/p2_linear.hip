@@ -6,6 +6,7 @@
 // each row (64 values of 16 bits, 32 of 32) that are brought to LDS straight from memory while the stage before is multiplied.  The MFMA's rows
 // are A's: a lane has four neighbouring columns of one row of C.
 #include <algorithm>
+#include <cmath>
 #include <limits>
 #include <type_traits>
 
@@ -699,42 +700,114 @@ int64_t tile_b(Cut c) { return kPrices16[c].b; }
 // k_linear_any takes some half more (us, as they are against put in order first, bf16: 700 x 701 x 703 10.4 against 12.8, 100 x 5001 x 9001 50 against 67, 2000 x 1001 x 4001 32 against 36,
 // 4085 x 2093 x 367 34 against 29; fp32 440 x 111 x 78 7.1 against 11.1, 3001 x 2001 x 1003 114 against 108).
 constexpr double kAny = 1.5;
-struct Offer { double us; Plan plan; };
-Offer offer_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t length) {
+// A way to cut a product: blocks that have a tile and those that have a part of one, a tile's stages and a part's, what joining takes, and what all takes in one launch.
+struct Offer { Plan plan; int64_t whole, rest, stages, part; double join, us; };
+// (Of the numbers of parts that keep the units equally long, the one that is worth joining: a call is planned in a few us.)
+constexpr int kOffers = 9;
+int offers_of(Cut cut, int32_t type, int64_t a_rows, int64_t b_rows, int64_t length, Offer (&offers)[kOffers]) {
     const int64_t stages = ceil_div(length, kLine);
     const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
     const int64_t tiles = ceil_div(a_rows, price.a) * ceil_div(b_rows, price.b), full = tiles / kUnits * kUnits;
-    const double load = (double)ceil_div(tiles, kUnits);
-    Offer best = {(double)stages * std::max(price.alone, load * price.shared) + load * price.end, {cut, tiles, 1}};
-    for (int64_t whole = 0; whole < tiles; whole += std::max<int64_t>(full, 1)) {
-        if (whole != 0 && whole != full) break;
+    int n = 0;
+    const auto offer = [&](int64_t whole, int64_t parts) {
+        const int64_t part = ceil_div(stages, parts);
+        const double before = (double)(whole / kUnits), after = (double)ceil_div((tiles - whole) * parts, kUnits), longest = (double)(whole ? stages : part);
+        const double bytes = (double)parts * std::min((double)(tiles - whole) * (double)(price.a * price.b), (double)a_rows * (double)b_rows) * 8.0;
+        const double join = parts == 1 ? 0.0 : 2.5 + 0.15 * (double)parts + bytes / 5e6;
+        const double us = std::max(price.alone * longest, price.shared * (before * (double)stages + after * (double)part)) + (before + after) * price.end + join;
+        if (parts == 1) offers[n++] = {{cut, tiles, 1}, tiles, 0, stages, 0, join, us};
+        else offers[n++] = {{cut, whole, (int32_t)parts}, whole, (tiles - whole) * parts, stages, part, join, us};
+    };
+    offer(0, 1);
+    for (const int64_t whole : {(int64_t)0, full}) {
         const int64_t rest = tiles - whole;
-        for (int32_t parts = 2; parts <= 32 && parts * 4 <= stages && rest * (parts - 1) < 16 * kUnits; ++parts) {       // (more parts than fill the units several times gain nothing)
-            const double before = (double)(whole / kUnits), after = (double)ceil_div(rest * parts, kUnits), long_part = (double)ceil_div(stages, parts);
-            const double bytes = (double)parts * std::min((double)rest * (double)(price.a * price.b), (double)a_rows * (double)b_rows) * 8.0;
-            const double us = std::max(price.alone * (whole ? (double)stages : long_part), price.shared * (before * (double)stages + after * long_part)) + (before + after) * price.end +
-                              2.5 + 0.15 * parts + bytes / 5e6;
-            if (us < best.us) best = {us, {cut, whole, parts}};
+        if (rest == 0 || (whole == 0 && n > 1)) break;                                 // (full may be 0, too)
+        const double each = 0.15 + std::min((double)rest * (double)(price.a * price.b), (double)a_rows * (double)b_rows) * 8.0 / 5e6;      // a part more, joined
+        int64_t before = 1;
+        for (int64_t load = 1; load <= 4; ++load) {
+            const int64_t most = std::min({(int64_t)32, stages / 4, load * kUnits / rest}), worth = (int64_t)(std::sqrt((double)(stages * load) * price.shared / each) + 0.5);
+            const int64_t parts = std::min(most, std::max<int64_t>(worth, 2));
+            if (parts > before) { offer(whole, parts); before = parts; }
         }
     }
-    return best;
+    return n;
 }
 Plan plan_of(int32_t type, int64_t a_rows, int64_t b_rows, int64_t length, bool small, double* us) {
-    Offer best = {std::numeric_limits<double>::infinity(), {}};
+    Offer best = {}, offers[kOffers];
+    best.us = std::numeric_limits<double>::infinity();
     for (const Cut cut : kCuts) {
         if (small && cut == k256) continue;
-        const Offer o = offer_of(cut, type, a_rows, b_rows, length);
-        if (o.us < best.us) best = o;
+        const int n = offers_of(cut, type, a_rows, b_rows, length, offers);
+        for (int i = 0; i < n; ++i)
+            if (offers[i].us < best.us) best = offers[i];
     }
     if (us) *us = best.us;
     return best.plan;
 }
-// Two products of one launch have one cut.
+// Units that are done at the same time.
+struct Shift {
+    double at[16]; int64_t units[16];
+    int n;
+    // `blocks` of `us` each go to the units that are done first
+    void take(int64_t blocks, double us) {
+        while (blocks > 0) {
+            int first = 0, last = 0;
+            for (int i = 1; i < n; ++i) {
+                if (at[i] < at[first]) first = i;
+                if (at[i] > at[last]) last = i;
+            }
+            if (blocks >= kUnits && at[last] - at[first] <= us) {                      // all units alike
+                for (int i = 0; i < n; ++i) at[i] += (double)(blocks / kUnits) * us;
+                blocks %= kUnits;
+                continue;
+            }
+            const int64_t some = n < 16 ? std::min(blocks, units[first]) : units[first];       // (16 shifts are more than four kinds of blocks make)
+            blocks -= some;
+            units[first] -= some;
+            const double end = at[first] + us;
+            int same = 0;
+            while (same < n && !(std::fabs(at[same] - end) < 1e-6 && same != first)) ++same;
+            if (same < n) {
+                units[same] += some;
+                if (units[first] == 0) { at[first] = at[n - 1]; units[first] = units[n - 1]; --n; }
+            } else if (units[first] == 0) {
+                at[first] = end;
+                units[first] = some;
+            } else {
+                at[n] = end;
+                units[n++] = some;
+            }
+        }
+    }
+    double end() const { return *std::max_element(at, at + n); }
+};
+// Two products of one launch have one cut.  What they take is found by dealing their blocks out to the units, of each product's a few ways to cut it.  (us, against the cuts that are best for
+// each by itself: fp16 2001 x 1023 x 515 29.7 -> 26.0, 3001 x 1501 x 2003 74 -> 66, fp32 100 x 3000 x 2000 56.6 -> 54.7; a plan takes the host 1 us)
 void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1, int64_t b1, int64_t length1, Plan& p0, Plan& p1) {
     double least = std::numeric_limits<double>::infinity();
+    Offer o[2][kOffers];
     for (const Cut cut : kCuts) {
-        const Offer o = offer_of(cut, type, a0, b0, length0), q = offer_of(cut, type, a1, b1, length1);
-        if (o.us + q.us < least) { least = o.us + q.us; p0 = o.plan; p1 = q.plan; }
+        const Price& price = type == P2_F32 ? kPrices32[cut] : kPrices16[cut];
+        int n[2] = {offers_of(cut, type, a0, b0, length0, o[0]), offers_of(cut, type, a1, b1, length1, o[1])};
+        if (price.shared * (double)(o[0][0].whole * o[0][0].stages + o[1][0].whole * o[1][0].stages) / kUnits >= least) continue;
+        for (int k = 0; k < 2; ++k) {                          // uncut, and the best two of the others
+            std::partial_sort(o[k] + 1, o[k] + std::min(n[k], 3), o[k] + n[k], [](const Offer& x, const Offer& y) { return x.us < y.us; });
+            n[k] = std::min(n[k], 3);
+        }
+        for (int i = 0; i < n[0]; ++i)
+            for (int k = 0; k < n[1]; ++k) {
+                const Offer &x = o[0][i], &y = o[1][k];
+                Shift shift;
+                shift.n = 1; shift.at[0] = 0.0; shift.units[0] = kUnits;
+                for (const Offer* f : {&x, &y}) {
+                    shift.take(f->whole, price.shared * (double)f->stages + price.end);
+                    shift.take(f->rest, price.shared * (double)f->part + price.end);
+                }
+                const double alone = price.alone * (double)std::max(x.whole ? x.stages : x.part, y.whole ? y.stages : y.part) + price.end;
+                double us = std::max(shift.end(), alone) + std::max(0.0, x.join - 2.5) + std::max(0.0, y.join - 2.5);      // (there is a launch for dbias anyway)
+                if (cut == k256 && type != P2_F32) us = x.us + y.us;                   // (turned operands: a launch each)
+                if (us < least) { least = us; p0 = x.plan; p1 = y.plan; }
+            }
     }
 }
 int64_t sums_bytes(const Plan& p, int64_t a_rows, int64_t b_rows) {
@@ -853,6 +926,10 @@ ForwardRoom forward_room(const LinearForward& a) {
 
 struct BackwardRoom { Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
 BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
+    // (A call asks twice, for its workspace and for itself: the last sizes' answer is kept.)
+    struct Last { int32_t type; int64_t rows, inner, outer; BackwardRoom room; };
+    static thread_local Last last = {};
+    if (last.rows == rows && last.type == type && last.inner == inner && last.outer == outer) return last.room;
     const int64_t size = (int64_t)type_bytes(type);
     BackwardRoom r = {};
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
@@ -866,6 +943,7 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     r.sums = r.lines + round_up(ceil_div(rows, 64) * outer * 4, 256);
     r.more_sums = r.sums + sums_bytes(r.dx, inner, rows);
     r.bytes = r.more_sums + sums_bytes(r.dweight, inner, outer);
+    last = {type, rows, inner, outer, r};
     return r;
 }
 
