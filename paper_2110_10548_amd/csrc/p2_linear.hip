@@ -32,11 +32,15 @@ int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 // has nothing to hide behind.)
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
 
+// z (1 + tanh u) / 2 = z sigmoid(2 u), and 2 u = 2 sqrt(2 / pi) (z + 0.044715 z^3), here times -log2 e: the sigmoid.
+__device__ __forceinline__ float gelu_part(float z, float square) {
+    constexpr float kOne = -1.5957691216057308f * kLog2e;
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * fmaf(kOne * 0.044715f, square, kOne)));
+}
 template <int kActivation> __device__ __forceinline__ float activated(float z) {
     if constexpr (kActivation == P2_RELU) return z < 0.0f ? 0.0f : z;
     else if constexpr (kActivation == P2_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    // (z (1 + tanh u) / 2 = z sigmoid(2 u))
-    else if constexpr (kActivation == P2_GELU_TANH) return z * sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+    else if constexpr (kActivation == P2_GELU_TANH) return z * gelu_part(z, z * z);
     else if constexpr (kActivation == P2_SILU) return z * sigmoid_of(z);
     else return z;
 }
@@ -46,9 +50,9 @@ template <int kActivation> __device__ __forceinline__ float slope(float z) {
     } else if constexpr (kActivation == P2_GELU) {
         return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
     } else if constexpr (kActivation == P2_GELU_TANH) {
-        const float p = sigmoid_of(1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.0f));
+        const float square = z * z, p = gelu_part(z, square);
         const float flat = p * (1.0f - p);                 // (0 far out, where what it is multiplied by may be infinite)
-        return flat == 0.0f ? p : p + flat * z * 1.5957691216057308f * fmaf(0.134145f * z, z, 1.0f);
+        return flat == 0.0f ? p : fmaf(flat, z * fmaf(1.5957691216057308f * 0.134145f, square, 1.5957691216057308f), p);
     } else if constexpr (kActivation == P2_SILU) {
         const float p = sigmoid_of(z);
         return p * (1.0f + z * (1.0f - p));
@@ -633,9 +637,11 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
             }
     }
     const int moved = last >= 0 ? (int)min(c - place, (int64_t)4) : c == 0 ? 0 : 4, there = (int)min(max(a.cols - c, (int64_t)0), (int64_t)4);
+    const bool inside = r0 + 64 <= a.rows && c0 + 64 <= a.cols;
     const auto in_place = [&](const vec_t<T, 4>& from, float (&v)[4], bool row) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = (float)from[q];
+        if (inside) return;
 #pragma unroll
         for (int m = 0; m < 3; ++m)
             if (m < moved) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; }
