@@ -117,13 +117,20 @@ template <typename T> __device__ __noinline__ void choose_exactly(const T* row, 
             one = 0;
         }
     }
-    // the largest, by the upper halves, the lower ones, the index (a reduction of 32 bits takes 8 instructions, one of 64 some 40)
+    // the largest, by the upper halves, and where they are equal the lower ones, the index (a reduction of 32 bits takes 8 instructions, one of 64 some 40)
     bool known = true;                                         // whether `two` is the lane's next
     for (int n = 0; n < k; ++n) {
         const uint32_t high = group_reduce<64>((uint32_t)(one >> 32), most_of);
-        const uint32_t low = group_reduce<64>((uint32_t)(one >> 32) == high ? (uint32_t)one : 0u, most_of);
-        const bool best = one == ((uint64_t)high << 32 | low);
-        const uint32_t expert = ~group_reduce<64>(best ? ~(uint32_t)first : 0u, most_of);
+        bool best = (uint32_t)(one >> 32) == high;
+        const uint64_t whose = __ballot(best);
+        uint32_t expert;
+        if (whose & (whose - 1)) {
+            const uint32_t low = group_reduce<64>(best ? (uint32_t)one : 0u, most_of);
+            best = one == ((uint64_t)high << 32 | low);
+            expert = ~group_reduce<64>(best ? ~(uint32_t)first : 0u, most_of);
+        } else {
+            expert = (uint32_t)__builtin_amdgcn_readlane(first, __builtin_ctzll(whose));
+        }
         if (lane == 0) slot[n] = high != 0 ? (int)expert : -1;
         if (high != 0 && best && (uint32_t)first == expert) {
             key[first] = 0;
@@ -532,12 +539,12 @@ template <typename T> __global__ __launch_bounds__(kBlock) void k_route_finish(R
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t waves = (int64_t)(gridDim.x - sum_blocks) * (kBlock / 64);
-    for (int64_t t0 = ((int64_t)(blockIdx.x - sum_blocks) * (kBlock / 64) + wave) * 16; t0 < a.tokens; t0 += waves * 16) {
-        uint64_t again = __ballot(lane < 16 && t0 + lane < a.tokens && a.again[min(t0 + lane, a.tokens - 1)]);
-        while (again) {
+    for (int64_t t0 = (int64_t)(blockIdx.x - sum_blocks) * 64; t0 < a.tokens; t0 += (int64_t)(gridDim.x - sum_blocks) * 64) {
+        uint64_t again = __ballot(t0 + lane < a.tokens && a.again[min(t0 + lane, a.tokens - 1)]);
+        for (int n = 0; again; ++n) {                          // (the block's wavefronts take them in turn)
             const int64_t t = t0 + __builtin_ctzll(again);
             again &= again - 1;
+            if (n % (kBlock / 64) != wave) continue;
             const T* row = static_cast<const T*>(a.logits) + t * a.stride;
             choose_exactly<T>(row, a.bias, a.experts, a.k, a.score, a.groups, exact_lanes, a.group_limit, a.group_best, keys + wave * a.experts, slots[wave]);
             float most = -INFINITY, inv = 1.0f;
@@ -716,7 +723,7 @@ template <typename T> hipError_t route(const RouteForward& a, const Shape& shape
     else route<T, false>(a, shape, blocks, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    const int64_t sums = ceil_div(a.experts + 1, 4), others = std::min<int64_t>(ceil_div(a.tokens, kBlock / 4), 2048);
+    const int64_t sums = ceil_div(a.experts + 1, 4), others = std::min<int64_t>(ceil_div(a.tokens, 64), 2048);
     k_route_finish<T><<<dim3((unsigned)(sums + others)), dim3(kBlock), key_bytes(a.experts), s>>>(a, (int32_t)blocks, (int32_t)sums, 64 / (shape.lanes / shape.group_lanes));
     return hipGetLastError();
 }
