@@ -643,6 +643,25 @@ def test_linear_large(T, rows, inner, outer, kind):
     check_linear_gradient(T, x, w, z, res, "gelu")
 
 
+@pytest.mark.parametrize("kind,rows,inner,outer,activation", [(BF16, 8200, 1032, 4104, None), (F16, 8200, 1032, 4104, "silu"), (BF16, 8192, 2056, 4104, "gelu_tanh"), (BF16, 16391, 1032, 1544, None)])
+def test_large_gradients_of_matrices_within_others(T, kind, rows, inner, outer, activation):
+    # what lies around them is NaN, which any product with it would show
+    def within(seed, r, c, scale=1.0):
+        around = torch.full((r + 9, c + 24), math.nan, device="cuda", dtype=kind)
+        around[4:4 + r, 8:8 + c] = draw(seed, r, c, scale=scale).to(kind)
+        return around[4:4 + r, 8:8 + c]
+
+    x, w, dy = within(1, rows, inner), within(2, outer, inner, inner ** -0.5), within(3, rows, outer)
+    z = within(4, rows, outer) if activation else None
+    dx, dw, db = check_linear_gradient(T, x, w, z, dy, activation)
+    one, _, _ = T.p2_linear_backward(dy, x, w, z, activation=activation, dweight=False, dbias=False)
+    _, two, _ = T.p2_linear_backward(dy, x, w, z, activation=activation, dx=False, dbias=False)
+    _, _, three = T.p2_linear_backward(dy, x, w, z, activation=activation, dx=False, dweight=False)
+    assert torch.equal(dx, one) and torch.equal(dw, two) and torch.equal(db, three)
+    again = T.p2_linear_backward(dy.contiguous(), x.contiguous(), w.contiguous(), None if z is None else z.contiguous(), activation=activation)
+    assert all(torch.equal(p, q) for p, q in zip((dx, dw, db), again))
+
+
 def test_linear_of_more_values_than_32_bits_count(T):
     rows, inner = 1 << 20, 2056
     x = torch.zeros(rows, inner, dtype=BF16, device="cuda")
@@ -857,6 +876,27 @@ def test_inputs_are_left_as_they_were(T):
     T.p2_route_bias(bias, r["counts"], 0.1)
     T.p2_square_sum([x, w])
     assert all(torch.equal(a, b) for a, b in zip(before, inputs))
+
+
+def test_results_are_ordinary_tensors(T):
+    x, w, _, _ = linear_inputs(6, 40, 24, BF16)
+    y, z = T.p2_linear_forward(x, w, keep=True)
+    like = torch.empty(6, 24, dtype=BF16, device="cuda")
+    for t in (y, z):
+        assert (t.shape, t.stride(), t.dtype, t.device, t.is_leaf, t.requires_grad, t.is_inference(), t._version) == (like.shape, like.stride(), BF16, like.device, True, False, False, 0)
+    want = 2 * y.double()
+    y.requires_grad_()
+    (y * y).sum().backward()
+    compare(y.grad, want, 0.0, "a result's gradient")
+    z.add_(1)
+    assert z._version == 1
+    with torch.inference_mode():
+        assert T.p2_linear_forward(x, w)[0].is_inference()
+    before = torch.cuda.memory_allocated()
+    big = T.p2_route_forward(torch.zeros(1 << 16, 64, device="cuda"), 8)
+    assert torch.cuda.memory_allocated() - before >= (1 << 16) * 64
+    del big
+    assert torch.cuda.memory_allocated() == before
 
 
 def test_a_parameter_that_would_not_train_is_warned_of(T):
