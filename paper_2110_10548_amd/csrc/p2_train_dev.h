@@ -190,7 +190,7 @@ struct RouteForward {
     float scale;
     int32_t experts, k, type, score, groups, group_limit, group_best, renormalise;
 };
-int64_t route_forward_blocks(int64_t tokens, int32_t experts, int32_t k, int32_t groups);
+int64_t route_forward_blocks(int64_t tokens, int32_t experts, int32_t k, int32_t groups);      // at most, with or without a bias
 hipError_t launch_route_forward(const RouteForward& a, hipStream_t stream);
 
 struct RouteBackward {
