@@ -570,15 +570,36 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_join(Join 
     store_typed(all.out, all.type, c, s);
 }
 
-// A few rows of x against all of the weight's, which are read once: a wavefront takes kEach of them at a time.  Bound by memory: 1 x 4096 x 16384 bf16 28.6 us, 4.7 TB/s.
-template <typename T, int kRows, int kEach> __global__ __launch_bounds__(256) void k_linear_rows(const T* x, int64_t x_stride, const T* weight, int64_t weight_stride, int64_t inner,
+// A few rows of x against all of the weight's, which are read once: a wavefront takes kEach of them at a time.  Bound by memory.
+template <typename T, int kRows, int kEach, int kAhead> __global__ __launch_bounds__(256) void k_linear_rows(const T* x, int64_t x_stride, const T* weight, int64_t weight_stride, int64_t inner,
                                                                                                  int64_t outer, Result r) {
     constexpr int V = 16 / sizeof(T);
     const int lane = threadIdx.x & 63;
     const int64_t i0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kEach;
     if (i0 >= outer) return;
     float sum[kRows][kEach] = {};
-    for (int64_t k = lane * V; k < inner; k += 64 * V) {
+    int64_t k = lane * V;
+    // of long rows, kAhead vectors of each under way at once (1 x 4096 x 16384 bf16 28.0 -> 24.4 us, part of it from the last cache; 1 x 8000 x 500 fp16 15.2 -> 7.4)
+    if constexpr (kAhead > 1) for (int64_t whole = kAhead * 64 * V; whole <= inner; whole += kAhead * 64 * V, k += kAhead * 64 * V) {
+        vec_t<T, V> w[kAhead][kEach], v[kAhead][kRows];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) w[u][e] = *reinterpret_cast<const vec_t<T, V>*>(weight + min(i0 + e, outer - 1) * weight_stride + k + u * 64 * V);
+#pragma unroll
+            for (int m = 0; m < kRows; ++m) v[u][m] = *reinterpret_cast<const vec_t<T, V>*>(x + m * x_stride + k + u * 64 * V);
+        }
+        in_this_order();
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int m = 0; m < kRows; ++m)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) sum[m][e] = fmaf((float)v[u][m][q], (float)w[u][e][q], sum[m][e]);
+    }
+    for (; k < inner; k += 64 * V) {
         float p[kRows][V], q[kEach][V];
 #pragma unroll
         for (int e = 0; e < kEach; ++e) load_part<T, V>(weight + min(i0 + e, outer - 1) * weight_stride + k, inner - k, q[e], 0.0f);
@@ -597,6 +618,90 @@ template <typename T, int kRows, int kEach> __global__ __launch_bounds__(256) vo
 #pragma unroll
         for (int e = 0; e < kEach; ++e) v[e] = group_sum<64>(sum[m][e]);
         if (lane == m) finish<T, 4>(r, m, i0, min((int64_t)kEach, outer - i0), v);
+    }
+}
+
+// Up to 32 rows of x against all of the weight's, straight into registers, of any alignment, without LDS and its barriers.  A block has kFragments * 16 of the weight's rows, and
+// its eight wavefronts share their length in pieces of 128 bytes, kAhead of them under way at once; their sums are added up in order.  x has up to kRows * 16 rows.  Bound by memory, or by a
+// wavefront's chain of loads: 16 x 4096 x 16384 bf16 34 to 37 us, 3.7 to 4.0 TB/s; 16 x 1000 x 1000 5.3 us.
+template <typename T, int kRows, int kFragments, int kAhead> __global__ __launch_bounds__(512) void k_linear_thin(const T* x, int64_t x_stride, const T* weight, int64_t weight_stride, int64_t rows,
+                                                                                                               int64_t inner, int64_t outer, Result r) {
+    typedef typename Fragment<T>::type F;
+    constexpr int V = 16 / sizeof(T), kPiece = kLine / (int)sizeof(T);
+    __shared__ float4_t part[8][kRows * kFragments][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), row = lane & 15, quad = lane >> 4;
+    const int64_t i0 = (int64_t)blockIdx.x * kFragments * 16;
+    const T *pw[kFragments], *px[kRows];
+#pragma unroll
+    for (int f = 0; f < kFragments; ++f) pw[f] = weight + min(i0 + f * 16 + row, outer - 1) * weight_stride + quad * V;          // (rows past the end: the last one again, whose results nobody writes)
+#pragma unroll
+    for (int f = 0; f < kRows; ++f) px[f] = x + min((int64_t)f * 16 + row, rows - 1) * x_stride + quad * V;
+    float4_t acc[kRows][kFragments];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+#pragma unroll
+        for (int f = 0; f < kFragments; ++f) acc[i][f] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const int whole = (int)(inner / kPiece);
+    const auto pieces = [&](int first, auto n) {               // n pieces, eight apart
+        constexpr int kN = decltype(n)::value;
+        vec_t<T, V> w[kN][kFragments][2], v[kN][kRows][2];
+#pragma unroll
+        for (int u = 0; u < kN; ++u) {
+            const int64_t at = (int64_t)(first + u * 8) * kPiece;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int f = 0; f < kFragments; ++f) w[u][f][c] = *reinterpret_cast<const vec_t<T, V>*>(pw[f] + at + c * 4 * V);
+#pragma unroll
+                for (int f = 0; f < kRows; ++f) v[u][f][c] = *reinterpret_cast<const vec_t<T, V>*>(px[f] + at + c * 4 * V);
+            }
+        }
+        in_this_order();                                       // (or the compiler asks for a piece when the one before it is there)
+#pragma unroll
+        for (int u = 0; u < kN; ++u)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                    for (int f = 0; f < kFragments; ++f) multiply(__builtin_bit_cast(F, w[u][f][c]), __builtin_bit_cast(F, v[u][i][c]), acc[i][f]);
+    };
+    int s = wave;
+    for (; s + 8 * (kAhead - 1) < whole; s += 8 * kAhead) pieces(s, std::integral_constant<int, kAhead>());
+    for (; s < whole; s += 8) pieces(s, std::integral_constant<int, 1>());
+    if (s == whole && inner % kPiece) {                        // the rest, past which there are zeros
+        const auto some = [&](const T* p, int c) {
+            const int64_t at = (int64_t)whole * kPiece + c * 4 * V;
+            vec_t<T, V> o;
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = at + quad * V + j < inner ? p[at + j] : (T)0.0f;
+            return __builtin_bit_cast(F, o);
+        };
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            F v[kRows];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v[i] = some(px[i], c);
+#pragma unroll
+            for (int f = 0; f < kFragments; ++f) {
+                const F w = some(pw[f], c);
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) multiply(w, v[i], acc[i][f]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+#pragma unroll
+        for (int f = 0; f < kFragments; ++f) part[wave][i * kFragments + f][lane] = acc[i][f];
+    __syncthreads();
+    for (int t = wave; t < kRows * kFragments; t += 8) {
+        float4_t sum = part[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) sum += part[w][t][lane];
+        const int64_t j = t / kFragments * 16 + row, i = i0 + t % kFragments * 16 + quad * 4;
+        float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+        if (j < rows && i < outer) finish<T, 4>(r, j, i, outer - i, v);
     }
 }
 
@@ -904,12 +1009,19 @@ bool in_order(const void* p, int64_t stride, int32_t type, int64_t cols) {
     const int64_t size = (int64_t)type_bytes(type);
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && cols * size % 16 == 0 && stride * size <= ((int64_t)1 << 22);
 }
-bool few_rows(int64_t rows) { return rows <= 4; }
+// So few that the products are worked out beside the loads (3 and 4 of 16 bits, which have to be converted: 4 x 4096 x 16384 bf16 50 us, by matrix instructions 34).
+bool few_rows(int64_t rows, int32_t type) { return rows <= (type == P2_F32 ? 4 : 2); }
+// What k_linear_thin takes, in us, as in offers_of: a wavefront's pieces one after the other, or the weight's bytes (of rows that are not in order the caches pass each line several times).
+double thin_us(const LinearForward& a, bool ordered) {
+    const double bytes = (double)a.inner * (double)type_bytes(a.type), blocks = (double)a.outer / (a.outer >= 32 * kUnits ? 32.0 : 16.0);
+    const double pieces = std::ceil(bytes / (8 * kLine)) * (a.rows <= 16 ? 0.55 : 1.2) * std::ceil(blocks / (2.0 * kUnits));
+    return 0.8 + std::max(pieces, bytes * (double)a.outer / 4.3e6 * (ordered ? 1.0 : 3.0));
+}
 
-struct ForwardRoom { bool pack_x, pack_weight, any; Plan plan; int64_t length, x, weight, sums, bytes; };
+struct ForwardRoom { bool thin, pack_x, pack_weight, any; Plan plan; int64_t length, x, weight, sums, bytes; };
 ForwardRoom forward_room(const LinearForward& a) {
     ForwardRoom r = {};
-    if (few_rows(a.rows)) return r;
+    if (few_rows(a.rows, a.type)) return r;
     const int64_t size = (int64_t)type_bytes(a.type), padded = round_up(a.inner * size, kLine);
     r.pack_x = !in_order(a.x, a.x_stride, a.type, a.inner);
     r.pack_weight = !in_order(a.weight, a.weight_stride, a.type, a.inner);
@@ -921,11 +1033,20 @@ ForwardRoom forward_room(const LinearForward& a) {
         const Plan any = plan_of(a.type, a.outer, a.rows, a.inner * size, true, &any_us);
         us += 4.0 + ((r.pack_x ? a.rows : 0) + (r.pack_weight ? a.outer : 0)) * (double)a.inner * size * 2.0 / 3.5e6;
         if (any_us * kAny < us) {
+            us = any_us * kAny;
             r.plan = any;
             r.any = true;
             r.pack_x = r.pack_weight = false;
             r.length = a.inner * size;
         }
+    }
+    // Few rows come out of registers where that takes less (rows x inner x outer, us: bf16 5 x 4096 x 16384 38 -> 34, 16 x 1000 x 1000 8.5 -> 5.3, fp32 8 x 4096 x 8192 44 -> 34, 8 x 1001 x 2003 10.6 -> 5.6; but
+    // fp16 30 x 8000 x 500 11 -> 22, bf16 16 x 4097 x 16383 54 -> 77).
+    const double weight_us = (double)a.outer * (double)a.inner * (double)size / 3.8e6;
+    if (a.rows <= 32 && thin_us(a, in_order(a.x, a.x_stride, a.type, 16 / size) && in_order(a.weight, a.weight_stride, a.type, 16 / size)) < std::max(us, weight_us)) {
+        ForwardRoom thin = {};
+        thin.thin = true;
+        return thin;
     }
     r.x = 0;
     r.weight = r.x + (r.pack_x ? round_up(a.rows * padded, 256) : 0);
@@ -962,17 +1083,41 @@ template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) 
     r.bias = a.bias; r.residual = a.residual; r.y = a.y; r.z = a.z;
     r.residual_stride = a.residual_stride; r.y_stride = a.y_stride; r.z_stride = a.z_stride;
     r.y_type = a.type; r.activation = a.activation;
-    if (few_rows(a.rows)) {
-        const T* x = static_cast<const T*>(a.x);
-        const T* w = static_cast<const T*>(a.weight);
+    const T* x = static_cast<const T*>(a.x);
+    const T* w = static_cast<const T*>(a.weight);
+    if (few_rows(a.rows, a.type)) {
         const dim3 grid((unsigned)ceil_div(a.outer, 8)), block(256);
-        if (a.rows == 1) k_linear_rows<T, 1, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
-        else if (a.rows == 2) k_linear_rows<T, 2, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
-        else if (a.rows == 3) k_linear_rows<T, 3, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
-        else k_linear_rows<T, 4, 2><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        const auto launch = [&](auto rows, auto ahead) {
+            k_linear_rows<T, decltype(rows)::value, 2, decltype(ahead)::value><<<grid, block, 0, s>>>(x, a.x_stride, w, a.weight_stride, a.inner, a.outer, r);
+        };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        const bool ahead = a.inner * (int64_t)sizeof(T) >= 4 * 64 * 16;
+        if (a.rows == 1) { if (ahead) launch(one, four); else launch(one, one); }
+        else if (a.rows == 2) { if (ahead) launch(two, four); else launch(two, one); }
+        else if constexpr (sizeof(T) == 4) {
+            if (a.rows == 3) launch(std::integral_constant<int, 3>(), one);
+            else launch(four, one);
+        }
         return hipGetLastError();
     }
     const ForwardRoom room = forward_room(a);
+    if (room.thin) {
+        const auto launch = [&](auto rows, auto fragments, auto ahead) {
+            constexpr int kFragments = decltype(fragments)::value;
+            k_linear_thin<T, decltype(rows)::value, kFragments, decltype(ahead)::value>
+                <<<dim3((unsigned)ceil_div(a.outer, kFragments * 16)), dim3(512), 0, s>>>(x, a.x_stride, w, a.weight_stride, a.rows, a.inner, a.outer, r);
+        };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        const bool wide = a.outer >= 32 * kUnits;              // (enough blocks of twice as many of the weight's rows)
+        if (a.rows <= 16) { if (wide) launch(one, two, four); else launch(one, one, four); }
+        else if (wide) launch(two, two, two);
+        else launch(two, one, four);
+        return hipGetLastError();
+    }
     const int64_t padded = round_up(a.inner * (int64_t)sizeof(T), kLine);
     Product p = {};
     p.a = static_cast<const char*>(a.weight);

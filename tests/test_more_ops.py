@@ -597,7 +597,8 @@ def check_linear_gradient(T, x, w, z, dy, activation, dtype=None):
 
 
 LINEAR = [(1, 1, 1), (1, 7, 3), (1, 8, 4), (1, 64, 17), (1, 1000, 777), (2, 513, 5), (3, 64, 64), (4, 200, 33), (5, 1, 1), (5, 63, 66), (5, 4096, 10), (8, 8, 8), (16, 16, 16),
-          (17, 72, 130), (63, 65, 64), (64, 64, 65), (65, 128, 129), (100, 1000, 50), (127, 40, 260), (300, 24, 515), (33, 5000, 40), (70, 20001, 66), (515, 136, 257)]
+          (17, 72, 130), (63, 65, 64), (64, 64, 65), (65, 128, 129), (100, 1000, 50), (127, 40, 260), (300, 24, 515), (33, 5000, 40), (70, 20001, 66), (515, 136, 257), (16, 1000, 1000), (32, 520, 8300), (20, 264, 8192), (9, 65, 33),
+          (31, 129, 70), (2, 2049, 100), (1, 8192, 40), (12, 2047, 8200)]
 
 
 @pytest.mark.parametrize("rows,inner,outer", LINEAR)
