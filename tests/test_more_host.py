@@ -182,6 +182,15 @@ def test_workspaces(T):
     assert L.p2_linear_backward_workspace(3, 1, 64, 64, C.byref(n)) == EINVAL
 
 
+@pytest.mark.parametrize("tokens,needed", [(0, False), (1, False), (16, False), (17, True), (32, True), (33, True)])
+def test_the_choice_s_workspace_is_enough_with_and_without_a_bias(T, tokens, needed):
+    n = C.c_int64()
+    assert T.lib().p2_route_forward_workspace(tokens, 256, 8, 8, C.byref(n)) == 0 and (n.value > 0) == needed
+    if needed:
+        for bias in (NULL, P):
+            assert _route_forward(T, tokens=tokens, experts=256, stride=256, k=8, groups=8, bias=bias, workspace=NULL, workspace_bytes=0) == EINVAL
+
+
 def test_tensors_elsewhere_or_of_other_kinds_are_refused(T):
     x, i = torch.ones(4, 8), torch.zeros(4, 2, dtype=torch.int32)
     s = T.p2_adamw_state([x])

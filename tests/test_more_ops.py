@@ -95,7 +95,8 @@ def check_route(T, logits, k, **kw):
 # tokens, experts, k, groups, limit, best
 CHOICES = [(1, 1, 1, 1, 1, 1), (3, 2, 2, 1, 1, 1), (5, 3, 2, 3, 2, 1), (9, 8, 8, 1, 1, 1), (33, 8, 8, 4, 3, 2), (257, 12, 3, 4, 2, 2), (100, 60, 4, 6, 3, 1), (1, 64, 2, 1, 1, 1),
            (513, 64, 6, 8, 3, 2), (301, 96, 8, 1, 1, 2), (77, 160, 6, 8, 3, 1), (1030, 256, 8, 8, 4, 2), (64, 256, 8, 1, 1, 1), (50, 254, 5, 2, 1, 2), (130, 255, 9, 5, 2, 2),
-           (40, 510, 8, 17, 5, 2), (21, 1023, 16, 33, 9, 2), (20, 1024, 64, 64, 64, 1), (19, 1024, 64, 1, 1, 1), (11, 1023, 64, 3, 1, 2), (13, 777, 33, 7, 6, 2), (40, 1000, 33, 40, 7, 1)]
+           (40, 510, 8, 17, 5, 2), (21, 1023, 16, 33, 9, 2), (20, 1024, 64, 64, 64, 1), (19, 1024, 64, 1, 1, 1), (11, 1023, 64, 3, 1, 2), (13, 777, 33, 7, 6, 2), (40, 1000, 33, 40, 7, 1),
+           (32, 256, 8, 1, 1, 1), (20, 256, 8, 8, 4, 2), (64, 64, 4, 4, 2, 1)]
 
 
 @pytest.mark.parametrize("tokens,experts,k,groups,limit,best", CHOICES)
