@@ -791,6 +791,122 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
     }
 }
 
+// The gradients of up to kRows rows, in one pass over weight and dweight: a wavefront has V columns a lane and kEach of the weight's rows, of which it reads each once, adds dz times it to dx's
+// sums and writes what dz and x make of it.  A block's four wavefronts have the same columns; their sums, and those of the blocks along `outer`, are added up in order.  Lanes that the row's end
+// cuts take its last V columns, which two lanes then work out alike.  Bound by memory:
+// 1 x 4096 x 16384 bf16 48 us, 5.6 TB/s of the two matrices, part of it from the last cache, 8 rows 59 (as products of matrices that are put in order 121 and 122); small ones by two launches, 16 bits'
+// eight rows by their vector instructions: 8 x 1000 x 1000 bf16 12.9 (14.9), 8 x 1001 x 2003 fp32 13.0 (23.9), 8 x 16384 x 100 bf16 16.1 (14.8).
+struct Thin {
+    const void* dy; const void* z; const void* x; const void* weight; void* dweight; void* dbias; float* sums;     // sums: [parts][rows][across * 64 V], or NULL
+    int64_t dy_stride, z_stride, x_stride, weight_stride, dweight_stride, inner, outer;
+    int32_t rows, activation, weight_type, across;
+};
+template <typename T, int kRows, int kEach> __global__ __launch_bounds__(256) void k_linear_thin_backward(Thin a) {
+    constexpr int V = 16 / sizeof(T), kOuter = 4 * kEach, kAhead = 8;
+    __shared__ float dz[kOuter][kRows];
+    __shared__ float part[4][64 * V];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int group = blockIdx.x % a.across, line = blockIdx.x / a.across;
+    const int64_t o0 = (int64_t)line * kOuter, c = min(((int64_t)group * 64 + lane) * V, a.inner - V);
+    // (rows past the last are that one again, and zeros once they are there: loads without conditions are under way together)
+    vec_t<T, V> raw[kRows];
+    if (a.dweight)
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) raw[j] = *reinterpret_cast<const vec_t<T, V>*>(static_cast<const T*>(a.x) + min(j, a.rows - 1) * a.x_stride + c);
+    // dz, whose sums over the rows are dbias
+    for (int t = threadIdx.x; t < kOuter; t += 256) {
+        const int64_t o = min(o0 + t, a.outer - 1);
+        T y[kRows], z[kRows];
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) y[j] = static_cast<const T*>(a.dy)[min(j, a.rows - 1) * a.dy_stride + o];
+        if (a.z)
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) z[j] = static_cast<const T*>(a.z)[min(j, a.rows - 1) * a.z_stride + o];
+        float v[kRows], slopes[kRows], sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) { v[j] = (float)y[j]; slopes[j] = a.z ? (float)z[j] : 0.0f; }
+        if (a.z) times_slope(v, slopes, a.activation);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            if (j >= a.rows) v[j] = 0.0f;
+            sum += v[j];
+            dz[t][j] = (float)(T)v[j];
+        }
+        if (a.dbias && group == 0 && o0 + t < a.outer) store_typed(a.dbias, a.weight_type, o, sum);
+    }
+    float x[kRows][V] = {}, dx[kRows][V] = {};
+    if (a.dweight)
+#pragma unroll
+        for (int j = 0; j < kRows; ++j)
+#pragma unroll
+            for (int q = 0; q < V; ++q) x[j][q] = j < a.rows ? (float)raw[j][q] : 0.0f;
+    __syncthreads();
+    const int64_t first = o0 + wave * kEach;
+    const int n = (int)max((int64_t)0, min(a.outer - first, (int64_t)kEach));
+    for (int e0 = 0; e0 < n; e0 += kAhead) {
+        vec_t<T, V> w[kAhead] = {};
+        if (a.sums) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) w[u] = *reinterpret_cast<const vec_t<T, V>*>(static_cast<const T*>(a.weight) + (first + min(e0 + u, n - 1)) * a.weight_stride + c);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (e0 + u >= n) break;
+            float d[kRows], out[V] = {};
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) d[j] = dz[wave * kEach + e0 + u][j];
+            if (a.sums) {
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) dx[j][q] = fmaf(d[j], (float)w[u][q], dx[j][q]);
+            }
+            if (a.dweight) {
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+#pragma unroll
+                    for (int q = 0; q < V; ++q) out[q] = fmaf(d[j], x[j][q], out[q]);
+                const int64_t at = (first + e0 + u) * a.dweight_stride + c;
+                if (a.weight_type == P2_F32) store_vec<float, V>(static_cast<float*>(a.dweight) + at, out);
+                else if (a.weight_type == P2_BF16) store_vec<bf16_t, V>(static_cast<bf16_t*>(a.dweight) + at, out);
+                else store_vec<half_t, V>(static_cast<half_t*>(a.dweight) + at, out);
+            }
+        }
+    }
+    if (!a.sums) return;
+    const int64_t pitch = (int64_t)a.across * 64 * V;
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        if (j >= a.rows) break;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < V; ++q) part[wave][q * 64 + lane] = dx[j][q];
+        __syncthreads();
+        for (int t = threadIdx.x; t < 64 * V; t += 256) {
+            const int at = t % V * 64 + t / V;                 // column t of the block's
+            a.sums[((int64_t)line * a.rows + j) * pitch + (int64_t)group * 64 * V + t] = part[0][at] + part[1][at] + part[2][at] + part[3][at];
+        }
+    }
+}
+// dx from its parts: a block has 16 columns of a row, and 16 threads a column.
+template <typename T> __global__ __launch_bounds__(256) void k_linear_thin_join(const float* sums, int64_t parts, int32_t rows, int64_t inner, int64_t pitch, T* dx, int64_t dx_stride) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float part[16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, across = (int)((inner + 15) / 16), j = blockIdx.x / across;
+    const int64_t i = (int64_t)(blockIdx.x % across) * 16 + x, cut = inner / V * V;
+    const int64_t at = i < cut ? i : cut + V - (inner - min(i, inner - 1));            // the last lane has the row's last V columns
+    const float* from = sums + j * pitch + at;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int64_t p = y; p < parts; p += 16) s += from[p * rows * pitch];
+    part[y][x] = s;
+    __syncthreads();
+    if (y > 0 || i >= inner) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += part[k][x];
+    dx[j * dx_stride + i] = (T)s;
+}
+
 __global__ __launch_bounds__(256) void k_linear_zero(void* out, int32_t type, int64_t stride, int64_t rows, int64_t cols) {
     for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < rows * cols; x += (int64_t)gridDim.x * 256) store_typed(out, type, x / cols * stride + x % cols, 0.0f);
 }
@@ -1055,7 +1171,7 @@ ForwardRoom forward_room(const LinearForward& a) {
     return r;
 }
 
-struct BackwardRoom { Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
+struct BackwardRoom { bool thin; int64_t each, across, parts; Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
 BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     // (A call asks twice, for its workspace and for itself: the last sizes' answer is kept.)
     struct Last { int32_t type; int64_t rows, inner, outer; BackwardRoom room; };
@@ -1063,6 +1179,16 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     if (last.rows == rows && last.type == type && last.inner == inner && last.outer == outer) return last.room;
     const int64_t size = (int64_t)type_bytes(type);
     BackwardRoom r = {};
+    const int64_t values = 16 / size;
+    if (rows <= 8 && inner >= values) {
+        r.thin = true;
+        r.across = ceil_div(inner, 64 * values);
+        r.each = r.across * ceil_div(outer, 256) >= 2 * kUnits ? 64 : 8;               // of the weight's rows a wavefront
+        r.parts = ceil_div(outer, 4 * r.each);
+        r.bytes = round_up(r.parts * rows * r.across * 64 * values * 4, 256);
+        last = {type, rows, inner, outer, r};
+        return r;
+    }
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
     r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
     plan_both(type, inner, rows, r.along, inner, outer, r.deep, r.dx, r.dweight);
@@ -1147,6 +1273,29 @@ template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) 
 
 template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s) {
     const BackwardRoom room = backward_room(a.type, a.rows, a.inner, a.outer);
+    if (room.thin) {
+        Thin t = {};
+        t.dy = a.dy; t.x = a.x; t.weight = a.weight; t.dweight = a.dweight; t.dbias = a.dbias;
+        if (a.activation != P2_NO_ACTIVATION) t.z = a.z;
+        if (a.dx) t.sums = reinterpret_cast<float*>(a.workspace);
+        t.dy_stride = a.dy_stride; t.z_stride = a.z_stride; t.x_stride = a.x_stride; t.weight_stride = a.weight_stride; t.dweight_stride = a.dweight_stride;
+        t.inner = a.inner; t.outer = a.outer; t.rows = (int32_t)a.rows; t.activation = a.activation; t.weight_type = a.weight_type; t.across = (int32_t)room.across;
+        const auto launch = [&](auto rows) {
+            constexpr int kRows = decltype(rows)::value;
+            const dim3 grid((unsigned)(room.across * room.parts)), block(256);
+            if (room.each == 64) k_linear_thin_backward<T, kRows, 64><<<grid, block, 0, s>>>(t);
+            else k_linear_thin_backward<T, kRows, 8><<<grid, block, 0, s>>>(t);
+        };
+        if (a.rows == 1) launch(std::integral_constant<int, 1>());
+        else if (a.rows == 2) launch(std::integral_constant<int, 2>());
+        else if (a.rows <= 4) launch(std::integral_constant<int, 4>());
+        else launch(std::integral_constant<int, 8>());
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || !a.dx) return e;
+        k_linear_thin_join<T><<<dim3((unsigned)(a.rows * ceil_div(a.inner, 16))), dim3(256), 0, s>>>(t.sums, room.parts, t.rows, a.inner, room.across * 64 * (16 / (int64_t)sizeof(T)), static_cast<T*>(a.dx),
+                                                                                                   a.dx_stride);
+        return hipGetLastError();
+    }
     const bool own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
     // Large 16-bit products take weight, x and dz turned as they lie in memory, and only dz is put in order
     // (us, bf16, without / with an activation: 8192 x 4096 x 4096 428 -> 394 / 460 -> 431, 32768 x 1024 x 1024 213 -> 156 / 248 -> 191, 4096^3 225 -> 207 / 238 -> 220).

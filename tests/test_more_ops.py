@@ -645,8 +645,9 @@ def test_linear_large(T, rows, inner, outer, kind):
     check_linear_gradient(T, x, w, z, res, "gelu")
 
 
-@pytest.mark.parametrize("kind,rows,inner,outer,activation", [(BF16, 8200, 1032, 4104, None), (F16, 8200, 1032, 4104, "silu"), (BF16, 8192, 2056, 4104, "gelu_tanh"), (BF16, 16391, 1032, 1544, None)])
-def test_large_gradients_of_matrices_within_others(T, kind, rows, inner, outer, activation):
+@pytest.mark.parametrize("kind,rows,inner,outer,activation", [(BF16, 8200, 1032, 4104, None), (F16, 8200, 1032, 4104, "silu"), (BF16, 8192, 2056, 4104, "gelu_tanh"), (BF16, 16391, 1032, 1544, None),
+                                                               (BF16, 8, 1003, 777, "silu"), (F16, 3, 100, 2000, None), (F32, 5, 515, 300, "gelu"), (BF16, 1, 4100, 9000, "relu")])
+def test_gradients_of_matrices_within_others(T, kind, rows, inner, outer, activation):
     # what lies around them is NaN, which any product with it would show
     def within(seed, r, c, scale=1.0):
         around = torch.full((r + 9, c + 24), math.nan, device="cuda", dtype=kind)
