@@ -708,12 +708,12 @@ template <typename T, int kRows, int kFragments, int kAhead> __global__ __launch
 // ------------------------------------------------------------------------------------- operands in order
 
 // A matrix as a product takes it: straight, turned, or both, with zeros from its end to whole stages.  With z the values are dy activation'(z), and
-// each tile's sums over its rows go to sums[tile][cols].
+// each tile's sums over its rows go to sums[tile][cols], or, where one tile has all rows, to dbias.
 struct Pack {
-    const void* from; const void* z; char* straight; char* turned; float* sums;
+    const void* from; const void* z; char* straight; char* turned; float* sums; void* dbias;
     int64_t from_stride, z_stride, straight_pitch, turned_pitch;       // pitches in bytes
     int64_t rows, cols;
-    int32_t activation;
+    int32_t activation, dbias_type;
 };
 // Bound by memory: dz of 8192 x 4096 bf16 with gelu_tanh's slope and dbias 42 us for 192 MB, 4.6 TB/s; small ones by the chain of a launch, a load and a store, 5.6 us and more.
 // Several matrices in one launch: the m-th has the blocks from begin[m] on, across[m] of them side by side.
@@ -771,7 +771,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
 #pragma unroll
         for (int q = 0; q < 4; ++q) tile[y + i * 16][x + q] = v[q];
     }
-    if (!a.turned && !a.sums) return;
+    if (!a.turned && !a.sums && !a.dbias) return;
     __syncthreads();
     if (a.turned) {
 #pragma unroll
@@ -783,11 +783,12 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
             if (c < a.cols) store_part<T, 4>(reinterpret_cast<T*>(a.turned + c * a.turned_pitch) + r, a.turned_pitch / (int)sizeof(T) - r, v);
         }
     }
-    if (a.sums && threadIdx.x < 64 && c0 + threadIdx.x < a.cols) {
+    if ((a.sums || a.dbias) && threadIdx.x < 64 && c0 + threadIdx.x < a.cols) {
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < 64; ++i) s += tile[i][threadIdx.x];
-        a.sums[(int64_t)line * a.cols + c0 + threadIdx.x] = s;
+        if (a.sums) a.sums[(int64_t)line * a.cols + c0 + threadIdx.x] = s;
+        else store_typed(a.dbias, a.dbias_type, c0 + threadIdx.x, s);
     }
 }
 
@@ -1012,9 +1013,9 @@ struct Shift {
     }
     double end() const { return *std::max_element(at, at + n); }
 };
-// Two products of one launch have one cut.  What they take is found by dealing their blocks out to the units, of each product's a few ways to cut it.  (us, against the cuts that are best for
+// Two products of one launch have one cut.  (joined: there is a launch that joins dbias anyway.)  What they take is found by dealing their blocks out to the units, of each product's a few ways to cut it.  (us, against the cuts that are best for
 // each by itself: fp16 2001 x 1023 x 515 29.7 -> 26.0, 3001 x 1501 x 2003 74 -> 66, fp32 100 x 3000 x 2000 56.6 -> 54.7; a plan takes the host 1 us)
-void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1, int64_t b1, int64_t length1, Plan& p0, Plan& p1) {
+void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1, int64_t b1, int64_t length1, bool joined, Plan& p0, Plan& p1) {
     double least = std::numeric_limits<double>::infinity();
     Offer o[2][kOffers];
     for (const Cut cut : kCuts) {
@@ -1035,7 +1036,7 @@ void plan_both(int32_t type, int64_t a0, int64_t b0, int64_t length0, int64_t a1
                     shift.take(f->rest, price.shared * (double)f->part + price.end);
                 }
                 const double alone = price.alone * (double)std::max(x.whole ? x.stages : x.part, y.whole ? y.stages : y.part) + price.end;
-                double us = std::max(shift.end(), alone) + std::max(0.0, x.join - 2.5) + std::max(0.0, y.join - 2.5);      // (there is a launch for dbias anyway)
+                double us = std::max(shift.end(), alone) + std::max(0.0, x.join - 2.5) + std::max(0.0, y.join - 2.5) + (!joined && (x.rest || y.rest) ? 2.5 : 0.0);
                 if (cut == k256 && type != P2_F32) us = x.us + y.us;                   // (turned operands: a launch each)
                 if (us < least) { least = us; p0 = x.plan; p1 = y.plan; }
             }
@@ -1191,7 +1192,7 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     }
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
     r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
-    plan_both(type, inner, rows, r.along, inner, outer, r.deep, r.dx, r.dweight);
+    plan_both(type, inner, rows, r.along, inner, outer, r.deep, rows > 64, r.dx, r.dweight);
     r.dz = 0;
     r.dz_turned = r.dz + round_up(rows * r.along, 256);
     r.x_turned = r.dz_turned + round_up(outer * r.deep, 256);
@@ -1311,8 +1312,9 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
     dz.rows = a.rows; dz.cols = a.outer; dz.activation = a.activation;
     if ((a.dx || (a.dweight && turned)) && own_dz) { dz.straight = a.workspace + room.dz; dz.straight_pitch = room.along; }
     if (a.dweight && !turned) { dz.turned = a.workspace + room.dz_turned; dz.turned_pitch = room.deep; }
-    if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + room.lines);
-    if (dz.straight || dz.turned || dz.sums) ++packs;
+    if (a.dbias && a.rows <= 64) { dz.dbias = a.dbias; dz.dbias_type = a.weight_type; }
+    else if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + room.lines);
+    if (dz.straight || dz.turned || dz.sums || dz.dbias) ++packs;
     Product p[2] = {};
     Plan plan[2];
     int products = 0;
@@ -1357,7 +1359,7 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
     const hipError_t e = pack<T>(k, packs, s);
     if (e != hipSuccess) return e;
     Join join = {};
-    if (a.dbias) {
+    if (dz.sums) {
         join.lines = dz.sums; join.n = ceil_div(a.rows, 64); join.cols = a.outer;
         join.out = a.dbias; join.type = a.weight_type;
     }

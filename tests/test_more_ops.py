@@ -646,7 +646,7 @@ def test_linear_large(T, rows, inner, outer, kind):
 
 
 @pytest.mark.parametrize("kind,rows,inner,outer,activation", [(BF16, 8200, 1032, 4104, None), (F16, 8200, 1032, 4104, "silu"), (BF16, 8192, 2056, 4104, "gelu_tanh"), (BF16, 16391, 1032, 1544, None),
-                                                               (BF16, 8, 1003, 777, "silu"), (F16, 3, 100, 2000, None), (F32, 5, 515, 300, "gelu"), (BF16, 1, 4100, 9000, "relu")])
+                                                               (BF16, 8, 1003, 777, "silu"), (BF16, 40, 300, 200, "silu"), (F16, 64, 1001, 500, None), (F16, 3, 100, 2000, None), (F32, 5, 515, 300, "gelu"), (BF16, 1, 4100, 9000, "relu")])
 def test_gradients_of_matrices_within_others(T, kind, rows, inner, outer, activation):
     # what lies around them is NaN, which any product with it would show
     def within(seed, r, c, scale=1.0):
