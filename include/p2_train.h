@@ -214,8 +214,9 @@ int32_t p2_linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, 
 
 /* With dz = dy * activation'(z):  dx = dz weight, dweight = dz^T x, dbias = sum over rows of dz; dx, dweight and dbias may each be NULL: not asked
  * for.  z is what the forward pass kept (NULL without an activation); at 0 the slope of P2_RELU is 0.  The residual's gradient is dy.  dweight and
- * dbias have `weight_type`, all else `type`.  dz is rounded to `type` for the products (dbias adds up what has not been rounded).
- * rows = 0 writes zeros to dweight and dbias.  */
+ * dbias have `weight_type`, all else `type`.  Where the matrix units make the products, as they do of more than eight rows, dz is rounded to `type` for
+ * them (in 16 bits with an activation: by half a step at most of each dz, which moves results by as much as rounding them does; a call in P2_F32 rounds
+ * nothing); where they do not, and for dbias, dz is taken as it is.  rows = 0 writes zeros to dweight and dbias.  */
 int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int64_t z_stride, const void* x, int64_t x_stride,
                            const void* weight, int64_t weight_stride, int32_t type, int32_t activation, int64_t rows, int64_t inner,
                            int64_t outer, void* dx, int64_t dx_stride, void* dweight, int64_t dweight_stride, void* dbias,

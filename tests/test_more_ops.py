@@ -665,6 +665,21 @@ def test_gradients_of_matrices_within_others(T, kind, rows, inner, outer, activa
     assert all(torch.equal(p, q) for p, q in zip((dx, dw, db), again))
 
 
+@pytest.mark.parametrize("rows,inner,outer", [(1, 64, 40), (2, 515, 300), (5, 1000, 777), (8, 4100, 1000)])
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("activation", ["gelu", "gelu_tanh", "silu"])
+def test_gradients_of_a_few_rows_take_dz_as_it_is(T, rows, inner, outer, kind, activation):
+    """Up to eight rows are multiplied in 32 bits: dz = dy activation'(z) is not rounded in between."""
+    x, w, _, dy = linear_inputs(rows, inner, outer, kind)
+    z = draw(7, rows, outer).to(kind)
+    dx, dw, db = T.p2_linear_backward(dy, x, w, z, activation=activation, dtype=F32)
+    dz = dy.double() * slope(z.double(), activation)
+    own = 2 * U * (40 + z.double().abs()) * dy.double().abs()
+    assert dw.dtype == F32
+    compare(dw, dz.t() @ x.double(), (rows + 1) * 2 * U * (dz.abs().t() @ x.double().abs()) + 1.1 * own.t() @ x.double().abs(), "dweight")
+    compare(dx, dz @ w.double(), (outer / 4 + 32) * 2 * U * (dz.abs() @ w.double().abs()) + 1.1 * own @ w.double().abs(), "dx")
+
+
 def test_linear_of_more_values_than_32_bits_count(T):
     rows, inner = 1 << 20, 2056
     x = torch.zeros(rows, inner, dtype=BF16, device="cuda")
