@@ -799,7 +799,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
 // sums and writes what dz and x make of it.  A block's four wavefronts have the same columns; their sums, and those of the blocks along `outer`, are added up in order.  Lanes that the row's end
 // cuts take its last V columns, which two lanes then work out alike.  Bound by memory:
 // 1 x 4096 x 16384 bf16 48 us, 5.6 TB/s of the two matrices, part of it from the last cache, 8 rows 59 (as products of matrices that are put in order 121 and 122); small ones by two launches, 16 bits'
-// eight rows by their vector instructions: 8 x 1000 x 1000 bf16 12.9 (14.9), 8 x 1001 x 2003 fp32 13.0 (23.9), 8 x 16384 x 100 bf16 16.1 (14.8).
+// eight rows by their vector instructions (least_thin): 8 x 1000 x 1000 bf16 12.9 (14.9), 8 x 1001 x 2003 fp32 13.0 (23.9).
 struct Thin {
     const void* dy; const void* z; const void* x; const void* weight; void* dweight; void* dbias; float* sums;     // sums: [parts][rows][across * 64 V], or NULL
     int64_t dy_stride, z_stride, x_stride, weight_stride, dweight_stride, inner, outer;
@@ -1175,6 +1175,15 @@ ForwardRoom forward_room(const LinearForward& a) {
     return r;
 }
 
+// From how many of the weight's rows on up to eight rows take k_linear_thin_backward, whose chain of vector instructions grows with x's rows (us on the device, against products of matrices put in
+// order, at 16 and 100 / 500 / 1000 of the weight's: bf16 8 x 1000 12.2 and 12.5 against 8.4 and 9.0 / 12.7, 11.4 / the same within 3 %; 5 x 1000 10.9 and 11.2 against 8.4 and 9.0 / the same;
+// 4 x 1000 9.2 and 9.5 against 8.5 and 9.0; fp32 8 x 1000 9.4 against 8.9 / less from 100 on; one and two rows less throughout; long rows pay earlier: 5 x 16384 14.2 against 12.9 at 100,
+// 21.1 against 27.8 at 500).
+int64_t least_thin(int32_t type, int64_t rows, int64_t inner) {
+    const int64_t least = type == P2_F32 ? (rows > 4 ? 64 : 1) : rows > 4 ? 768 : rows > 2 ? 128 : 1;
+    return inner > 8192 ? ceil_div(least, 3) : least;
+}
+
 struct BackwardRoom { bool thin; int64_t each, across, parts; Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
 BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     // (A call asks twice, for its workspace and for itself: the last sizes' answer is kept.)
@@ -1184,7 +1193,7 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     const int64_t size = (int64_t)type_bytes(type);
     BackwardRoom r = {};
     const int64_t values = 16 / size;
-    if (rows <= 8 && inner >= values) {
+    if (rows <= 8 && inner >= values && outer >= least_thin(type, rows, inner)) {
         r.thin = true;
         r.across = ceil_div(inner, 64 * values);
         r.each = r.across * ceil_div(outer, 256) >= 2 * kUnits ? 64 : 8;               // of the weight's rows a wavefront

@@ -680,6 +680,17 @@ def test_gradients_of_a_few_rows_take_dz_as_it_is(T, rows, inner, outer, kind, a
     compare(dx, dz @ w.double(), (outer / 4 + 32) * 2 * U * (dz.abs() @ w.double().abs()) + 1.1 * own @ w.double().abs(), "dx")
 
 
+@pytest.mark.parametrize("rows,outer,kinds", [(3, 127, (BF16, F16)), (4, 128, (BF16, F16)), (8, 767, (BF16, F16)), (5, 768, (BF16, F16)), (8, 63, (F32,)), (5, 64, (F32,)), (4, 5, (F32,))])
+@pytest.mark.parametrize("inner", [8, 77, 520])
+def test_gradients_of_a_few_rows_and_few_of_the_weight_s(T, rows, outer, kinds, inner):
+    """On either side of what decides which kernels make them."""
+    for kind in kinds:
+        x, w, _, dy = linear_inputs(rows, inner, outer, kind, pad=outer % 2)
+        z = draw(7, rows, outer).to(kind)
+        for activation in (None, "silu"):
+            check_linear_gradient(T, x, w, z if activation else None, dy, activation)
+
+
 def test_linear_of_more_values_than_32_bits_count(T):
     rows, inner = 1 << 20, 2056
     x = torch.zeros(rows, inner, dtype=BF16, device="cuda")
