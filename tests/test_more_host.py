@@ -245,3 +245,27 @@ def test_states_have_their_tensors_shapes(T):
     assert s["means"][0].dtype == torch.int8 and s["squares"][0].dtype == torch.uint8 and s["step"].dtype == torch.int64
     s = T.p2_adamw_state(p)
     assert s["mean_scales"] is None and s["means"][0].dtype == torch.float32
+
+
+def test_tensors_that_stand_for_shapes_alone_are_refused(T):
+    """Under a mode that follows shapes, and its tensors outside of it: no result without values, and no argument taken for one that is not given."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    calls = T._native_calls()
+    with FakeTensorMode():
+        q, s, x, w = torch.zeros(300, dtype=torch.int8, device="cuda:0"), torch.zeros(2, device="cuda:0"), torch.zeros(4, 8, device="cuda:0"), torch.zeros(8, device="cuda:0")
+        u, n = q.to(torch.uint8), torch.zeros((), dtype=torch.int64, device="cuda:0")
+        w2 = torch.zeros(6, 8, device="cuda:0")
+    meta = [t.to("meta") for t in (torch.zeros(300, dtype=torch.int8), torch.zeros(300, dtype=torch.uint8), torch.zeros(2), torch.zeros(2))]
+
+    def refused(call):
+        with pytest.raises(T.P2Error) as e:
+            call()
+        assert e.value.code == EINVAL and "no values" in str(e.value)
+
+    with FakeTensorMode(allow_non_fake_inputs=True):
+        refused(lambda: calls.adamw_values([q], [u], [s], [s], 0))
+        refused(lambda: calls.layer_norm_forward(x, w, None, 1e-5, 0))
+        refused(lambda: calls.linear_forward(x, w2, None, 0, None, False, 0))
+        refused(lambda: calls.adamw([x], [x], [x], [x], n, None, None, None, None, 1e-3, 0.9, 0.9, 1e-8, 0.0, 1.0, None, 1.0, 0))
+    refused(lambda: calls.adamw_values(*([t] for t in meta), 0))
+    refused(lambda: calls.square_sum([meta[2]], 0))

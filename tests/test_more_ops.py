@@ -928,6 +928,37 @@ def test_results_are_ordinary_tensors(T):
     assert torch.cuda.memory_allocated() == before
 
 
+FIRST_CALL_FOLLOWS_SHAPES = """
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+from paper_2110_10548_amd import train as T
+x = torch.randn(5, 64, device="cuda")
+with FakeTensorMode(allow_non_fake_inputs=True):
+    for call in (lambda: T.p2_layer_norm_forward(torch.zeros(5, 64, device="cuda")), lambda: T.p2_layer_norm_forward(x)):
+        try:
+            call()
+            raise SystemExit("not refused")
+        except T.P2Error:
+            pass
+y, mean, rstd = T.p2_layer_norm_forward(x)
+r = T.p2_route_forward(x, 3)
+for t in (y, mean, rstd, r["gate"], T.p2_square_sum([x])):
+    assert t.device == x.device and t.untyped_storage().device == x.device and type(t) is torch.Tensor, t.device
+assert abs(float(T.p2_square_sum([x])) / float(x.double().square().sum()) - 1) < 1e-12
+assert (y - torch.nn.functional.layer_norm(x, (64,))).abs().max() < 1e-5
+print("as ever")
+"""
+
+
+def test_a_first_call_that_follows_shapes_alone_leaves_the_others_as_they_are(T):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FIRST_CALL_FOLLOWS_SHAPES], cwd=root, capture_output=True, text=True, timeout=100)
+    assert run.returncode == 0 and "as ever" in run.stdout, run.stdout + run.stderr
+
+
 def test_a_parameter_that_would_not_train_is_warned_of(T):
     import warnings
     x, w, b, res = linear_inputs(6, 40, 12, F32)
