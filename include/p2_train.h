@@ -120,7 +120,7 @@ int32_t p2_route_forward_workspace(int64_t tokens, int32_t experts, int32_t k, i
 
 /* Routes each token to k experts by scores: s = softmax of its logits, or their sigmoids; v = s + bias (NULL: 0), compared in 64 bits, is
  * what is chosen by, and s what the gates are made of.  An expert whose logit or bias is -inf is not on offer; NaN counts as larger
- * than every number.  (A softmax over a logit of NaN or +inf is NaN throughout.)
+ * than every number.  (A softmax over a logit of NaN or +inf is NaN throughout.  Logits may differ whose scores are one in 64 bits, as sigmoids of more than 37 are: these tie.)
  *   The experts are in `groups` groups of equal size, one after the other.  A group's value is the sum of its group_best (1 or 2) largest
  *   v (of as many as are on offer), and the choice is made within the group_limit groups of the largest values.
  *   expert[t][i] = the i-th best of those; gate[t][i] = scale * s, or with `renormalise` scale * s / (sum of the chosen experts' s), which

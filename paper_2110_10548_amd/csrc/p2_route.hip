@@ -64,8 +64,7 @@ __device__ __forceinline__ double over_wavefront(double v, bool sum) {
 }
 
 // One token's choice by a whole wavefront, each group with 64 / (groups rounded up to a power of two) lanes.  What the experts are compared by, as ordered
-// numbers, is kept in `key`, of which a lane touches its own experts' places alone; the chosen experts go to `slot`.  Without a bias experts are compared by
-// their logits.  (A call of its own, so that its 64-bit numbers take no registers from the kernel; arguments one by one, because a reference would put the
+// numbers, is kept in `key`, of which a lane touches its own experts' places alone; the chosen experts go to `slot`.  (A call of its own, so that its 64-bit numbers take no registers from the kernel; arguments one by one, because a reference would put the
 // kernel's own into memory.  A token takes some 3 us, so it is latency that counts.)
 template <typename T> __device__ __noinline__ void choose_exactly(const T* row, const float* bias, int experts, int k, int score_kind, int groups, int group_lanes, int group_limit,
                                                                   int group_best, uint64_t* key, int* slot) {
@@ -80,14 +79,13 @@ template <typename T> __device__ __noinline__ void choose_exactly(const T* row, 
         sum = over_wavefront(sum, true);
     }
     const auto score = [&](double z) { return score_kind == P2_SOFTMAX ? exp(z - most) / sum : 1.0 / (1.0 + exp(-z)); };
-    const bool by_logits = !bias && sum == sum;
     uint64_t one = 0, two = 0;                                 // this lane's largest
     int first = 0, second = 0;
 #pragma unroll 4
     for (int e = begin; e < end; e += group_lanes) {
         const double z = (double)(float)row[e];
         const float b = bias ? bias[e] : 0.0f;
-        const uint64_t x = z == minus || b == -INFINITY ? 0 : ordered(by_logits ? z : score(z) + (double)b);
+        const uint64_t x = z == minus || b == -INFINITY ? 0 : ordered(score(z) + (double)b);
         key[e] = x;
         if (x > one) { two = one; second = first; one = x; first = e; }
         else if (x > two) { two = x; second = e; }
@@ -100,14 +98,7 @@ template <typename T> __device__ __noinline__ void choose_exactly(const T* row, 
             top = larger(top, o);
         }
         uint64_t value = top;
-        if (group_best == 2 && top != 0) {
-            if (by_logits) {
-                const double s = score(value_of(top));
-                value = ordered(next != 0 ? s + score(value_of(next)) : s);
-            } else if (next != 0) {
-                value = ordered(value_of(top) + value_of(next));
-            }
-        }
+        if (group_best == 2 && top != 0 && next != 0) value = ordered(value_of(top) + value_of(next));
         int rank = 0;                                          // groups that come before this one
         for (int g = 0; g < groups; ++g) {
             const uint64_t v = __shfl(value, g * group_lanes, 64);
@@ -155,7 +146,7 @@ template <typename T> __device__ __noinline__ void choose_exactly(const T* row, 
 // place in the list, and a reduction over lanes one a step.  0: not on offer.
 //  - With a bias it is the bits of score + bias + 1 + the largest bias, which is 1 or more: whole numbers are in the order of such floats, and one step of
 //    them is 2^-23 at least.
-//  - Without one it is the logit's bits in their order.
+//  - Without one it is the logit's bits in their order, which is that of the scores but where two logits have one score in 64 bits (one_score).
 // What the lowest bits and the 32 bits leave open is found out by the gaps: where two neighbours among the k + 1 best, or the last group taken and the
 // first one left, are nearer to each other than they may be off, or where something is not finite, or a lane has no more of its list, the token is chosen for
 // again in 64 bits.  16-bit logits without a bias need no gaps: they leave 13 bits for the whole index.
@@ -164,6 +155,22 @@ __device__ __forceinline__ uint32_t in_order(float f) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float out_of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+
+// Whether a logit and a smaller one next to it in the order may have one score, or scores that 64 bits round off to the wrong order.  Logits differ by 2^-24 of the larger one at least, scores
+// of normal size by some 2^-52 once they are rounded, so that has to do with
+//  - sigmoids next to 1: at 16 a step of a logit moves them by 2^-42 (`smaller` is asked about); below -700 they come near what 64 bits hold (`larger` is);
+//  - exponentials that far below the row's largest, `most` (0 for sigmoids);
+//  - logits next to 0, where those up to 2^-16 may differ by any little: both are asked about.  (Two zeros are one logit, but what comes after them is asked about, too.)
+// (Asking takes 3 to 8 % of a choice without a bias: 65536 x 256 fp32 28.4 -> 29.6 us, in four groups of which two 31.5 -> 33.4; at most 12 %, 131072 x 128 bf16 30.1 -> 33.8.)
+constexpr float kNextToOne = 16.0f, kNextToNothing = -700.0f, kNextToZero = 0x1p-16f;
+__device__ __forceinline__ bool little(float z) { return fabsf(z) < kNextToZero && z != 0.0f; }
+__device__ __forceinline__ bool one_score(int32_t score, float larger, float smaller, float most) {
+    return larger - most < kNextToNothing || (score == P2_SIGMOID && smaller > kNextToOne) || little(larger) || little(smaller);
+}
+// Whether that has to be asked at all: of the larger one.
+__device__ __forceinline__ bool far_out(int32_t score, float z, float most) {
+    return z - most < kNextToNothing || z > (score == P2_SIGMOID ? kNextToOne : INFINITY) || fabsf(z) < kNextToZero;
+}
 
 // The same number, which the compiler takes for a new one: tests of its bits are not made ahead of a loop, where they would take two scalar registers each.
 __device__ __forceinline__ uint32_t opaque(uint32_t v) {
@@ -393,12 +400,19 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
                     rank += (uint32_t)__shfl((int)value, (int)(threadIdx.x & 63) - lane + ((lane + d) & (kLanes - 1)), 64) > value;
             }
             const bool taken = rank < a.group_limit && value;
-            if (!kExact || a.group_best == 2) {
+            // (without a bias: whether some group's largest is where logits have one score)
+            const bool doubt = !kBiased && a.group_best == 1 && __any(far_out(a.score, out_of_order(value & ~group_bits), most));
+            if (!kExact || a.group_best == 2 || doubt) {
                 const uint32_t last = ~group_reduce<kLanes>(taken ? ~value : 0u, most_of), left = group_reduce<kLanes>(taken ? 0u : value, most_of);
                 // (a softmax's scores go by differences of logits, of which the lowest bits are off by steps of the logits' size)
                 const float size = !kBiased && !kExact && a.score == P2_SOFTMAX ? 4.0f * kItems * 0x1p-23f * fabsf(most) : 0.0f;
                 if (a.group_best == 2) odd |= left && !(__uint_as_float(last) - __uint_as_float(left) > apart_sum + size);
-                else odd |= left && last - left <= apart + kLanes;
+                else if (!kExact) odd |= left && last - left <= apart + kLanes;
+                if (doubt) {
+                    const float taken_last = out_of_order(last & ~group_bits), left_first = out_of_order(left & ~group_bits);
+                    const bool behind = group_reduce<kLanes>((uint32_t)(value && little(out_of_order(value & ~group_bits))), most_of) != 0;
+                    odd |= left && (one_score(a.score, taken_last, left_first, most) || (taken_last == 0.0f && left_first == 0.0f && behind));
+                }
             }
             if (!taken) list = List<kDepth>();
         }
@@ -434,6 +448,24 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
         wavefront_exchange();
         const int my_slot = lane < found ? slots[threadIdx.x / kLanes][lane] : 0;
         int chosen = keep && lane < found ? expert_of(my_slot) : -1;
+        const int at_first = chosen;
+        float logit = -INFINITY;
+        if constexpr (!kBiased) {
+            if (chosen >= 0) logit = (float)row_of(t)[chosen];
+            if (__any(chosen >= 0 && far_out(a.score, logit, most))) {
+                const float after = out_of_order(best & ~kMask);
+                bool doubt = chosen >= 0 && one_score(a.score, logit, lane > 0 ? logit : after, most);
+                const bool zeros = chosen >= 0 && logit == 0.0f && after == 0.0f;      // (behind which there may be logits next to 0)
+                if (__any(zeros)) {
+                    const T* row = row_of(t);
+                    bool any = false;
+                    for (int e = lane; e < a.experts; e += kLanes) any |= little((float)row[e]);
+                    doubt |= any && group_reduce<kLanes>((uint32_t)zeros, most_of) != 0;
+                }
+                odd = odd || group_reduce<kLanes>((uint32_t)doubt, most_of) != 0;
+                near = near && !odd;
+            }
+        }
         if (!kExact && __any(near)) {
             // The k + 1 best in 64 bits, one a lane, if the next one is far enough from all of them.
             const uint64_t there_next = __ballot(list.v[0] == best && best != 0) >> ((threadIdx.x & 63) - lane) & (~0ull >> (64 - kLanes));
@@ -488,7 +520,8 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
         } else {
             if (lane == 0 && there) a.again[t] = odd;
         }
-        const float gate = gate_of<kLanes>(a, chosen, chosen >= 0 ? (float)row_of(t)[chosen] : -INFINITY, most, inv);
+        if (kBiased || chosen != at_first) logit = chosen >= 0 ? (float)row_of(t)[chosen] : -INFINITY;
+        const float gate = gate_of<kLanes>(a, chosen, logit, most, inv);
         if (there && lane < a.k) {
             a.expert[t * a.k + lane] = chosen;
             a.gate[t * a.k + lane] = chosen >= 0 ? gate * a.scale : 0.0f;

@@ -149,6 +149,56 @@ def test_route_far_and_odd_logits(T, score, kind):
     assert abs(float(got["gate"].sum(1).double().mean()) - 1) < 1e-6
 
 
+def check_scores_decide(T, z, k, **kw):
+    """Without a bias, and with one of zeros: the choice is that of the scores in 64 bits."""
+    for bias in (None, torch.zeros(z.shape[1], device="cuda")):
+        got, want = T.p2_route_forward(z, k, bias=bias, **kw), route_reference(z, k, bias=bias, **kw)
+        assert torch.equal(got["expert"], want["expert"]), (bias is None, (got["expert"] != want["expert"]).nonzero()[:4].tolist())
+        assert torch.equal(got["counts"], want["counts"])
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("score,scale", [("sigmoid", 30.0), ("sigmoid", 1000.0), ("softmax", 1000.0)])
+@pytest.mark.parametrize("tokens,experts,k,groups,limit,best", [(1, 8, 8, 1, 1, 1), (300, 8, 1, 1, 1, 1), (300, 8, 2, 4, 2, 1), (20, 64, 6, 1, 1, 1), (700, 64, 6, 8, 3, 1), (700, 64, 6, 8, 3, 2),
+                                                                (300, 256, 8, 8, 4, 1), (90, 255, 9, 5, 2, 2), (40, 1024, 64, 1, 1, 1), (40, 1000, 33, 40, 7, 1)])
+def test_route_without_a_bias_goes_by_scores(T, kind, score, scale, tokens, experts, k, groups, limit, best):
+    """Logits far out have one score: 1 above some 37 as sigmoids, 0 below some -709, or that far below a row's largest as a softmax.  Ties go to the lowest index."""
+    check_scores_decide(T, draw(experts, tokens, experts, scale=scale).to(kind), k, score=score, groups=groups, group_limit=limit, group_best=best)
+
+
+def test_route_without_a_bias_of_a_few_logits_with_one_score(T):
+    z = torch.tensor([[38.0, 60.0, 45.0, 1.0]], device="cuda")
+    assert T.p2_route_forward(z, 2, score="sigmoid")["expert"].tolist() == [[0, 1]]
+    for tokens in (1, 200):
+        one = z.repeat(tokens, 1)
+        assert (T.p2_route_forward(one, 2, score="sigmoid")["expert"] == torch.tensor([0, 1], device="cuda")).all()
+        assert (T.p2_route_forward(one, 1, score="sigmoid", groups=4, group_limit=1)["expert"] == 0).all()
+        assert (T.p2_route_forward(one, 1, score="sigmoid")["expert"] == 0).all()
+        soft = torch.tensor([[-3e4, -1e4, 2.0, -2e4]], device="cuda").repeat(tokens, 1)                    # masks that are no infinities
+        for kind in (F32, BF16, F16):
+            assert (T.p2_route_forward(soft.to(kind), 3)["expert"] == torch.tensor([2, 0, 1], device="cuda")).all()
+            assert (T.p2_route_forward(soft.to(kind), 2, groups=4, group_limit=2)["expert"] == torch.tensor([2, 0], device="cuda")).all()
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("tokens,experts,groups,limit,best", [(3, 6, 1, 1, 1), (500, 64, 1, 1, 1), (500, 64, 8, 3, 1), (500, 64, 8, 3, 2)])
+def test_route_of_logits_next_to_zero(T, kind, score, tokens, experts, groups, limit, best):
+    """1e-20 and 2e-20 differ, their scores do not; 0 is not always the smaller one."""
+    z = (draw(1, tokens, experts) * 10.0 ** torch.from_numpy(np.random.RandomState(2).randint(-45, -17, (tokens, experts))).cuda()).to(kind)
+    z[::3, ::5] = 0.0
+    for k in (1, 2, 5):
+        check_scores_decide(T, z, k, score=score, groups=groups, group_limit=limit, group_best=best)
+        first = z.clone()
+        first[:, 1] = 0.5
+        check_scores_decide(T, first, k, score=score, groups=groups, group_limit=limit, group_best=best)
+        check_scores_decide(T, -z.abs(), k, score=score, groups=groups, group_limit=limit, group_best=best)
+        behind = -z.abs()                                      # zeros, and behind them what is next to them, with lower indices
+        behind[1::2, experts // 3::2] = 0.0
+        check_scores_decide(T, behind, k, score=score, groups=groups, group_limit=limit, group_best=best)
+        check_scores_decide(T, 0 * z, k, score=score, groups=groups, group_limit=limit, group_best=best)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("offset", [1000.0, -30000.0])
 def test_route_of_logits_far_from_zero(T, score, offset):
