@@ -182,7 +182,7 @@ int32_t p2_adamw_workspace(int64_t* bytes);
  * square_sum (device; NULL: no clipping, every step is made) is what p2_square_sum gave, of all devices' gradients where they share a norm.  Where it
  * is not finite the step is left out: nothing is changed, step[0] neither.  Else step[0] (device) becomes t; in between its upper bits
  * may count what is done.  max_norm may be infinity: only
- * this check.  state_bits: 32 or 8; 8 takes eps >= 1e-12 (smaller squares would be held as 0).  Nothing that is written may overlap, nor a gradient any of it; it may
+ * this check.  state_bits: 32 or 8; 8 takes eps >= 1e-12 (smaller squares would be held as 0).  Nothing that is written, step and workspace included, may overlap, nor what is read any of it; a gradient may
  * be its own tensor's copy (same type). */
 int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_t grad_type, int32_t copy_type, int32_t state_bits,
                  int64_t* step, const float* rate, double lr, double beta1, double beta2, double eps, double weight_decay,
@@ -204,7 +204,8 @@ int32_t p2_linear_forward_workspace(const void* x, int64_t x_stride, const void*
 
 /* y = activation(z) + residual with z = x weight^T + bias:  x [rows][inner], weight [outer][inner], y, z and residual [rows][outer], bias
  * [outer], all of one type.  bias, residual and z (not kept) may be NULL.  y may be residual (same stride).  Products are summed, and
- * everything up to y worked out, in 32 bits: y goes by the z that has not been rounded yet. */
+ * everything up to y worked out, in 32 bits: y goes by the z that has not been rounded yet.  What is written may lie between the rows of something
+ * of the same stride (each has columns of its own in a buffer), else everything from its first to its last byte is its own; so for the gradients. */
 int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, const void* bias,
                           const void* residual, int64_t residual_stride, int32_t type, int32_t activation, int64_t rows,
                           int64_t inner, int64_t outer, void* y, int64_t y_stride, void* z, int64_t z_stride, void* workspace,

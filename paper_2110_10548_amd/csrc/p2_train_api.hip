@@ -112,6 +112,24 @@ bool overlap(const std::vector<Range>& ranges, const Range& one) {
     return after != ranges.begin() && std::prev(after)->second > one.first;
 }
 
+// A matrix of a product, in bytes.
+struct Extent { int64_t at, rows, row, stride; };
+Extent extent_of(const void* p, int32_t type, int64_t stride, int64_t rows, int64_t cols) {
+    const int64_t size = (int64_t)type_bytes(type);
+    return {(int64_t)reinterpret_cast<uintptr_t>(p), p ? rows : 0, cols * size, rows > 1 ? stride * size : 0};
+}
+// Whether two matrices share bytes.  Of one stride each may have columns of its own in a buffer; of different ones it is by the first and the last byte.
+bool overlap(const Extent& a, const Extent& b) {
+    if (a.rows <= 0 || b.rows <= 0) return false;
+    if (a.at + (a.rows - 1) * a.stride + a.row <= b.at || b.at + (b.rows - 1) * b.stride + b.row <= a.at) return false;
+    const int64_t stride = std::max(a.stride, b.stride), off = b.at - a.at;
+    if (stride == 0 || (a.stride != b.stride && a.rows > 1 && b.rows > 1)) return true;
+    // row i of a and row j of b, i - j = m:  m stride < off + b.row  and  off < m stride + a.row
+    const auto floor_div = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };
+    const int64_t least = std::max(floor_div(off - a.row, stride) + 1, 1 - b.rows), most = std::min(floor_div(off + b.row - 1, stride), a.rows - 1);
+    return least <= most;
+}
+
 constexpr int64_t kMostLinear = (int64_t)1 << 20;
 int32_t check_linear(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     if (!known_type(type)) return api_fail(P2_EINVAL, "unknown element type");
@@ -461,6 +479,16 @@ int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_
         if (!step || !aligned_to(step, 8) || !aligned_to(rate, 4) || !aligned_to(square_sum, 8)) return api_fail(P2_EINVAL, "step null, or pointer not aligned to its elements");
         if (!workspace || !aligned_to(workspace, 256)) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < 256) return api_fail(P2_ENOSPC, "workspace too small");
+        const Range own[2] = {range_of(step, 1, 8), range_of(workspace, 256, 1)}, read[2] = {range_of(rate, rate ? 1 : 0, 4), range_of(square_sum, square_sum ? 1 : 0, 8)};
+        const auto apart = [](const Range& x, const Range& y) { return x.second <= y.first || y.second <= x.first; };
+        for (const Range& w : own)
+            if (overlap(written, w) || !apart(w, read[0]) || !apart(w, read[1])) return api_fail(P2_EINVAL, "step or workspace overlaps what is written or read");
+        if (!apart(own[0], own[1])) return api_fail(P2_EINVAL, "step and workspace overlap");
+        for (const Range& r : read)
+            if (r.first != r.second && overlap(written, r)) return api_fail(P2_EINVAL, "rate or square_sum overlaps what is written");
+        for (int64_t i = 0; i < n; ++i)
+            for (const Range& w : own)
+                if (tensors[i].count > 0 && !apart(range_of(tensors[i].grad, tensors[i].count, type_bytes(grad_type)), w)) return api_fail(P2_EINVAL, "a gradient overlaps step or workspace");
         Adamw a = {};
         a.tensors = tensors; a.n = n; a.numbers = static_cast<AdamwStep*>(workspace); a.eps = eps;
         a.call = {step, rate, square_sum, lr, beta1, beta2, weight_decay, grad_factor, max_norm};
@@ -520,6 +548,13 @@ int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, i
         if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
         if (rows == 0) return P2_OK;
+        const Extent of_y = extent_of(y, type, y_stride, rows, outer), of_z = extent_of(z, type, z_stride, rows, outer), of_work = extent_of(room ? workspace : nullptr, P2_F32, 0, 1, room / 4);
+        const Extent of_residual = extent_of(residual, type, residual_stride, rows, outer);
+        const Extent read[] = {extent_of(x, type, x_stride, rows, inner), extent_of(weight, type, weight_stride, outer, inner), extent_of(bias, type, 0, 1, outer)};
+        for (const Extent& r : read)
+            if (overlap(of_y, r) || overlap(of_z, r) || overlap(of_work, r)) return api_fail(P2_EINVAL, "y, z or workspace overlaps an input");
+        if ((y != residual && overlap(of_y, of_residual)) || overlap(of_z, of_residual) || overlap(of_work, of_residual)) return api_fail(P2_EINVAL, "y, z or workspace overlaps the residual");
+        if (overlap(of_y, of_z) || overlap(of_y, of_work) || overlap(of_z, of_work)) return api_fail(P2_EINVAL, "y, z and workspace overlap");
         return launched(launch_linear_forward(a, (hipStream_t)stream), "linear");
     });
 }
@@ -553,6 +588,16 @@ int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int
         const int64_t room = linear_backward_workspace(type, rows, inner, outer);
         if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
+        const Extent written[] = {extent_of(dx, type, dx_stride, rows, inner), extent_of(dweight, weight_type, dweight_stride, outer, inner), extent_of(dbias, weight_type, 0, 1, outer),
+                                  extent_of(room ? workspace : nullptr, P2_F32, 0, 1, room / 4)};
+        const Extent read[] = {extent_of(dy, type, dy_stride, rows, outer), extent_of(slope ? z : nullptr, type, z_stride, rows, outer), extent_of(dweight ? x : nullptr, type, x_stride, rows, inner),
+                               extent_of(dx ? weight : nullptr, type, weight_stride, outer, inner)};
+        for (int i = 0; i < 4; ++i) {
+            for (const Extent& r : read)
+                if (overlap(written[i], r)) return api_fail(P2_EINVAL, "a gradient or workspace overlaps an input");
+            for (int j = 0; j < i; ++j)
+                if (overlap(written[i], written[j])) return api_fail(P2_EINVAL, "gradients or workspace overlap");
+        }
         LinearBackward a = {};
         a.dy = dy; a.z = z; a.x = x; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.workspace = static_cast<char*>(workspace);
         a.dy_stride = dy_stride; a.z_stride = z_stride; a.x_stride = x_stride; a.weight_stride = weight_stride; a.dx_stride = dx_stride;

@@ -269,3 +269,37 @@ def test_tensors_that_stand_for_shapes_alone_are_refused(T):
         refused(lambda: calls.adamw([x], [x], [x], [x], n, None, None, None, None, 1e-3, 0.9, 0.9, 1e-8, 0.0, 1.0, None, 1.0, 0))
     refused(lambda: calls.adamw_values(*([t] for t in meta), 0))
     refused(lambda: calls.square_sum([meta[2]], 0))
+
+
+Q = 1 << 20                          # far apart
+APART = dict(x=1 * Q, weight=2 * Q, bias=3 * Q, residual=4 * Q, y=5 * Q, z=6 * Q, workspace=7 * Q)
+APART_BACKWARD = dict(dy=1 * Q, z=2 * Q, x=3 * Q, weight=4 * Q, dx=5 * Q, dweight=6 * Q, dbias=7 * Q, workspace=8 * Q)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(y=Q + 4), dict(y=Q - 64 * 100 + 4), dict(y=2 * Q + 32 * 15), dict(y=3 * Q - 4), dict(y=4 * Q + 4), dict(y=6 * Q + 64 * 99 + 60), dict(z=Q + 32 * 99 + 28), dict(z=2 * Q - 4),
+    dict(z=3 * Q), dict(z=4 * Q + 60), dict(z=5 * Q - 60),
+    dict(x_stride=40, y_stride=40, y=Q + 28), dict(x_stride=40, y_stride=40, y=Q + 160 * 3 + 28), dict(x_stride=40, y_stride=40, y=Q - 160 * 99 - 60),         # columns of one buffer, one of them both's
+    dict(x_stride=24, y_stride=24, y=Q + 36), dict(x_stride=40, y_stride=41, y=Q + 32), dict(y_stride=40, z_stride=40, z=5 * Q + 60), dict(y_stride=40, z_stride=40, z=5 * Q + 100),
+    dict(residual_stride=40, y_stride=40, y=4 * Q + 160), dict(rows=1, residual_stride=40, y=4 * Q + 4), dict(LONG, workspace=5 * Q), dict(LONG, workspace=2 * Q)])
+def test_linear_forward_refuses_results_in_what_it_reads_or_writes(T, bad):
+    assert _linear_forward(T, **(APART | bad)) == EINVAL and b"overlap" in T.B.lib().p2_last_error()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dx=Q + 4), dict(dx=2 * Q + 64 * 99 + 60), dict(dx=3 * Q - 4), dict(dx=4 * Q + 32 * 15 + 28), dict(dx=6 * Q + 8), dict(dx=7 * Q), dict(dweight=Q - 4), dict(dweight=2 * Q + 4), dict(dweight=3 * Q + 4),
+    dict(dweight=4 * Q + 4, dx=NULL, weight=4 * Q, dy=4 * Q + 64), dict(dbias=Q + 4), dict(dbias=2 * Q - 4), dict(dbias=3 * Q + 12), dict(dbias=4 * Q), dict(dbias=5 * Q + 32 * 99 + 28), dict(dbias=6 * Q),
+    dict(rows=0, dbias=6 * Q + 4), dict(rows=1, dx=Q + 60), dict(workspace=Q), dict(workspace=5 * Q), dict(workspace=7 * Q), dict(dx_stride=40, x_stride=40, dx=3 * Q + 28),
+    dict(dx_stride=40, x_stride=40, dx=3 * Q + 160 * 5 - 4), dict(dx_stride=40, dy_stride=41, dx=Q + 80), dict(weight_type=1, dbias=6 * Q + 16 * 15 + 14)])
+def test_linear_backward_refuses_results_in_what_it_reads_or_writes(T, bad):
+    assert _linear_backward(T, **(APART_BACKWARD | bad)) == EINVAL and b"overlap" in T.B.lib().p2_last_error()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(step=1 << 12), dict(step=(1 << 16) + 392), dict(step=(1 << 17) - 8, tensor=dict(square=(1 << 17) - 4)), dict(step=1 << 20), dict(square_sum=1 << 12), dict(square_sum=(1 << 16) + 8),
+    dict(rate=(1 << 17) + 396), dict(step=1 << 22, square_sum=1 << 22), dict(step=1 << 22, rate=(1 << 22) + 4), dict(workspace=1 << 16), dict(workspace=1 << 20), dict(workspace=1 << 21),
+    dict(workspace=1 << 23, step=(1 << 23) + 8), dict(workspace=1 << 23, rate=(1 << 23) + 8)])
+def test_adamw_refuses_its_numbers_in_what_it_reads_or_writes(T, bad):
+    a = dict(step=1 << 21, square_sum=NULL, workspace=1 << 24) | bad
+    tensor = a.pop("tensor", {})
+    assert _adamw(T, [_tensor(T, **tensor)], **a) == EINVAL and b"overlap" in T.B.lib().p2_last_error()

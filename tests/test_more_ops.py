@@ -799,6 +799,33 @@ def test_linear_forms_of_the_arguments(T):
     assert dx.shape == (0, 40) and not dw.any() and not db.any()
 
 
+def test_results_in_columns_of_the_buffer_they_are_made_from(T):
+    """The C ABI's: every matrix has columns of its own in one buffer."""
+    import ctypes as C
+    rows, inner, outer = 70, 40, 24
+    x, w, b, res = linear_inputs(rows, inner, outer, F32)
+    want, z = T.p2_linear_forward(x, w, b, activation="silu", residual=res, keep=True)
+    wide = torch.full((rows, 2 * inner + 4 * outer), 7.0, device="cuda")
+    at, part = 0, {}
+    for name, n in (("x", inner), ("y", outer), ("dx", inner), ("z", outer), ("dy", outer), ("res", outer)):
+        part[name], at = wide[:, at:at + n], at + n
+    part["x"].copy_(x), part["res"].copy_(res), part["dy"].copy_(res)
+    p, s = {k: v.data_ptr() for k, v in part.items()}, wide.stride(0)
+    L, n, stream = T.lib(), C.c_int64(), torch.cuda.current_stream().cuda_stream
+    assert L.p2_linear_forward_workspace(p["x"], s, w.data_ptr(), inner, 0, rows, inner, outer, C.byref(n)) == 0
+    work = torch.empty(max(n.value, 256), dtype=torch.uint8, device="cuda")
+    assert L.p2_linear_forward(p["x"], s, w.data_ptr(), inner, b.data_ptr(), p["res"], s, 0, 4, rows, inner, outer, p["y"], s, p["z"], s, work.data_ptr(), n.value, stream) == 0
+    assert torch.equal(part["y"], want) and torch.equal(part["z"], z)
+    assert L.p2_linear_forward(p["x"], s, w.data_ptr(), inner, b.data_ptr(), p["res"], s, 0, 4, rows, inner, outer, p["res"], s, p["z"], s, work.data_ptr(), n.value, stream) == 0
+    assert torch.equal(part["res"], want)                      # y may be the residual
+    dx, dw, db = T.p2_linear_backward(res, x, w, z, activation="silu")
+    assert L.p2_linear_backward_workspace(0, rows, inner, outer, C.byref(n)) == 0
+    work = torch.empty(max(n.value, 256), dtype=torch.uint8, device="cuda")
+    dw2, db2 = torch.empty_like(dw), torch.empty_like(db)
+    assert L.p2_linear_backward(p["dy"], s, p["z"], s, p["x"], s, w.data_ptr(), inner, 0, 4, rows, inner, outer, p["dx"], s, dw2.data_ptr(), inner, db2.data_ptr(), 0, work.data_ptr(), n.value, stream) == 0
+    assert torch.equal(part["dx"], dx) and torch.equal(dw2, dw) and torch.equal(db2, db) and torch.equal(part["x"], x)
+
+
 # ------------------------------------------------------------------------------------------- as they are used
 
 def _step_inputs(seed):
