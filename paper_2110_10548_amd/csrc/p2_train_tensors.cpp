@@ -522,9 +522,10 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t given) {
         const at::Tensor work = workspace(bytes, params[0]);
         check(calls.adamw(t.data(), (int64_t)t.size(), type, grad_type, copy_type, small ? 8 : 32, (int64_t*)ptr(step), (const float*)ptr(rate), lr, beta1, beta2, eps, decay,
                           factor, (const double*)ptr(square_sum), most, ptr(work), bytes, stream));
-        // (what autograd has saved of them is out of date)
-        for (const at::Tensor& p : params) p.unsafeGetTensorImpl()->bump_version();
-        for (const at::Tensor& p : copies) p.unsafeGetTensorImpl()->bump_version();
+        // (what autograd has saved of them is out of date; of tensors made in inference mode it saves nothing, and their changes are not counted)
+        for (const auto* all : {&params, static_cast<const std::vector<at::Tensor>*>(&copies)})
+            for (const at::Tensor& p : *all)
+                if (!p.is_inference()) p.unsafeGetTensorImpl()->bump_version();
         Py_RETURN_NONE;
     });
 }

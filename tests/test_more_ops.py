@@ -578,6 +578,20 @@ def test_a_step_that_is_refused_leaves_what_autograd_saved(T):
     assert (p.grad == 6.0).all()
 
 
+def test_adamw_of_parameters_made_in_inference_mode(T):
+    """Autograd keeps no count of their changes, so there is nothing to be out of date; the step is that of ordinary tensors, and no error comes after it."""
+    with torch.inference_mode():
+        p, copy = torch.ones(300, device="cuda"), torch.zeros(300, dtype=BF16, device="cuda")
+    q, g = torch.ones(300, device="cuda"), torch.linspace(-1, 1, 300, device="cuda")
+    state, other = T.p2_adamw_state([p]), T.p2_adamw_state([q])
+    T.p2_adamw([p], [g], **state, copies=[copy])
+    T.p2_adamw([q], [g], **other)
+    with torch.inference_mode():
+        T.p2_adamw([p], [g], **state, copies=[copy])
+        T.p2_adamw([q], [g], **other)
+        assert torch.equal(p, q) and torch.equal(copy, q.to(BF16)) and int(state["step"]) == 2
+
+
 def test_adamw_of_more_values_than_32_bits_count(T):
     n = (1 << 31) + 1001
     p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
