@@ -180,9 +180,10 @@ int32_t p2_adamw_workspace(int64_t* bytes);
  * with lr = lr * rate[0] (a float on the device; NULL: 1), so that a captured step may follow a schedule.  The new weights are worked out from
  * mean and square before these are rounded to 8 bits; without a 32-bit copy of its own a 16-bit param is rounded to nearest each step.
  * square_sum (device; NULL: no clipping, every step is made) is what p2_square_sum gave, of all devices' gradients where they share a norm.  Where it
- * is not finite the step is left out: nothing is changed, step[0] neither.  Else step[0] (device) becomes t; in between its upper bits
- * may count what is done.  max_norm may be infinity: only
- * this check.  state_bits: 32 or 8; 8 takes eps >= 1e-12 (smaller squares would be held as 0).  Nothing that is written, step and workspace included, may overlap, nor what is read any of it; a gradient may
+ * is not finite, or step[0] is negative or 2^40 - 1, the step is left out: nothing is changed, step[0] neither.  Else step[0] (device) becomes t; in
+ * between its upper bits may count what is done.  (Two calls of one step, for groups of other types or decays, have a step[0] each: a call counts it up.)
+ * max_norm may be infinity: only this check.  state_bits: 32 or 8; 8 takes eps >= 1e-12 (smaller squares would be held as 0).  Nothing that is written,
+ * step and workspace included, may overlap, nor what is read any of it; a gradient may
  * be its own tensor's copy (same type). */
 int32_t p2_adamw(const p2_adamw_tensor* tensors, int64_t n, int32_t type, int32_t grad_type, int32_t copy_type, int32_t state_bits,
                  int64_t* step, const float* rate, double lr, double beta1, double beta2, double eps, double weight_decay,

@@ -173,14 +173,16 @@ __device__ __forceinline__ double power(double b, int64_t t) {
     }
     return r;
 }
-// The numbers of step t, by a whole wavefront: latency is all they take, so the betas' powers are two lanes'.
+// The numbers of step t, by a whole wavefront: latency is all they take, so the betas' powers are two lanes'.  (A t outside 1 to 2^40 - 1, as of a negative step, is no step's.)
+constexpr int kStepBits = 40;
 __device__ __forceinline__ AdamwStep numbers_of(const AdamwCall& a, int64_t t) {
     AdamwStep r = {};
+    r.left_out = t < 1 || t >> kStepBits != 0;
     const double left = 1.0 - power((threadIdx.x & 1) == 0 ? a.beta1 : a.beta2, t), left1 = __shfl(left, 0, 64), left2 = __shfl(left, 1, 64);
     double factor = a.grad_factor;
     if (a.square_sum) {
         const double sum = a.square_sum[0];
-        r.left_out = !(sum >= 0.0 && sum < __builtin_huge_val());
+        r.left_out |= !(sum >= 0.0 && sum < __builtin_huge_val());
         factor *= fmin(1.0, a.max_norm / (a.grad_factor * sqrt(sum)));
     }
     const double lr = a.lr * (a.rate ? (double)a.rate[0] : 1.0);
@@ -191,7 +193,7 @@ __device__ __forceinline__ AdamwStep numbers_of(const AdamwCall& a, int64_t t) {
     return r;
 }
 __global__ __launch_bounds__(64) void k_adamw_numbers(AdamwCall a, AdamwStep* numbers) {
-    const int64_t t = a.step[0] + 1;
+    const int64_t t = a.step[0] < 0 ? 0 : a.step[0] + 1;
     const AdamwStep r = numbers_of(a, t);
     if (threadIdx.x != 0) return;
     numbers[0] = r;
@@ -360,9 +362,9 @@ template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock
 // A step of one launch with a block a chunk works out the numbers itself, in every wavefront, which saves the launch before it (0.1 million values in 20 tensors with
 // their sum of squares: 20.9 -> 17.3 us, both calls, of which 16 are the host's; above kAlone chunks it is not noticed).  step[0] may become t once every block has read it: blocks that are done count themselves
 // in its upper bits, which nothing else uses, and the last one writes t.
-constexpr int kAlone = 1024, kStepBits = 40;
+constexpr int kAlone = 1024;
 template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock) void k_adamw_alone(AdamwTable table, AdamwConstants c, AdamwCall a) {
-    const int64_t t = (__hip_atomic_load(a.step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & (((int64_t)1 << kStepBits) - 1)) + 1;
+    const int64_t before = __hip_atomic_load(a.step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), t = before < 0 ? 0 : (before & (((int64_t)1 << kStepBits) - 1)) + 1;
     const AdamwStep step = numbers_of(a, t);
     if (step.left_out) return;
     adamw_chunk<P, G, kBits>(table, c, step, blockIdx.x);

@@ -202,7 +202,8 @@ def p2_adamw_state(params, bits=32):
 def p2_adamw(params, grads, means, squares, step, mean_scales=None, square_scales=None, copies=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
              rate=None, grad_factor=1.0, square_sum=None, max_norm=None):
     """One AdamW step in place: lists of tensors, all of a list of one type, contiguous (gradients may be otherwise).  p2_adamw_state makes the
-    states.  step: one int64, which the call counts up; rate: one float32 on the device that lr is multiplied by.
+    states.  step: one int64, which the call counts up, so that groups of other types or decays have a state and a step each; rate: one float32 on the
+    device that lr is multiplied by.
 
     square_sum: what p2_square_sum gave, perhaps summed over devices; where it is not finite the step is left out, and with max_norm the
     gradients are scaled down to that norm.  Parameters that require a gradient are updated all the same."""

@@ -592,6 +592,16 @@ def test_adamw_of_parameters_made_in_inference_mode(T):
         assert torch.equal(p, q) and torch.equal(copy, q.to(BF16)) and int(state["step"]) == 2
 
 
+@pytest.mark.parametrize("values", [300, 256 * 8 * 1024 + 1])
+@pytest.mark.parametrize("step", [-1, -5, -2 ** 63, 2 ** 40 - 1])
+def test_adamw_leaves_out_a_step_whose_number_is_none(T, values, step):
+    p, g = torch.ones(values, device="cuda"), torch.ones(values, device="cuda")
+    state = T.p2_adamw_state([p])
+    state["step"].fill_(step)
+    T.p2_adamw([p], [g], **state, lr=0.1)
+    assert (p == 1).all() and not state["means"][0].any() and not state["squares"][0].any() and int(state["step"]) == step
+
+
 def test_adamw_of_more_values_than_32_bits_count(T):
     n = (1 << 31) + 1001
     p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
