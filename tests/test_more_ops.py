@@ -453,6 +453,43 @@ def check_8_bits(q, scale, want, slack, square):
     assert ok[s > 0].all() and (q[s == 0] == 0).all()
 
 
+def to_8_bits(v, square):
+    """The formula in 32 bits, operation by operation, by numpy, whose roots and divisions are rounded as they are defined (torch's roots on the CPU are off by a step): stored numbers and their places."""
+    blocks = v.numpy().reshape(-1, 256)
+    scale = np.abs(blocks).max(1, keepdims=True)
+    part = np.abs(blocks) * (np.float32(1) / scale)
+    place = np.float32(255) * np.sqrt(np.sqrt(part)) if square else np.float32(127) * np.sqrt(part)
+    assert place.dtype == np.float32
+    q = np.rint(place)
+    q = np.where(blocks > 0, np.maximum(q, np.float32(1)), q) if square else np.copysign(q, blocks)
+    return (torch.from_numpy(x.reshape(-1)) for x in (q, scale, place))
+
+
+@pytest.mark.parametrize("shape", [(512 * 256,), (3, 100 * 256)])
+def test_adamw_8_bits_next_to_the_middle_of_two_numbers(T, shape):
+    """Without what was there before (betas of 0) the mean is g and the square g^2, each at most a few steps off a place where rounding turns: the numbers stored are those of the formula, all of them."""
+    n = math.prod(shape)
+    r = np.random.RandomState(1)
+    sizes = np.repeat(np.exp(3 * r.standard_normal(n // 256)), 256)
+
+    def near(middles, power):                                  # size * middle^power and its neighbours, a block's first value being its size
+        x = (sizes * middles ** power).astype(np.float32)
+        x = (x.view(np.int32) + r.randint(-4, 5, n).astype(np.int32)).view(np.float32)
+        x[::256] = sizes[::256]
+        return torch.from_numpy(x * np.where(r.rand(n) < 0.5, -1, 1).astype(np.float32))
+
+    for g, square in ((near((r.randint(0, 126, n) + 0.5) / 127, 2), False), (near((r.randint(1, 254, n) + 0.5) / 255, 2), True)):
+        q, scale, place = to_8_bits(g * g if square else g, square)
+        turning = ((place - place.floor() - 0.5).abs() < (9.9e-5 if square else 3.8e-5)).double().mean()
+        assert turning > 0.5, float(turning)                   # where a root that is off by a step could matter
+        p = torch.zeros(shape, device="cuda")
+        state = T.p2_adamw_state([p], 8)
+        T.p2_adamw([p], [g.view(shape).cuda()], **state, betas=(0.0, 0.0))
+        got, got_scale = (state["squares"][0], state["square_scales"][0]) if square else (state["means"][0], state["mean_scales"][0])
+        assert torch.equal(got_scale.cpu(), scale)
+        assert torch.equal(got.cpu().view(-1).float(), q), int((got.cpu().view(-1).float() != q).sum())
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_steps_that_are_left_out(T, bits):
     shapes = [(300,), (7, 9)]
