@@ -212,7 +212,12 @@ int32_t p2_linear_forward(const void* x, int64_t x_stride, const void* weight, i
                           int64_t inner, int64_t outer, void* y, int64_t y_stride, void* z, int64_t z_stride, void* workspace,
                           int64_t workspace_bytes, void* stream);
 
+/* What any call of these sizes takes; _for: what the call of these arguments takes, which may be far less (pointers are looked at for their alignment
+ * alone; dx, dweight, dbias: whether they are asked for). */
 int32_t p2_linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer, int64_t* bytes);
+int32_t p2_linear_backward_workspace_for(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
+                                         int32_t type, int32_t activation, int64_t rows, int64_t inner, int64_t outer, int32_t dx, int32_t dweight,
+                                         int32_t dbias, int64_t* bytes);
 
 /* With dz = dy * activation'(z):  dx = dz weight, dweight = dz^T x, dbias = sum over rows of dz; dx, dweight and dbias may each be NULL: not asked
  * for.  z is what the forward pass kept (NULL without an activation); at 0 the slope of P2_RELU is 0.  The residual's gradient is dy.  dweight and

@@ -1184,7 +1184,7 @@ int64_t least_thin(int32_t type, int64_t rows, int64_t inner) {
     return inner > 8192 ? ceil_div(least, 3) : least;
 }
 
-struct BackwardRoom { bool thin; int64_t each, across, parts; Plan dx, dweight; int64_t along, deep, dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
+struct BackwardRoom { bool thin; int64_t each, across, parts; Plan dx, dweight; int64_t along, deep, bytes; };      // bytes: enough for any call of these sizes
 BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t outer) {
     // (A call asks twice, for its workspace and for itself: the last sizes' answer is kept.)
     struct Last { int32_t type; int64_t rows, inner, outer; BackwardRoom room; };
@@ -1205,16 +1205,38 @@ BackwardRoom backward_room(int32_t type, int64_t rows, int64_t inner, int64_t ou
     r.along = round_up(outer * size, kLine);               // a row of dz, and of the weight turned
     r.deep = round_up(rows * size, kLine);                 // a row of dz turned, and of x turned
     plan_both(type, inner, rows, r.along, inner, outer, r.deep, rows > 64, r.dx, r.dweight);
-    r.dz = 0;
-    r.dz_turned = r.dz + round_up(rows * r.along, 256);
-    r.x_turned = r.dz_turned + round_up(outer * r.deep, 256);
-    r.weight_turned = r.x_turned + round_up(inner * r.deep, 256);
-    r.lines = r.weight_turned + round_up(inner * r.along, 256);
-    r.sums = r.lines + round_up(ceil_div(rows, 64) * outer * 4, 256);
-    r.more_sums = r.sums + sums_bytes(r.dx, inner, rows);
-    r.bytes = r.more_sums + sums_bytes(r.dweight, inner, outer);
+    r.bytes = round_up(rows * r.along, 256) + round_up(outer * r.deep, 256) + round_up(inner * r.deep, 256) + round_up(inner * r.along, 256) + round_up(ceil_div(rows, 64) * outer * 4, 256) +
+              sums_bytes(r.dx, inner, rows) + sums_bytes(r.dweight, inner, outer);
     last = {type, rows, inner, outer, r};
     return r;
+}
+
+// What a call of these arguments uses of its workspace, and where.
+struct BackwardLayout { bool own_dz, turned; int64_t dz, dz_turned, x_turned, weight_turned, lines, sums, more_sums, bytes; };
+BackwardLayout layout_of(const LinearBackward& a, const BackwardRoom& r) {
+    BackwardLayout l = {};
+    if (r.thin) {
+        l.bytes = a.dx ? r.bytes : 0;
+        return l;
+    }
+    l.own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
+    // Large 16-bit products take weight, x and dz turned as they lie in memory, and only dz is put in order
+    // (us, bf16, without / with an activation: 8192 x 4096 x 4096 428 -> 394 / 460 -> 431, 32768 x 1024 x 1024 213 -> 156 / 248 -> 191, 4096^3 225 -> 207 / 238 -> 220).
+    l.turned = a.type != P2_F32 && r.dx.cut == k256 && r.dweight.cut == k256 && a.outer % 8 == 0 && (!a.dx || in_order(a.weight, a.weight_stride, a.type, a.inner)) &&
+               (!a.dweight || in_order(a.x, a.x_stride, a.type, a.inner));
+    const auto place = [&](bool used, int64_t bytes) {
+        const int64_t at = l.bytes;
+        if (used) l.bytes += round_up(bytes, 256);
+        return at;
+    };
+    l.dz = place(l.own_dz && (a.dx || (a.dweight && l.turned)), a.rows * r.along);
+    l.dz_turned = place(a.dweight && !l.turned, a.outer * r.deep);
+    l.x_turned = place(a.dweight && !l.turned, a.inner * r.deep);
+    l.weight_turned = place(a.dx && !l.turned, a.inner * r.along);
+    l.lines = place(a.dbias && a.rows > 64, ceil_div(a.rows, 64) * a.outer * 4);
+    l.sums = place(a.dx != nullptr, sums_bytes(r.dx, a.inner, a.rows));
+    l.more_sums = place(a.dweight != nullptr, sums_bytes(r.dweight, a.inner, a.outer));
+    return l;
 }
 
 template <typename T> hipError_t forward(const LinearForward& a, hipStream_t s) {
@@ -1309,12 +1331,9 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
                                                                                                    a.dx_stride);
         return hipGetLastError();
     }
-    const bool own_dz = a.activation != P2_NO_ACTIVATION || !in_order(a.dy, a.dy_stride, a.type, a.outer);
-    // Large 16-bit products take weight, x and dz turned as they lie in memory, and only dz is put in order
-    // (us, bf16, without / with an activation: 8192 x 4096 x 4096 428 -> 394 / 460 -> 431, 32768 x 1024 x 1024 213 -> 156 / 248 -> 191, 4096^3 225 -> 207 / 238 -> 220).
-    const bool turned = sizeof(T) == 2 && room.dx.cut == k256 && room.dweight.cut == k256 && a.outer % 8 == 0 && (!a.dx || in_order(a.weight, a.weight_stride, a.type, a.inner)) &&
-                        (!a.dweight || in_order(a.x, a.x_stride, a.type, a.inner));
-    const char* const dz_rows = own_dz ? a.workspace + room.dz : static_cast<const char*>(a.dy);
+    const BackwardLayout at = layout_of(a, room);
+    const bool own_dz = at.own_dz, turned = at.turned;
+    const char* const dz_rows = own_dz ? a.workspace + at.dz : static_cast<const char*>(a.dy);
     const int64_t dz_pitch = own_dz ? room.along : a.dy_stride * (int64_t)sizeof(T);
     Pack k[3] = {};
     int packs = 0;
@@ -1322,10 +1341,10 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
     dz.from = a.dy; dz.from_stride = a.dy_stride;
     if (a.activation != P2_NO_ACTIVATION) { dz.z = a.z; dz.z_stride = a.z_stride; }
     dz.rows = a.rows; dz.cols = a.outer; dz.activation = a.activation;
-    if ((a.dx || (a.dweight && turned)) && own_dz) { dz.straight = a.workspace + room.dz; dz.straight_pitch = room.along; }
-    if (a.dweight && !turned) { dz.turned = a.workspace + room.dz_turned; dz.turned_pitch = room.deep; }
+    if ((a.dx || (a.dweight && turned)) && own_dz) { dz.straight = a.workspace + at.dz; dz.straight_pitch = room.along; }
+    if (a.dweight && !turned) { dz.turned = a.workspace + at.dz_turned; dz.turned_pitch = room.deep; }
     if (a.dbias && a.rows <= 64) { dz.dbias = a.dbias; dz.dbias_type = a.weight_type; }
-    else if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + room.lines);
+    else if (a.dbias) dz.sums = reinterpret_cast<float*>(a.workspace + at.lines);
     if (dz.straight || dz.turned || dz.sums || dz.dbias) ++packs;
     Product p[2] = {};
     Plan plan[2];
@@ -1338,13 +1357,13 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
             Pack& w = k[packs++];
             w = Pack();
             w.from = a.weight; w.from_stride = a.weight_stride; w.rows = a.outer; w.cols = a.inner;
-            w.turned = a.workspace + room.weight_turned; w.turned_pitch = room.along;
+            w.turned = a.workspace + at.weight_turned; w.turned_pitch = room.along;
             q.a = w.turned; q.a_pitch = room.along;
         }
         q.a_rows = a.inner;
         q.b = dz_rows; q.b_pitch = dz_pitch; q.b_rows = a.rows;
         q.length = own_dz && !turned ? room.along : a.outer * (int64_t)sizeof(T);
-        q.sums = reinterpret_cast<float*>(a.workspace + room.sums);
+        q.sums = reinterpret_cast<float*>(a.workspace + at.sums);
         q.r.y = a.dx; q.r.y_stride = a.dx_stride; q.r.y_type = a.type;
         plan[products++] = room.dx;
     }
@@ -1358,13 +1377,13 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
             Pack& x = k[packs++];
             x = Pack();
             x.from = a.x; x.from_stride = a.x_stride; x.rows = a.rows; x.cols = a.inner;
-            x.turned = a.workspace + room.x_turned; x.turned_pitch = room.deep;
+            x.turned = a.workspace + at.x_turned; x.turned_pitch = room.deep;
             q.a = x.turned; q.a_pitch = room.deep;
-            q.b = a.workspace + room.dz_turned; q.b_pitch = room.deep;
+            q.b = a.workspace + at.dz_turned; q.b_pitch = room.deep;
             q.length = room.deep;
         }
         q.a_rows = a.inner; q.b_rows = a.outer;
-        q.sums = reinterpret_cast<float*>(a.workspace + room.more_sums);
+        q.sums = reinterpret_cast<float*>(a.workspace + at.more_sums);
         q.r.y = a.dweight; q.r.y_stride = a.dweight_stride; q.r.y_type = a.weight_type;
         plan[products++] = room.dweight;
     }
@@ -1381,6 +1400,7 @@ template <typename T> hipError_t backward(const LinearBackward& a, hipStream_t s
 }  // namespace
 
 int64_t linear_forward_workspace(const LinearForward& a) { return a.rows ? forward_room(a).bytes : 0; }
+int64_t linear_backward_workspace(const LinearBackward& a) { return a.rows ? layout_of(a, backward_room(a.type, a.rows, a.inner, a.outer)).bytes : 0; }
 int64_t linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer) { return rows ? backward_room(type, rows, inner, outer).bytes : 0; }
 
 hipError_t launch_linear_forward(const LinearForward& a, hipStream_t s) {

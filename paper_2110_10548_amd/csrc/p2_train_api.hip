@@ -569,6 +569,22 @@ int32_t p2_linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, 
     });
 }
 
+int32_t p2_linear_backward_workspace_for(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t type,
+                                         int32_t activation, int64_t rows, int64_t inner, int64_t outer, int32_t dx, int32_t dweight, int32_t dbias, int64_t* bytes) {
+    return guarded([&]() -> int32_t {
+        int32_t rc = check_linear(type, rows, inner, outer);
+        if (rc != P2_OK) return rc;
+        if (activation < P2_NO_ACTIVATION || activation > P2_SILU) return api_fail(P2_EINVAL, "unknown activation");
+        if (!bytes) return api_fail(P2_EINVAL, "null argument");
+        LinearBackward a = {};
+        a.dy = dy; a.dy_stride = dy_stride; a.x = x; a.x_stride = x_stride; a.weight = weight; a.weight_stride = weight_stride;
+        a.dx = dx ? bytes : nullptr; a.dweight = dweight ? bytes : nullptr; a.dbias = dbias ? bytes : nullptr;         // (asked for or not)
+        a.rows = rows; a.inner = inner; a.outer = outer; a.type = type; a.activation = activation;
+        *bytes = linear_backward_workspace(a);
+        return P2_OK;
+    });
+}
+
 int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int64_t z_stride, const void* x, int64_t x_stride, const void* weight,
                            int64_t weight_stride, int32_t type, int32_t activation, int64_t rows, int64_t inner, int64_t outer, void* dx, int64_t dx_stride,
                            void* dweight, int64_t dweight_stride, void* dbias, int32_t weight_type, void* workspace, int64_t workspace_bytes, void* stream) {
@@ -585,7 +601,11 @@ int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int
         if (!aligned_to(dbias, type_bytes(weight_type))) return api_fail(P2_EINVAL, "pointer not aligned to its elements");
         if (dx && (dx == dy || dx == x || dx == weight || dx == z || dx == dweight)) return api_fail(P2_EINVAL, "dx is an input, or dweight");
         if (dweight && (dweight == dy || dweight == x || dweight == weight || dweight == z)) return api_fail(P2_EINVAL, "dweight is an input");
-        const int64_t room = linear_backward_workspace(type, rows, inner, outer);
+        LinearBackward a = {};
+        a.dy = dy; a.z = z; a.x = x; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.workspace = static_cast<char*>(workspace);
+        a.dy_stride = dy_stride; a.z_stride = z_stride; a.x_stride = x_stride; a.weight_stride = weight_stride; a.dx_stride = dx_stride;
+        a.dweight_stride = dweight_stride; a.rows = rows; a.inner = inner; a.outer = outer; a.type = type; a.activation = activation; a.weight_type = weight_type;
+        const int64_t room = linear_backward_workspace(a);
         if (room && (!workspace || !aligned_to(workspace, 256))) return api_fail(P2_EINVAL, "workspace null or not aligned to 256");
         if (workspace_bytes < room) return api_fail(P2_ENOSPC, "workspace too small");
         const Extent written[] = {extent_of(dx, type, dx_stride, rows, inner), extent_of(dweight, weight_type, dweight_stride, outer, inner), extent_of(dbias, weight_type, 0, 1, outer),
@@ -598,10 +618,6 @@ int32_t p2_linear_backward(const void* dy, int64_t dy_stride, const void* z, int
             for (int j = 0; j < i; ++j)
                 if (overlap(written[i], written[j])) return api_fail(P2_EINVAL, "gradients or workspace overlap");
         }
-        LinearBackward a = {};
-        a.dy = dy; a.z = z; a.x = x; a.weight = weight; a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.workspace = static_cast<char*>(workspace);
-        a.dy_stride = dy_stride; a.z_stride = z_stride; a.x_stride = x_stride; a.weight_stride = weight_stride; a.dx_stride = dx_stride;
-        a.dweight_stride = dweight_stride; a.rows = rows; a.inner = inner; a.outer = outer; a.type = type; a.activation = activation; a.weight_type = weight_type;
         return launched(launch_linear_backward(a, (hipStream_t)stream), "linear's gradients");
     });
 }

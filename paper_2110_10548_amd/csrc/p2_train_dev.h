@@ -238,7 +238,8 @@ struct LinearBackward {
     int64_t dy_stride, z_stride, x_stride, weight_stride, dx_stride, dweight_stride, rows, inner, outer;
     int32_t type, activation, weight_type;
 };
-int64_t linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer);
+int64_t linear_backward_workspace(const LinearBackward& a);         // (pointers of what is asked for need only not be null)
+int64_t linear_backward_workspace(int32_t type, int64_t rows, int64_t inner, int64_t outer);        // at most
 hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream);
 
 }  // namespace p2

@@ -41,6 +41,7 @@ struct Calls {
     decltype(&p2_linear_forward_workspace) linear_forward_workspace;
     decltype(&p2_linear_forward) linear_forward;
     decltype(&p2_linear_backward_workspace) linear_backward_workspace;
+    decltype(&p2_linear_backward_workspace_for) linear_backward_workspace_for;
     decltype(&p2_linear_backward) linear_backward;
 } calls;
 PyObject* raise_status = nullptr;              // (status): raises the library's last error
@@ -617,7 +618,7 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t given) {
         if (wanted[1]) dweight = fresh({w.n, r.cols}, scalar_of(weight_type), x);
         if (wanted[2]) dbias = fresh({w.n}, scalar_of(weight_type), x);
         int64_t bytes = 0;
-        check(calls.linear_backward_workspace(type, r.n, r.cols, w.n, &bytes));
+        check(calls.linear_backward_workspace_for(ptr(d.t), d.stride, ptr(r.t), r.stride, ptr(w.t), w.stride, type, activation, r.n, r.cols, w.n, wanted[0], wanted[1], wanted[2], &bytes));
         const at::Tensor work = workspace(bytes, x);
         check(calls.linear_backward(ptr(d.t), d.stride, ptr(s.t), s.stride, ptr(r.t), r.stride, ptr(w.t), w.stride, type, activation, r.n, r.cols, w.n, ptr(dx), r.cols,
                                     ptr(dweight), r.cols, ptr(dbias), weight_type, ptr(work), bytes, stream));

@@ -23,7 +23,7 @@ EXPORTS = ("p2_layer_norm_forward", "p2_layer_norm_backward_workspace", "p2_laye
            "p2_balance_forward", "p2_balance_loss", "p2_balance_backward", "p2_orthogonalize_workspace", "p2_orthogonalize",
            "p2_route_forward_workspace", "p2_route_forward", "p2_route_backward", "p2_route_bias", "p2_square_sum_workspace", "p2_square_sum",
            "p2_adamw_workspace", "p2_adamw", "p2_adamw_values", "p2_linear_forward_workspace", "p2_linear_forward", "p2_linear_backward_workspace",
-           "p2_linear_backward")
+           "p2_linear_backward_workspace_for", "p2_linear_backward")
 
 _lib = _native = None
 
@@ -61,6 +61,7 @@ def lib():
                 ("p2_linear_forward_workspace", [p, i64, p, i64, i32, i64, i64, i64, sizes]),
                 ("p2_linear_forward", [p, i64, p, i64, p, p, i64, i32, i32, i64, i64, i64, p, i64, p, i64, p, i64, p]),
                 ("p2_linear_backward_workspace", [i32, i64, i64, i64, sizes]),
+                ("p2_linear_backward_workspace_for", [p, i64, p, i64, p, i64, i32, i32, i64, i64, i64, i32, i32, i32, sizes]),
                 ("p2_linear_backward", [p, i64, p, i64, p, i64, p, i64, i32, i32, i64, i64, i64, p, i64, p, i64, p, i32, p, i64, p])):
             getattr(L, name).restype = i32
             getattr(L, name).argtypes = args

@@ -303,3 +303,33 @@ def test_adamw_refuses_its_numbers_in_what_it_reads_or_writes(T, bad):
     a = dict(step=1 << 21, square_sum=NULL, workspace=1 << 24) | bad
     tensor = a.pop("tensor", {})
     assert _adamw(T, [_tensor(T, **tensor)], **a) == EINVAL and b"overlap" in T.B.lib().p2_last_error()
+
+
+def _rooms(T, rows, inner, outer, kind=1, activation=0, wanted=(1, 1, 1), dy=P, x=P, weight=P, pad=0):
+    n, most = C.c_int64(), C.c_int64()
+    assert T.lib().p2_linear_backward_workspace_for(dy, outer + pad, x, inner + pad, weight, inner + pad, kind, activation, rows, inner, outer, *wanted, C.byref(n)) == 0
+    assert T.lib().p2_linear_backward_workspace(kind, rows, inner, outer, C.byref(most)) == 0 and n.value <= most.value and n.value % 256 == 0
+    return n.value, most.value
+
+
+def test_gradients_take_room_for_what_they_use(T):
+    mib = 1 << 20
+    lines = 128 * 4096 * 4
+    assert _rooms(T, 8192, 4096, 4096)[0] == lines                                     # operands that are taken as they lie in memory
+    assert _rooms(T, 8192, 4096, 4096, activation=2)[0] == 64 * mib + lines            # dz
+    assert _rooms(T, 8192, 4096, 4096, activation=2, wanted=(1, 1, 0))[0] == 64 * mib
+    assert _rooms(T, 8192, 4096, 4096, wanted=(0, 0, 1))[0] == lines
+    assert _rooms(T, 8192, 4096, 4096, wanted=(0, 0, 0))[0] == 0
+    everything, most = _rooms(T, 8192, 4096, 4096, activation=2, x=P + 2, weight=P + 2)
+    assert everything == most
+    assert _rooms(T, 1, 64, 4096, wanted=(0, 1, 1))[0] == 0 and _rooms(T, 1, 64, 4096, wanted=(1, 0, 0))[0] > 0
+    assert _rooms(T, 0, 64, 64) == (0, 0)
+    for rows, inner, outer, kind in ((100, 300, 200, 0), (2001, 1023, 515, 2), (16384, 512, 2048, 1), (5, 700, 900, 1), (64, 40, 70, 1)):
+        parts = [_rooms(T, rows, inner, outer, kind, activation=1, wanted=w)[0] for w in ((1, 0, 0), (0, 1, 0), (0, 0, 1))]
+        assert max(parts) <= _rooms(T, rows, inner, outer, kind, activation=1)[0] <= sum(parts)
+    n, f = C.c_int64(), T.lib().p2_linear_backward_workspace_for
+    for bad, code in ((dict(kind=3), EINVAL), (dict(rows=-1), EINVAL), (dict(activation=5), EINVAL), (dict(outer=0), EINVAL), (dict(inner=(1 << 20) + 1), EUNSUPPORTED)):
+        a = dict(kind=1, activation=0, rows=10, inner=64, outer=64) | bad
+        assert f(P, 64, P, 64, P, 64, *a.values(), 1, 1, 1, C.byref(n)) == code
+    assert f(P, 64, P, 64, P, 64, 1, 0, 10, 64, 64, 1, 1, 1, None) == EINVAL
+    assert _linear_backward(T, workspace_bytes=_rooms(T, 100, 8, 16, 0, activation=1)[0] - 256) == ENOSPC

@@ -860,6 +860,21 @@ def test_linear_forms_of_the_arguments(T):
     assert dx.shape == (0, 40) and not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("activation,room", [(None, 1 << 22), ("silu", (64 << 20) + (1 << 22))])
+def test_gradients_allocate_what_they_use(T, activation, room):
+    x, w, _, dy = linear_inputs(8192, 4096, 4096, BF16)
+    z = dy.clone()
+    for wanted in ((True, True, True), (True, False, False), (False, True, False), (False, False, True)):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        out = T.p2_linear_backward(dy, x, w, z if activation else None, activation=activation, dx=wanted[0], dweight=wanted[1], dbias=wanted[2])
+        results = sum(t.numel() * t.element_size() for t in out if t is not None)
+        assert torch.cuda.max_memory_allocated() - before <= results + room
+        if not any(wanted[:2]):
+            assert torch.cuda.max_memory_allocated() - before <= results + (1 << 22)
+
+
 def test_results_in_columns_of_the_buffer_they_are_made_from(T):
     """The C ABI's: every matrix has columns of its own in one buffer."""
     import ctypes as C
