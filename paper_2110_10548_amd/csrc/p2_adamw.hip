@@ -51,7 +51,7 @@ __device__ __forceinline__ double block_sum(double v, double* buf) {       // th
 }
 
 // Squares are added up in 64 bits: gradients of any size, and no overflow before the root.  A block takes chunks of kSumChunk values, four vectors a thread at a time.
-// Bound by memory: 0.1 billion bf16 values 39 us with the launch that joins the blocks' sums, 5.2 TB/s.
+// Bound by memory: 0.1 billion bf16 values 46 us, 4.4 TB/s, and 4.6 for the launch that joins the blocks' sums (39 for both behind themselves, part of the values from the last cache).
 template <typename T> __global__ __launch_bounds__(kBlock) void k_square_sum(SumTable table, double* parts) {
     constexpr int V = kSumChunk / kBlock / 4;
     __shared__ double buf[kBlock / 64];
@@ -289,7 +289,7 @@ __device__ __forceinline__ void squares_of(words2 q, float scale, float (&v)[kEa
     }
 }
 
-// Values for which the caches have no use: the values of 0.1 billion 8-bit states take 204 us instead of 238.
+// Values for which the caches have no use: the values of 0.1 billion 8-bit states take 204 us by themselves instead of 238, 226 behind a step.
 typedef float float4_a __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void store_past(float* p, int64_t n, const float (&v)[kEach]) {
     if (n < kEach) { store_part<float, kEach>(p, n, v); return; }
@@ -351,7 +351,7 @@ template <typename P, typename G, int kBits> __device__ __forceinline__ void ada
     }
 }
 
-// Bound by memory, each value read and written once: 0.2 billion fp32 weights with bf16 gradients and copies 1046 us, 5.4 TB/s; 0.1 billion bf16 weights with 8-bit states 181 us, 5.6 TB/s.
+// Bound by memory, each value read and written once: 0.2 billion fp32 weights with bf16 gradients and copies 1044 us, 5.4 TB/s; 0.1 billion bf16 weights with 8-bit states 183 us, 5.6 TB/s.
 // A block has 2048 values, eight a thread, so that half a wavefront has the 256 values of a scale.
 template <typename P, typename G, int kBits> __global__ __launch_bounds__(kBlock) void k_adamw(AdamwTable table, AdamwConstants c, const AdamwStep* numbers) {
     const AdamwStep step = numbers[0];
@@ -391,7 +391,7 @@ __device__ __forceinline__ void values_of_chunk(const AdamwTable& table, int chu
     }
 }
 
-// Bound by what is written: 0.1 billion values of each 204 us, 4.9 TB/s.
+// Bound by what is written: 0.1 billion values of each 226 us behind a step, 4.5 TB/s with what is read (204 by itself, 4.9).
 __global__ __launch_bounds__(kBlock) void k_adamw_values(AdamwTable table) {
     for (int chunk = blockIdx.x; chunk < table.begin[table.n]; chunk += gridDim.x) values_of_chunk(table, chunk);
 }

@@ -281,7 +281,7 @@ __device__ __forceinline__ void write_results(const Product& a, const Place& pla
 
 // An operand may be turned: its memory has the summed index's rows, of which a stage takes 64, and a half's columns of them lie in LDS as 64 rows of 256 bytes.  Their
 // 32-byte parts are exchanged by the row's number, so that what is read at once lies in different banks.  (16 bits and 256 x 256 tiles alone.)
-// Bound by the matrix units, busy for 70 to 77 % of the time: 8192 x 4096 x 16384 bf16 843 to 860 us with gelu, bias and z, 1.28 to 1.30 P/s; its main loop alone runs at 1.56, and a tile's end takes 9 of 97 us, the
+// Bound by the matrix units, which are busy for 70 to 77 % of the compute units' busy cycles, at the 1.8 to 2.0 GHz that such a load leaves (50 % of cycles at 2.4 GHz): 8192 x 4096 x 16384 bf16 843 to 860 us with gelu, bias and z, 1.28 to 1.30 P/s; its main loop alone runs at 1.56, and a tile's end takes 9 of 97 us, the
 // epilogue's vector instructions, which 256 x 256 sums in registers leave no second block to hide behind.  Turned, 8192 x 4096 x 4096: 226 us with one operand, 220 with both, 1.22 and 1.25 P/s.
 template <typename T, int kWavesA, int kWavesB, int FA, int FB, bool kTurnA = false, bool kTurnB = false>
 __global__ __launch_bounds__(kWavesA * kWavesB * 64) void k_linear_wide(Products all_of) {
@@ -579,7 +579,7 @@ template <typename T, int kRows, int kEach, int kAhead> __global__ __launch_boun
     if (i0 >= outer) return;
     float sum[kRows][kEach] = {};
     int64_t k = lane * V;
-    // of long rows, kAhead vectors of each under way at once (1 x 4096 x 16384 bf16 28.0 -> 24.4 us, part of it from the last cache; 1 x 8000 x 500 fp16 15.2 -> 7.4)
+    // of long rows, kAhead vectors of each under way at once (1 x 4096 x 16384 bf16 28.0 -> 24.3 us, the weight from memory, 5.5 TB/s, and 21.2 from the last cache; 1 x 8000 x 500 fp16 15.2 -> 7.4)
     if constexpr (kAhead > 1) for (int64_t whole = kAhead * 64 * V; whole <= inner; whole += kAhead * 64 * V, k += kAhead * 64 * V) {
         vec_t<T, V> w[kAhead][kEach], v[kAhead][kRows];
 #pragma unroll
@@ -798,7 +798,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear_pack(Packs
 // The gradients of up to kRows rows, in one pass over weight and dweight: a wavefront has V columns a lane and kEach of the weight's rows, of which it reads each once, adds dz times it to dx's
 // sums and writes what dz and x make of it.  A block's four wavefronts have the same columns; their sums, and those of the blocks along `outer`, are added up in order.  Lanes that the row's end
 // cuts take its last V columns, which two lanes then work out alike.  Bound by memory:
-// 1 x 4096 x 16384 bf16 48 us, 5.6 TB/s of the two matrices, part of it from the last cache, 8 rows 59 (as products of matrices that are put in order 121 and 122); small ones by two launches, 16 bits'
+// 1 x 4096 x 16384 bf16 48 us from memory, 5.6 TB/s of the two matrices, 8 rows 59 (as products of matrices that are put in order 121 and 122); small ones by two launches, 16 bits'
 // eight rows by their vector instructions (least_thin): 8 x 1000 x 1000 bf16 12.9 (14.9), 8 x 1001 x 2003 fp32 13.0 (23.9).
 struct Thin {
     const void* dy; const void* z; const void* x; const void* weight; void* dweight; void* dbias; float* sums;     // sums: [parts][rows][across * 64 V], or NULL

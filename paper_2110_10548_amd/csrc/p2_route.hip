@@ -247,9 +247,11 @@ template <int kLanes> __device__ __forceinline__ float gate_of(const RouteForwar
     return a.renormalise ? gate * __builtin_amdgcn_rcpf(group_sum<kLanes>(gate)) : gate;
 }
 
-// Bound by its vector instructions: 65536 tokens over 256 experts in eight groups, eight each, 35 us (fp32, sigmoid, bias), of which 70 % go to issuing some 190 a token and lane; the
+// Bound by its vector instructions: 65536 tokens over 256 experts in eight groups, eight each, 35 us (fp32, sigmoid, bias): some 190 a token and lane, whose issue takes 66 % of the units' busy cycles; the
 // logits alone would take 14.  Few, wide lanes a token: every reduction over lanes is DPP, and a lane's sorted list saves k passes over its values.  Blocks take tokens in turn, the next
 // one's logits under way.
+// A list of kDepth is spent where a lane has to give up that many, which for k of 6 and more is common with few lanes in the groups that are open: 65536 tokens over 256 experts in 16 groups, eight each, 40 us
+// with four groups open and 232 with one, where every token is chosen for again.
 // kAlone: one block has all tokens, and chooses in 64 bits itself; else such tokens are marked for the next kernel.
 template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __global__ __launch_bounds__(kBlock, kBiased || kAlone || kItems > 16 ? 2 : 4) void k_route_forward(RouteForward a, int32_t group_lanes) {
     typedef Part<T, kItems> P;
