@@ -462,7 +462,8 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
                     const T* row = row_of(t);
                     bool any = false;
                     for (int e = lane; e < a.experts; e += kLanes) any |= little((float)row[e]);
-                    doubt |= any && group_reduce<kLanes>((uint32_t)zeros, most_of) != 0;
+                    const bool some = group_reduce<kLanes>((uint32_t)zeros, most_of) != 0;         // (by all lanes)
+                    doubt |= any && some;
                 }
                 odd = odd || group_reduce<kLanes>((uint32_t)doubt, most_of) != 0;
                 near = near && !odd;

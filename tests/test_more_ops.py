@@ -199,6 +199,20 @@ def test_route_of_logits_next_to_zero(T, kind, score, tokens, experts, groups, l
         check_scores_decide(T, 0 * z, k, score=score, groups=groups, group_limit=limit, group_best=best)
 
 
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("experts,at", [(48, 7), (48, 3), (8, 0), (64, 41), (256, 100), (1000, 999)])
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_route_of_one_logit_next_to_zero_among_zeros(T, kind, experts, at, tokens):
+    """It comes behind the zeros by its logit, has their score, and one lane alone sees it."""
+    z = torch.zeros(tokens, experts, device="cuda")
+    z[:, at] = -1e-6
+    z = z.mul(1e-14 if kind != F16 else 0.25).to(kind)
+    z[:, :at:2] = -INF
+    for k in (1, min(at // 2 + 1, 64), min(experts - (at + 1) // 2, 8)):
+        check_scores_decide(T, z, k, score="sigmoid")
+        check_scores_decide(T, z, k, score="sigmoid", groups=2, group_limit=1)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("offset", [1000.0, -30000.0])
 def test_route_of_logits_far_from_zero(T, score, offset):
