@@ -155,6 +155,11 @@ __device__ __forceinline__ uint32_t in_order(float f) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float out_of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+// The logit of a number whose lowest bits (`taken`) say something else.  16-bit logits have zeros there, a negative one's number has ones: it is that logit itself.  32-bit ones come out less by up to
+// `taken` steps.
+template <bool kExact> __device__ __forceinline__ float logit_of(uint32_t o, uint32_t taken) {
+    return out_of_order(kExact && !(o & 0x80000000u) ? o | taken : o & ~taken);
+}
 
 // Whether a logit and a smaller one next to it in the order may have one score, or scores that 64 bits round off to the wrong order.  Logits differ by 2^-24 of the larger one at least, scores
 // of normal size by some 2^-52 once they are rounded, so that has to do with
@@ -385,7 +390,7 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
             if (a.group_best == 2) {
                 const auto score = [&](uint32_t key) {
                     if constexpr (kBiased) return __uint_as_float(key & ~kMask);
-                    const float x = out_of_order(key & ~kMask);
+                    const float x = logit_of<kExact>(key, kMask);
                     return a.score == P2_SOFTMAX ? __builtin_amdgcn_exp2f((x - most) * kLog2e) * inv : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
                 };
                 // (a group with one on offer has one bias alone: the other's part, which every sum of two has, is added)
@@ -403,7 +408,7 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
             }
             const bool taken = rank < a.group_limit && value;
             // (without a bias: whether some group's largest is where logits have one score)
-            const bool doubt = !kBiased && a.group_best == 1 && __any(far_out(a.score, out_of_order(value & ~group_bits), most));
+            const bool doubt = !kBiased && a.group_best == 1 && __any(far_out(a.score, logit_of<kExact>(value, group_bits), most));
             if (!kExact || a.group_best == 2 || doubt) {
                 const uint32_t last = ~group_reduce<kLanes>(taken ? ~value : 0u, most_of), left = group_reduce<kLanes>(taken ? 0u : value, most_of);
                 // (a softmax's scores go by differences of logits, of which the lowest bits are off by steps of the logits' size)
@@ -411,8 +416,8 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
                 if (a.group_best == 2) odd |= left && !(__uint_as_float(last) - __uint_as_float(left) > apart_sum + size);
                 else if (!kExact) odd |= left && last - left <= apart + kLanes;
                 if (doubt) {
-                    const float taken_last = out_of_order(last & ~group_bits), left_first = out_of_order(left & ~group_bits);
-                    const bool behind = group_reduce<kLanes>((uint32_t)(value && little(out_of_order(value & ~group_bits))), most_of) != 0;
+                    const float taken_last = logit_of<kExact>(last, group_bits), left_first = logit_of<kExact>(left, group_bits);
+                    const bool behind = group_reduce<kLanes>((uint32_t)(value && little(logit_of<kExact>(value, group_bits))), most_of) != 0;
                     odd |= left && (one_score(a.score, taken_last, left_first, most) || (taken_last == 0.0f && left_first == 0.0f && behind));
                 }
             }
@@ -455,7 +460,7 @@ template <typename T, int kLanes, int kItems, bool kBiased, bool kAlone> __globa
         if constexpr (!kBiased) {
             if (chosen >= 0) logit = (float)row_of(t)[chosen];
             if (__any(chosen >= 0 && far_out(a.score, logit, most))) {
-                const float after = out_of_order(best & ~kMask);
+                const float after = logit_of<kExact>(best, kMask);
                 bool doubt = chosen >= 0 && one_score(a.score, logit, lane > 0 ? logit : after, most);
                 const bool zeros = chosen >= 0 && logit == 0.0f && after == 0.0f;      // (behind which there may be logits next to 0)
                 if (__any(zeros)) {

@@ -124,6 +124,27 @@ def test_route_ties_go_to_the_lowest_index(T, score, kind, groups, limit, best):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("size", [2, 4, 8])
+@pytest.mark.parametrize("scale", [0.5, 2.0])
+def test_route_groups_whose_best_two_add_up_to_nearly_the_same(T, score, kind, size, scale):
+    """Many small groups of logits of either sign, without a bias: sums that differ in the fourth digit and less."""
+    z = draw(size, 1200, 32 * size, scale=scale).to(kind)
+    for limit in (1, 13, 31):
+        check_route(T, z, 2, score=score, groups=32, group_limit=limit, group_best=2)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("tokens", [1, 50])
+def test_route_groups_whose_best_two_add_up_to_the_same(T, kind, tokens):
+    """sigmoid(x) + sigmoid(-x) is 1 whatever x."""
+    for first in (0.5, 1.0, 1.5):
+        z = torch.tensor([[-9.0, first, -9.0, -first, 0.0, -9.0, 0.0, -9.0]], device="cuda").to(kind).repeat(tokens, 1)
+        assert (T.p2_route_forward(z, 1, score="sigmoid", groups=2, group_limit=1, group_best=2)["expert"] == 1).all()
+        assert (T.p2_route_forward(z.roll(4, 1), 1, score="sigmoid", groups=2, group_limit=1, group_best=2)["expert"] == 0).all()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_route_tells_scores_apart_that_32_bits_do_not(T, score):
     """Neighbouring 32-bit logits, far out where their scores differ in the ninth digit and less, and biases that all but even them out."""
     r = np.random.RandomState(6)
